@@ -10,10 +10,7 @@
 // values: ga_attn_wide_kernel (and, for the smallest calls, ga_attn_bf16_kernel); float32 values: ga_attn_f32_kernel (and, for
 // short calls, ga_attn_f32_short_kernel).
 // Each describes its own scheme.
-#include <algorithm>
-
-#include "ps_device.h"
-#include "ps_train.h"
+#include "ps_train_device.h"
 #include "ps_draft_debug.h"
 
 namespace {
@@ -22,37 +19,9 @@ constexpr int GA_THREADS = 256, GA_WAVES = GA_THREADS / 64;
 constexpr float GA_LAZY = 8.f;
 // A launch may have 2^32 - 1 work items in x at most: workgroups beyond GA_GRID_X go on in y (blockIdx.y is 0 but in huge calls)
 constexpr unsigned GA_GRID_X = 1u << 22;
-constexpr long long GA_MAX_WG = 0x7FFFFFFF;                // the kernels number their workgroups in 31 bits (the float32 ones in 32)
 
-// Wide accesses to the caller's q, k, v and out, which are only promised to be aligned to 4 bytes: the types say so, and the
-// compiler emits the same 16-byte instructions (global memory takes them at any multiple of 4).
-typedef unsigned u32x4_q __attribute__((ext_vector_type(4), aligned(4)));
-typedef unsigned u32x2_q __attribute__((ext_vector_type(2), aligned(4)));
-typedef float f32x4_q __attribute__((ext_vector_type(4), aligned(4)));
-__device__ __forceinline__ uint4 ld16_q(const void* p) { return __builtin_bit_cast(uint4, (u32x4)*reinterpret_cast<const u32x4_q*>(p)); }
-__device__ __forceinline__ uint4 ldg_stream16_q(const void* p) {
-    return __builtin_bit_cast(uint4, (u32x4)__builtin_nontemporal_load(reinterpret_cast<const u32x4_q*>(p)));
-}
-template <typename WT> __device__ __forceinline__ f32x4 load4_q(const void* p) {
-    if constexpr (Traits<WT>::BF) {
-        const u32x2 v = *reinterpret_cast<const u32x2_q*>(p);
-        return f32x4{bf16_to_f32(v[0] & 0xFFFFu), bf16_to_f32(v[0] >> 16), bf16_to_f32(v[1] & 0xFFFFu), bf16_to_f32(v[1] >> 16)};
-    } else {
-        return *reinterpret_cast<const f32x4_q*>(p);
-    }
-}
-__device__ __forceinline__ void stg_stream16_q(float* p, f32x4 v) { __builtin_nontemporal_store((f32x4_q)v, reinterpret_cast<f32x4_q*>(p)); }
-
-// Division of numbers below 2^31 by one that the host knows: n / d = (n * mul) >> shift
-struct GaDiv {
-    unsigned mul, shift;
-    __device__ __forceinline__ unsigned operator()(unsigned n) const { return (unsigned)((u64)n * mul >> shift); }
-};
-GaDiv ga_div(unsigned d) {
-    unsigned s = 0;
-    while ((1ull << s) < d) ++s;
-    return GaDiv{(unsigned)(((1ull << (31 + s)) + d - 1) / d), 31 + s};   // (mul * d exceeds 2^(31 + s) by less than d <= 2^s)
-}
+// the natural logarithm of a row's sum of exponentials den, taken against the reference m (both in units of ln 2)
+__device__ __forceinline__ void ga_store_lse(float* lse, size_t at, float m, float den) { lse[at] = (m + __builtin_amdgcn_logf(den)) * 0.6931471805599453f; }
 struct GaParams {
     int seqs, T, k, nq, nkv, rows, gpt, ntiles;   // gpt: groups per query tile
     unsigned k1_magic;    // ceil(2^32 / (k + 1)): a row's group is the upper half of the product (rows < 2^28; k > 0)
@@ -61,41 +30,11 @@ struct GaParams {
     int group;            // query heads per kv head
     const void *q, *k_, *v;
     float* out;
+    float* lse;         // [seqs][rows][nq], or null
     float2* table;      // [T + k][d / 2]
     void* k_rot;        // rotated keys, storage type: [seqs][rows][nkv][d], or real tokens only as [seqs][nkv][T][d]
     double log2_base;
 };
-
-// 2^x: Taylor's series of e^(f ln 2), |f| <= 1/2, to the 13th power (the next is 4e-18)
-__device__ __forceinline__ double ga_exp2(double x) {
-    const double n = rint(x), y = (x - n) * 0.69314718055994530942;
-    double p = 1.0 / 6227020800.0;
-    constexpr double c[13] = {1.0, 1.0, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320, 1.0 / 362880,
-                              1.0 / 3628800, 1.0 / 39916800, 1.0 / 479001600};
-#pragma unroll
-    for (int i = 12; i >= 0; --i) p = fma(p, y, c[i]);
-    return ldexp(p, (int)n);
-}
-// cosine and sine of a >= 0: the multiple of pi / 2 taken off in two parts (Cody and Waite's reduction; the first product is exact inside its fma, the second
-// part is below 1e-9), Taylor's series on [-pi / 4, pi / 4] to r^16 and r^17 (what follows is below 2e-18).  Angles beyond
-// 2^22 (a base below 1) are the library's business
-__device__ __forceinline__ float2 ga_cos_sin(double a) {
-    if (!(a <= 4194304.0)) return make_float2((float)cos(a), (float)sin(a));
-    const double n = rint(a * 0.63661977236758134308);
-    const double r = fma(-n, 6.123233995736766036e-17, fma(-n, 1.5707963267948965580, a)), z = r * r;
-    constexpr double cc[9] = {1.0, -1.0 / 2, 1.0 / 24, -1.0 / 720, 1.0 / 40320, -1.0 / 3628800, 1.0 / 479001600, -1.0 / 87178291200.0, 1.0 / 20922789888000.0};
-    constexpr double sc[9] = {1.0, -1.0 / 6, 1.0 / 120, -1.0 / 5040, 1.0 / 362880, -1.0 / 39916800, 1.0 / 6227020800.0, -1.0 / 1307674368000.0, 1.0 / 355687428096000.0};
-    double c = cc[8], s = sc[8];
-#pragma unroll
-    for (int i = 7; i >= 0; --i) {
-        c = fma(c, z, cc[i]);
-        s = fma(s, z, sc[i]);
-    }
-    const float fc = (float)c, fs = (float)(s * r);
-    const int q = (int)n;                                   // quarter turns
-    const float x = q & 1 ? fs : fc, y = q & 1 ? fc : fs;
-    return make_float2((q + 1) & 2 ? -x : x, q & 2 ? -y : y);
-}
 
 // Rotary table and keys in one launch.  A workgroup takes one position, works out its cosines and sines (double precision,
 // once for all heads, sequences and slots) and rotates the key rows that stand there, rounded as the inference path caches
@@ -149,11 +88,6 @@ __global__ void __launch_bounds__(256) ga_rope_kernel(const GaParams P) {
         x += (long long)gridDim.y * 256;
         if (x < n) request(x);
     }
-}
-
-// the largest of z, |a|, |b|, or NaN if there is one
-__device__ __forceinline__ float abs_max3(float z, float a, float b) {
-    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(z, __builtin_fabsf(a)), __builtin_fabsf(b));
 }
 
 // One output row by itself, from the keys and values that it sees and no others.  The kernels below multiply whole tiles: a
@@ -276,8 +210,6 @@ __device__ __attribute__((noinline)) void ga_rows_alone(ga_args_t args, int seq,
 //   rows on (8 heads x 64: T 700, k 3 48.0 / 40.6 / 37.5, T 512, k 5 41.6 / 34.3 / 35.3), x 128 from 400 on (2 x T 300 46.2 / 42.0 / 46.8), not.
 // Before 16x16x4 tiles, P.V was FMA work against probabilities broadcast from LDS: 724 and 40.5 us for the first two.
 // ------------------------------------------------------------------------------------------
-constexpr int GF_ROWS = 64;
-
 template <int D, int QT, int KH>
 __device__ __forceinline__ void ga_attn_f32(const GaParams& P) {
     constexpr int THREADS = 64 * QT * KH, ROWS = 16 * QT, KEYS = 16 * KH, TPR = THREADS / KEYS;   // keys of a stage, threads that stage a row
@@ -456,6 +388,7 @@ __device__ __forceinline__ void ga_attn_f32(const GaParams& P) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) stg_stream16_q(orow + 64 * v + 4 * i, f32x4{o[4 * v][i], o[4 * v + 1][i], o[4 * v + 2][i], o[4 * v + 3][i]});
         }
+        if (P.lse && kb == 0 && r0 + c < P.rows) ga_store_lse(P.lse, ((size_t)seq * P.rows + r0 + c) * P.nq + h, M, den);
         const unsigned alone = (unsigned)(b | b >> 16 | b >> 32 | b >> 48) & 0xFFFFu;
         if (alone) ga_rows_alone<float, D>(ga_args(), seq, h, r0, alone, lane);
     }
@@ -771,6 +704,7 @@ __global__ void __launch_bounds__(GA_THREADS, 4) ga_attn_bf16_kernel(const GaPar
             const int rr = x / D, dd = x - rr * D;
             obase[(size_t)(r0 + rr) * P.nq * D + dd] = sO[x] / sA[rr];   // (every row sees at least its own real token: the sum is > 0)
         }
+        if (P.lse && kb == 0 && c < nrows) ga_store_lse(P.lse, ((size_t)seq * P.rows + r0 + c) * P.nq + h, m_run, l_run);
         if (alone) ga_rows_alone<WT, D>(ga_args(), seq, h, r0, alone, lane);
     }
 }
@@ -815,23 +749,6 @@ __global__ void __launch_bounds__(GA_THREADS, 4) ga_attn_bf16_kernel(const GaPar
 // value) 0.6 .. 5.5 % slower; MFMAs and vector instructions in a given alternation (sched_group_barrier) 2 .. 12 % slower.
 // ------------------------------------------------------------------------------------------
 constexpr int GW_ROWS = 32 * GA_WAVES;                     // query rows of a workgroup
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-__device__ __forceinline__ bf16x8 split_hi(const float (&v)[8], unsigned (&hi)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) hi[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-    return __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-}
-__device__ __forceinline__ bf16x8 split_lo(const float (&v)[8], const unsigned (&hi)[4]) {
-    unsigned lo[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        lo[i] = pack_bf16x2(v[2 * i] - __uint_as_float(hi[i] << 16), v[2 * i + 1] - __uint_as_float(hi[i] & 0xFFFF0000u));
-    return __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-}
-
 template <int D>
 __global__ void __launch_bounds__(GA_THREADS, 2) ga_attn_wide_kernel(const GaParams P) {   // two workgroups per compute unit
     constexpr int STEPS = D / 16;                           // MFMA steps of a score tile
@@ -1244,23 +1161,9 @@ __global__ void __launch_bounds__(GA_THREADS, 2) ga_attn_wide_kernel(const GaPar
         lds_sync_wave();
         __builtin_amdgcn_wave_barrier();
     }
+    if (P.lse && half == 0 && r0 + c < P.rows) ga_store_lse(P.lse, ((size_t)seq * P.rows + r0 + c) * P.nq + h, m_run, den);
     const unsigned alone = (unsigned)(zb | zb >> 32);
     if (alone) ga_rows_alone<bf16_t, D>(ga_args(), seq, h, r0, alone, lane);
-}
-
-size_t a256(size_t v) { return (v + 255) & ~(size_t)255; }
-
-int check(const ps_group_attn_args* a) {
-    if (!a) return PS_ERR_NULL;
-    if (a->seqs < 1 || a->tokens < 1 || a->k < 0 || a->n_heads < 1 || a->n_kv_heads < 1 || a->head_dim < 1) return PS_ERR_SHAPE;
-    if (a->dtype != PS_F32 && a->dtype != PS_BF16) return PS_ERR_SHAPE;
-    if (a->n_heads % a->n_kv_heads != 0 || !(a->rope_base > 0.f)) return PS_ERR_SHAPE;
-    if (a->head_dim != 64 && a->head_dim != 128) return PS_ERR_UNSUPPORTED;
-    if (a->k > 15 || (long long)a->tokens + a->k > (1 << 20)) return PS_ERR_UNSUPPORTED;
-    if (a->n_heads > 65535 || a->seqs > 65535) return PS_ERR_UNSUPPORTED;
-    if ((long long)(a->k + 1) * a->n_kv_heads * a->head_dim * 4 > (1LL << 27)) return PS_ERR_UNSUPPORTED;   // 32-bit offsets inside a key tile
-    if (a->dtype == PS_F32 && ((long long)a->tokens * (a->k + 1) + GF_ROWS - 1) / GF_ROWS * a->n_heads > GA_MAX_WG) return PS_ERR_UNSUPPORTED;   // (its rows would be terabytes)
-    return PS_OK;
 }
 
 struct GaLayout { size_t table, k_rot, total; };
@@ -1355,18 +1258,19 @@ GaParams shape(const ps_group_attn_args* a) {
 }   // namespace
 
 extern "C" size_t ps_group_attention_workspace_bytes(const ps_group_attn_args* a) {
-    return check(a) == PS_OK ? layout(a).total : 0;
+    return ga_check(a) == PS_OK ? layout(a).total : 0;
 }
 
-extern "C" int ps_group_attention(const ps_group_attn_args* a, void* stream) {
-    const int st = check(a);
+// (lse: the forward pass for training, else null)
+static int attention(const ps_group_attn_args* a, float* lse, void* stream) {
+    const int st = ga_check(a);
     if (st != PS_OK) return st;
     if (!a->q || !a->k_ || !a->v || !a->out || !a->workspace) return PS_ERR_NULL;
     const GaLayout L = layout(a);
     if (a->workspace_bytes < L.total || ((uintptr_t)a->workspace & 255)) return PS_ERR_WORKSPACE;
     GaParams P = shape(a);
     const GaLaunch G = plan(P, a->dtype, a->head_dim);
-    P.q = a->q; P.k_ = a->k_; P.v = a->v; P.out = a->out;
+    P.q = a->q; P.k_ = a->k_; P.v = a->v; P.out = a->out; P.lse = lse;
     char* ws = (char*)a->workspace;
     P.table = (float2*)(ws + L.table); P.k_rot = ws + L.k_rot;
     hipStream_t s = (hipStream_t)stream;
@@ -1374,9 +1278,17 @@ extern "C" int ps_group_attention(const ps_group_attn_args* a, void* stream) {
     return a->head_dim == 128 ? launch<float, 128>(P, G, s) : launch<float, 64>(P, G, s);
 }
 
+extern "C" int ps_group_attention(const ps_group_attn_args* a, void* stream) { return attention(a, nullptr, stream); }
+
+extern "C" int ps_group_attention_lse(const ps_group_attn_args* a, float* lse, void* stream) {
+    const int st = ga_check(a);
+    if (st != PS_OK) return st;
+    return lse ? attention(a, lse, stream) : (int)PS_ERR_NULL;
+}
+
 // see ps_draft_debug.h
 extern "C" int ps_train_debug_launch(const ps_group_attn_args* a, unsigned* out) {
-    const int st = check(a);
+    const int st = ga_check(a);
     if (st != PS_OK) return st;
     if (!out) return PS_ERR_NULL;
     const GaLaunch G = plan(shape(a), a->dtype, a->head_dim);
