@@ -266,6 +266,232 @@ __global__ void __launch_bounds__(VL_THREADS, 2) vl_grad_kernel(const VlParams P
             }
 }
 
+// ------------------------------------------------------------------------------------------
+// bf16, many rows: tiles of 256 x 256, eight wavefronts (two per SIMD) of 128 x 64 each, 64 elements of the contraction per stage in
+// two LDS buffers of 64 KiB.  A stage is brought in by the memory unit itself (no registers): 1 KiB per request, lanes in
+// the order of the LDS, their source addresses permuted so that rows read together fall into different banks.  Per stage a
+// wavefront reads its operands, asks for the next stage, and multiplies.
+// ------------------------------------------------------------------------------------------
+constexpr int VW_THREADS = 512, VW_TILE = 256, VW_A = VW_TILE * 128, VW_BUF = 2 * VW_A;
+typedef __attribute__((address_space(3))) void lds_void;
+__device__ __forceinline__ void vw_copy(rsrc_t from, unsigned off, unsigned soff, char* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, soff, 0, 0);
+}
+// 256 rows of 128 bytes: chunk j of 16 bytes stands at j ^ (row / 2) % 8
+struct VwRows {
+    rsrc_t src;
+    unsigned off[4];
+    // rows first .. first + 255 of a matrix (rows beyond last: the last), wavefront w's 32 of them
+    __device__ __forceinline__ VwRows(const char* m, size_t first, size_t last, unsigned stride, int wave, int lane) {
+        src = make_rsrc(m + first * stride);
+        const unsigned most = (unsigned)min((size_t)VW_TILE, last - first + 1) - 1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned row = 32 * wave + 8 * i + lane / 8, chunk = (lane & 7) ^ ((row >> 1) & 7);
+            off[i] = min(row, most) * stride + chunk * 16;
+        }
+    }
+    __device__ __forceinline__ void stage(int k, bool half_stage, char* lds, int wave, int lane) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // (a last stage of 32 elements: the other half, which nobody reads, is the same again)
+            const unsigned chunk = (lane & 7) ^ ((((8 * i + lane / 8)) >> 1) & 7);
+            vw_copy(src, half_stage ? off[i] - (chunk & 4) * 16 : off[i], k * 128, lds + (32 * wave + 8 * i) * 128);
+        }
+    }
+};
+
+// A tile's workgroup number -> the tile: workgroups go to the XCDs in turn; an XCD gets a stretch of the order, in which
+// 32 neighbours (its compute units) share four rows' and eight columns' operands
+__device__ __forceinline__ void vw_tile(unsigned id, unsigned nx, unsigned ny, unsigned& x, unsigned& y) {
+    const unsigned n = nx * ny, q = n / 8, r = n % 8, xcd = id % 8;
+    id = xcd * q + min(xcd, r) + id / 8;
+    const unsigned g = id / (4 * nx), h = min(ny - 4 * g, 4u);
+    id -= g * 4 * nx;
+    x = id / h;
+    y = 4 * g + id % h;
+}
+
+__global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlParams P, int nx, int ny) {
+    __shared__ __attribute__((aligned(16))) char smem[2 * VW_BUF];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
+    unsigned tx, ty;
+    vw_tile(blockIdx.x, nx, ny, tx, ty);
+    const int vt = tx * VW_TILE, rt = ty * VW_TILE, wm = wave & 1, wn = wave >> 1;
+    const unsigned rb = P.H * 2;
+    const VwRows A(P.w, P.v0 + vt, P.V - 1, rb, wave, lane), B(P.h, P.row0 + rt, P.row0 + P.rows_c - 1, rb, wave, lane);
+    const int steps = (P.H + 63) / 64;
+    auto stage = [&](int k) __attribute__((always_inline)) {
+        char* b = smem + (k & 1) * VW_BUF;
+        const bool part = k == steps - 1 && (P.H & 32);
+        A.stage(k, part, b, wave, lane);
+        B.stage(k, part, b + VW_A, wave, lane);
+    };
+    f32x16 acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    const int at = c * 128 + ((half ^ ((c >> 1) & 7)) << 4), a0 = 128 * wm * 128 + at, b0 = VW_A + 64 * wn * 128 + at;
+    auto multiply = [&](int k, auto halves, bool more) __attribute__((always_inline)) {
+        const char* b = smem + (k & 1) * VW_BUF;
+        bf16x8 x[4][2 * halves], y[2][2 * halves];
+#pragma unroll
+        for (int t = 0; t < 2 * halves; ++t) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) y[j][t] = __builtin_bit_cast(bf16x8, ld16(b + ((b0 ^ (t << 5)) + j * 4096)));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i][t] = __builtin_bit_cast(bf16x8, ld16(b + ((a0 ^ (t << 5)) + i * 4096)));
+        }
+        if (more) stage(k + 1);
+#pragma unroll
+        for (int t = 0; t < 2 * halves; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][t], y[j][t], acc[i][j], 0, 0, 0);
+    };
+    stage(0);
+    __syncthreads();
+    for (int k = 0; k < P.H / 64; ++k) {
+        multiply(k, std::integral_constant<int, 2>{}, k + 1 < steps);
+        __syncthreads();
+    }
+    if (P.H & 32) {
+        multiply(steps - 1, std::integral_constant<int, 1>{}, false);
+        __syncthreads();
+    }
+    // ---- lane (c, half) holds of row 64 wn + 32 j + c the tokens 128 wm + 32 i + 8 (e / 4) + 4 half + e % 4; they leave by way of the LDS,
+    // rows of 512 bytes, 16-byte piece p at p ^ row % 32
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int rr = 64 * wn + 32 * j + c, r = rt + rr, row = P.row0 + min(r, P.rows_c - 1);
+        const int base = P.v0 + vt + 128 * wm, t = P.targets[row] - base - 4 * half, end = P.V - base - 4 * half;
+        const float ref = -P.tl[row] * VL_LOG2E - VL_SHIFT;
+        float sum[2] = {0.f, 0.f}, top = -INFINITY;
+        // (a target among the wavefront's tokens, or the vocabulary's end: those count nothing)
+        if (__any(((unsigned)(t + 4) < 132u) | (end < 128))) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int tok = 32 * i + 8 * (e / 4) + e % 4;
+                    acc[i][j][e] = tok != t && tok < end ? acc[i][j][e] : -INFINITY;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float y = fmaf(acc[i][j][4 * q + e], VL_LOG2E, ref);
+                    top = fmaxf(top, y);
+                    v[e] = __builtin_amdgcn_exp2f(y);
+                    sum[e & 1] += v[e];
+                }
+                if (P.x) {
+                    const int piece = 16 * wm + 4 * i + q;
+                    *reinterpret_cast<u32x2*>(smem + rr * 512 + ((piece ^ (rr & 31)) << 4) + 8 * half) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                }
+            }
+        const float mine = sum[0] + sum[1];
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mine), __float_as_uint(mine), false, false);
+        if (r < P.rows_c) {
+            if (top > VL_FAR && top < INFINITY) P.far[row] = 1;
+            if (half == 0) P.sums[(size_t)r * P.nsum + (P.v0 + vt) / 128 + wm] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+        }
+    }
+    if (!P.x) return;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        const int rr = 32 * wave + 2 * i + (lane >> 5), r = rt + rr, p = lane & 31;
+        const uint4 v = ld16(smem + rr * 512 + ((p ^ (rr & 31)) << 4));
+        if (r < P.rows_c) *reinterpret_cast<uint4*>(P.x + ((size_t)r * P.ldx + vt + 8 * p) * 2) = v;
+    }
+}
+
+__global__ void __launch_bounds__(VW_THREADS, 2) vl_grad_wide_kernel(const VlParams P, int nx, int ny) {
+    __shared__ __attribute__((aligned(16))) char smem[2 * VW_BUF];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
+    unsigned tx, ty;
+    vw_tile(blockIdx.x, nx, ny, tx, ty);
+    const int split = blockIdx.y, ct = tx * VW_TILE, rt = ty * VW_TILE, wm = wave & 1, wn = wave >> 1;
+    const unsigned rb = P.H * 2;
+    const VwRows A(P.x, rt, P.rows_c - 1, P.ldx * 2, wave, lane);
+    const int k0 = split * (P.split_n / 64), k1 = min((split + 1) * P.split_n, (P.nv + 63) / 64 * 64) / 64;
+    // W: 64 rows of 512 bytes (columns beyond H: the last), wavefront w's 8 of them; 32-byte chunk j stands at j ^ 2 f(row),
+    // f = row % 4 + 4 (row / 8 % 2), so that the eight rows of a transposed read fall into different banks
+    unsigned col[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned row = 8 * wave + 2 * i + (lane >> 5), f = (row & 3) | ((row >> 3 & 1) << 2), chunk = ((lane & 31) >> 1) ^ (f << 1);
+        col[i] = min((unsigned)ct * 2 + chunk * 32 + (lane & 1) * 16, rb - 16);
+    }
+    auto stage = [&](int k) __attribute__((always_inline)) {
+        char* b = smem + (k & 1) * VW_BUF;
+        A.stage(k, false, b, wave, lane);
+        const int v = P.v0 + 64 * k;
+        const rsrc_t src = make_rsrc(P.w + (size_t)v * rb);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vw_copy(src, (unsigned)min(8 * wave + 2 * i + (lane >> 5), P.V - 1 - v) * rb + col[i], 0, b + VW_A + (8 * wave + 2 * i) * 512);
+    };
+    if (k0 < k1) stage(k0);
+    f32x16 acc[4][2];
+    float* out = P.acc + (size_t)split * P.rows_c * P.H;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = rt + 128 * wm + 32 * i + 8 * (e / 4) + 4 * half + e % 4, x = ct + 64 * wn + 32 * j + c;
+                acc[i][j][e] = P.first ? 0.f : out[(size_t)min(r, P.rows_c - 1) * P.H + min(x, P.H - 1)];
+            }
+    const int a0 = 128 * wm * 128 + c * 128 + ((half ^ ((c >> 1) & 7)) << 4);
+    const int vkey = (lane & 15) >> 2, vhi = (lane >> 4) & 1, f = vkey | half << 2;
+    const int b0 = VW_A + (8 * half + vkey) * 512 + ((vhi ^ (f << 1)) << 5) + (lane & 3) * 8;
+    __syncthreads();
+    for (int k = k0; k < k1; ++k) {
+        const char* b = smem + (k & 1) * VW_BUF;
+        bf16x8 x[4][4], y[2][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const char* a = b + (b0 ^ ((4 * wn + 2 * j) << 5)) + t * 16 * 512;
+                const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a), w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 4 * 512));
+                y[j][t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, w, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i][t] = __builtin_bit_cast(bf16x8, ld16(b + ((a0 ^ (t << 5)) + i * 4096)));
+        }
+        if (k + 1 < k1) stage(k + 1);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][t], y[j][t], acc[i][j], 0, 0, 0);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = rt + 128 * wm + 32 * i + 8 * (e / 4) + 4 * half + e % 4, x = ct + 64 * wn + 32 * j + c;
+                if (r < P.rows_c && x < P.H) out[(size_t)r * P.H + x] = acc[i][j][e];
+            }
+}
+
 // sum over the workgroup in a fixed order, for every thread
 __device__ __forceinline__ float vl_block_sum(float v, float* s, int tid) {
     v = wave_sum(v);
@@ -394,45 +620,62 @@ int check(const ps_vocab_loss_args* a) {
 }
 
 // How a call is cut: chunks of rows, pieces of the vocabulary, parts of a piece's tokens in the second product
+constexpr long long VL_PIECE_BYTES = 288ll << 20;            // of exponentials at a time
 struct VlPlan {
-    int rows_c, piece, splits, split_n, nsum;
+    bool wide;
+    int tile, rows_c, piece, nsum;
     size_t tl, far, sums, acc, x, total;
 };
+// where a chunk's tiles of the second product leave workgroups idle, several share a tile's tokens, of which each keeps at least 512
+int splits_of(const VlPlan& L, int hidden, int rows) {
+    const int tiles = (rows + L.tile - 1) / L.tile * ((hidden + L.tile - 1) / L.tile);
+    return std::max(1, std::min((L.wide ? 256 : 512) / tiles, L.piece / 512));
+}
 VlPlan plan(const ps_vocab_loss_args* a) {
-    const int esz = a->dtype == PS_BF16 ? 2 : 4, tile = VL_TILE;
+    const int esz = a->dtype == PS_BF16 ? 2 : 4;
     const bool grad = a->d_hidden != nullptr;
     VlPlan L;
-    const int chunks = (a->rows + 4095) / 4096;
-    L.rows_c = std::min(a->rows, ((a->rows + chunks - 1) / chunks + tile - 1) / tile * tile);
-    const int row_tiles = (L.rows_c + tile - 1) / tile, vocab = (a->vocab + tile - 1) / tile * tile;
-    const int pieces = grad ? (int)(((long long)L.rows_c * vocab * esz + (128 << 20) - 1) / (128 << 20)) : 1;
-    L.piece = ((vocab + pieces - 1) / pieces + tile - 1) / tile * tile;
-    // few tiles of the second product: several workgroups share a tile's tokens, of which each keeps at least 512
-    const int tiles = row_tiles * ((a->hidden + tile - 1) / tile);
-    L.splits = grad ? std::max(1, std::min(512 / tiles, L.piece / 512)) : 1;
-    L.split_n = ((L.piece + L.splits - 1) / L.splits + tile - 1) / tile * tile;
-    L.splits = (L.piece + L.split_n - 1) / L.split_n;
-    L.nsum = vocab / 64;
+    L.wide = a->dtype == PS_BF16 && a->rows > 256;
+    L.tile = L.wide ? VW_TILE : VL_TILE;
+    // rows at a time: as many as give the second product one tile for every workgroup that can run (two or one per compute unit)
+    L.rows_c = std::min(a->rows, std::max(1, (L.wide ? 256 : 512) / ((a->hidden + L.tile - 1) / L.tile)) * L.tile);
+    const int vocab = (a->vocab + L.tile - 1) / L.tile * L.tile;
+    const int pieces = grad ? (int)(((long long)L.rows_c * vocab * esz + VL_PIECE_BYTES - 1) / VL_PIECE_BYTES) : 1;
+    L.piece = ((vocab + pieces - 1) / pieces + L.tile - 1) / L.tile * L.tile;
+    L.nsum = vocab / (L.tile / 2);
+    size_t acc = 0;                                          // of all chunks (whole ones, the last)
+    if (grad)
+        for (const int rows : {L.rows_c, a->rows % L.rows_c})
+            if (rows > 0) acc = std::max(acc, (size_t)splits_of(L, a->hidden, rows) * rows * a->hidden * 4);
     L.tl = 0;
     L.far = L.tl + a256((size_t)a->rows * 4);
     L.sums = L.far + a256((size_t)a->rows * 4);
     L.acc = L.sums + a256((size_t)L.rows_c * L.nsum * 4);
-    L.x = L.acc + (grad ? a256((size_t)L.splits * L.rows_c * a->hidden * 4) : 0);
+    L.x = L.acc + a256(acc);
     L.total = L.x + (grad ? a256((size_t)L.rows_c * L.piece * esz) : 0);
     return L;
 }
 
 template <typename WT> int run(VlParams P, const VlPlan& L, hipStream_t s) {
     hipLaunchKernelGGL((vl_target_kernel<WT>), dim3((P.rows + 3) / 4), dim3(VL_THREADS), 0, s, P);
+    const unsigned cols = (P.H + L.tile - 1) / L.tile;
     for (P.row0 = 0; P.row0 < P.rows; P.row0 += L.rows_c) {
         P.rows_c = std::min(L.rows_c, P.rows - P.row0);
-        const unsigned row_tiles = (P.rows_c + VL_TILE - 1) / VL_TILE;
+        const unsigned row_tiles = (P.rows_c + L.tile - 1) / L.tile;
+        P.splits = splits_of(L, P.H, P.rows_c);
+        P.split_n = ((L.piece + P.splits - 1) / P.splits + L.tile - 1) / L.tile * L.tile;
         for (P.v0 = 0; P.v0 < P.V; P.v0 += L.piece) {
             P.nv = std::min(L.piece, P.V - P.v0);
             P.first = P.v0 == 0;
-            hipLaunchKernelGGL((vl_score_kernel<WT>), dim3((P.nv + VL_TILE - 1) / VL_TILE, row_tiles), dim3(VL_THREADS), 0, s, P);
-            if (P.d_hidden)
-                hipLaunchKernelGGL((vl_grad_kernel<WT>), dim3((P.H + VL_TILE - 1) / VL_TILE, row_tiles, L.splits), dim3(VL_THREADS), 0, s, P);
+            const unsigned tokens = (P.nv + L.tile - 1) / L.tile;
+            if (L.wide) {
+                hipLaunchKernelGGL(vl_score_wide_kernel, dim3(tokens * row_tiles), dim3(VW_THREADS), 0, s, P, (int)tokens, (int)row_tiles);
+                if (P.d_hidden)
+                    hipLaunchKernelGGL(vl_grad_wide_kernel, dim3(cols * row_tiles, P.splits), dim3(VW_THREADS), 0, s, P, (int)cols, (int)row_tiles);
+            } else {
+                hipLaunchKernelGGL((vl_score_kernel<WT>), dim3(tokens, row_tiles), dim3(VL_THREADS), 0, s, P);
+                if (P.d_hidden) hipLaunchKernelGGL((vl_grad_kernel<WT>), dim3(cols, row_tiles, P.splits), dim3(VL_THREADS), 0, s, P);
+            }
         }
         hipLaunchKernelGGL((vl_finish_kernel<WT>), dim3(P.rows_c), dim3(VL_THREADS), 0, s, P);
     }
@@ -454,7 +697,7 @@ extern "C" int ps_vocab_loss(const ps_vocab_loss_args* a, void* stream) {
     char* ws = (char*)a->workspace;
     VlParams P = {};
     P.rows = a->rows; P.H = a->hidden; P.V = a->vocab;
-    P.ldx = L.piece; P.nsum = L.nsum; P.splits = L.splits; P.split_n = L.split_n;
+    P.ldx = L.piece; P.nsum = L.nsum;
     P.h = (const char*)a->h; P.w = (const char*)a->w_lm; P.targets = a->targets; P.weights = a->weights;
     P.loss = a->loss; P.d_hidden = (char*)a->d_hidden;
     P.tl = (float*)(ws + L.tl); P.far = (int*)(ws + L.far); P.sums = (float*)(ws + L.sums);

@@ -90,7 +90,10 @@ def _check(h, w, t, weights, dtype, loss, d, grad=True):
 CASES = [  # dtype, rows, hidden, vocab
     ("f32", 1, 16, 1), ("bf16", 1, 32, 1), ("bf16", 1, 32, 2), ("f32", 3, 48, 129),
     ("f32", 130, 256, 1024), ("bf16", 5, 512, 2064), ("bf16", 127, 96, 127), ("bf16", 129, 160, 1000), ("bf16", 257, 288, 4099),
-    ("f32", 300, 80, 513), ("bf16", 1218, 1056, 3001), ("bf16", 64, 4096, 32000), ("bf16", 700, 512, 20000), ("f32", 33, 512, 2064)]
+    ("f32", 300, 80, 513), ("bf16", 1218, 1056, 3001), ("bf16", 64, 4096, 32000), ("bf16", 700, 512, 20000), ("f32", 33, 512, 2064),
+    # tiles of 256 x 256: one row and one token more than a tile, half a stage at the end, one stage and less, several chunks of rows, pieces
+    ("bf16", 513, 64, 257), ("bf16", 511, 32, 255), ("bf16", 300, 2080, 770), ("bf16", 1030, 4096, 1000), ("bf16", 4200, 4096, 600),
+    ("bf16", 2500, 8192, 700), ("bf16", 1400, 256, 128256)]
 
 
 @pytest.mark.parametrize("dtype,rows,hidden,vocab", CASES)
