@@ -28,7 +28,7 @@ struct GbParams {
     float2* table;        // [T + k][d / 2] cosines and sines
     char* k_rot;          // [seqs][nkv][rows][d], storage type
     char* q_rot;          // [parts][seqs][nq][rows][d], storage type: times log2(e) / sqrt(d); bf16: high parts, low parts
-    float2* stats;        // [seqs][nq][rows]: -lse / ln 2, -delta
+    float *lse2, *delta;  // [seqs][nq][rows]: -lse / ln 2, -sum of d_out out
 };
 template <typename WT> struct GbTraits { static constexpr int PARTS = Traits<WT>::BF ? 2 : 1; };
 
@@ -89,7 +89,10 @@ __global__ void __launch_bounds__(256) gb_prep_kernel(const GbParams P) {
         for (int e = 0; e < 4; ++e) sum += oa[e] * da[e] + ob[e] * db[e];
 #pragma unroll
         for (int m = Q4 / 2; m >= 1; m >>= 1) sum += __shfl_xor(sum, m, 64);
-        if (g4 == 0) P.stats[to] = make_float2(-P.lse[at] * 1.4426950408889634f, -sum);
+        if (g4 == 0) {
+            P.lse2[to] = -P.lse[at] * 1.4426950408889634f;
+            P.delta[to] = -sum;
+        }
     }
 }
 
@@ -100,12 +103,18 @@ __global__ void __launch_bounds__(256) gb_prep_kernel(const GbParams P) {
 template <typename WT, int D> struct GbTile {
     static constexpr int ESZ = Traits<WT>::ESZ, ROWB = D * ESZ, BYTES = 32 * ROWB, STEPS = ROWB / 32, NJ = D / 32;
     static constexpr bool BF = Traits<WT>::BF;
-    static constexpr int U = BYTES / (GB_THREADS * 16), PPR = ROWB / 16;   // 16-byte pieces per thread, per row
-    static constexpr int WU = BYTES / (64 * 16);                           // ... per lane of a single wavefront
+    static constexpr int PPR = ROWB / 16;                    // 16-byte pieces of a row
     static __device__ __forceinline__ int f(int row) { return ROWB == 128 ? (row >> 1) & 3 : row & 7; }
     static __device__ __forceinline__ int at(int row, int piece) { return row * ROWB + (((piece >> 1) ^ f(row)) << 5) + (piece & 1) * 16; }
 
     int rd, cd;           // this lane's places: of its row (chunk 0), of its column (tile 0, keys 0 ..)
+    // the same, but the compiler does not know: what is derived from them is worked out where it is needed (an instruction each) and does
+    // not occupy registers across the loop
+    __device__ __forceinline__ GbTile here() const {
+        GbTile t = *this;
+        asm volatile("" : "+v"(t.rd), "+v"(t.cd));
+        return t;
+    }
     __device__ __forceinline__ GbTile(int lane) {
         const int c = lane & 31, half = lane >> 5;
         rd = at(c, half);
@@ -140,62 +149,71 @@ template <typename WT, int D> struct GbTile {
     }
 };
 
-// scores += rows . own: the lane's i-th is that of row 8 (i / 4) + i % 4 + 4 half and the lane's own query or key
-template <typename WT, int D>
-__device__ __forceinline__ void gb_scores(const GbTile<WT, D>& L, const char* tile, const uint4 (&own)[GbTile<WT, D>::STEPS], f32x16& x) {
+// scores += rows . own: the lane's i-th is that of row 8 (i / 4) + i % 4 + 4 half and the lane's own query or key, whose
+// operands own(step) gives
+template <typename WT, int D, typename F>
+__device__ __forceinline__ void gb_scores(const GbTile<WT, D>& at, const char* tile, F own, f32x16& x) {
+    const GbTile<WT, D> L = at.here();
 #pragma unroll
     for (int st = 0; st < GbTile<WT, D>::STEPS; ++st) {
-        const uint4 a = L.row(tile, st);
+        const uint4 a = L.row(tile, st), b = own(L, st);
         if constexpr (Traits<WT>::BF) {
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, own[st]), x, 0, 0, 0);
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), x, 0, 0, 0);
         } else {
-            const f32x4 u = __builtin_bit_cast(f32x4, a), w = __builtin_bit_cast(f32x4, own[st]);
+            const f32x4 u = __builtin_bit_cast(f32x4, a), w = __builtin_bit_cast(f32x4, b);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(u[e], w[e], x, 0, 0, 0);
         }
     }
 }
-// y^T += rows^T . p, p as gb_scores leaves it
+// p as gb_scores leaves it, as operand (bf16: rounded)
+template <typename WT> struct GbOperand {
+    bf16x8 b[2];
+    __device__ __forceinline__ GbOperand(const f32x16& p) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            b[m] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(p[8 * m], p[8 * m + 1]), pack_bf16x2(p[8 * m + 2], p[8 * m + 3]),
+                                                         pack_bf16x2(p[8 * m + 4], p[8 * m + 5]), pack_bf16x2(p[8 * m + 6], p[8 * m + 7])));
+    }
+};
+template <> struct GbOperand<float> {
+    f32x16 b;
+    __device__ __forceinline__ GbOperand(const f32x16& p) : b(p) {}
+};
+// y^T += rows^T . p
 template <typename WT, int D, bool CLEAN>
-__device__ __forceinline__ void gb_products(const GbTile<WT, D>& L, const char* tile, const f32x16& p, f32x16 (&y)[D / 32]) {
+__device__ __forceinline__ void gb_products(const GbTile<WT, D>& at, const char* tile, const GbOperand<WT>& p, f32x16 (&y)[D / 32]) {
+    const GbTile<WT, D> L = at.here();
     if constexpr (Traits<WT>::BF) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            uint4 b;
-            b.x = pack_bf16x2(p[8 * m], p[8 * m + 1]);
-            b.y = pack_bf16x2(p[8 * m + 2], p[8 * m + 3]);
-            b.z = pack_bf16x2(p[8 * m + 4], p[8 * m + 5]);
-            b.w = pack_bf16x2(p[8 * m + 6], p[8 * m + 7]);
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j)
-                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(L.template column<CLEAN>(tile, j, m), __builtin_bit_cast(bf16x8, b), y[j], 0, 0, 0);
-        }
+            for (int j = 0; j < D / 32; ++j) {
+                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(L.template column<CLEAN>(tile, j, m), p.b[m], y[j], 0, 0, 0);
+                if constexpr (CLEAN) __builtin_amdgcn_sched_barrier(0);   // (few tiles come here: no registers for operands ahead)
+            }
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) y[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(L.template element<CLEAN>(tile, j, i), p[i], y[j], 0, 0, 0);
+            for (int j = 0; j < D / 32; ++j) y[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(L.template element<CLEAN>(tile, j, i), p.b[i], y[j], 0, 0, 0);
     }
 }
-// rows first + (own thread's) .. of a matrix with `stride` bytes between rows, rows beyond lo .. hi replaced by the nearest
-template <typename WT, int D, int THREADS, int U>
-__device__ __forceinline__ void gb_load(const char* base, size_t stride, int first, int step, int lo, int hi, int t, uint4 (&x)[U]) {
-    constexpr int PPR = GbTile<WT, D>::PPR;
+typedef __attribute__((address_space(3))) void lds_void;
+__device__ __forceinline__ void gb_copy(rsrc_t from, unsigned off, char* to) { __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, 0, 0, 0); }
+// A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: this wavefront's share of WAVES, 1 KiB per request
+template <typename WT, int D, int WAVES>
+__device__ __forceinline__ void gb_stage(const char* m, unsigned stride, int most, char* tile, int wave, int lane) {
+    constexpr int ROWB = GbTile<WT, D>::ROWB, PPR = ROWB / 16, RPI = 1024 / ROWB, N = 32 / RPI;   // rows per request, requests
+    const rsrc_t src = make_rsrc(m);
+    if (N < WAVES && wave >= N) return;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int i = t + THREADS * u, row = min(max(first + i / PPR, lo), hi) * step;
-        x[u] = ld16_q(base + (size_t)(unsigned)row * stride + (i % PPR) * 16);
+    for (int u = 0; u < (N + WAVES - 1) / WAVES; ++u) {
+        const int i = wave + u * WAVES, row = RPI * i + lane / PPR, slot = lane % PPR, piece = (((slot >> 1) ^ GbTile<WT, D>::f(row)) << 1) | (slot & 1);
+        gb_copy(src, (unsigned)min(row, most) * stride + piece * 16, tile + i * 1024);
     }
 }
-template <typename WT, int D, int THREADS, int U>
-__device__ __forceinline__ void gb_store(char* tile, int t, const uint4 (&x)[U]) {
-    constexpr int PPR = GbTile<WT, D>::PPR;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int i = t + THREADS * u;
-        *reinterpret_cast<uint4*>(tile + GbTile<WT, D>::at(i / PPR, i % PPR)) = x[u];
-    }
-}
+
 // a lane's row as operand, straight from memory
 template <typename WT, int D> __device__ __forceinline__ void gb_own_rows(const char* row, int half, uint4 (&x)[GbTile<WT, D>::STEPS]) {
 #pragma unroll
@@ -241,12 +259,13 @@ __device__ __forceinline__ void gb_write(char* row, const float2* turn, float sc
 // which the queries see their own groups' [MASK] rows, then the real tokens up to the last group.
 // ------------------------------------------------------------------------------------------
 template <typename WT, int D>
-__global__ void __launch_bounds__(GB_THREADS) gb_dq_kernel(const GbParams P) {
+__global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2) gb_dq_kernel(const GbParams P) {
     typedef GbTile<WT, D> Tile;
     constexpr int ESZ = Traits<WT>::ESZ, PARTS = GbTraits<WT>::PARTS, NJ = D / 32, BUF = 2 * Tile::BYTES;
     __shared__ __attribute__((aligned(16))) char smem[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
-    const int K1 = P.k + 1, blk = gridDim.x - 1 - blockIdx.x, h = blockIdx.y, seq = blockIdx.z, hk = h / P.group;
+    // (the rows with the most keys start first; neighbours, which go to different XCDs, take different heads)
+    const int K1 = P.k + 1, blk = gridDim.y - 1 - blockIdx.y, h = blockIdx.x, seq = blockIdx.z, hk = h / P.group;
     const int R0 = GB_ROWS * blk, r0 = R0 + 32 * wave, r_last = min(R0 + GB_ROWS, P.rows) - 1, g_last = gb_group(P, r_last);
     const bool active = r0 < P.rows;
     const int n_own = P.k > 0 ? GB_WAVES + 1 : 0, n_tiles = n_own + g_last / 32 + 1;
@@ -255,61 +274,65 @@ __global__ void __launch_bounds__(GB_THREADS) gb_dq_kernel(const GbParams P) {
     const char* krows = P.k_rot + ((size_t)seq * P.nkv + hk) * P.rows * D * ESZ;
     const char* vrows = P.v + ((size_t)seq * P.rows * P.nkv + hk) * D * ESZ;
     const size_t vstride = (size_t)P.nkv * D * ESZ;
-    uint4 sk[Tile::U], sv[Tile::U];
-    auto load = [&](int t) __attribute__((always_inline)) {
+    auto stage = [&](int t) __attribute__((always_inline)) {
         const bool own = t < n_own;
-        const int first = own ? R0 - 32 + 32 * t : 32 * (t - n_own), hi = own ? r_last : g_last, step = own ? 1 : K1;
-        gb_load<WT, D, GB_THREADS>(krows, (size_t)D * ESZ, first, step, 0, hi, tid, sk);
-        gb_load<WT, D, GB_THREADS>(vrows, vstride, first, step, 0, hi, tid, sv);
+        const int hi = own ? r_last : g_last, first = min(max(own ? R0 - 32 + 32 * t : 32 * (t - n_own), 0), hi), step = own ? 1 : K1;
+        char* b = smem + (t & 1) * BUF;
+        gb_stage<WT, D, GB_WAVES>(krows + (size_t)first * step * D * ESZ, step * D * ESZ, hi - first, b, wave, lane);
+        gb_stage<WT, D, GB_WAVES>(vrows + (size_t)first * step * vstride, step * (unsigned)vstride, hi - first, b + Tile::BYTES, wave, lane);
     };
-    auto store = [&](int t) __attribute__((always_inline)) {
-        gb_store<WT, D, GB_THREADS>(smem + (t & 1) * BUF, tid, sk);
-        gb_store<WT, D, GB_THREADS>(smem + (t & 1) * BUF + Tile::BYTES, tid, sv);
-    };
-    load(0);
+    stage(0);
     const size_t qat = ((size_t)seq * P.nq + h) * P.rows + qrow, part = (size_t)P.seqs * P.nq * P.rows * D * ESZ;
     uint4 q[PARTS][Tile::STEPS], d_o[Tile::STEPS];
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) gb_own_rows<WT, D>(P.q_rot + p * part + qat * D * ESZ, half, q[p]);
     gb_own_rows<WT, D>(P.d_out + (((size_t)seq * P.rows + qrow) * P.nq + h) * D * ESZ, half, d_o);
-    const float2 st = P.stats[qat];
+    const float2 st = make_float2(P.lse2[qat], P.delta[qat]);
     f32x16 y[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 16; ++i) y[j][i] = 0.f;
-    store(0);
-    if (n_tiles > 1) load(1);
     __syncthreads();
-    for (int t = 0; t < n_tiles; ++t) {
-        if (t + 1 < n_tiles) store(t + 1);
-        if (t + 2 < n_tiles) load(t + 2);
+    // one key tile; masked: keys lo .. hi of it (counted from 4 half) are seen
+    auto work = [&](int t, auto masked, int lo, int hi) __attribute__((always_inline)) {
         const char *kt = smem + (t & 1) * BUF, *vt = kt + Tile::BYTES;
-        const bool own = t < n_own;
-        const int first = own ? R0 - 32 + 32 * t : 32 * (t - n_own);
-        // (own rows: the wavefront's own tile and, where its first row is not the first of its group, the one before)
-        const bool busy = active && (own ? t == wave + 1 || (t == wave && wg0 * K1 != r0) : first <= wg1);
-        if (busy) {
-            f32x16 s, dp;
+        float lse = st.x, delta = st.y;
+        asm volatile("" : "+v"(lse), "+v"(delta));          // (32 copies of them would be kept in registers across the loop)
+        f32x16 s, dp;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) { s[i] = st.x; dp[i] = st.y; }
+        for (int i = 0; i < 16; ++i) s[i] = lse;
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) gb_scores<WT, D>(L, kt, q[p], s);
-            gb_scores<WT, D>(L, vt, d_o, dp);
-            if (!own && first + 31 <= wg0) {
+        for (int p = 0; p < PARTS; ++p) gb_scores<WT, D>(L, kt, [&](const Tile&, int t) __attribute__((always_inline)) { return q[p][t]; }, s);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * dp[i];
-                gb_products<WT, D, false>(L, kt, s, y);
-            } else {
-                const int lo = (own ? qg * K1 + 1 : 0) - first - 4 * half, hi = (own ? qrow : qg) - first - 4 * half;
+        for (int i = 0; i < 16; ++i) dp[i] = delta;
+        gb_scores<WT, D>(L, vt, [&](const Tile&, int t) __attribute__((always_inline)) { return d_o[t]; }, dp);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = 8 * (i / 4) + i % 4;
-                    s[i] = key >= lo && key <= hi ? __builtin_amdgcn_exp2f(s[i]) * dp[i] : 0.f;
-                }
-                gb_products<WT, D, true>(L, kt, s, y);
-            }
+        for (int i = 0; i < 16; ++i) {
+            const int key = 8 * (i / 4) + i % 4;
+            const float x = __builtin_amdgcn_exp2f(s[i]) * dp[i];
+            s[i] = !masked || (key >= lo && key <= hi) ? x : 0.f;
         }
+        gb_products<WT, D, masked>(L, kt, s, y);
+    };
+    int t = 0;
+    for (; t < n_own; ++t) {
+        if (t + 1 < n_tiles) stage(t + 1);
+        // (the wavefront's own rows and, where its first row is not the first of its group, the tile before)
+        const int first = R0 - 32 + 32 * t + 4 * half;
+        if (active && (t == wave + 1 || (t == wave && wg0 * K1 != r0))) work(t, std::true_type{}, qg * K1 + 1 - first, qrow - first);
+        __syncthreads();
+    }
+    // real tokens: tiles that all of the wavefront's queries see, some of them, none
+    for (const int end = active ? n_own + (wg0 + 1) / 32 : n_own; t < end; ++t) {
+        if (t + 1 < n_tiles) stage(t + 1);
+        work(t, std::false_type{}, 0, 0);
+        __syncthreads();
+    }
+    for (; t < n_tiles; ++t) {
+        if (t + 1 < n_tiles) stage(t + 1);
+        const int first = 32 * (t - n_own);
+        if (active && first <= wg1) work(t, std::true_type{}, -first - 4 * half, qg - first - 4 * half);
         __syncthreads();
     }
     if (r0 + c < P.rows)
@@ -317,12 +340,16 @@ __global__ void __launch_bounds__(GB_THREADS) gb_dq_kernel(const GbParams P) {
 }
 
 // ------------------------------------------------------------------------------------------
-// A wavefront's 32 keys: their rows as operands, their gradients; one tile of 32 query rows at a time.
+// Gradients of keys and values.  A wavefront owns 32 keys (rows as operands, gradients as accumulators) and takes a tile of 32 query rows
+// at a time.  A workgroup is KW wavefronts of keys by two of rows: a stage holds two row tiles (rotated queries' parts, d_out,
+// statistics), brought in by the memory unit itself; the two row wavefronts' sums meet in the LDS at the end.
+// bf16, head_dim 128: the values' rows stay in LDS, so that two wavefronts per SIMD find room for everything else in their 256 registers.
 // ------------------------------------------------------------------------------------------
-template <typename WT, int D> struct GbKeys {
+template <typename WT, int D, bool V_LDS> struct GbKeys {
     typedef GbTile<WT, D> Tile;
     static constexpr int PARTS = GbTraits<WT>::PARTS, NJ = D / 32;
-    uint4 kf[Tile::STEPS], vf[Tile::STEPS];
+    uint4 kf[Tile::STEPS], vf[V_LDS ? 1 : Tile::STEPS];
+    const char* v_tile;
     f32x16 dk[NJ], dv[NJ];
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -330,20 +357,27 @@ template <typename WT, int D> struct GbKeys {
 #pragma unroll
             for (int i = 0; i < 16; ++i) { dk[j][i] = 0.f; dv[j][i] = 0.f; }
     }
-    // buf: the tiles of the rotated queries' parts, then of d_out; stats: the rows' (-lse / ln 2, -delta); the lane's key is seen by
-    // rows lo .. hi of the tile (counted from 4 half), all of them if not masked
-    template <bool MASKED> __device__ __forceinline__ void step(const Tile& L, const char* buf, const float2* stats, int half, int lo, int hi) {
+    // buf: the tiles of the rotated queries' parts, then of d_out; stats: the 32 rows' -lse / ln 2, then (behind `two` floats) -delta; the lane's
+    // key is seen by rows lo .. hi of the tile (counted from 4 half), all of them if not masked
+    template <bool MASKED> __device__ __forceinline__ void step(const Tile& L, const char* buf, const float* stats, int two, int half, int lo, int hi) {
         f32x16 s, dp;
+        auto start = [&](const float* x, f32x16& y) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float2 x = stats[8 * (i / 4) + i % 4 + 4 * half];
-            s[i] = x.x;
-            dp[i] = x.y;
-        }
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(x + 8 * q + 4 * half);
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) gb_scores<WT, D>(L, buf + p * Tile::BYTES, kf, s);
+                for (int e = 0; e < 4; ++e) y[4 * q + e] = v[e];
+            }
+        };
+        start(stats, s);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) gb_scores<WT, D>(L, buf + p * Tile::BYTES, [&](const Tile&, int t) __attribute__((always_inline)) { return kf[t]; }, s);
         const char* dt = buf + PARTS * Tile::BYTES;
-        gb_scores<WT, D>(L, dt, vf, dp);
+        start(stats + two, dp);
+        gb_scores<WT, D>(L, dt, [&](const Tile& l, int t) __attribute__((always_inline)) {
+            if constexpr (V_LDS) return l.row(v_tile, t);
+            else return vf[t];
+        }, dp);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int row = 8 * (i / 4) + i % 4;
@@ -352,108 +386,193 @@ template <typename WT, int D> struct GbKeys {
             s[i] = p;
             dp[i] = in ? p * dp[i] : 0.f;
         }
-        gb_products<WT, D, MASKED>(L, dt, s, dv);
+        const GbOperand<WT> p(s), ds(dp);
+        gb_products<WT, D, MASKED>(L, dt, p, dv);
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) gb_products<WT, D, MASKED>(L, buf + p * Tile::BYTES, dp, dk);
-    }
-    __device__ __forceinline__ void write(const GbParams& P, int seq, int hk, int row, int pos, int half) const {
-        const size_t at = (((size_t)seq * P.rows + row) * P.nkv + hk) * D * Traits<WT>::ESZ;
-        gb_write<WT, D>(P.d_k + at, P.table + (size_t)pos * (D / 2), 0.6931471805599453f, half, dk);   // (the queries carry log2(e) / sqrt(d))
-        gb_write<WT, D>(P.d_v + at, nullptr, 1.f, half, dv);
+        for (int q = 0; q < PARTS; ++q) gb_products<WT, D, MASKED>(L, buf + q * Tile::BYTES, ds, dk);
     }
 };
-
-// Gradients of real tokens' keys and values: 128 tokens per workgroup, 32 per wavefront, and all rows from the first token's group on,
-// of every query head that shares the kv head.
 template <typename WT, int D>
-__global__ void __launch_bounds__(GB_THREADS) gb_dkv_kernel(const GbParams P) {
-    typedef GbTile<WT, D> Tile;
-    constexpr int ESZ = Traits<WT>::ESZ, PARTS = GbTraits<WT>::PARTS, OFF_S = (PARTS + 1) * Tile::BYTES, BUF = OFF_S + 32 * 8;
-    __shared__ __attribute__((aligned(16))) char smem[2 * BUF];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
-    const int K1 = P.k + 1, hk = blockIdx.y, seq = blockIdx.z;
-    const int t0 = GB_ROWS * blockIdx.x, w0 = t0 + 32 * wave, key = min(w0 + c, P.T - 1);
-    const int first_row = t0 * K1, per_head = (P.rows - first_row + 31) / 32, n_tiles = per_head * P.group;
-    const Tile L(lane);
-    const size_t part = (size_t)P.seqs * P.nq * P.rows * D * ESZ, ostride = (size_t)P.nq * D * ESZ;
-    uint4 sq[PARTS][Tile::U], so[Tile::U];
-    float2 ss;
-    int load_head = 0, load_tile = 0;
-    auto load = [&]() __attribute__((always_inline)) {       // the next tile, head by head
-        const int h = hk * P.group + load_head, first = first_row + 32 * load_tile;
-        const size_t at = ((size_t)seq * P.nq + h) * P.rows;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) gb_load<WT, D, GB_THREADS>(P.q_rot + p * part + at * D * ESZ, (size_t)D * ESZ, first, 1, 0, P.rows - 1, tid, sq[p]);
-        gb_load<WT, D, GB_THREADS>(P.d_out + ((size_t)seq * P.rows * P.nq + h) * D * ESZ, ostride, first, 1, 0, P.rows - 1, tid, so);
-        ss = P.stats[at + min(first + (tid & 31), P.rows - 1)];
-        if (++load_tile == per_head) { load_tile = 0; ++load_head; }
-    };
-    auto store = [&](int t) __attribute__((always_inline)) {
-        char* b = smem + (t & 1) * BUF;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) gb_store<WT, D, GB_THREADS>(b + p * Tile::BYTES, tid, sq[p]);
-        gb_store<WT, D, GB_THREADS>(b + PARTS * Tile::BYTES, tid, so);
-        if (tid < 32) *reinterpret_cast<float2*>(b + OFF_S + tid * 8) = ss;
-    };
-    load();
-    GbKeys<WT, D> keys;
-    gb_own_rows<WT, D>(P.k_rot + (((size_t)seq * P.nkv + hk) * P.rows + (size_t)key * K1) * D * ESZ, half, keys.kf);
-    gb_own_rows<WT, D>(P.v + (((size_t)seq * P.rows + (size_t)key * K1) * P.nkv + hk) * D * ESZ, half, keys.vf);
-    keys.clear();
-    store(0);
-    if (n_tiles > 1) load();
-    __syncthreads();
-    int tile = 0;
-    for (int t = 0; t < n_tiles; ++t) {
-        if (t + 1 < n_tiles) store(t + 1);
-        if (t + 2 < n_tiles) load();
-        const char* buf = smem + (t & 1) * BUF;
-        const int first = first_row + 32 * tile;
-        if (w0 < P.T && first + 31 >= w0 * K1) {
-            if (first >= (w0 + 31) * K1 && first + 31 < P.rows)
-                keys.template step<false>(L, buf, reinterpret_cast<const float2*>(buf + OFF_S), half, 0, 31);
-            else
-                keys.template step<true>(L, buf, reinterpret_cast<const float2*>(buf + OFF_S), half, key * K1 - first - 4 * half, P.rows - 1 - first - 4 * half);
-        }
-        if (++tile == per_head) tile = 0;
-        __syncthreads();
-    }
-    if (w0 + c < P.T) keys.write(P, seq, hk, key * K1, key, half);
+__device__ __forceinline__ void gb_write_keys(const GbParams& P, int seq, int hk, int row, int pos, int half, const f32x16 (&dk)[D / 32], const f32x16 (&dv)[D / 32]) {
+    const size_t at = (((size_t)seq * P.rows + row) * P.nkv + hk) * D * Traits<WT>::ESZ;
+    gb_write<WT, D>(P.d_k + at, P.table + (size_t)pos * (D / 2), 0.6931471805599453f, half, dk);   // (the queries carry log2(e) / sqrt(d))
+    gb_write<WT, D>(P.d_v + at, nullptr, 1.f, half, dv);
 }
 
-// Gradients of [MASK] tokens' keys and values, which the later rows of their own group see: a wavefront takes as many whole groups as
-// fit into 32 rows, every query head that shares the kv head in turn.
-template <typename WT, int D>
-__global__ void __launch_bounds__(64) gb_own_kernel(const GbParams P) {
+// Work of a launch of gb_dkv_kernel.  Workgroups units * splits: (key tile, part, head), the tiles with the most rows first, neighbours
+// different heads; `splits` workgroups share a key tile's rows and leave partial sums.  Then those of [MASK] keys (four tiles each).
+struct GbWork { int heads, splits, units, own_tiles; float* partial; };
+
+template <typename WT, int D, int KW> struct GbDkv {
     typedef GbTile<WT, D> Tile;
-    constexpr int ESZ = Traits<WT>::ESZ, PARTS = GbTraits<WT>::PARTS, OFF_S = (PARTS + 1) * Tile::BYTES;
-    __shared__ __attribute__((aligned(16))) char smem[OFF_S + 32 * 8];
-    const int lane = threadIdx.x, c = lane & 31, half = lane >> 5;
-    const int K1 = P.k + 1, hk = blockIdx.y, seq = blockIdx.z, first = blockIdx.x * P.gpt * K1, last = min(first + P.gpt * K1, P.rows) - 1;
-    const int krow = min(first + c, last), g = gb_group(P, krow), slot = krow - g * K1;
+    static constexpr bool V_LDS = Traits<WT>::BF && D == 128;
+    static constexpr int WAVES = 2 * KW, KEYS = 32 * KW, PER_SIMD = D * Traits<WT>::ESZ > 256 ? 1 : 2;
+    static constexpr int PARTS = GbTraits<WT>::PARTS, SET = (PARTS + 1) * Tile::BYTES, OFF_S = 2 * SET, BUF = OFF_S + 2 * 32 * 8;
+    static constexpr int OFF_V = 2 * BUF, STAGES = OFF_V + (V_LDS ? KW * Tile::BYTES : 0);
+    static constexpr int OWNERS = V_LDS ? 4 : WAVES;         // wavefronts with tiles of [MASK] keys: one set of tiles each, and their values
+    static constexpr int OWN = SET + (V_LDS ? Tile::BYTES : 0) + 32 * 8, SMEM = STAGES > OWNERS * OWN ? STAGES : OWNERS * OWN;
+    static_assert(SMEM <= 160 * 1024 && KW * D / 32 * 16 * 64 * 4 <= SMEM, "");
+};
+
+template <typename WT, int D, int KW>
+__global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, KW>::PER_SIMD)) gb_dkv_kernel(const GbParams P, const GbWork W) {
+    typedef GbTile<WT, D> Tile;
+    typedef GbDkv<WT, D, KW> C;
+    constexpr int ESZ = Traits<WT>::ESZ, PARTS = C::PARTS, NJ = D / 32;
+    __shared__ __attribute__((aligned(16))) char smem[C::SMEM];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
+    const int K1 = P.k + 1;
     const Tile L(lane);
-    const size_t part = (size_t)P.seqs * P.nq * P.rows * D * ESZ, ostride = (size_t)P.nq * D * ESZ;
-    GbKeys<WT, D> keys;
-    gb_own_rows<WT, D>(P.k_rot + (((size_t)seq * P.nkv + hk) * P.rows + krow) * D * ESZ, half, keys.kf);
-    gb_own_rows<WT, D>(P.v + (((size_t)seq * P.rows + krow) * P.nkv + hk) * D * ESZ, half, keys.vf);
+    const size_t part = (size_t)P.seqs * P.nq * P.rows * D * ESZ;
+    const unsigned ostride = (unsigned)(P.nq * D * ESZ), vstride = (unsigned)(P.nkv * D * ESZ);
+    GbKeys<WT, D, C::V_LDS> keys;
     keys.clear();
-    for (int i = 0; i < P.group; ++i) {
-        const int h = hk * P.group + i;
-        const size_t at = ((size_t)seq * P.nq + h) * P.rows;
-        uint4 x[Tile::WU];
-        __syncthreads();
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            gb_load<WT, D, 64>(P.q_rot + p * part + at * D * ESZ, (size_t)D * ESZ, first, 1, 0, last, lane, x);
-            gb_store<WT, D, 64>(smem + p * Tile::BYTES, lane, x);
+    if ((int)blockIdx.x >= W.units * W.splits) {
+        // ---- [MASK] keys, which the later rows of their own group see: a wavefront takes as many whole groups as fit into 32 rows, every
+        // query head that shares the kv head in turn
+        const int x = C::OWNERS * ((int)blockIdx.x - W.units * W.splits) + wave, tiles = (P.T + P.gpt - 1) / P.gpt;
+        if (wave >= C::OWNERS || x >= W.own_tiles) return;
+        const int head = x / tiles, first = (x - head * tiles) * P.gpt * K1, last = min(first + P.gpt * K1, P.rows) - 1, seq = head / P.nkv, hk = head - seq * P.nkv;
+        const int krow = min(first + c, last), g = gb_group(P, krow), slot = krow - g * K1;
+        char* const buf = smem + wave * C::OWN;
+        gb_own_rows<WT, D>(P.k_rot + (((size_t)seq * P.nkv + hk) * P.rows + krow) * D * ESZ, half, keys.kf);
+        const char* v = P.v + (((size_t)seq * P.rows + first) * P.nkv + hk) * D * ESZ;
+        if constexpr (C::V_LDS) {
+            gb_stage<WT, D, 1>(v, vstride, last - first, buf + C::SET, 0, lane);
+            keys.v_tile = buf + C::SET;
+        } else {
+            gb_own_rows<WT, D>(v + (size_t)(krow - first) * vstride, half, keys.vf);
         }
-        gb_load<WT, D, 64>(P.d_out + ((size_t)seq * P.rows * P.nq + h) * D * ESZ, ostride, first, 1, 0, last, lane, x);
-        gb_store<WT, D, 64>(smem + PARTS * Tile::BYTES, lane, x);
-        if (lane < 32) *reinterpret_cast<float2*>(smem + OFF_S + lane * 8) = P.stats[at + krow];
-        __syncthreads();
-        keys.template step<true>(L, smem, reinterpret_cast<const float2*>(smem + OFF_S), half, slot > 0 ? krow - first - 4 * half : 99, g * K1 + P.k - first - 4 * half);
+        float* const stats = reinterpret_cast<float*>(buf + C::OWN - 32 * 8);
+        for (int i = 0; i < P.group; ++i) {
+            const int h = hk * P.group + i;
+            const size_t at = ((size_t)seq * P.nq + h) * P.rows;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) gb_stage<WT, D, 1>(P.q_rot + p * part + (at + first) * D * ESZ, D * ESZ, last - first, buf + p * Tile::BYTES, 0, lane);
+            gb_stage<WT, D, 1>(P.d_out + (((size_t)seq * P.rows + first) * P.nq + h) * D * ESZ, ostride, last - first, buf + PARTS * Tile::BYTES, 0, lane);
+            stats[lane] = (lane < 32 ? P.lse2 : P.delta)[at + krow];
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");   // (the tiles have arrived, for this wavefront's own reads)
+            __builtin_amdgcn_wave_barrier();
+            keys.template step<true>(L, buf, stats, 32, half, slot > 0 ? krow - first - 4 * half : 99, g * K1 + P.k - first - 4 * half);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (first + c <= last && slot > 0) gb_write_keys<WT, D>(P, seq, hk, krow, krow - g * P.k, half, keys.dk, keys.dv);
+        return;
     }
-    if (first + c <= last && slot > 0) keys.write(P, seq, hk, krow, krow - g * P.k, half);
+    const int y = blockIdx.x / W.heads, head = blockIdx.x - y * W.heads, kt = y / W.splits, split = y - kt * W.splits;
+    const int seq = head / P.nkv, hk = head - seq * P.nkv, kw = wave % KW, rw = wave / KW;
+    const int t0 = C::KEYS * kt, w0 = t0 + 32 * kw, key = min(w0 + c, P.T - 1);   // the workgroup's and the wavefront's first token, the lane's
+    const int first_row = t0 * K1, per_head = (P.rows - first_row + 63) / 64, all = per_head * P.group;
+    const int i0 = (int)((long long)all * split / W.splits), i1 = (int)((long long)all * (split + 1) / W.splits);
+    float stat = 0.f;
+    auto stage = [&](int i) __attribute__((always_inline)) {
+        const int g = i / per_head, h = hk * P.group + g, first = first_row + 64 * (i - g * per_head);
+        const size_t at = ((size_t)seq * P.nq + h) * P.rows + first;
+        char* b = smem + (i & 1) * C::BUF;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int from = min(32 * r, P.rows - 1 - first), most = P.rows - 1 - first - from;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+                gb_stage<WT, D, C::WAVES>(P.q_rot + p * part + (at + from) * D * ESZ, D * ESZ, most, b + r * C::SET + p * Tile::BYTES, wave, lane);
+            gb_stage<WT, D, C::WAVES>(P.d_out + (((size_t)seq * P.rows + first + from) * P.nq + h) * D * ESZ, ostride, most, b + r * C::SET + PARTS * Tile::BYTES, wave, lane);
+        }
+        // (a row beyond the last: probability 0, whatever the last row, which it repeats, holds)
+        if (wave < 2) stat = (wave ? P.delta : P.lse2)[at + min(lane, P.rows - 1 - first)];
+        if (wave == 0 && lane > P.rows - 1 - first) stat = -INFINITY;
+    };
+    auto stage_stats = [&](int i) __attribute__((always_inline)) {
+        if (wave < 2) reinterpret_cast<float*>(smem + (i & 1) * C::BUF + C::OFF_S)[64 * wave + lane] = stat;
+    };
+    if (i0 < i1) stage(i0);
+    gb_own_rows<WT, D>(P.k_rot + (((size_t)seq * P.nkv + hk) * P.rows + (size_t)key * K1) * D * ESZ, half, keys.kf);
+    if constexpr (C::V_LDS) {
+        const int first = min(w0, P.T - 1);                  // (either row wavefront brings in half of the rows)
+        gb_stage<WT, D, 2>(P.v + (((size_t)seq * P.rows + (size_t)first * K1) * P.nkv + hk) * D * ESZ, K1 * vstride, P.T - 1 - first, smem + C::OFF_V + kw * Tile::BYTES, rw, lane);
+        keys.v_tile = smem + C::OFF_V + kw * Tile::BYTES;
+    } else {
+        gb_own_rows<WT, D>(P.v + (((size_t)seq * P.rows + (size_t)key * K1) * P.nkv + hk) * D * ESZ, half, keys.vf);
+    }
+    if (i0 < i1) stage_stats(i0);
+    __syncthreads();
+    auto step = [&](int i, auto masked) __attribute__((always_inline)) {
+        if (i + 1 < i1) stage(i + 1);
+        const char* buf = smem + (i & 1) * C::BUF;
+        const int first = first_row + 64 * (i % per_head) + 32 * rw;
+        if (!masked || (w0 < P.T && first + 31 >= w0 * K1))
+            keys.template step<masked>(L, buf + rw * C::SET, reinterpret_cast<const float*>(buf + C::OFF_S) + 32 * rw, 64, half, key * K1 - first - 4 * half, 31);
+        if (i + 1 < i1) stage_stats(i + 1);
+        __syncthreads();
+    };
+    // of every head the row tiles that see some of the wavefront's keys, then those that see all of them
+    const int see_all = w0 < P.T ? min(max((w0 + 31) * K1 - first_row - 32 * rw + 63, 0) / 64, per_head) : per_head;
+    for (int i = i0; i < i1;) {
+        const int head0 = i / per_head * per_head;
+        for (const int end = min(i1, head0 + see_all); i < end; ++i) step(i, std::true_type{});
+        for (const int end = min(i1, head0 + per_head); i < end; ++i) step(i, std::false_type{});
+    }
+    // ---- the row wavefronts' sums, one gradient after the other by way of the LDS
+    auto meet = [&](f32x16 (&y)[NJ]) __attribute__((always_inline)) {
+        f32x4* area = reinterpret_cast<f32x4*>(smem) + kw * NJ * 4 * 64 + lane;
+        if (rw) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) area[(j * 4 + q) * 64] = f32x4{y[j][4 * q], y[j][4 * q + 1], y[j][4 * q + 2], y[j][4 * q + 3]};
+        }
+        __syncthreads();
+        if (!rw) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 v = area[(j * 4 + q) * 64];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[j][4 * q + e] += v[e];
+                }
+        }
+        __syncthreads();
+    };
+    meet(keys.dk);
+    meet(keys.dv);
+    if (rw) return;
+    if (W.splits > 1) {
+        // [tile of 32 keys][split][dk, dv][NJ * 4][64 lanes] of 16 bytes
+        f32x4* to = reinterpret_cast<f32x4*>(W.partial) + (((size_t)(kt * W.heads + head) * KW + kw) * W.splits + split) * (2 * NJ * 4 * 64) + lane;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x16 &a = keys.dk[j], &b = keys.dv[j];
+                to[(j * 4 + q) * 64] = f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                to[((NJ + j) * 4 + q) * 64] = f32x4{b[4 * q], b[4 * q + 1], b[4 * q + 2], b[4 * q + 3]};
+            }
+        return;
+    }
+    if (w0 + c < P.T) gb_write_keys<WT, D>(P, seq, hk, key * K1, key, half, keys.dk, keys.dv);
+}
+
+// The parts' sums, added in order: a wavefront per tile of 32 keys
+template <typename WT, int D>
+__global__ void __launch_bounds__(64) gb_merge_kernel(const GbParams P, const GbWork W, int keys_wg) {
+    constexpr int NJ = D / 32;
+    const int lane = threadIdx.x, c = lane & 31, half = lane >> 5, per_wg = keys_wg / 32;
+    const int sub = blockIdx.x % per_wg, unit = blockIdx.x / per_wg, kt = unit / W.heads, head = unit - kt * W.heads, seq = head / P.nkv, hk = head - seq * P.nkv;
+    const int key = kt * keys_wg + 32 * sub + c;
+    if (kt * keys_wg + 32 * sub >= P.T) return;
+    const f32x4* from = reinterpret_cast<const f32x4*>(W.partial) + (size_t)blockIdx.x * W.splits * (2 * NJ * 4 * 64) + lane;
+    f32x16 y[2][NJ];
+#pragma unroll
+    for (int j = 0; j < 2 * NJ; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            f32x4 v = from[(j * 4 + q) * 64];
+            for (int i = 1; i < W.splits; ++i) v += from[(size_t)i * (2 * NJ * 4 * 64) + (j * 4 + q) * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[j / NJ][j % NJ][4 * q + e] = v[e];
+        }
+    if (key < P.T) gb_write_keys<WT, D>(P, seq, hk, key * (P.k + 1), key, half, y[0], y[1]);
 }
 
 // the checks are those of ps_group_attention
@@ -469,27 +588,55 @@ int check(const ps_group_attn_grad_args* a) {
     return ga_check(&f);
 }
 
-struct GbLayout { size_t table, k_rot, q_rot, stats, total; };
+// How the gradients of keys are cut: keys of a workgroup, parts of their rows
+struct GbPlan { int keys, heads, tiles, splits; };
+GbPlan plan(const ps_group_attn_grad_args* a) {
+    GbPlan L;
+    L.heads = a->n_kv_heads * a->seqs;
+    const bool big = a->dtype == PS_F32 && a->head_dim == 128;   // (one wavefront per SIMD)
+    L.keys = !big && (long long)((a->tokens + 127) / 128) * L.heads >= 256 ? 128 : 64;
+    L.tiles = (a->tokens + L.keys - 1) / L.keys;
+    const long long units = (long long)L.tiles * L.heads;
+    const int stages = (a->tokens * (a->k + 1) + 63) / 64 * (a->n_heads / a->n_kv_heads);
+    L.splits = (int)std::max(1LL, std::min(std::min(1024 / units, 16LL), (long long)stages / 4));
+    return L;
+}
+
+struct GbLayout { size_t table, k_rot, q_rot, stats, partial, total; };
 GbLayout layout(const ps_group_attn_grad_args* a) {
     GbLayout L;
     const bool bf = a->dtype == PS_BF16;
     const size_t rows = (size_t)a->seqs * a->tokens * (a->k + 1), row = (size_t)a->head_dim * (bf ? 2 : 4);
+    const GbPlan G = plan(a);
     L.table = 0;
     L.k_rot = a256((size_t)(a->tokens + a->k) * (a->head_dim / 2) * sizeof(float2));
     L.q_rot = L.k_rot + a256(rows * a->n_kv_heads * row);
     L.stats = L.q_rot + a256(rows * a->n_heads * row * (bf ? 2 : 1));
-    L.total = L.stats + a256(rows * a->n_heads * sizeof(float2));
+    L.partial = L.stats + 2 * a256(rows * a->n_heads * sizeof(float));
+    L.total = L.partial + (G.splits > 1 ? (size_t)G.tiles * G.heads * G.splits * G.keys * a->head_dim * 2 * sizeof(float) : 0);
     return L;
 }
 
-template <typename WT, int D> int launch(const GbParams& P, hipStream_t s) {
+template <typename WT, int D, int KW> void launch_keys(const GbParams& P, const GbPlan& G, GbWork W, hipStream_t s) {
+    typedef GbDkv<WT, D, KW> C;
+    const unsigned own = (unsigned)((W.own_tiles + C::OWNERS - 1) / C::OWNERS);
+    hipLaunchKernelGGL((gb_dkv_kernel<WT, D, KW>), dim3((unsigned)(W.units * W.splits) + own), dim3(C::WAVES * 64), 0, s, P, W);
+    if (W.splits > 1) hipLaunchKernelGGL((gb_merge_kernel<WT, D>), dim3(W.units * KW), dim3(64), 0, s, P, W, G.keys);
+}
+
+template <typename WT, int D> int launch(const GbParams& P, const GbPlan& G, float* partial, hipStream_t s) {
     // (as ga_rope_kernel: where positions are few, several workgroups of at most one item per thread share one)
     const long long items = (long long)P.seqs * P.nq * (D / 8) * (P.k + 1);
     const unsigned share = (unsigned)std::max(1LL, std::min((items + 255) / 256, 4096LL / (P.T + P.k)));
     hipLaunchKernelGGL((gb_prep_kernel<WT, D>), dim3(P.T + P.k, share), dim3(256), 0, s, P);
-    hipLaunchKernelGGL((gb_dq_kernel<WT, D>), dim3((P.rows + GB_ROWS - 1) / GB_ROWS, P.nq, P.seqs), dim3(GB_THREADS), 0, s, P);
-    hipLaunchKernelGGL((gb_dkv_kernel<WT, D>), dim3((P.T + GB_ROWS - 1) / GB_ROWS, P.nkv, P.seqs), dim3(GB_THREADS), 0, s, P);
-    if (P.k > 0) hipLaunchKernelGGL((gb_own_kernel<WT, D>), dim3((P.T + P.gpt - 1) / P.gpt, P.nkv, P.seqs), dim3(64), 0, s, P);
+    hipLaunchKernelGGL((gb_dq_kernel<WT, D>), dim3(P.nq, (P.rows + GB_ROWS - 1) / GB_ROWS, P.seqs), dim3(GB_THREADS), 0, s, P);
+    const GbWork W = {G.heads, G.splits, G.tiles * G.heads, P.k > 0 ? (P.T + P.gpt - 1) / P.gpt * G.heads : 0, partial};
+    if constexpr (D * Traits<WT>::ESZ > 256) {
+        launch_keys<WT, D, 2>(P, G, W, s);
+    } else {
+        if (G.keys == 64) launch_keys<WT, D, 2>(P, G, W, s);
+        else launch_keys<WT, D, 4>(P, G, W, s);
+    }
     return hipGetLastError() == hipSuccess ? PS_OK : PS_ERR_DEVICE;
 }
 
@@ -515,8 +662,11 @@ extern "C" int ps_group_attention_grad(const ps_group_attn_grad_args* a, void* s
     P.q = (const char*)a->q; P.k_ = (const char*)a->k_; P.v = (const char*)a->v; P.d_out = (const char*)a->d_out;
     P.out = a->out; P.lse = a->lse;
     P.d_q = (char*)a->d_q; P.d_k = (char*)a->d_k; P.d_v = (char*)a->d_v;
-    P.table = (float2*)(ws + L.table); P.k_rot = ws + L.k_rot; P.q_rot = ws + L.q_rot; P.stats = (float2*)(ws + L.stats);
+    P.table = (float2*)(ws + L.table); P.k_rot = ws + L.k_rot; P.q_rot = ws + L.q_rot; P.lse2 = (float*)(ws + L.stats);
+    P.delta = (float*)(ws + L.stats + (L.partial - L.stats) / 2);
     hipStream_t s = (hipStream_t)stream;
-    if (a->dtype == PS_BF16) return a->head_dim == 128 ? launch<bf16_t, 128>(P, s) : launch<bf16_t, 64>(P, s);
-    return a->head_dim == 128 ? launch<float, 128>(P, s) : launch<float, 64>(P, s);
+    const GbPlan G = plan(a);
+    float* partial = (float*)(ws + L.partial);
+    if (a->dtype == PS_BF16) return a->head_dim == 128 ? launch<bf16_t, 128>(P, G, partial, s) : launch<bf16_t, 64>(P, G, partial, s);
+    return a->head_dim == 128 ? launch<float, 128>(P, G, partial, s) : launch<float, 64>(P, G, partial, s);
 }
