@@ -267,39 +267,89 @@ __global__ void __launch_bounds__(VL_THREADS, 2) vl_grad_kernel(const VlParams P
 }
 
 // ------------------------------------------------------------------------------------------
-// bf16, many rows: tiles of 256 x 256, eight wavefronts (two per SIMD) of 128 x 64 each, 64 elements of the contraction per stage in
-// two LDS buffers of 64 KiB.  A stage is brought in by the memory unit itself (no registers): 1 KiB per request, lanes in
-// the order of the LDS, their source addresses permuted so that rows read together fall into different banks.  Per stage a
-// wavefront reads its operands, asks for the next stage, and multiplies.
+// bf16, many rows: tiles of 256 x 256, eight wavefronts (two per SIMD) of 128 x 64 each, 32 elements of the contraction per stage.
+// A stage (32 KiB) is brought in by the memory unit itself (no registers): 1 KiB per request, lanes in the order of the LDS,
+// their source addresses permuted so that rows read together fall into different banks.  Four buffers: while a stage is multiplied from
+// registers, the next is read from LDS, two more are on their way and the one that has just been read is filled anew.  The wait at
+// a stage's barrier leaves the youngest two stages in flight.  The buffers are arrays of their own: the compiler then knows that a
+// read from one need not wait for what is on its way into another.
 // ------------------------------------------------------------------------------------------
-constexpr int VW_THREADS = 512, VW_TILE = 256, VW_A = VW_TILE * 128, VW_BUF = 2 * VW_A;
+constexpr int VW_THREADS = 512, VW_TILE = 256, VW_A = VW_TILE * 64, VW_BUF = 2 * VW_A;
 typedef __attribute__((address_space(3))) void lds_void;
 __device__ __forceinline__ void vw_copy(rsrc_t from, unsigned off, unsigned soff, char* to) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, soff, 0, 0);
 }
-// 256 rows of 128 bytes: chunk j of 16 bytes stands at j ^ (row / 2) % 8
+// 256 rows of 64 bytes, as vl_at places them
 struct VwRows {
     rsrc_t src;
-    unsigned off[4];
+    unsigned off[2];
     // rows first .. first + 255 of a matrix (rows beyond last: the last), wavefront w's 32 of them
     __device__ __forceinline__ VwRows(const char* m, size_t first, size_t last, unsigned stride, int wave, int lane) {
         src = make_rsrc(m + first * stride);
         const unsigned most = (unsigned)min((size_t)VW_TILE, last - first + 1) - 1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned row = 32 * wave + 8 * i + lane / 8, chunk = (lane & 7) ^ ((row >> 1) & 7);
-            off[i] = min(row, most) * stride + chunk * 16;
+        for (int i = 0; i < 2; ++i) {
+            const unsigned row = 32 * wave + 16 * i + lane / 4;
+            off[i] = min(row, most) * stride + ((lane & 3) ^ ((row >> 2) & 3)) * 16;
         }
     }
-    __device__ __forceinline__ void stage(int k, bool half_stage, char* lds, int wave, int lane) const {
+    __device__ __forceinline__ void stage(int k, char* lds, int wave) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            // (a last stage of 32 elements: the other half, which nobody reads, is the same again)
-            const unsigned chunk = (lane & 7) ^ ((((8 * i + lane / 8)) >> 1) & 7);
-            vw_copy(src, half_stage ? off[i] - (chunk & 4) * 16 : off[i], k * 128, lds + (32 * wave + 8 * i) * 128);
-        }
+        for (int i = 0; i < 2; ++i) vw_copy(src, off[i], k * 64, lds + (32 * wave + 16 * i) * 64);
     }
 };
+struct VwOperands { bf16x8 a[4][2], b[2][2]; };
+// steps stages from `first` on: stage(k, buffer) requests (four requests per wavefront), read(buffer, operands), then the products
+template <int READS, typename STAGE, typename READ>
+__device__ __forceinline__ void vw_pipeline(int first, int steps, char* b0, char* b1, char* b2, char* b3, STAGE stage, READ read, f32x16 (&acc)[4][2]) {
+    const int last = first + steps - 1;
+    stage(first, b0);
+    stage(min(first + 1, last), b1);
+    stage(min(first + 2, last), b2);
+    stage(min(first + 3, last), b3);
+    VwOperands x[2];
+    asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    read(b0, x[0]);
+    auto step = [&](int k, char* mine, char* next, const VwOperands& now, VwOperands& then) __attribute__((always_inline)) {
+        // stage k is in registers (now); every wavefront has read it once all have come here, so that its buffer may be filled again
+        asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        stage(min(k + 4, last), mine);
+        read(next, then);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now.a[i][t], now.b[j][t], acc[i][j], 0, 0, 0);
+        // (requests and reads between the MFMAs, none of the latter beyond the barriers)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, (READS + 7) / 8, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int k = first;
+    for (; k + 3 <= last; k += 4) {
+        step(k, b0, b1, x[0], x[1]);
+        step(k + 1, b1, b2, x[1], x[0]);
+        step(k + 2, b2, b3, x[0], x[1]);
+        step(k + 3, b3, b0, x[1], x[0]);
+    }
+    if (k <= last) step(k, b0, b1, x[0], x[1]);
+    if (k + 1 <= last) step(k + 1, b1, b2, x[1], x[0]);
+    if (k + 2 <= last) step(k + 2, b2, b3, x[0], x[1]);
+    __syncthreads();                                        // (nothing is on its way into the buffers any more)
+}
 
 // A tile's workgroup number -> the tile: workgroups go to the XCDs in turn; an XCD gets a stretch of the order, in which
 // 32 neighbours (its compute units) share four rows' and eight columns' operands
@@ -313,20 +363,13 @@ __device__ __forceinline__ void vw_tile(unsigned id, unsigned nx, unsigned ny, u
 }
 
 __global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlParams P, int nx, int ny) {
-    __shared__ __attribute__((aligned(16))) char smem[2 * VW_BUF];
+    __shared__ __attribute__((aligned(16))) char b0[VW_BUF], b1[VW_BUF], b2[VW_BUF], b3[VW_BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
     unsigned tx, ty;
     vw_tile(blockIdx.x, nx, ny, tx, ty);
     const int vt = tx * VW_TILE, rt = ty * VW_TILE, wm = wave & 1, wn = wave >> 1;
     const unsigned rb = P.H * 2;
     const VwRows A(P.w, P.v0 + vt, P.V - 1, rb, wave, lane), B(P.h, P.row0 + rt, P.row0 + P.rows_c - 1, rb, wave, lane);
-    const int steps = (P.H + 63) / 64;
-    auto stage = [&](int k) __attribute__((always_inline)) {
-        char* b = smem + (k & 1) * VW_BUF;
-        const bool part = k == steps - 1 && (P.H & 32);
-        A.stage(k, part, b, wave, lane);
-        B.stage(k, part, b + VW_A, wave, lane);
-    };
     f32x16 acc[4][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -334,37 +377,21 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlPa
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    const int at = c * 128 + ((half ^ ((c >> 1) & 7)) << 4), a0 = 128 * wm * 128 + at, b0 = VW_A + 64 * wn * 128 + at;
-    auto multiply = [&](int k, auto halves, bool more) __attribute__((always_inline)) {
-        const char* b = smem + (k & 1) * VW_BUF;
-        bf16x8 x[4][2 * halves], y[2][2 * halves];
+    const int at = vl_at(c, half), a0 = 128 * wm * 64 + at, w0 = VW_A + 64 * wn * 64 + at;
+    vw_pipeline<12>(0, P.H / 32, b0, b1, b2, b3,
+                [&](int k, char* b) __attribute__((always_inline)) { A.stage(k, b, wave); B.stage(k, b + VW_A, wave); },
+                [&](const char* b, VwOperands& x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < 2 * halves; ++t) {
+                    for (int t = 0; t < 2; ++t) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) y[j][t] = __builtin_bit_cast(bf16x8, ld16(b + ((b0 ^ (t << 5)) + j * 4096)));
+                        for (int j = 0; j < 2; ++j) x.b[j][t] = __builtin_bit_cast(bf16x8, ld16(b + (w0 ^ (t << 5)) + j * 2048));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i][t] = __builtin_bit_cast(bf16x8, ld16(b + ((a0 ^ (t << 5)) + i * 4096)));
-        }
-        if (more) stage(k + 1);
-#pragma unroll
-        for (int t = 0; t < 2 * halves; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][t], y[j][t], acc[i][j], 0, 0, 0);
-    };
-    stage(0);
-    __syncthreads();
-    for (int k = 0; k < P.H / 64; ++k) {
-        multiply(k, std::integral_constant<int, 2>{}, k + 1 < steps);
-        __syncthreads();
-    }
-    if (P.H & 32) {
-        multiply(steps - 1, std::integral_constant<int, 1>{}, false);
-        __syncthreads();
-    }
+                        for (int i = 0; i < 4; ++i) x.a[i][t] = __builtin_bit_cast(bf16x8, ld16(b + (a0 ^ (t << 5)) + i * 2048));
+                    }
+                }, acc);
     // ---- lane (c, half) holds of row 64 wn + 32 j + c the tokens 128 wm + 32 i + 8 (e / 4) + 4 half + e % 4; they leave by way of the LDS,
-    // rows of 512 bytes, 16-byte piece p at p ^ row % 32
+    // rows of 512 bytes, 16-byte piece p at p ^ row % 32 (64 rows to a buffer)
+    char* const mine = wn < 2 ? wn ? b1 : b0 : wn == 2 ? b2 : b3;   // (also the one of the rows that the wavefront stores)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int rr = 64 * wn + 32 * j + c, r = rt + rr, row = P.row0 + min(r, P.rows_c - 1);
@@ -397,7 +424,7 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlPa
                 }
                 if (P.x) {
                     const int piece = 16 * wm + 4 * i + q;
-                    *reinterpret_cast<u32x2*>(smem + rr * 512 + ((piece ^ (rr & 31)) << 4) + 8 * half) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                    *reinterpret_cast<u32x2*>(mine + (rr & 63) * 512 + ((piece ^ (rr & 31)) << 4) + 8 * half) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
                 }
             }
         const float mine = sum[0] + sum[1];
@@ -412,37 +439,28 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlPa
 #pragma unroll 4
     for (int i = 0; i < 16; ++i) {
         const int rr = 32 * wave + 2 * i + (lane >> 5), r = rt + rr, p = lane & 31;
-        const uint4 v = ld16(smem + rr * 512 + ((p ^ (rr & 31)) << 4));
+        const uint4 v = ld16(mine + (rr & 63) * 512 + ((p ^ (rr & 31)) << 4));
         if (r < P.rows_c) *reinterpret_cast<uint4*>(P.x + ((size_t)r * P.ldx + vt + 8 * p) * 2) = v;
     }
 }
 
 __global__ void __launch_bounds__(VW_THREADS, 2) vl_grad_wide_kernel(const VlParams P, int nx, int ny) {
-    __shared__ __attribute__((aligned(16))) char smem[2 * VW_BUF];
+    __shared__ __attribute__((aligned(16))) char b0[VW_BUF], b1[VW_BUF], b2[VW_BUF], b3[VW_BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
     unsigned tx, ty;
     vw_tile(blockIdx.x, nx, ny, tx, ty);
     const int split = blockIdx.y, ct = tx * VW_TILE, rt = ty * VW_TILE, wm = wave & 1, wn = wave >> 1;
     const unsigned rb = P.H * 2;
     const VwRows A(P.x, rt, P.rows_c - 1, P.ldx * 2, wave, lane);
-    const int k0 = split * (P.split_n / 64), k1 = min((split + 1) * P.split_n, (P.nv + 63) / 64 * 64) / 64;
-    // W: 64 rows of 512 bytes (columns beyond H: the last), wavefront w's 8 of them; 32-byte chunk j stands at j ^ 2 f(row),
+    const int k0 = split * (P.split_n / 32), k1 = min((split + 1) * P.split_n, (P.nv + 31) / 32 * 32) / 32;
+    // W: 32 rows of 512 bytes (columns beyond H: the last), wavefront w's 4 of them; 32-byte chunk j stands at j ^ 2 f(row),
     // f = row % 4 + 4 (row / 8 % 2), so that the eight rows of a transposed read fall into different banks
-    unsigned col[4];
+    unsigned col[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned row = 8 * wave + 2 * i + (lane >> 5), f = (row & 3) | ((row >> 3 & 1) << 2), chunk = ((lane & 31) >> 1) ^ (f << 1);
+    for (int i = 0; i < 2; ++i) {
+        const unsigned row = 4 * wave + 2 * i + (lane >> 5), f = (row & 3) | ((row >> 3 & 1) << 2), chunk = ((lane & 31) >> 1) ^ (f << 1);
         col[i] = min((unsigned)ct * 2 + chunk * 32 + (lane & 1) * 16, rb - 16);
     }
-    auto stage = [&](int k) __attribute__((always_inline)) {
-        char* b = smem + (k & 1) * VW_BUF;
-        A.stage(k, false, b, wave, lane);
-        const int v = P.v0 + 64 * k;
-        const rsrc_t src = make_rsrc(P.w + (size_t)v * rb);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) vw_copy(src, (unsigned)min(8 * wave + 2 * i + (lane >> 5), P.V - 1 - v) * rb + col[i], 0, b + VW_A + (8 * wave + 2 * i) * 512);
-    };
-    if (k0 < k1) stage(k0);
     f32x16 acc[4][2];
     float* out = P.acc + (size_t)split * P.rows_c * P.H;
 #pragma unroll
@@ -454,33 +472,31 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_grad_wide_kernel(const VlPar
                 const int r = rt + 128 * wm + 32 * i + 8 * (e / 4) + 4 * half + e % 4, x = ct + 64 * wn + 32 * j + c;
                 acc[i][j][e] = P.first ? 0.f : out[(size_t)min(r, P.rows_c - 1) * P.H + min(x, P.H - 1)];
             }
-    const int a0 = 128 * wm * 128 + c * 128 + ((half ^ ((c >> 1) & 7)) << 4);
+    const int a0 = 128 * wm * 64 + vl_at(c, half);
     const int vkey = (lane & 15) >> 2, vhi = (lane >> 4) & 1, f = vkey | half << 2;
-    const int b0 = VW_A + (8 * half + vkey) * 512 + ((vhi ^ (f << 1)) << 5) + (lane & 3) * 8;
-    __syncthreads();
-    for (int k = k0; k < k1; ++k) {
-        const char* b = smem + (k & 1) * VW_BUF;
-        bf16x8 x[4][4], y[2][4];
+    const int w0 = (VW_A + (8 * half + vkey) * 512 + ((vhi ^ (f << 1)) << 5) + (lane & 3) * 8) ^ (4 * wn << 5);
+    if (k0 < k1)
+        vw_pipeline<16>(k0, k1 - k0, b0, b1, b2, b3,
+                    [&](int k, char* b) __attribute__((always_inline)) {
+                        A.stage(k, b, wave);
+                        const int v = P.v0 + 32 * k;
+                        const rsrc_t src = make_rsrc(P.w + (size_t)v * rb);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+                        for (int i = 0; i < 2; ++i) vw_copy(src, (unsigned)min(4 * wave + 2 * i + (lane >> 5), P.V - 1 - v) * rb + col[i], 0, b + VW_A + (4 * wave + 2 * i) * 512);
+                    },
+                    [&](const char* b, VwOperands& x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const char* a = b + (b0 ^ ((4 * wn + 2 * j) << 5)) + t * 16 * 512;
-                const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a), w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 4 * 512));
-                y[j][t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, w, 0, 1, 2, 3, 4, 5, 6, 7));
-            }
+                        for (int t = 0; t < 2; ++t) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i][t] = __builtin_bit_cast(bf16x8, ld16(b + ((a0 ^ (t << 5)) + i * 4096)));
-        }
-        if (k + 1 < k1) stage(k + 1);
+                            for (int j = 0; j < 2; ++j) {
+                                const char* a = b + (w0 ^ (2 * j << 5)) + t * 16 * 512;
+                                const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a), w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 4 * 512));
+                                x.b[j][t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, w, 0, 1, 2, 3, 4, 5, 6, 7));
+                            }
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i][t], y[j][t], acc[i][j], 0, 0, 0);
-        __syncthreads();
-    }
+                            for (int i = 0; i < 4; ++i) x.a[i][t] = __builtin_bit_cast(bf16x8, ld16(b + (a0 ^ (t << 5)) + i * 2048));
+                        }
+                    }, acc);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll

@@ -12,6 +12,7 @@
 // -delta are the accumulators' initial values.  The other side's rows are staged in LDS once per workgroup and read both ways: as rows
 // (scores) and as columns (gradients; bf16: transposed by the LDS unit).
 #include "ps_train_device.h"
+#include <stdlib.h>
 
 namespace {
 
@@ -34,65 +35,45 @@ template <typename WT> struct GbTraits { static constexpr int PARTS = Traits<WT>
 
 __device__ __forceinline__ int gb_group(const GbParams& P, int row) { return P.k > 0 ? (int)__umulhi((unsigned)row, P.k1_magic) : row; }
 
-// ---- the table, rotated q and k, and the rows' statistics; a workgroup takes one position (as ga_rope_kernel)
+// ---- the table and the rotated keys; a workgroup takes one position (as ga_rope_kernel, whose keys lie otherwise)
 template <typename WT, int D>
 __global__ void __launch_bounds__(256) gb_prep_kernel(const GbParams P) {
     constexpr int ESZ = Traits<WT>::ESZ, Q4 = D / 8;
     __shared__ float2 cs[D / 2];
-    const int pos = blockIdx.x, tid = threadIdx.x;
+    const int pos = blockIdx.x, tid = threadIdx.x, g4 = tid % Q4;
+    const int s0 = max(0, pos - P.T + 1), slots = min(pos, P.k) - s0 + 1;
+    const long long n = (long long)slots * P.seqs * P.nkv * Q4;
+    char* to = nullptr;
+    f32x4 a, b;
+    auto request = [&](long long x) __attribute__((always_inline)) {
+        const unsigned y = (unsigned)(x / Q4), z = y / P.nkv, head = y - z * P.nkv, slot = z / P.seqs, seq = z - slot * P.seqs;
+        const int sl = s0 + (int)slot;
+        const size_t row = (size_t)(pos - sl) * (P.k + 1) + sl;
+        const char* p = P.k_ + ((((size_t)seq * P.rows + row) * P.nkv + head) * D + 4 * g4) * ESZ;
+        to = P.k_rot + ((((size_t)seq * P.nkv + head) * P.rows + row) * D + 4 * g4) * ESZ;
+        a = load4_q<WT>(p);
+        b = load4_q<WT>(p + D / 2 * ESZ);
+    };
+    long long x = (long long)blockIdx.y * 256 + tid;
+    if (x < n) request(x);                                  // (on its way while the table is worked out)
     if (tid < D / 2) {
         const float2 t = ga_cos_sin((double)pos * ga_exp2(-2.0 * tid / D * P.log2_base));
         cs[tid] = t;
         if (blockIdx.y == 0) P.table[(size_t)pos * (D / 2) + tid] = t;
     }
     __syncthreads();
-    const int s0 = max(0, pos - P.T + 1), slots = min(pos, P.k) - s0 + 1, g4 = tid % Q4;
-    auto turn = [&](f32x4 a, f32x4 b, float scale, f32x4& ra, f32x4& rb) __attribute__((always_inline)) {
+    while (x < n) {
+        f32x4 ra, rb;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float2 t = cs[4 * g4 + e];
-            ra[e] = (a[e] * t.x - b[e] * t.y) * scale;
-            rb[e] = (b[e] * t.x + a[e] * t.y) * scale;
+            ra[e] = a[e] * t.x - b[e] * t.y;
+            rb[e] = b[e] * t.x + a[e] * t.y;
         }
-    };
-    const long long nk = (long long)slots * P.seqs * P.nkv * Q4, nq = (long long)slots * P.seqs * P.nq * Q4;
-    for (long long x = (long long)blockIdx.y * 256 + tid; x < nk; x += (long long)gridDim.y * 256) {
-        const unsigned y = (unsigned)(x / Q4), z = y / P.nkv, head = y - z * P.nkv, slot = z / P.seqs, seq = z - slot * P.seqs;
-        const int sl = s0 + (int)slot;
-        const size_t row = (size_t)(pos - sl) * (P.k + 1) + sl;
-        const char* p = P.k_ + ((((size_t)seq * P.rows + row) * P.nkv + head) * D + 4 * g4) * ESZ;
-        f32x4 ra, rb;
-        turn(load4_q<WT>(p), load4_q<WT>(p + D / 2 * ESZ), 1.f, ra, rb);
-        char* o = P.k_rot + ((((size_t)seq * P.nkv + head) * P.rows + row) * D + 4 * g4) * ESZ;
-        store4<WT>(o, ra);
-        store4<WT>(o + D / 2 * ESZ, rb);
-    }
-    const size_t part = (size_t)P.seqs * P.nq * P.rows * D * ESZ;
-    for (long long x = (long long)blockIdx.y * 256 + tid; x < nq; x += (long long)gridDim.y * 256) {
-        const unsigned y = (unsigned)(x / Q4), z = y / P.nq, head = y - z * P.nq, slot = z / P.seqs, seq = z - slot * P.seqs;
-        const int sl = s0 + (int)slot;
-        const size_t row = (size_t)(pos - sl) * (P.k + 1) + sl;
-        const size_t at = ((size_t)seq * P.rows + row) * P.nq + head, from = at * D + 4 * g4;
-        f32x4 ra, rb;
-        turn(load4_q<WT>(P.q + from * ESZ), load4_q<WT>(P.q + (from + D / 2) * ESZ), P.inv_sqrt_d * 1.4426950408889634f, ra, rb);
-        const size_t to = ((size_t)seq * P.nq + head) * P.rows + row;
-        char* o = P.q_rot + (to * D + 4 * g4) * ESZ;
-        const f32x4 ha = store4<WT>(o, ra), hb = store4<WT>(o + D / 2 * ESZ, rb);
-        if constexpr (Traits<WT>::BF) {
-            store4<WT>(o + part, ra - ha);
-            store4<WT>(o + part + D / 2 * ESZ, rb - hb);
-        }
-        const f32x4 oa = load4_q<float>(P.out + from), ob = load4_q<float>(P.out + from + D / 2);
-        const f32x4 da = load4_q<WT>(P.d_out + from * ESZ), db = load4_q<WT>(P.d_out + (from + D / 2) * ESZ);
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum += oa[e] * da[e] + ob[e] * db[e];
-#pragma unroll
-        for (int m = Q4 / 2; m >= 1; m >>= 1) sum += __shfl_xor(sum, m, 64);
-        if (g4 == 0) {
-            P.lse2[to] = -P.lse[at] * 1.4426950408889634f;
-            P.delta[to] = -sum;
-        }
+        store4<WT>(to, ra);
+        store4<WT>(to + D / 2 * ESZ, rb);
+        x += (long long)gridDim.y * 256;
+        if (x < n) request(x);
     }
 }
 
@@ -149,24 +130,27 @@ template <typename WT, int D> struct GbTile {
     }
 };
 
-// scores += rows . own: the lane's i-th is that of row 8 (i / 4) + i % 4 + 4 half and the lane's own query or key, whose
-// operands own(step) gives
-template <typename WT, int D, typename F>
-__device__ __forceinline__ void gb_scores(const GbTile<WT, D>& at, const char* tile, F own, f32x16& x) {
+// float32: scores += rows . own: the lane's i-th is that of row 8 (i / 4) + i % 4 + 4 half and the lane's own query or key
+template <typename WT, int D>
+__device__ __forceinline__ void gb_scores(const GbTile<WT, D>& at, const char* tile, const uint4 (&own)[GbTile<WT, D>::STEPS], f32x16& x) {
     const GbTile<WT, D> L = at.here();
 #pragma unroll
     for (int st = 0; st < GbTile<WT, D>::STEPS; ++st) {
-        const uint4 a = L.row(tile, st), b = own(L, st);
-        if constexpr (Traits<WT>::BF) {
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), x, 0, 0, 0);
-        } else {
-            const f32x4 u = __builtin_bit_cast(f32x4, a), w = __builtin_bit_cast(f32x4, b);
+        const f32x4 u = __builtin_bit_cast(f32x4, L.row(tile, st)), w = __builtin_bit_cast(f32x4, own[st]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(u[e], w[e], x, 0, 0, 0);
-        }
+        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(u[e], w[e], x, 0, 0, 0);
     }
 }
-// p as gb_scores leaves it, as operand (bf16: rounded)
+// float32: y^T += rows^T . p, p as gb_scores leaves it
+template <typename WT, int D, bool CLEAN>
+__device__ __forceinline__ void gb_products(const GbTile<WT, D>& at, const char* tile, const f32x16& p, f32x16 (&y)[D / 32]) {
+    const GbTile<WT, D> L = at.here();
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) y[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(L.template element<CLEAN>(tile, j, i), p[i], y[j], 0, 0, 0);
+}
+// bf16: p as operand of the two MFMAs over its 32 rows (rounded)
 template <typename WT> struct GbOperand {
     bf16x8 b[2];
     __device__ __forceinline__ GbOperand(const f32x16& p) {
@@ -176,29 +160,6 @@ template <typename WT> struct GbOperand {
                                                          pack_bf16x2(p[8 * m + 4], p[8 * m + 5]), pack_bf16x2(p[8 * m + 6], p[8 * m + 7])));
     }
 };
-template <> struct GbOperand<float> {
-    f32x16 b;
-    __device__ __forceinline__ GbOperand(const f32x16& p) : b(p) {}
-};
-// y^T += rows^T . p
-template <typename WT, int D, bool CLEAN>
-__device__ __forceinline__ void gb_products(const GbTile<WT, D>& at, const char* tile, const GbOperand<WT>& p, f32x16 (&y)[D / 32]) {
-    const GbTile<WT, D> L = at.here();
-    if constexpr (Traits<WT>::BF) {
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
-                y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(L.template column<CLEAN>(tile, j, m), p.b[m], y[j], 0, 0, 0);
-                if constexpr (CLEAN) __builtin_amdgcn_sched_barrier(0);   // (few tiles come here: no registers for operands ahead)
-            }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) y[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(L.template element<CLEAN>(tile, j, i), p.b[i], y[j], 0, 0, 0);
-    }
-}
 typedef __attribute__((address_space(3))) void lds_void;
 __device__ __forceinline__ void gb_copy(rsrc_t from, unsigned off, char* to) { __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, 0, 0, 0); }
 // A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: this wavefront's share of WAVES, 1 KiB per request
@@ -214,129 +175,290 @@ __device__ __forceinline__ void gb_stage(const char* m, unsigned stride, int mos
     }
 }
 
+// bf16: a tile's work as N chunks of up to four operands from LDS and the MFMAs that take them.  A chunk's operands are asked for before the
+// MFMAs of the chunk in front of it and the compiler keeps that order: left alone it asks for one or two ahead, and an MFMA
+// waits for most of the LDS's latency.
+template <int N, typename LOAD, typename MULTIPLY> __device__ __forceinline__ void gb_chunks(LOAD load, MULTIPLY multiply) {
+    bf16x8 x[2][4];
+    load(std::integral_constant<int, 0>{}, x[0]);
+    auto run = [&](auto self, auto n) __attribute__((always_inline)) {
+        if constexpr (n < N) {
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (n + 1 < N) load(std::integral_constant<int, n + 1>{}, x[(n + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(n, x[n & 1]);
+            self(self, std::integral_constant<int, n + 1>{});
+        }
+    };
+    run(run, std::integral_constant<int, 0>{});
+}
 // a lane's row as operand, straight from memory
 template <typename WT, int D> __device__ __forceinline__ void gb_own_rows(const char* row, int half, uint4 (&x)[GbTile<WT, D>::STEPS]) {
 #pragma unroll
     for (int st = 0; st < GbTile<WT, D>::STEPS; ++st) x[st] = ld16_q(row + st * 32 + half * 16);
 }
-// the lane's row of a gradient, y[j][i] = column 32 j + 8 (i / 4) + 4 half + i % 4, times scale; with turn, rotated back
+constexpr float GB_LN2 = 0.6931471805599453f;
+// columns col .. col + 3 and col + D / 2 .. of a row of a gradient, times scale; with turn, rotated back
+template <typename WT, int D> __device__ __forceinline__ void gb_write4(char* row, const float2* turn, int col, float scale, f32x4 a, f32x4 b) {
+    constexpr int ESZ = Traits<WT>::ESZ;
+    a *= scale;
+    b *= scale;
+    if (turn) {
+        const f32x4 t0 = *reinterpret_cast<const f32x4*>(turn + col), t1 = *reinterpret_cast<const f32x4*>(turn + col + 2);
+        const float c[4] = {t0[0], t0[2], t1[0], t1[2]}, s[4] = {t0[1], t0[3], t1[1], t1[3]};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = a[e];
+            a[e] = x * c[e] + b[e] * s[e];
+            b[e] = b[e] * c[e] - x * s[e];
+        }
+    }
+    if constexpr (Traits<WT>::BF) {
+        *reinterpret_cast<u32x2_q*>(row + col * ESZ) = (u32x2_q)u32x2{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])};
+        *reinterpret_cast<u32x2_q*>(row + (col + D / 2) * ESZ) = (u32x2_q)u32x2{pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+    } else {
+        *reinterpret_cast<f32x4_q*>(row + col * ESZ) = (f32x4_q)a;
+        *reinterpret_cast<f32x4_q*>(row + (col + D / 2) * ESZ) = (f32x4_q)b;
+    }
+}
+// the lane's row, y[j][i] = column 32 j + 8 (i / 4) + 4 half + i % 4
 template <typename WT, int D>
 __device__ __forceinline__ void gb_write(char* row, const float2* turn, float scale, int half, const f32x16 (&y)[D / 32]) {
-    constexpr int ESZ = Traits<WT>::ESZ, NJ = D / 32;
+    constexpr int NJ = D / 32;
 #pragma unroll
     for (int j = 0; j < NJ / 2; ++j)
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
+        for (int u = 0; u < 4; ++u) {
             f32x4 a, b;
-            const int col = 32 * j + 8 * i4 + 4 * half;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                a[e] = y[j][4 * i4 + e] * scale;
-                b[e] = y[j + NJ / 2][4 * i4 + e] * scale;
+                a[e] = y[j][4 * u + e];
+                b[e] = y[j + NJ / 2][4 * u + e];
             }
-            if (turn) {
-                const f32x4 t0 = *reinterpret_cast<const f32x4*>(turn + col), t1 = *reinterpret_cast<const f32x4*>(turn + col + 2);
-                const float c[4] = {t0[0], t0[2], t1[0], t1[2]}, s[4] = {t0[1], t0[3], t1[1], t1[3]};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = a[e];
-                    a[e] = x * c[e] + b[e] * s[e];
-                    b[e] = b[e] * c[e] - x * s[e];
-                }
-            }
-            if constexpr (Traits<WT>::BF) {
-                *reinterpret_cast<u32x2_q*>(row + col * ESZ) = (u32x2_q)u32x2{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])};
-                *reinterpret_cast<u32x2_q*>(row + (col + D / 2) * ESZ) = (u32x2_q)u32x2{pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
-            } else {
-                *reinterpret_cast<f32x4_q*>(row + col * ESZ) = (f32x4_q)a;
-                *reinterpret_cast<f32x4_q*>(row + (col + D / 2) * ESZ) = (f32x4_q)b;
-            }
+            gb_write4<WT, D>(row, turn, 32 * j + 8 * u + 4 * half, scale, a, b);
         }
 }
 
 // ------------------------------------------------------------------------------------------
-// Gradients of the queries: 128 layout rows per workgroup, 32 per wavefront.  Key tiles: the layout rows R0 - 32 .. R0 + 127, among
-// which the queries see their own groups' [MASK] rows, then the real tokens up to the last group.
+// Gradients of the queries.  A wavefront owns 32 layout rows.  It rotates its queries (and leaves them, and the rows' statistics, for the
+// kernel of the keys), looks at its own groups' [MASK] keys - among its own 32 rows and, where its first row is not the first of its
+// group, the 32 before - and walks the real tokens up to its last group, 64 per stage, two buffers.  KW = 1: a workgroup is four wavefronts
+// of 32 rows; 2 (few rows): two, each shared by two wavefronts that take every other key tile and meet in the LDS at the end.
 // ------------------------------------------------------------------------------------------
-template <typename WT, int D>
+template <typename WT, int D, int KW>
 __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2) gb_dq_kernel(const GbParams P) {
     typedef GbTile<WT, D> Tile;
-    constexpr int ESZ = Traits<WT>::ESZ, PARTS = GbTraits<WT>::PARTS, NJ = D / 32, BUF = 2 * Tile::BYTES;
+    constexpr int ESZ = Traits<WT>::ESZ, GE = Traits<WT>::GE, PARTS = GbTraits<WT>::PARTS, NJ = D / 32, STEPS = Tile::STEPS, ROWS = GB_ROWS / KW;
+    constexpr int BUF = 4 * Tile::BYTES;                    // two key tiles, K and V each
+    static_assert(2 * BUF == GB_WAVES * 2 * Tile::BYTES, "a stage's buffers, or one key tile for each wavefront");
     __shared__ __attribute__((aligned(16))) char smem[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
+    const int rw = wave / KW, kw = wave % KW;
     // (the rows with the most keys start first; neighbours, which go to different XCDs, take different heads)
     const int K1 = P.k + 1, blk = gridDim.y - 1 - blockIdx.y, h = blockIdx.x, seq = blockIdx.z, hk = h / P.group;
-    const int R0 = GB_ROWS * blk, r0 = R0 + 32 * wave, r_last = min(R0 + GB_ROWS, P.rows) - 1, g_last = gb_group(P, r_last);
+    const int R0 = ROWS * blk, r0 = R0 + 32 * rw, r_last = min(R0 + ROWS, P.rows) - 1, g_last = gb_group(P, r_last);
     const bool active = r0 < P.rows;
-    const int n_own = P.k > 0 ? GB_WAVES + 1 : 0, n_tiles = n_own + g_last / 32 + 1;
+    const int n_stages = g_last / 64 + 1;
     const int qrow = min(r0 + c, r_last), qg = gb_group(P, qrow), w_first = min(r0, r_last), wg0 = gb_group(P, w_first), wg1 = gb_group(P, min(r0 + 31, r_last));
     const Tile L(lane);
     const char* krows = P.k_rot + ((size_t)seq * P.nkv + hk) * P.rows * D * ESZ;
     const char* vrows = P.v + ((size_t)seq * P.rows * P.nkv + hk) * D * ESZ;
-    const size_t vstride = (size_t)P.nkv * D * ESZ;
-    auto stage = [&](int t) __attribute__((always_inline)) {
-        const bool own = t < n_own;
-        const int hi = own ? r_last : g_last, first = min(max(own ? R0 - 32 + 32 * t : 32 * (t - n_own), 0), hi), step = own ? 1 : K1;
-        char* b = smem + (t & 1) * BUF;
-        gb_stage<WT, D, GB_WAVES>(krows + (size_t)first * step * D * ESZ, step * D * ESZ, hi - first, b, wave, lane);
-        gb_stage<WT, D, GB_WAVES>(vrows + (size_t)first * step * vstride, step * (unsigned)vstride, hi - first, b + Tile::BYTES, wave, lane);
+    const unsigned vstride = (unsigned)(P.nkv * D * ESZ);
+    auto stage_own = [&](int first) __attribute__((always_inline)) {   // layout rows first .. first + 31, to the wavefront's own tiles
+        char* b = smem + wave * 2 * Tile::BYTES;
+        const int from = min(max(first, 0), r_last);
+        gb_stage<WT, D, 1>(krows + (size_t)from * D * ESZ, D * ESZ, r_last - from, b, 0, lane);
+        gb_stage<WT, D, 1>(vrows + (size_t)from * vstride, vstride, r_last - from, b + Tile::BYTES, 0, lane);
     };
-    stage(0);
-    const size_t qat = ((size_t)seq * P.nq + h) * P.rows + qrow, part = (size_t)P.seqs * P.nq * P.rows * D * ESZ;
-    uint4 q[PARTS][Tile::STEPS], d_o[Tile::STEPS];
+    auto stage = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) gb_own_rows<WT, D>(P.q_rot + p * part + qat * D * ESZ, half, q[p]);
-    gb_own_rows<WT, D>(P.d_out + (((size_t)seq * P.rows + qrow) * P.nq + h) * D * ESZ, half, d_o);
-    const float2 st = make_float2(P.lse2[qat], P.delta[qat]);
+        for (int i = 0; i < 2; ++i) {
+            const int first = min(64 * t + 32 * i, g_last);
+            char* b = smem + (t & 1) * BUF + i * 2 * Tile::BYTES;
+            gb_stage<WT, D, GB_WAVES>(krows + (size_t)first * K1 * D * ESZ, K1 * D * ESZ, g_last - first, b, wave, lane);
+            gb_stage<WT, D, GB_WAVES>(vrows + (size_t)first * K1 * vstride, K1 * vstride, g_last - first, b + Tile::BYTES, wave, lane);
+        }
+    };
+    // own [MASK] keys: the wavefront's own tile and the one before (KW = 2: one of the two each)
+    const bool before = wg0 * K1 != r0;
+    if (P.k > 0) stage_own(r0 - 32 * kw);
+
+    // ---- the lane's row: statistics, the rotated query as operand
+    const size_t at = ((size_t)seq * P.rows + qrow) * P.nq + h, to = ((size_t)seq * P.nq + h) * P.rows + qrow, part = (size_t)P.seqs * P.nq * P.rows * D * ESZ;
+    uint4 q[PARTS][STEPS], d_o[STEPS];
+    gb_own_rows<WT, D>(P.q + at * D * ESZ, half, q[0]);
+    gb_own_rows<WT, D>(P.d_out + at * D * ESZ, half, d_o);
+    float delta0 = 0.f;
+    {
+        const float* o = P.out + at * D + half * GE;
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) {
+            float x[GE];
+            unpack_group<WT>(d_o[t], x);
+#pragma unroll
+            for (int e = 0; e < GE; e += 4) {
+                const f32x4 y = load4_q<float>(o + 2 * GE * t + e);
+                delta0 -= (x[e] * y[0] + x[e + 1] * y[1]) + (x[e + 2] * y[2] + x[e + 3] * y[3]);
+            }
+        }
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta0), __float_as_uint(delta0), false, false);
+        delta0 = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    }
+    const float lse0 = -P.lse[at] * 1.4426950408889634f, qscale = P.inv_sqrt_d * 1.4426950408889634f;
+    const float2* turn = P.table + (size_t)(qrow - qg * P.k) * (D / 2);
+    const bool owner = kw == 0 && r0 + c < P.rows;
+    if (owner && half == 0) {
+        P.lse2[to] = lse0;
+        P.delta[to] = delta0;
+    }
+#pragma unroll
+    for (int t = 0; t < STEPS / 2; ++t) {
+        float a[GE], b[GE], ra[GE], rb[GE];
+        unpack_group<WT>(q[0][t], a);
+        unpack_group<WT>(q[0][t + STEPS / 2], b);
+        const f32x4* cs = reinterpret_cast<const f32x4*>(turn + GE * (2 * t + half));
+#pragma unroll
+        for (int e = 0; e < GE; e += 2) {
+            const f32x4 x = cs[e / 2];
+            ra[e] = (a[e] * x[0] - b[e] * x[1]) * qscale;
+            rb[e] = (b[e] * x[0] + a[e] * x[1]) * qscale;
+            ra[e + 1] = (a[e + 1] * x[2] - b[e + 1] * x[3]) * qscale;
+            rb[e + 1] = (b[e + 1] * x[2] + a[e + 1] * x[3]) * qscale;
+        }
+        if constexpr (Traits<WT>::BF) {
+            unsigned hi[4];
+            q[0][t] = __builtin_bit_cast(uint4, split_hi(ra, hi));
+            q[1][t] = __builtin_bit_cast(uint4, split_lo(ra, hi));
+            q[0][t + STEPS / 2] = __builtin_bit_cast(uint4, split_hi(rb, hi));
+            q[1][t + STEPS / 2] = __builtin_bit_cast(uint4, split_lo(rb, hi));
+        } else {
+            q[0][t] = __builtin_bit_cast(uint4, f32x4{ra[0], ra[1], ra[2], ra[3]});
+            q[0][t + STEPS / 2] = __builtin_bit_cast(uint4, f32x4{rb[0], rb[1], rb[2], rb[3]});
+        }
+    }
+    if (owner) {
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int t = 0; t < STEPS; ++t) *reinterpret_cast<uint4*>(P.q_rot + p * part + to * D * ESZ + t * 32 + half * 16) = q[p][t];
+    }
     f32x16 y[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 16; ++i) y[j][i] = 0.f;
-    __syncthreads();
+
     // one key tile; masked: keys lo .. hi of it (counted from 4 half) are seen
-    auto work = [&](int t, auto masked, int lo, int hi) __attribute__((always_inline)) {
-        const char *kt = smem + (t & 1) * BUF, *vt = kt + Tile::BYTES;
-        float lse = st.x, delta = st.y;
+    auto work = [&](const char* kt, auto masked, int lo, int hi) __attribute__((always_inline)) {
+        const char* vt = kt + Tile::BYTES;
+        float lse = lse0, delta = delta0;
         asm volatile("" : "+v"(lse), "+v"(delta));          // (32 copies of them would be kept in registers across the loop)
         f32x16 s, dp;
+        auto probabilities = [&]() __attribute__((always_inline)) {   // dS in the place of s
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = lse;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) gb_scores<WT, D>(L, kt, [&](const Tile&, int t) __attribute__((always_inline)) { return q[p][t]; }, s);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) dp[i] = delta;
-        gb_scores<WT, D>(L, vt, [&](const Tile&, int t) __attribute__((always_inline)) { return d_o[t]; }, dp);
+            for (int i = 0; i < 16; ++i) {
+                const int key = 8 * (i / 4) + i % 4;
+                const float x = __builtin_amdgcn_exp2f(s[i]) * dp[i];
+                s[i] = !masked || (key >= lo && key <= hi) ? x : 0.f;
+            }
+        };
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int key = 8 * (i / 4) + i % 4;
-            const float x = __builtin_amdgcn_exp2f(s[i]) * dp[i];
-            s[i] = !masked || (key >= lo && key <= hi) ? x : 0.f;
+            s[i] = lse;
+            dp[i] = delta;
         }
-        gb_products<WT, D, masked>(L, kt, s, y);
+        if constexpr (Traits<WT>::BF) {
+            const Tile l = L.here();
+            bf16x8 ds[2];
+            constexpr int H = STEPS / 4, N = 2 * H + NJ / 2; // chunks: K rows, V rows, K columns
+            gb_chunks<N>(
+                [&](auto n, bf16x8(&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if constexpr (n < 2 * H) x[u] = __builtin_bit_cast(bf16x8, l.row(n < H ? kt : vt, 4 * (n % H) + u));
+                        else x[u] = l.template column<masked>(kt, (4 * (n - 2 * H) + u) % NJ, (4 * (n - 2 * H) + u) / NJ);
+                    }
+                },
+                [&](auto n, const bf16x8(&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if constexpr (n < H) {
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, q[0][4 * n + u]), s, 0, 0, 0);
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, q[PARTS - 1][4 * n + u]), s, 0, 0, 0);
+                        } else if constexpr (n < 2 * H) {
+                            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, d_o[4 * (n - H) + u]), dp, 0, 0, 0);
+                        } else {
+                            const int o = 4 * (n - 2 * H) + u;
+                            y[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], ds[o / NJ], y[o % NJ], 0, 0, 0);
+                        }
+                    }
+                    if constexpr (n == 2 * H - 1) {
+                        probabilities();
+                        const GbOperand<WT> p(s);
+                        ds[0] = p.b[0];
+                        ds[1] = p.b[1];
+                    }
+                });
+        } else {
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) gb_scores<WT, D>(L, kt, q[p], s);
+            gb_scores<WT, D>(L, vt, d_o, dp);
+            probabilities();
+            gb_products<WT, D, masked>(L, kt, s, y);
+        }
     };
+    if (P.k > 0) {
+        const char* mine = smem + wave * 2 * Tile::BYTES;
+        const int lo = qg * K1 + 1 - 4 * half, hi = qrow - 4 * half;
+        for (int i = kw; i < 2; i += KW) {                   // 0: rows r0 .., 1: rows r0 - 32 ..
+            if (KW == 1 && i == 1) {
+                if (before) stage_own(r0 - 32);              // (nobody else reads these tiles)
+            }
+            __syncthreads();
+            if (active && (i == 0 || before)) work(mine, std::true_type{}, lo - (r0 - 32 * i), hi - (r0 - 32 * i));
+        }
+        __syncthreads();
+    }
+    // real tokens: stages that all of the wavefront's queries see, some of them, none
+    stage(0);
+    __syncthreads();
     int t = 0;
-    for (; t < n_own; ++t) {
-        if (t + 1 < n_tiles) stage(t + 1);
-        // (the wavefront's own rows and, where its first row is not the first of its group, the tile before)
-        const int first = R0 - 32 + 32 * t + 4 * half;
-        if (active && (t == wave + 1 || (t == wave && wg0 * K1 != r0))) work(t, std::true_type{}, qg * K1 + 1 - first, qrow - first);
+    auto tile = [&](int i) __attribute__((always_inline)) { return smem + (t & 1) * BUF + i * 2 * Tile::BYTES; };
+    for (const int end = active ? (wg0 + 1) / 64 : 0; t < end; ++t) {
+        if (t + 1 < n_stages) stage(t + 1);
+#pragma unroll
+        for (int i = 0; i < 2 / KW; ++i) work(tile(i * KW + kw), std::false_type{}, 0, 0);
         __syncthreads();
     }
-    // real tokens: tiles that all of the wavefront's queries see, some of them, none
-    for (const int end = active ? n_own + (wg0 + 1) / 32 : n_own; t < end; ++t) {
-        if (t + 1 < n_tiles) stage(t + 1);
-        work(t, std::false_type{}, 0, 0);
+    for (; t < n_stages; ++t) {
+        if (t + 1 < n_stages) stage(t + 1);
+#pragma unroll 1
+        for (int i = kw; i < 2; i += KW) {
+            const int first = 64 * t + 32 * i;
+            if (active && first <= wg1) work(tile(i), std::true_type{}, -first - 4 * half, qg - first - 4 * half);
+        }
         __syncthreads();
     }
-    for (; t < n_tiles; ++t) {
-        if (t + 1 < n_tiles) stage(t + 1);
-        const int first = 32 * (t - n_own);
-        if (active && first <= wg1) work(t, std::true_type{}, -first - 4 * half, qg - first - 4 * half);
+    if constexpr (KW == 2) {
+        f32x4* area = reinterpret_cast<f32x4*>(smem) + rw * NJ * 4 * 64 + lane;
+        if (kw) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) area[(j * 4 + u) * 64] = f32x4{y[j][4 * u], y[j][4 * u + 1], y[j][4 * u + 2], y[j][4 * u + 3]};
+        }
         __syncthreads();
+        if (kw) return;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const f32x4 v = area[(j * 4 + u) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[j][4 * u + e] += v[e];
+            }
     }
-    if (r0 + c < P.rows)
-        gb_write<WT, D>(P.d_q + (((size_t)seq * P.rows + qrow) * P.nq + h) * D * ESZ, P.table + (size_t)(qrow - qg * P.k) * (D / 2), P.inv_sqrt_d, half, y);
+    if (r0 + c < P.rows) gb_write<WT, D>(P.d_q + at * D * ESZ, turn, P.inv_sqrt_d, half, y);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -369,33 +491,76 @@ template <typename WT, int D, bool V_LDS> struct GbKeys {
                 for (int e = 0; e < 4; ++e) y[4 * q + e] = v[e];
             }
         };
-        start(stats, s);
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) gb_scores<WT, D>(L, buf + p * Tile::BYTES, [&](const Tile&, int t) __attribute__((always_inline)) { return kf[t]; }, s);
         const char* dt = buf + PARTS * Tile::BYTES;
-        start(stats + two, dp);
-        gb_scores<WT, D>(L, dt, [&](const Tile& l, int t) __attribute__((always_inline)) {
-            if constexpr (V_LDS) return l.row(v_tile, t);
-            else return vf[t];
-        }, dp);
+        auto probabilities = [&]() __attribute__((always_inline)) {   // P in the place of s, dS in that of dp
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int row = 8 * (i / 4) + i % 4;
-            const bool in = !MASKED || (row >= lo && row <= hi);
-            const float p = in ? __builtin_amdgcn_exp2f(s[i]) : 0.f;
-            s[i] = p;
-            dp[i] = in ? p * dp[i] : 0.f;
+            for (int i = 0; i < 16; ++i) {
+                const int row = 8 * (i / 4) + i % 4;
+                const bool in = !MASKED || (row >= lo && row <= hi);
+                const float p = in ? __builtin_amdgcn_exp2f(s[i]) : 0.f;
+                s[i] = p;
+                dp[i] = in ? p * dp[i] : 0.f;
+            }
+        };
+        start(stats, s);
+        if constexpr (Traits<WT>::BF) {
+            const Tile l = L.here();
+            bf16x8 p[2], ds[2];
+            // chunks: rows of the queries' high and low parts; of d_out (with the values', if they stand in LDS); columns of d_out, of the parts
+            constexpr int ST = Tile::STEPS, A = 2 * ST / 4, B = A + (V_LDS ? ST / 2 : ST / 4), C = NJ / 2, N = B + 3 * C;
+            gb_chunks<N>(
+                [&](auto n, bf16x8(&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if constexpr (n < A) {
+                            x[u] = __builtin_bit_cast(bf16x8, l.row(buf + (4 * n + u) / ST * Tile::BYTES, (4 * n + u) % ST));
+                        } else if constexpr (n < B) {
+                            if constexpr (V_LDS) x[u] = __builtin_bit_cast(bf16x8, l.row(u & 1 ? v_tile : dt, 2 * (n - A) + u / 2));
+                            else x[u] = __builtin_bit_cast(bf16x8, l.row(dt, 4 * (n - A) + u));
+                        } else {
+                            const int o = 4 * ((n - B) % C) + u;
+                            x[u] = l.template column<MASKED>((n - B) / C == 0 ? dt : buf + ((n - B) / C - 1) * Tile::BYTES, o % NJ, o / NJ);
+                        }
+                    }
+                    if constexpr (n == A) start(stats + two, dp);
+                },
+                [&](auto n, const bf16x8(&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if constexpr (n < A) {
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, kf[(4 * n + u) % ST]), s, 0, 0, 0);
+                        } else if constexpr (n < B) {
+                            if constexpr (V_LDS) {
+                                if (u & 1) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u - 1], x[u], dp, 0, 0, 0);
+                            } else {
+                                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, vf[4 * (n - A) + u]), dp, 0, 0, 0);
+                            }
+                        } else {
+                            const int o = 4 * ((n - B) % C) + u;
+                            if constexpr (n < B + C) dv[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], p[o / NJ], dv[o % NJ], 0, 0, 0);
+                            else dk[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], ds[o / NJ], dk[o % NJ], 0, 0, 0);
+                        }
+                    }
+                    if constexpr (n == B - 1) {
+                        probabilities();
+                        const GbOperand<WT> a(s), b(dp);
+                        p[0] = a.b[0]; p[1] = a.b[1]; ds[0] = b.b[0]; ds[1] = b.b[1];
+                    }
+                });
+        } else {
+            start(stats + two, dp);
+            gb_scores<WT, D>(L, buf, kf, s);
+            gb_scores<WT, D>(L, dt, vf, dp);
+            probabilities();
+            gb_products<WT, D, MASKED>(L, dt, s, dv);
+            gb_products<WT, D, MASKED>(L, buf, dp, dk);
         }
-        const GbOperand<WT> p(s), ds(dp);
-        gb_products<WT, D, MASKED>(L, dt, p, dv);
-#pragma unroll
-        for (int q = 0; q < PARTS; ++q) gb_products<WT, D, MASKED>(L, buf + q * Tile::BYTES, ds, dk);
     }
 };
 template <typename WT, int D>
 __device__ __forceinline__ void gb_write_keys(const GbParams& P, int seq, int hk, int row, int pos, int half, const f32x16 (&dk)[D / 32], const f32x16 (&dv)[D / 32]) {
     const size_t at = (((size_t)seq * P.rows + row) * P.nkv + hk) * D * Traits<WT>::ESZ;
-    gb_write<WT, D>(P.d_k + at, P.table + (size_t)pos * (D / 2), 0.6931471805599453f, half, dk);   // (the queries carry log2(e) / sqrt(d))
+    gb_write<WT, D>(P.d_k + at, P.table + (size_t)pos * (D / 2), GB_LN2, half, dk);   // (the queries carry log2(e) / sqrt(d))
     gb_write<WT, D>(P.d_v + at, nullptr, 1.f, half, dv);
 }
 
@@ -553,26 +718,30 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
     if (w0 + c < P.T) gb_write_keys<WT, D>(P, seq, hk, key * K1, key, half, keys.dk, keys.dv);
 }
 
-// The parts' sums, added in order: a wavefront per tile of 32 keys
+// The parts' sums, added in order.  A workgroup takes a tile of 32 keys, a wavefront one gradient's column blocks j and j + NJ / 2, which
+// the rotation mixes
 template <typename WT, int D>
-__global__ void __launch_bounds__(64) gb_merge_kernel(const GbParams P, const GbWork W, int keys_wg) {
-    constexpr int NJ = D / 32;
-    const int lane = threadIdx.x, c = lane & 31, half = lane >> 5, per_wg = keys_wg / 32;
+__global__ void __launch_bounds__(D * 2) gb_merge_kernel(const GbParams P, const GbWork W, int keys_wg) {
+    constexpr int ESZ = Traits<WT>::ESZ, NJ = D / 32, PART = 2 * NJ * 4 * 64;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, half = lane >> 5, per_wg = keys_wg / 32;
+    const int which = wave / (NJ / 2), j0 = wave % (NJ / 2);   // dk, dv
     const int sub = blockIdx.x % per_wg, unit = blockIdx.x / per_wg, kt = unit / W.heads, head = unit - kt * W.heads, seq = head / P.nkv, hk = head - seq * P.nkv;
     const int key = kt * keys_wg + 32 * sub + c;
-    if (kt * keys_wg + 32 * sub >= P.T) return;
-    const f32x4* from = reinterpret_cast<const f32x4*>(W.partial) + (size_t)blockIdx.x * W.splits * (2 * NJ * 4 * 64) + lane;
-    f32x16 y[2][NJ];
+    if (key >= P.T) return;
+    const f32x4* from = reinterpret_cast<const f32x4*>(W.partial) + (size_t)blockIdx.x * W.splits * PART + (which * NJ + j0) * 4 * 64 + lane;
+    f32x4 a[4], b[4];
 #pragma unroll
-    for (int j = 0; j < 2 * NJ; ++j)
+    for (int u = 0; u < 4; ++u) { a[u] = f32x4{0.f, 0.f, 0.f, 0.f}; b[u] = a[u]; }
+#pragma unroll 2
+    for (int i = 0; i < W.splits; ++i, from += PART)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            f32x4 v = from[(j * 4 + q) * 64];
-            for (int i = 1; i < W.splits; ++i) v += from[(size_t)i * (2 * NJ * 4 * 64) + (j * 4 + q) * 64];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[j / NJ][j % NJ][4 * q + e] = v[e];
+        for (int u = 0; u < 4; ++u) {
+            a[u] += from[u * 64];
+            b[u] += from[(NJ / 2 * 4 + u) * 64];
         }
-    if (key < P.T) gb_write_keys<WT, D>(P, seq, hk, key * (P.k + 1), key, half, y[0], y[1]);
+    char* row = (which ? P.d_v : P.d_k) + (((size_t)seq * P.rows + (size_t)key * (P.k + 1)) * P.nkv + hk) * D * ESZ;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) gb_write4<WT, D>(row, which ? nullptr : P.table + (size_t)key * (D / 2), 32 * j0 + 8 * u + 4 * half, which ? 1.f : GB_LN2, a[u], b[u]);
 }
 
 // the checks are those of ps_group_attention
@@ -588,17 +757,21 @@ int check(const ps_group_attn_grad_args* a) {
     return ga_check(&f);
 }
 
-// How the gradients of keys are cut: keys of a workgroup, parts of their rows
-struct GbPlan { int keys, heads, tiles, splits; };
+// How a call is cut: wavefronts that share 32 query rows; keys of a workgroup, parts of their rows
+struct GbPlan { int kw, keys, heads, tiles, splits; };
+static int env(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
 GbPlan plan(const ps_group_attn_grad_args* a) {
     GbPlan L;
+    const long long row_blocks = ((long long)a->tokens * (a->k + 1) + GB_ROWS - 1) / GB_ROWS * a->n_heads * a->seqs;
+    L.kw = env("GB_KW", row_blocks < 512 ? 2 : 1);
     L.heads = a->n_kv_heads * a->seqs;
     const bool big = a->dtype == PS_F32 && a->head_dim == 128;   // (one wavefront per SIMD)
     L.keys = !big && (long long)((a->tokens + 127) / 128) * L.heads >= 256 ? 128 : 64;
+    if (!big) L.keys = env("GB_KEYS", L.keys);
     L.tiles = (a->tokens + L.keys - 1) / L.keys;
     const long long units = (long long)L.tiles * L.heads;
     const int stages = (a->tokens * (a->k + 1) + 63) / 64 * (a->n_heads / a->n_kv_heads);
-    L.splits = (int)std::max(1LL, std::min(std::min(1024 / units, 16LL), (long long)stages / 4));
+    L.splits = env("GB_SPLITS", (int)std::max(1LL, std::min(std::min(1024 / units, 16LL), (long long)stages / 4)));
     return L;
 }
 
@@ -621,15 +794,16 @@ template <typename WT, int D, int KW> void launch_keys(const GbParams& P, const 
     typedef GbDkv<WT, D, KW> C;
     const unsigned own = (unsigned)((W.own_tiles + C::OWNERS - 1) / C::OWNERS);
     hipLaunchKernelGGL((gb_dkv_kernel<WT, D, KW>), dim3((unsigned)(W.units * W.splits) + own), dim3(C::WAVES * 64), 0, s, P, W);
-    if (W.splits > 1) hipLaunchKernelGGL((gb_merge_kernel<WT, D>), dim3(W.units * KW), dim3(64), 0, s, P, W, G.keys);
+    if (W.splits > 1) hipLaunchKernelGGL((gb_merge_kernel<WT, D>), dim3(W.units * KW), dim3(D * 2), 0, s, P, W, G.keys);
 }
 
 template <typename WT, int D> int launch(const GbParams& P, const GbPlan& G, float* partial, hipStream_t s) {
     // (as ga_rope_kernel: where positions are few, several workgroups of at most one item per thread share one)
-    const long long items = (long long)P.seqs * P.nq * (D / 8) * (P.k + 1);
-    const unsigned share = (unsigned)std::max(1LL, std::min((items + 255) / 256, 4096LL / (P.T + P.k)));
-    hipLaunchKernelGGL((gb_prep_kernel<WT, D>), dim3(P.T + P.k, share), dim3(256), 0, s, P);
-    hipLaunchKernelGGL((gb_dq_kernel<WT, D>), dim3(P.nq, (P.rows + GB_ROWS - 1) / GB_ROWS, P.seqs), dim3(GB_THREADS), 0, s, P);
+    const long long items = (long long)P.seqs * P.nkv * (D / 8) * (P.k + 1);
+    hipLaunchKernelGGL((gb_prep_kernel<WT, D>), dim3(P.T + P.k, (unsigned)std::max(1LL, std::min((items + 255) / 256, 2048LL / (P.T + P.k)))), dim3(256), 0, s, P);
+    const dim3 grid(P.nq, (P.rows + GB_ROWS / G.kw - 1) / (GB_ROWS / G.kw), P.seqs);
+    if (G.kw == 2) hipLaunchKernelGGL((gb_dq_kernel<WT, D, 2>), grid, dim3(GB_THREADS), 0, s, P);
+    else hipLaunchKernelGGL((gb_dq_kernel<WT, D, 1>), grid, dim3(GB_THREADS), 0, s, P);
     const GbWork W = {G.heads, G.splits, G.tiles * G.heads, P.k > 0 ? (P.T + P.gpt - 1) / P.gpt * G.heads : 0, partial};
     if constexpr (D * Traits<WT>::ESZ > 256) {
         launch_keys<WT, D, 2>(P, G, W, s);
