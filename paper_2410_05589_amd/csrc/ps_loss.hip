@@ -13,7 +13,7 @@
 // The vocabulary is gone through in pieces; two products for each, the floor being their 4 V H operations a row:
 //   vl_score_kernel   W h^T, one tile of 128 x 128 per workgroup: exponentials to the workspace (storage type), sums of rows beside them
 //   vl_grad_kernel    exponentials . W, added to what the pieces before left, in float32
-// then vl_finish_kernel adds up the rows' sums and makes losses and gradients of them.
+// before the last of which vl_rows_kernel adds up the rows' sums and makes their losses and the gradients' factors.
 #include <math.h>
 
 #include "ps_train_device.h"
@@ -21,7 +21,8 @@
 namespace {
 
 constexpr int VL_THREADS = 256, VL_TILE = 128;
-constexpr float VL_SHIFT = 64.f, VL_FAR = 80.f, VL_LOG2E = 1.4426950408889634f, VL_LN2 = 0.6931471805599453f;
+enum { VL_NEAR = 0, VL_FAR_APART = 1, VL_DONE = 2, VL_ZERO = 3 };
+constexpr float VL_SHIFT = 64.f, VL_FAR = 0x1p80f, VL_LOG2E = 1.4426950408889634f, VL_LN2 = 0.6931471805599453f;
 
 struct VlParams {
     int rows, H, V, row0, rows_c;     // this chunk: rows row0 .. row0 + rows_c - 1
@@ -33,8 +34,9 @@ struct VlParams {
     const float* weights;
     float* loss;
     char* d_hidden;
-    float *tl, *sums, *acc;           // target logits; sums [rows_c][nsum]; products [splits][rows_c][H]
-    int* far;                         // rows whose logits lie too far apart
+    float *tl, *sums, *acc, *alone;   // target logits; sums [rows_c][nsum]; products [splits][rows_c][H]; those of rows by themselves [rows_c][H]
+    int* state;                       // rows: VL_NEAR, VL_FAR_APART (set by the scores), then VL_DONE, VL_ZERO (vl_rows_kernel)
+    float2* factor;                   // of a row's products, of its target's row of the LM head
     char* x;                          // exponentials [rows_c][ldx], storage type
 };
 
@@ -64,7 +66,7 @@ template <typename WT> __global__ void __launch_bounds__(VL_THREADS) vl_target_k
     const float t = counts ? vl_dot<WT>(P, row, P.targets[row], lane) : 0.f;
     if (lane == 0) {
         P.tl[row] = t;
-        P.far[row] = 0;
+        P.state[row] = VL_NEAR;
     }
 }
 
@@ -147,7 +149,6 @@ __global__ void __launch_bounds__(VL_THREADS, 2) vl_score_kernel(const VlParams 
         const int t = P.targets[row] - P.v0 - vt - wv - 4 * half, end = P.V - P.v0 - vt - wv - 4 * half;
         const float ref = -P.tl[row] * VL_LOG2E - VL_SHIFT;
         float sum = 0.f;
-        bool far = false;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -158,7 +159,6 @@ __global__ void __launch_bounds__(VL_THREADS, 2) vl_score_kernel(const VlParams 
                     const int at = 32 * i + 8 * q + e;
                     const float y = fmaf(acc[i][j][4 * q + e], VL_LOG2E, ref);
                     const bool in = at != t && at < end;
-                    far |= in && y > VL_FAR && y < INFINITY;
                     v[e] = in ? __builtin_amdgcn_exp2f(y) : 0.f;
                     sum += v[e];
                 }
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(VL_THREADS, 2) vl_score_kernel(const VlParams 
         const auto sw2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
         sum = __uint_as_float(sw2[0]) + __uint_as_float(sw2[1]);
         if (r < P.rows_c) {
-            if (far) P.far[row] = 1;
+            if (sum > VL_FAR) P.state[row] = VL_FAR_APART;   // (infinite among them)
             if (half == 0) P.sums[(size_t)r * P.nsum + (P.v0 + vt + wv) / 64] = sum;
         }
     }
@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlPa
         const int rr = 64 * wn + 32 * j + c, r = rt + rr, row = P.row0 + min(r, P.rows_c - 1);
         const int base = P.v0 + vt + 128 * wm, t = P.targets[row] - base - 4 * half, end = P.V - base - 4 * half;
         const float ref = -P.tl[row] * VL_LOG2E - VL_SHIFT;
-        float sum[2] = {0.f, 0.f}, top = -INFINITY;
+        float sum[2] = {0.f, 0.f};
         // (a target among the wavefront's tokens, or the vocabulary's end: those count nothing)
         if (__any(((unsigned)(t + 4) < 132u) | (end < 128))) {
 #pragma unroll
@@ -418,7 +418,6 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlPa
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float y = fmaf(acc[i][j][4 * q + e], VL_LOG2E, ref);
-                    top = fmaxf(top, y);
                     v[e] = __builtin_amdgcn_exp2f(y);
                     sum[e & 1] += v[e];
                 }
@@ -430,8 +429,9 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlPa
         const float mine = sum[0] + sum[1];
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mine), __float_as_uint(mine), false, false);
         if (r < P.rows_c) {
-            if (top > VL_FAR && top < INFINITY) P.far[row] = 1;
-            if (half == 0) P.sums[(size_t)r * P.nsum + (P.v0 + vt) / 128 + wm] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+            const float both = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+            if (both > VL_FAR) P.state[row] = VL_FAR_APART;
+            if (half == 0) P.sums[(size_t)r * P.nsum + (P.v0 + vt) / 128 + wm] = both;
         }
     }
     if (!P.x) return;
@@ -444,6 +444,8 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_score_wide_kernel(const VlPa
     }
 }
 
+// (LAST: of a whole row's products the gradient is made at once)
+template <bool LAST>
 __global__ void __launch_bounds__(VW_THREADS, 2) vl_grad_wide_kernel(const VlParams P, int nx, int ny) {
     __shared__ __attribute__((aligned(16))) char b0[VW_BUF], b1[VW_BUF], b2[VW_BUF], b3[VW_BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
@@ -460,6 +462,12 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_grad_wide_kernel(const VlPar
     for (int i = 0; i < 2; ++i) {
         const unsigned row = 4 * wave + 2 * i + (lane >> 5), f = (row & 3) | ((row >> 3 & 1) << 2), chunk = ((lane & 31) >> 1) ^ (f << 1);
         col[i] = min((unsigned)ct * 2 + chunk * 32 + (lane & 1) * 16, rb - 16);
+    }
+    __shared__ float4 info[LAST ? VW_TILE : 1];              // the rows' factors, state, target
+    if (LAST && tid < VW_TILE) {
+        const int r = min(rt + tid, P.rows_c - 1), state = P.state[P.row0 + r];
+        const float2 f = P.factor[r];
+        info[tid] = make_float4(f.x, f.y, (float)state, __int_as_float(state == VL_NEAR ? P.targets[P.row0 + r] : 0));
     }
     f32x16 acc[4][2];
     float* out = P.acc + (size_t)split * P.rows_c * P.H;
@@ -497,24 +505,63 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_grad_wide_kernel(const VlPar
                             for (int i = 0; i < 4; ++i) x.a[i][t] = __builtin_bit_cast(bf16x8, ld16(b + (a0 ^ (t << 5)) + i * 2048));
                         }
                     }, acc);
+    // ---- lane (c, half) holds columns 64 wn + 32 j + c of rows 128 wm + 32 i + 8 (e / 4) + 4 half + e % 4
+    if constexpr (LAST) {
+        // the targets' rows come into the LDS (rows of 512 bytes, 64 to a buffer, 64-byte blocks 2 m and 2 m + 1 exchanged in every second
+        // four rows: the halves' rows fall into different banks), turn into the gradient there and leave in whole lines
+        auto buffer = [&](int row) __attribute__((always_inline)) { return row < 128 ? row < 64 ? b0 : b1 : row < 192 ? b2 : b3; };
+        char* const mine = buffer(32 * wave);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 16; ++i) {
+            const int rr = 32 * wave + 2 * i + (lane >> 5), piece = (lane & 31) ^ ((rr & 4) ? 4 : 0);
+            const char* from = P.w + (size_t)(unsigned)__float_as_int(info[rr].w) * rb + min((unsigned)ct * 2 + piece * 16, rb - 16);
+            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)from, (lds_void*)(mine + ((32 * wave + 2 * i) & 63) * 512), 16, 0, 0);
+        }
+        __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < 4; ++i) {
+            char* const at = buffer(128 * wm + 32 * i) + 32 * (i & 1) * 512 + (64 * wn + c) * 2;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int r = rt + 128 * wm + 32 * i + 8 * (e / 4) + 4 * half + e % 4, x = ct + 64 * wn + 32 * j + c;
-                if (r < P.rows_c && x < P.H) out[(size_t)r * P.H + x] = acc[i][j][e];
+                const int rr = 8 * (e / 4) + 4 * half + e % 4;   // of the 32
+                const f32x4 f = *reinterpret_cast<const f32x4*>(info + 128 * wm + 32 * i + rr);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint16_t* p = reinterpret_cast<uint16_t*>(at + rr * 512 + 64 * (j ^ half));
+                    const float v = acc[i][j][e] * f[0] + bf16_to_f32(*p) * f[1];
+                    *p = (uint16_t)pack_bf16x2(f[2] != 0.f ? 0.f : v, 0.f);
+                }
             }
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+            const int rr = 32 * wave + 2 * i + (lane >> 5), piece = (lane & 31) ^ ((rr & 4) ? 4 : 0);
+            const uint4 v = ld16(mine + (rr & 63) * 512 + (lane & 31) * 16);
+            if (rt + rr < P.rows_c && ct + 8 * piece < P.H && info[rr].z != (float)VL_DONE)
+                *reinterpret_cast<uint4*>(P.d_hidden + ((size_t)(P.row0 + rt + rr) * P.H + ct + 8 * piece) * 2) = v;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int r = rt + 128 * wm + 32 * i + 8 * (e / 4) + 4 * half + e % 4, x = ct + 64 * wn + 32 * j + c;
+                    if (r < P.rows_c && x < P.H) out[(size_t)r * P.H + x] = acc[i][j][e];
+                }
+    }
 }
 
-// sum over the workgroup in a fixed order, for every thread
-__device__ __forceinline__ float vl_block_sum(float v, float* s, int tid) {
-    v = wave_sum(v);
-    __syncthreads();
-    if ((tid & 63) == 0) s[tid >> 6] = v;
-    __syncthreads();
-    return (s[0] + s[1]) + (s[2] + s[3]);
+template <typename WT> __device__ __forceinline__ void vl_store_group(char* p, const float* v) {
+    u32x4 r;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if constexpr (Traits<WT>::BF) r[u] = pack_bf16x2(v[2 * u], v[2 * u + 1]);
+        else r[u] = __float_as_uint(v[u]);
+    }
+    *reinterpret_cast<u32x4*>(p) = r;
 }
 
 // A row whose logits lie too far above its target's: its maximum, then sums against it, 256 tokens at a time.  Returns log2 of
@@ -540,7 +587,7 @@ __device__ __attribute__((noinline)) float vl_row_alone(const VlParams& P, int r
     const float top = fmaxf(fmaxf(s[0], s[2]), fmaxf(s[4], s[6]));
     total = 0.f;
     for (int i = 0; i < 4; ++i) total += s[2 * i + 1] * __builtin_amdgcn_exp2f(s[2 * i] - top);
-    const float z = top + __builtin_amdgcn_logf(total) - P.tl[row] * VL_LOG2E;
+    const float z = top < INFINITY ? top + __builtin_amdgcn_logf(total) - P.tl[row] * VL_LOG2E : top;   // (an infinite logit: NaN among the probabilities)
     if (!P.d_hidden) return z;
     const float lse = top + __builtin_amdgcn_logf(total + __builtin_amdgcn_exp2f(P.tl[row] * VL_LOG2E - top));
     for (int v0 = 0; v0 < P.V; v0 += 256) {
@@ -569,61 +616,84 @@ __device__ __attribute__((noinline)) float vl_row_alone(const VlParams& P, int r
     return z;
 }
 
+// The rows' losses and the factors of their gradients, a wavefront per row; then the workgroup takes rows that are far apart one by one
 template <typename WT>
-__global__ void __launch_bounds__(VL_THREADS) vl_finish_kernel(const VlParams P) {
+__global__ void __launch_bounds__(VL_THREADS) vl_rows_kernel(const VlParams P) {
     constexpr int GE = Traits<WT>::GE, ESZ = Traits<WT>::ESZ;
     __shared__ float s[VL_THREADS];
-    const int tid = threadIdx.x, r = blockIdx.x, row = P.row0 + r;
-    char* out = P.d_hidden ? P.d_hidden + (size_t)row * P.H * ESZ : nullptr;
-    if (!vl_counts(P, row)) {
-        if (tid == 0) P.loss[row] = 0.f;
-        for (int c = tid; out && c < P.H / GE; c += VL_THREADS) *reinterpret_cast<uint4*>(out + (size_t)c * 16) = make_uint4(0u, 0u, 0u, 0u);
-        return;
-    }
-    const int target = P.targets[row];
-    const float weight = P.weights ? P.weights[row] : 1.f;
-    float* acc = P.acc + (size_t)r * P.H;
-    float z, scale = 1.f;                                    // log2 of sum_{v != t} exp(l_v - l_t)
-    int splits = P.splits;
-    if (P.far[row]) {
-        z = vl_row_alone<WT>(P, row, target, acc, s, tid);
-        splits = 1;
-    } else {
-        float sum = 0.f;
-        for (int i = tid; i < P.nsum; i += VL_THREADS) sum += P.sums[(size_t)r * P.nsum + i];
-        sum = vl_block_sum(sum, s, tid);
-        z = __builtin_amdgcn_logf(sum) + VL_SHIFT;
-        scale = 1.f / (sum + 0x1p-64f);
-    }
-    // log(1 + 2^z) and 2^z / (1 + 2^z)
-    const float e = __builtin_amdgcn_exp2f(-fabsf(z));
-    const float loss = z > 0.f ? z * VL_LN2 + log1pf(e) : log1pf(e), others = z > 0.f ? 1.f / (1.f + e) : e / (1.f + e);
-    if (tid == 0) P.loss[row] = weight * (z == z ? loss : z);
-    if (!out) return;
-    scale *= weight;
-    const float back = -weight * others;
-    for (int c = tid; c < P.H / GE; c += VL_THREADS) {
-        float sum[GE], wt[GE];
-#pragma unroll
-        for (int e4 = 0; e4 < GE; e4 += 4) *reinterpret_cast<f32x4*>(sum + e4) = *reinterpret_cast<const f32x4*>(acc + c * GE + e4);
-        for (int i = 1; i < splits; ++i)
-#pragma unroll
-            for (int e4 = 0; e4 < GE; e4 += 4) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(acc + (size_t)i * P.rows_c * P.H + c * GE + e4);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) sum[e4 + u] += v[u];
-            }
-        load_group<WT>(P.w + ((size_t)target * P.H + c * GE) * ESZ, wt);
-        uint4 v;
-        unsigned* o = &v.x;
-#pragma unroll
-        for (int u = 0; u < GE; ++u) sum[u] = sum[u] * scale + wt[u] * back;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if constexpr (Traits<WT>::BF) o[u] = pack_bf16x2(sum[2 * u], sum[2 * u + 1]);
-            else o[u] = __float_as_uint(sum[u]);
+    __shared__ int far_apart[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r0 = 4 * blockIdx.x;
+    // z: log2 of sum_{v != t} exp(l_v - l_t); the loss is log(1 + 2^z), the others' probability 2^z / (1 + 2^z)
+    auto finish = [&](int r, float z, float scale) __attribute__((always_inline)) {
+        const float weight = P.weights ? P.weights[P.row0 + r] : 1.f, e = __builtin_amdgcn_exp2f(-fabsf(z));
+        const float loss = z > 0.f ? z * VL_LN2 + log1pf(e) : log1pf(e), others = z > 0.f ? 1.f / (1.f + e) : e / (1.f + e);
+        const float2 f = make_float2(scale * weight, -weight * others);
+        if (lane == 0) {
+            P.loss[P.row0 + r] = weight * (z == z ? loss : z);
+            P.factor[r] = f;
         }
-        *reinterpret_cast<uint4*>(out + (size_t)c * 16) = v;
+        return f;
+    };
+    {
+        const int r = r0 + wave, row = P.row0 + min(r, P.rows_c - 1);
+        const int state = P.state[row];
+        const bool counts = vl_counts(P, row);
+        float sum = 0.f;
+        for (int i = lane; i < P.nsum; i += 64) sum += P.sums[(size_t)(row - P.row0) * P.nsum + i];
+        sum = wave_sum(sum);
+        const bool far = r < P.rows_c && counts && state == VL_FAR_APART;
+        if (r < P.rows_c && counts && !far) finish(r, __builtin_amdgcn_logf(sum) + VL_SHIFT, 1.f / (sum + 0x1p-64f));
+        if (lane == 0) {
+            far_apart[wave] = far;
+            if (r < P.rows_c && !counts) {
+                P.loss[row] = 0.f;
+                P.factor[r] = make_float2(0.f, 0.f);
+                P.state[row] = VL_ZERO;
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = 0; i < 4; ++i) {
+        if (!far_apart[i]) continue;
+        const int r = r0 + i, row = P.row0 + r, target = P.targets[row];
+        float* acc = P.alone + (size_t)r * P.H;
+        const float2 f = finish(r, vl_row_alone<WT>(P, row, target, acc, s, tid), 1.f);
+        if (tid == 0) P.state[row] = VL_DONE;
+        if (!P.d_hidden) continue;
+        for (int c = tid; c < P.H / GE; c += VL_THREADS) {
+            float sum[GE], wt[GE];
+            load_group<WT>(P.w + ((size_t)target * P.H + c * GE) * ESZ, wt);
+#pragma unroll
+            for (int u = 0; u < GE; ++u) sum[u] = acc[c * GE + u] * f.x + wt[u] * f.y;
+            vl_store_group<WT>(P.d_hidden + ((size_t)row * P.H + c * GE) * ESZ, sum);
+        }
+    }
+}
+
+// The gradient of rows whose products are in parts: a workgroup per row
+template <typename WT>
+__global__ void __launch_bounds__(VL_THREADS) vl_join_kernel(const VlParams P) {
+    constexpr int GE = Traits<WT>::GE, ESZ = Traits<WT>::ESZ;
+    const int r = blockIdx.x, row = P.row0 + r, state = P.state[row];
+    if (state == VL_DONE) return;
+    const float2 f = P.factor[r];
+    const char* wt = P.w + (size_t)(state == VL_NEAR ? P.targets[row] : 0) * P.H * ESZ;
+    for (int c = threadIdx.x; c < P.H / GE; c += VL_THREADS) {
+        float sum[GE], w[GE];
+#pragma unroll
+        for (int u = 0; u < GE; ++u) sum[u] = 0.f;
+        const float* acc = P.acc + (size_t)r * P.H + c * GE;
+        for (int i = 0; i < P.splits; ++i, acc += (size_t)P.rows_c * P.H)
+#pragma unroll
+            for (int q = 0; q < GE; q += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(acc + q);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sum[q + u] += v[u];
+            }
+        load_group<WT>(wt + (size_t)c * 16, w);
+#pragma unroll
+        for (int u = 0; u < GE; ++u) sum[u] = state == VL_NEAR ? sum[u] * f.x + w[u] * f.y : 0.f;
+        vl_store_group<WT>(P.d_hidden + ((size_t)row * P.H + c * GE) * ESZ, sum);
     }
 }
 
@@ -640,12 +710,23 @@ constexpr long long VL_PIECE_BYTES = 288ll << 20;            // of exponentials 
 struct VlPlan {
     bool wide;
     int tile, rows_c, piece, nsum;
-    size_t tl, far, sums, acc, x, total;
+    size_t tl, state, factor, sums, acc, alone, x, total;
 };
-// where a chunk's tiles of the second product leave workgroups idle, several share a tile's tokens, of which each keeps at least 512
+// Where a chunk's tiles of the second product leave workgroups idle, several share a tile's tokens: the fewest that leave the
+// least time, counted in rounds of all workgroups over the share of the tokens (a part costs about as much as 2048 tokens: its sums are
+// written, read and added)
 int splits_of(const VlPlan& L, int hidden, int rows) {
-    const int tiles = (rows + L.tile - 1) / L.tile * ((hidden + L.tile - 1) / L.tile);
-    return std::max(1, std::min((L.wide ? 256 : 512) / tiles, L.piece / 512));
+    const int slots = L.wide ? 256 : 512, tiles = (rows + L.tile - 1) / L.tile * ((hidden + L.tile - 1) / L.tile);
+    int best = 1;
+    double least = 0.;
+    for (int n = 1; n <= 16 && n * 512 <= std::max(L.piece, 512); ++n) {
+        const double t = (double)((tiles * n + slots - 1) / slots) * L.piece / n + 2048. * (n > 1 ? n : 0) * tiles / slots;
+        if (n == 1 || t < least) {
+            least = t;
+            best = n;
+        }
+    }
+    return best;
 }
 VlPlan plan(const ps_vocab_loss_args* a) {
     const int esz = a->dtype == PS_BF16 ? 2 : 4;
@@ -664,10 +745,12 @@ VlPlan plan(const ps_vocab_loss_args* a) {
         for (const int rows : {L.rows_c, a->rows % L.rows_c})
             if (rows > 0) acc = std::max(acc, (size_t)splits_of(L, a->hidden, rows) * rows * a->hidden * 4);
     L.tl = 0;
-    L.far = L.tl + a256((size_t)a->rows * 4);
-    L.sums = L.far + a256((size_t)a->rows * 4);
+    L.state = L.tl + a256((size_t)a->rows * 4);
+    L.factor = L.state + a256((size_t)a->rows * 4);
+    L.sums = L.factor + a256((size_t)L.rows_c * sizeof(float2));
     L.acc = L.sums + a256((size_t)L.rows_c * L.nsum * 4);
-    L.x = L.acc + a256(acc);
+    L.alone = L.acc + a256(acc);
+    L.x = L.alone + (grad ? a256((size_t)L.rows_c * a->hidden * 4) : 0);
     L.total = L.x + (grad ? a256((size_t)L.rows_c * L.piece * esz) : 0);
     return L;
 }
@@ -680,20 +763,21 @@ template <typename WT> int run(VlParams P, const VlPlan& L, hipStream_t s) {
         const unsigned row_tiles = (P.rows_c + L.tile - 1) / L.tile;
         P.splits = splits_of(L, P.H, P.rows_c);
         P.split_n = ((L.piece + P.splits - 1) / P.splits + L.tile - 1) / L.tile * L.tile;
+        const bool at_once = L.wide && P.splits == 1;        // the last piece's products become gradients
         for (P.v0 = 0; P.v0 < P.V; P.v0 += L.piece) {
             P.nv = std::min(L.piece, P.V - P.v0);
             P.first = P.v0 == 0;
             const unsigned tokens = (P.nv + L.tile - 1) / L.tile;
-            if (L.wide) {
-                hipLaunchKernelGGL(vl_score_wide_kernel, dim3(tokens * row_tiles), dim3(VW_THREADS), 0, s, P, (int)tokens, (int)row_tiles);
-                if (P.d_hidden)
-                    hipLaunchKernelGGL(vl_grad_wide_kernel, dim3(cols * row_tiles, P.splits), dim3(VW_THREADS), 0, s, P, (int)cols, (int)row_tiles);
-            } else {
-                hipLaunchKernelGGL((vl_score_kernel<WT>), dim3(tokens, row_tiles), dim3(VL_THREADS), 0, s, P);
-                if (P.d_hidden) hipLaunchKernelGGL((vl_grad_kernel<WT>), dim3(cols, row_tiles, P.splits), dim3(VL_THREADS), 0, s, P);
-            }
+            const bool last = P.v0 + L.piece >= P.V;
+            if (L.wide) hipLaunchKernelGGL(vl_score_wide_kernel, dim3(tokens * row_tiles), dim3(VW_THREADS), 0, s, P, (int)tokens, (int)row_tiles);
+            else hipLaunchKernelGGL((vl_score_kernel<WT>), dim3(tokens, row_tiles), dim3(VL_THREADS), 0, s, P);
+            if (last) hipLaunchKernelGGL((vl_rows_kernel<WT>), dim3((P.rows_c + 3) / 4), dim3(VL_THREADS), 0, s, P);
+            if (!P.d_hidden) continue;
+            if (last && at_once) hipLaunchKernelGGL(vl_grad_wide_kernel<true>, dim3(cols * row_tiles), dim3(VW_THREADS), 0, s, P, (int)cols, (int)row_tiles);
+            else if (L.wide) hipLaunchKernelGGL(vl_grad_wide_kernel<false>, dim3(cols * row_tiles, P.splits), dim3(VW_THREADS), 0, s, P, (int)cols, (int)row_tiles);
+            else hipLaunchKernelGGL((vl_grad_kernel<WT>), dim3(cols, row_tiles, P.splits), dim3(VL_THREADS), 0, s, P);
         }
-        hipLaunchKernelGGL((vl_finish_kernel<WT>), dim3(P.rows_c), dim3(VL_THREADS), 0, s, P);
+        if (P.d_hidden && !at_once) hipLaunchKernelGGL((vl_join_kernel<WT>), dim3(P.rows_c), dim3(VL_THREADS), 0, s, P);
     }
     return hipGetLastError() == hipSuccess ? PS_OK : PS_ERR_DEVICE;
 }
@@ -716,7 +800,7 @@ extern "C" int ps_vocab_loss(const ps_vocab_loss_args* a, void* stream) {
     P.ldx = L.piece; P.nsum = L.nsum;
     P.h = (const char*)a->h; P.w = (const char*)a->w_lm; P.targets = a->targets; P.weights = a->weights;
     P.loss = a->loss; P.d_hidden = (char*)a->d_hidden;
-    P.tl = (float*)(ws + L.tl); P.far = (int*)(ws + L.far); P.sums = (float*)(ws + L.sums);
-    P.acc = (float*)(ws + L.acc); P.x = a->d_hidden ? ws + L.x : nullptr;
+    P.tl = (float*)(ws + L.tl); P.state = (int*)(ws + L.state); P.factor = (float2*)(ws + L.factor); P.sums = (float*)(ws + L.sums);
+    P.acc = (float*)(ws + L.acc); P.alone = (float*)(ws + L.alone); P.x = a->d_hidden ? ws + L.x : nullptr;
     return a->dtype == PS_BF16 ? run<bf16_t>(P, L, (hipStream_t)stream) : run<float>(P, L, (hipStream_t)stream);
 }
