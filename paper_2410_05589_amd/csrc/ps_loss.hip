@@ -11,7 +11,7 @@
 // out again one by one, against their maximum.
 //
 // The vocabulary is gone through in pieces; two products for each, the floor being their 4 V H operations a row:
-//   vl_score_kernel   W h^T, one tile of 128 x 128 per workgroup: exponentials to the workspace (storage type), sums of rows beside them
+//   vl_score_kernel   W h^T, one tile per workgroup: exponentials to the workspace (storage type), sums of rows beside them
 //   vl_grad_kernel    exponentials . W, added to what the pieces before left, in float32
 // before the last of which vl_rows_kernel adds up the rows' sums and makes their losses and the gradients' factors.
 #include <math.h>
@@ -20,7 +20,7 @@
 
 namespace {
 
-constexpr int VL_THREADS = 256, VL_TILE = 128;
+constexpr int VL_THREADS = 256, VL_AHEAD = 4;             // stages that are requested ahead of the one in LDS
 enum { VL_NEAR = 0, VL_FAR_APART = 1, VL_DONE = 2, VL_ZERO = 3 };
 constexpr float VL_SHIFT = 64.f, VL_FAR = 0x1p80f, VL_LOG2E = 1.4426950408889634f, VL_LN2 = 0.6931471805599453f;
 
@@ -84,73 +84,91 @@ template <typename WT> __device__ __forceinline__ void vl_mma(uint4 a, uint4 b, 
 // place of 16-byte chunk j of a 64-byte row (16 rows' chunks of one number fill the banks)
 __device__ __forceinline__ int vl_at(int row, int j) { return row * 64 + ((j ^ ((row >> 2) & 3)) << 4); }
 
-template <typename WT>
-__global__ void __launch_bounds__(VL_THREADS, 2) vl_score_kernel(const VlParams P) {
-    constexpr int ESZ = Traits<WT>::ESZ, BUF = VL_TILE * 64;
-    __shared__ __attribute__((aligned(16))) char smem[4 * BUF];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
-    const int vt = blockIdx.x * VL_TILE, rt = blockIdx.y * VL_TILE;   // in the piece, in the chunk
-    const int wv = (wave & 1) * 64, wr = (wave >> 1) * 64;
-    const size_t rb = (size_t)P.H * ESZ;
-    const char *wsrc[2], *hsrc[2];
+// steps first .. end - 1: load(step, x) requests a stage into registers, store(buffer, x) puts it into LDS, multiply(buffer)
+template <typename STAGE, typename LOAD, typename STORE, typename MULTIPLY>
+__device__ __forceinline__ void vl_pipeline(int first, int end, char* smem, int buf, LOAD load, STORE store, MULTIPLY multiply) {
+    if (first >= end) return;
+    STAGE x[VL_AHEAD];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int u = 0; u < VL_AHEAD; ++u)
+        if (first + u < end) load(first + u, x[u]);
+    store(smem, x[0]);
+    if (first + VL_AHEAD < end) load(first + VL_AHEAD, x[0]);
+    __syncthreads();
+    for (int k0 = first; k0 < end; k0 += VL_AHEAD) {
+#pragma unroll
+        for (int u = 0; u < VL_AHEAD; ++u) {
+            const int k = k0 + u;
+            if (k >= end) break;
+            STAGE& y = x[(u + 1) % VL_AHEAD];
+            if (k + 1 < end) store(smem + ((u + 1) & 1) * buf, y);
+            if (k + 1 + VL_AHEAD < end) load(k + 1 + VL_AHEAD, y);
+            multiply(smem + (u & 1) * buf);
+            __syncthreads();
+        }
+    }
+}
+static_assert(VL_AHEAD % 2 == 0, "a stage's buffer follows from its number");
+
+// Tiles of TILE x TILE (64, where 128 would leave compute units without one), four wavefronts of half the side each
+template <typename WT, int TILE>
+__global__ void __launch_bounds__(VL_THREADS, 2) vl_score_kernel(const VlParams P) {
+    constexpr int ESZ = Traits<WT>::ESZ, HALF = TILE / 2, N = TILE / 64, SIDE = TILE * 64, BUF = 2 * SIDE;
+    __shared__ __attribute__((aligned(16))) char smem[2 * BUF];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
+    const int vt = blockIdx.x * TILE, rt = blockIdx.y * TILE;   // in the piece, in the chunk
+    const int wv = (wave & 1) * HALF, wr = (wave >> 1) * HALF;
+    const size_t rb = (size_t)P.H * ESZ;
+    const char *wsrc[N], *hsrc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
         wsrc[i] = P.w + (size_t)min(P.v0 + vt + tid / 4 + 64 * i, P.V - 1) * rb + (tid & 3) * 16;
         hsrc[i] = P.h + (size_t)(P.row0 + min(rt + tid / 4 + 64 * i, P.rows_c - 1)) * rb + (tid & 3) * 16;
     }
-    uint4 sw[2], sh[2];
-    auto load = [&](int k) __attribute__((always_inline)) {
+    f32x16 acc[N][N];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) { sw[i] = ld16(wsrc[i] + (size_t)k * 64); sh[i] = ld16(hsrc[i] + (size_t)k * 64); }
-    };
-    auto store = [&](int k) __attribute__((always_inline)) {
-        char* b = smem + (k & 1) * 2 * BUF;
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            *reinterpret_cast<uint4*>(b + vl_at(tid / 4 + 64 * i, tid & 3)) = sw[i];
-            *reinterpret_cast<uint4*>(b + BUF + vl_at(tid / 4 + 64 * i, tid & 3)) = sh[i];
-        }
-    };
-    f32x16 acc[2][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    const int steps = P.H * ESZ / 64;
-    load(0);
-    store(0);
-    if (steps > 1) load(1);
-    __syncthreads();
-    for (int k = 0; k < steps; ++k) {
-        if (k + 1 < steps) store(k + 1);
-        if (k + 2 < steps) load(k + 2);
-        const char* b = smem + (k & 1) * 2 * BUF;
+    struct Stage { uint4 w[N], h[N]; };
+    vl_pipeline<Stage>(0, P.H * ESZ / 64, smem, BUF,
+        [&](int k, Stage& x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            uint4 a[2], q[2];
+            for (int i = 0; i < N; ++i) { x.w[i] = ld16(wsrc[i] + (size_t)k * 64); x.h[i] = ld16(hsrc[i] + (size_t)k * 64); }
+        },
+        [&](char* b, const Stage& x) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                a[i] = ld16(b + vl_at(wv + 32 * i + c, 2 * t + half));
-                q[i] = ld16(b + BUF + vl_at(wr + 32 * i + c, 2 * t + half));
+            for (int i = 0; i < N; ++i) {
+                *reinterpret_cast<uint4*>(b + vl_at(tid / 4 + 64 * i, tid & 3)) = x.w[i];
+                *reinterpret_cast<uint4*>(b + SIDE + vl_at(tid / 4 + 64 * i, tid & 3)) = x.h[i];
             }
+        },
+        [&](const char* b) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int t = 0; t < 2; ++t) {
+                uint4 a[N], q[N];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) vl_mma<WT>(a[i], q[j], acc[i][j]);
-        }
-        __syncthreads();
-    }
+                for (int i = 0; i < N; ++i) {
+                    a[i] = ld16(b + vl_at(wv + 32 * i + c, 2 * t + half));
+                    q[i] = ld16(b + SIDE + vl_at(wr + 32 * i + c, 2 * t + half));
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) vl_mma<WT>(a[i], q[j], acc[i][j]);
+            }
+        });
     // ---- lane (c, half) holds of row 32 j + c the tokens 32 i + 8 (e / 4) + 4 half + e % 4
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < N; ++j) {
         const int r = rt + wr + 32 * j + c, row = P.row0 + min(r, P.rows_c - 1);
         const int t = P.targets[row] - P.v0 - vt - wv - 4 * half, end = P.V - P.v0 - vt - wv - 4 * half;
         const float ref = -P.tl[row] * VL_LOG2E - VL_SHIFT;
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 f32x4 v;
@@ -168,48 +186,32 @@ __global__ void __launch_bounds__(VL_THREADS, 2) vl_score_kernel(const VlParams 
         sum = __uint_as_float(sw2[0]) + __uint_as_float(sw2[1]);
         if (r < P.rows_c) {
             if (sum > VL_FAR) P.state[row] = VL_FAR_APART;   // (infinite among them)
-            if (half == 0) P.sums[(size_t)r * P.nsum + (P.v0 + vt + wv) / 64] = sum;
+            if (half == 0) P.sums[(size_t)r * P.nsum + (P.v0 + vt + wv) / HALF] = sum;
         }
     }
 }
 
-template <typename WT>
+template <typename WT, int TILE>
 __global__ void __launch_bounds__(VL_THREADS, 2) vl_grad_kernel(const VlParams P) {
-    constexpr int ESZ = Traits<WT>::ESZ, KV = 64 / ESZ;      // tokens of a step
-    constexpr int ABUF = VL_TILE * 64, WSTR = VL_TILE * ESZ + (Traits<WT>::BF ? 64 : 32), WBUF = KV * WSTR, BUF = ABUF + WBUF;
+    constexpr int ESZ = Traits<WT>::ESZ, KV = 64 / ESZ, HALF = TILE / 2, N = TILE / 64;   // KV: tokens of a step
+    constexpr int ABUF = TILE * 64, WSTR = TILE * ESZ + (Traits<WT>::BF ? 64 : 32), WBUF = KV * WSTR, BUF = ABUF + WBUF;
     __shared__ __attribute__((aligned(16))) char smem[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
-    const int ct = blockIdx.x * VL_TILE, rt = blockIdx.y * VL_TILE, split = blockIdx.z;
-    const int wc = (wave & 1) * 64, wr = (wave >> 1) * 64;
+    const int ct = blockIdx.x * TILE, rt = blockIdx.y * TILE, split = blockIdx.z;
+    const int wc = (wave & 1) * HALF, wr = (wave >> 1) * HALF;
     const int k0 = split * (P.split_n / KV), k1 = min((split + 1) * P.split_n, (P.nv + KV - 1) / KV * KV) / KV;
-    constexpr int TPV = VL_TILE * ESZ / 16;                  // 16-byte pieces of a staged row of W
-    const char* xsrc[2];
+    constexpr int TPV = TILE * ESZ / 16;                     // 16-byte pieces of a staged row of W
+    const char* xsrc[N];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) xsrc[i] = P.x + (size_t)min(rt + tid / 4 + 64 * i, P.rows_c - 1) * P.ldx * ESZ + (tid & 3) * 16;
+    for (int i = 0; i < N; ++i) xsrc[i] = P.x + (size_t)min(rt + tid / 4 + 64 * i, P.rows_c - 1) * P.ldx * ESZ + (tid & 3) * 16;
     const int wk = tid / TPV, wp = tid % TPV;                // this thread's tokens wk + (256 / TPV) i, its piece (beyond H: the last)
     const size_t wcol = (size_t)min(ct * ESZ + wp * 16, P.H * ESZ - 16);
-    uint4 sx[2], sw[2];
-    auto load = [&](int k) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            sx[i] = ld16(xsrc[i] + (size_t)k * 64);
-            sw[i] = ld16(P.w + (size_t)min(P.v0 + k * KV + wk + VL_THREADS / TPV * i, P.V - 1) * P.H * ESZ + wcol);
-        }
-    };
-    auto store = [&](int k) __attribute__((always_inline)) {
-        char* b = smem + (k & 1) * BUF;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            *reinterpret_cast<uint4*>(b + vl_at(tid / 4 + 64 * i, tid & 3)) = sx[i];
-            *reinterpret_cast<uint4*>(b + ABUF + (wk + VL_THREADS / TPV * i) * WSTR + wp * 16) = sw[i];
-        }
-    };
-    f32x16 acc[2][2];
+    f32x16 acc[N][N];
     float* out = P.acc + (size_t)split * P.rows_c * P.H;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = rt + wr + 32 * i + 8 * (e / 4) + 4 * half + e % 4, col = ct + wc + 32 * j + c;
@@ -230,35 +232,41 @@ __global__ void __launch_bounds__(VL_THREADS, 2) vl_grad_kernel(const VlParams P
             return __builtin_bit_cast(uint4, r);
         }
     };
-    if (k0 < k1) {
-        load(k0);
-        store(k0);
-        if (k0 + 1 < k1) load(k0 + 1);
-        __syncthreads();
-        for (int k = k0; k < k1; ++k) {
-            if (k + 1 < k1) store(k + 1);
-            if (k + 2 < k1) load(k + 2);
-            const char* b = smem + (k & 1) * BUF;
+    struct Stage { uint4 x[N], w[N]; };
+    vl_pipeline<Stage>(k0, k1, smem, BUF,
+        [&](int k, Stage& s) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                s.x[i] = ld16(xsrc[i] + (size_t)k * 64);
+                s.w[i] = ld16(P.w + (size_t)min(P.v0 + k * KV + wk + VL_THREADS / TPV * i, P.V - 1) * P.H * ESZ + wcol);
+            }
+        },
+        [&](char* b, const Stage& s) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                *reinterpret_cast<uint4*>(b + vl_at(tid / 4 + 64 * i, tid & 3)) = s.x[i];
+                *reinterpret_cast<uint4*>(b + ABUF + (wk + VL_THREADS / TPV * i) * WSTR + wp * 16) = s.w[i];
+            }
+        },
+        [&](const char* b) __attribute__((always_inline)) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                uint4 a[2], q[2];
+                uint4 a[N], q[N];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < N; ++i) {
                     a[i] = ld16(b + vl_at(wr + 32 * i + c, 2 * t + half));
                     q[i] = column(b, t, i);
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < N; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) vl_mma<WT>(a[i], q[j], acc[i][j]);
+                    for (int j = 0; j < N; ++j) vl_mma<WT>(a[i], q[j], acc[i][j]);
             }
-            __syncthreads();
-        }
-    }
+        });
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = rt + wr + 32 * i + 8 * (e / 4) + 4 * half + e % 4, col = ct + wc + 32 * j + c;
@@ -708,19 +716,20 @@ int check(const ps_vocab_loss_args* a) {
 // How a call is cut: chunks of rows, pieces of the vocabulary, parts of a piece's tokens in the second product
 constexpr long long VL_PIECE_BYTES = 288ll << 20;            // of exponentials at a time
 struct VlPlan {
-    bool wide;
-    int tile, rows_c, piece, nsum;
+    int tile, slots;      // 256 (the wide kernels), 128 or 64; workgroups of such tiles that run at a time
+    int rows_c, piece, nsum;
     size_t tl, state, factor, sums, acc, alone, x, total;
 };
 // Where a chunk's tiles of the second product leave workgroups idle, several share a tile's tokens: the fewest that leave the
-// least time, counted in rounds of all workgroups over the share of the tokens (a part costs about as much as 2048 tokens: its sums are
-// written, read and added)
+// least time, counted in rounds of all workgroups over the share of the tokens.  A part costs about as much as more tokens would: its sums
+// are written, read and added.  (Counting 1000, 2000 or 5000 in the place of 3000: within 2 %.  500 rows, V 32000: 1 part 318 us, 8 274.)
 int splits_of(const VlPlan& L, int hidden, int rows) {
-    const int slots = L.wide ? 256 : 512, tiles = (rows + L.tile - 1) / L.tile * ((hidden + L.tile - 1) / L.tile);
+    const int tiles = (rows + L.tile - 1) / L.tile * ((hidden + L.tile - 1) / L.tile), part = L.tile == VW_TILE ? 3000 : 64;
+    const int fewest = L.tile == VW_TILE ? 512 : 128;
     int best = 1;
     double least = 0.;
-    for (int n = 1; n <= 16 && n * 512 <= std::max(L.piece, 512); ++n) {
-        const double t = (double)((tiles * n + slots - 1) / slots) * L.piece / n + 2048. * (n > 1 ? n : 0) * tiles / slots;
+    for (int n = 1; n <= 32 && n * fewest <= std::max(L.piece, fewest); ++n) {
+        const double t = (double)((tiles * n + L.slots - 1) / L.slots) * L.piece / n + (double)part * (n > 1 ? n : 0) * (L.tile == VW_TILE ? (double)tiles / L.slots : std::max(1., (double)tiles / L.slots));
         if (n == 1 || t < least) {
             least = t;
             best = n;
@@ -732,10 +741,18 @@ VlPlan plan(const ps_vocab_loss_args* a) {
     const int esz = a->dtype == PS_BF16 ? 2 : 4;
     const bool grad = a->d_hidden != nullptr;
     VlPlan L;
-    L.wide = a->dtype == PS_BF16 && a->rows > 256;
-    L.tile = L.wide ? VW_TILE : VL_TILE;
-    // rows at a time: as many as give the second product one tile for every workgroup that can run (two or one per compute unit)
-    L.rows_c = std::min(a->rows, std::max(1, (L.wide ? 256 : 512) / ((a->hidden + L.tile - 1) / L.tile)) * L.tile);
+    // Tiles.  The wide kernels where they have a tile for about half of the compute units: us, wide / 128 at H 4096, V 32000: 130 rows (125
+    // tiles) 196 / 212, 300 rows 247 / 313; V 128256, 130 rows 527 / 903; H 512, V 2064: 5000 rows (180 tiles) 78 / 84, 1500 (54) 57 / 51.
+    // But a tile of few rows: 65 rows 173 / 157 (V 128256, 501 tiles: 501 / 545, 30 rows 481 / 506).
+    // 64 / 128: 30 rows 130 / 140 (V 128256 549 / 522), 130 rows 266 / 211; H 512, V 2064: 500 rows 32 / 43.  float32, which is
+    // bound by its matrix rate and by few workgroups: 64 always (H 256, V 1024: 30 rows 29 / 56, 5000 88 / 116; H 512, V 2064, 2000 rows 112 / 153).
+    const bool bf = a->dtype == PS_BF16;
+    const long long tiles128 = (long long)((a->vocab + 127) / 128) * ((a->rows + 127) / 128), tiles256 = (long long)((a->vocab + 255) / 256) * ((a->rows + 255) / 256);
+    if (bf && tiles256 >= 120 && (a->rows > 96 || tiles256 >= 400)) L.tile = VW_TILE, L.slots = 256;
+    else if (!bf || tiles128 < 200 || (a->rows <= 64 && tiles128 < 512)) L.tile = 64, L.slots = 1024;
+    else L.tile = 128, L.slots = 512;
+    // rows at a time: as many as give the second product one tile for every workgroup that can run
+    L.rows_c = std::min(a->rows, std::max(1, L.slots / ((a->hidden + L.tile - 1) / L.tile)) * L.tile);
     const int vocab = (a->vocab + L.tile - 1) / L.tile * L.tile;
     const int pieces = grad ? (int)(((long long)L.rows_c * vocab * esz + VL_PIECE_BYTES - 1) / VL_PIECE_BYTES) : 1;
     L.piece = ((vocab + pieces - 1) / pieces + L.tile - 1) / L.tile * L.tile;
@@ -755,27 +772,37 @@ VlPlan plan(const ps_vocab_loss_args* a) {
     return L;
 }
 
+template <typename WT, int TILE> void launch_score(const VlParams& P, hipStream_t s) {
+    hipLaunchKernelGGL((vl_score_kernel<WT, TILE>), dim3((P.nv + TILE - 1) / TILE, (P.rows_c + TILE - 1) / TILE), dim3(VL_THREADS), 0, s, P);
+}
+template <typename WT, int TILE> void launch_grad(const VlParams& P, hipStream_t s) {
+    hipLaunchKernelGGL((vl_grad_kernel<WT, TILE>), dim3((P.H + TILE - 1) / TILE, (P.rows_c + TILE - 1) / TILE, P.splits), dim3(VL_THREADS), 0, s, P);
+}
+
 template <typename WT> int run(VlParams P, const VlPlan& L, hipStream_t s) {
     hipLaunchKernelGGL((vl_target_kernel<WT>), dim3((P.rows + 3) / 4), dim3(VL_THREADS), 0, s, P);
-    const unsigned cols = (P.H + L.tile - 1) / L.tile;
+    const bool wide = L.tile == VW_TILE;
+    const int cols = (P.H + VW_TILE - 1) / VW_TILE;
     for (P.row0 = 0; P.row0 < P.rows; P.row0 += L.rows_c) {
         P.rows_c = std::min(L.rows_c, P.rows - P.row0);
-        const unsigned row_tiles = (P.rows_c + L.tile - 1) / L.tile;
+        const int row_tiles = (P.rows_c + VW_TILE - 1) / VW_TILE;
         P.splits = splits_of(L, P.H, P.rows_c);
         P.split_n = ((L.piece + P.splits - 1) / P.splits + L.tile - 1) / L.tile * L.tile;
-        const bool at_once = L.wide && P.splits == 1;        // the last piece's products become gradients
+        const bool at_once = wide && P.splits == 1;          // the last piece's products become gradients
         for (P.v0 = 0; P.v0 < P.V; P.v0 += L.piece) {
             P.nv = std::min(L.piece, P.V - P.v0);
             P.first = P.v0 == 0;
-            const unsigned tokens = (P.nv + L.tile - 1) / L.tile;
+            const int tokens = (P.nv + VW_TILE - 1) / VW_TILE;
             const bool last = P.v0 + L.piece >= P.V;
-            if (L.wide) hipLaunchKernelGGL(vl_score_wide_kernel, dim3(tokens * row_tiles), dim3(VW_THREADS), 0, s, P, (int)tokens, (int)row_tiles);
-            else hipLaunchKernelGGL((vl_score_kernel<WT>), dim3(tokens, row_tiles), dim3(VL_THREADS), 0, s, P);
+            if (wide) hipLaunchKernelGGL(vl_score_wide_kernel, dim3(tokens * row_tiles), dim3(VW_THREADS), 0, s, P, tokens, row_tiles);
+            else if (L.tile == 64) launch_score<WT, 64>(P, s);
+            else if constexpr (Traits<WT>::BF) launch_score<WT, 128>(P, s);
             if (last) hipLaunchKernelGGL((vl_rows_kernel<WT>), dim3((P.rows_c + 3) / 4), dim3(VL_THREADS), 0, s, P);
             if (!P.d_hidden) continue;
-            if (last && at_once) hipLaunchKernelGGL(vl_grad_wide_kernel<true>, dim3(cols * row_tiles), dim3(VW_THREADS), 0, s, P, (int)cols, (int)row_tiles);
-            else if (L.wide) hipLaunchKernelGGL(vl_grad_wide_kernel<false>, dim3(cols * row_tiles, P.splits), dim3(VW_THREADS), 0, s, P, (int)cols, (int)row_tiles);
-            else hipLaunchKernelGGL((vl_grad_kernel<WT>), dim3(cols, row_tiles, P.splits), dim3(VL_THREADS), 0, s, P);
+            if (last && at_once) hipLaunchKernelGGL(vl_grad_wide_kernel<true>, dim3(cols * row_tiles), dim3(VW_THREADS), 0, s, P, cols, row_tiles);
+            else if (wide) hipLaunchKernelGGL(vl_grad_wide_kernel<false>, dim3(cols * row_tiles, P.splits), dim3(VW_THREADS), 0, s, P, cols, row_tiles);
+            else if (L.tile == 64) launch_grad<WT, 64>(P, s);
+            else if constexpr (Traits<WT>::BF) launch_grad<WT, 128>(P, s);
         }
         if (P.d_hidden && !at_once) hipLaunchKernelGGL((vl_join_kernel<WT>), dim3(P.rows_c), dim3(VL_THREADS), 0, s, P);
     }

@@ -12,7 +12,6 @@
 // -delta are the accumulators' initial values.  The other side's rows are staged in LDS once per workgroup and read both ways: as rows
 // (scores) and as columns (gradients; bf16: transposed by the LDS unit).
 #include "ps_train_device.h"
-#include <stdlib.h>
 
 namespace {
 
@@ -759,19 +758,26 @@ int check(const ps_group_attn_grad_args* a) {
 
 // How a call is cut: wavefronts that share 32 query rows; keys of a workgroup, parts of their rows
 struct GbPlan { int kw, keys, heads, tiles, splits; };
-static int env(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
 GbPlan plan(const ps_group_attn_grad_args* a) {
     GbPlan L;
+    const bool bf = a->dtype == PS_BF16, d128 = a->head_dim == 128;
+    // Two wavefronts for 32 query rows where four rows' workgroups would leave compute units without one.  Whole calls, us, one / two:
+    // T 64, k 4, 8 heads x 64 (24 workgroups) 31 / 29, T 1000, k 2 (192) 69 / 62, float32 2 x T 300, k 3 (160) 90 / 83; but 8 x T 128, k 3, 8 heads x 128
+    // (256) 76 / 79, T 203, k 5, 40 heads (400) 122 / 131
     const long long row_blocks = ((long long)a->tokens * (a->k + 1) + GB_ROWS - 1) / GB_ROWS * a->n_heads * a->seqs;
-    L.kw = env("GB_KW", row_blocks < 512 ? 2 : 1);
+    L.kw = row_blocks < 256 ? 2 : 1;
+    // 128 keys per workgroup at head_dim 128 in bf16; 64 where two wavefronts per SIMD do not fit (float32), or, at head_dim 64, where there are few
+    // (64 / 128: T 1000, k 2, 8 heads 57 / 61, float32 2 x T 300 83 / 92)
     L.heads = a->n_kv_heads * a->seqs;
-    const bool big = a->dtype == PS_F32 && a->head_dim == 128;   // (one wavefront per SIMD)
-    L.keys = !big && (long long)((a->tokens + 127) / 128) * L.heads >= 256 ? 128 : 64;
-    if (!big) L.keys = env("GB_KEYS", L.keys);
+    L.keys = d128 ? (bf ? 128 : 64) : (long long)((a->tokens + 127) / 128) * L.heads >= 256 ? 128 : 64;
     L.tiles = (a->tokens + L.keys - 1) / L.keys;
-    const long long units = (long long)L.tiles * L.heads;
-    const int stages = (a->tokens * (a->k + 1) + 63) / 64 * (a->n_heads / a->n_kv_heads);
-    L.splits = env("GB_SPLITS", (int)std::max(1LL, std::min(std::min(1024 / units, 16LL), (long long)stages / 4)));
+    // Parts of a key tile's rows, for a workgroup on every compute unit (two where the LDS takes two) as long as a part has a few stages of 64
+    // rows, for twice as many where parts stay long: a causal call's key tiles are unlike each other.  Whole calls, us, parts 1 / 2 / 3 / 4 / 8:
+    // T 2048, k 4, 32 heads (512 tiles) 1134 / 1191 / 1229 / 1248 / 1371; 4 x T 1024, k 8, 32 / 8 heads (256) 2880 / 2538 / 2533 / 2559 / 2658; T 203, k 5,
+    // 40 heads (80) 142 / 117 / 113 / 120 / 132; T 512, k 4, 32 / 8 heads (32) 559 / 330 / 269 / 217 / 172
+    const long long units = (long long)L.tiles * L.heads, places = d128 || L.keys == 128 ? 256 : 512;
+    const long long stages = ((long long)a->tokens * (a->k + 1) + 63) / 64 * (a->n_heads / a->n_kv_heads);
+    L.splits = (int)std::max(1LL, std::max(std::min(places / units, stages / (bf && d128 ? 4 : 2)), std::min(2 * places / units, stages / 64)));
     return L;
 }
 
@@ -805,8 +811,8 @@ template <typename WT, int D> int launch(const GbParams& P, const GbPlan& G, flo
     if (G.kw == 2) hipLaunchKernelGGL((gb_dq_kernel<WT, D, 2>), grid, dim3(GB_THREADS), 0, s, P);
     else hipLaunchKernelGGL((gb_dq_kernel<WT, D, 1>), grid, dim3(GB_THREADS), 0, s, P);
     const GbWork W = {G.heads, G.splits, G.tiles * G.heads, P.k > 0 ? (P.T + P.gpt - 1) / P.gpt * G.heads : 0, partial};
-    if constexpr (D * Traits<WT>::ESZ > 256) {
-        launch_keys<WT, D, 2>(P, G, W, s);
+    if constexpr (D == 128) {
+        launch_keys<WT, D, Traits<WT>::BF ? 4 : 2>(P, G, W, s);
     } else {
         if (G.keys == 64) launch_keys<WT, D, 2>(P, G, W, s);
         else launch_keys<WT, D, 4>(P, G, W, s);
