@@ -78,14 +78,19 @@ __global__ void __launch_bounds__(256) gb_prep_kernel(const GbParams P) {
 
 // ------------------------------------------------------------------------------------------
 // Tiles of 32 rows in LDS, read as rows (16 bytes of lane c's row) and as columns.  Within a row, 32-byte chunks stand at
-// chunk ^ f(row): rows read together, and the four or eight rows of a column read, fall into different banks.
+// chunk ^ f(row), and in rows 8 .. 15 and 24 .. 31 their halves are exchanged: the 16 rows that a quarter of a wavefront reads, and the
+// rows and chunks that half of one reads by columns, fall into different banks.  (Chunks at chunk ^ row % 8 alone: 46 % of the LDS's
+// busy cycles were conflicts, T 2048, k 4.)
 // ------------------------------------------------------------------------------------------
 template <typename WT, int D> struct GbTile {
     static constexpr int ESZ = Traits<WT>::ESZ, ROWB = D * ESZ, BYTES = 32 * ROWB, STEPS = ROWB / 32, NJ = D / 32;
     static constexpr bool BF = Traits<WT>::BF;
     static constexpr int PPR = ROWB / 16;                    // 16-byte pieces of a row
-    static __device__ __forceinline__ int f(int row) { return ROWB == 128 ? (row >> 1) & 3 : row & 7; }
-    static __device__ __forceinline__ int at(int row, int piece) { return row * ROWB + (((piece >> 1) ^ f(row)) << 5) + (piece & 1) * 16; }
+    static __device__ __forceinline__ int f(int row) {
+        return !BF ? row & 7 : ROWB == 128 ? (row & 2) | (row >> 2 & 1) : (row & 3) << 1 | (row >> 2 & 1);
+    }
+    // the piece of a row at place i, the place of piece i
+    static __device__ __forceinline__ int swap(int row, int i) { return i ^ f(row) << 1 ^ (row >> 3 & 1); }
 
     int rd, cd;           // this lane's places: of its row (chunk 0), of its column (tile 0, keys 0 ..)
     // the same, but the compiler does not know: what is derived from them is worked out where it is needed (an instruction each) and does
@@ -97,12 +102,12 @@ template <typename WT, int D> struct GbTile {
     }
     __device__ __forceinline__ GbTile(int lane) {
         const int c = lane & 31, half = lane >> 5;
-        rd = at(c, half);
+        rd = c * ROWB + swap(c, half) * 16;
         if constexpr (BF) {
             const int row = 4 * half + ((lane & 15) >> 2), vhi = (lane >> 4) & 1;
             cd = row * ROWB + ((vhi ^ f(row)) << 5) + (lane & 3) * 8;
         } else {
-            cd = 4 * half * ROWB + (((c >> 3) ^ (4 * half)) << 5) + (c & 7) * 4;
+            cd = 4 * half * ROWB + (((c >> 3) ^ f(4 * half)) << 5) + (c & 7) * 4;
         }
     }
     // 16 bytes of the lane's row: step st's operand
@@ -111,7 +116,7 @@ template <typename WT, int D> struct GbTile {
     template <bool CLEAN> __device__ __forceinline__ bf16x8 column(const char* tile, int j, int m) const {
         const char* a = tile + m * 16 * ROWB + (cd ^ (j << 6));
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a);
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(a + 8 * ROWB));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + (m * 16 + 8) * ROWB + (cd ^ (j << 6) ^ 16)));
         u32x4 v = __builtin_bit_cast(u32x4, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         if constexpr (CLEAN) {
 #pragma unroll
@@ -124,7 +129,7 @@ template <typename WT, int D> struct GbTile {
     }
     // column 32 j + c of row 8 (i / 4) + i % 4 + 4 half (float32)
     template <bool CLEAN> __device__ __forceinline__ float element(const char* tile, int j, int i) const {
-        const float v = *reinterpret_cast<const float*>(tile + (8 * (i / 4) + i % 4) * ROWB + (cd ^ (j << 7) ^ ((i & 3) << 5)));
+        const float v = *reinterpret_cast<const float*>(tile + (8 * (i / 4) + i % 4) * ROWB + (cd ^ (j << 7) ^ ((i & 3) << 5) ^ ((i >> 2 & 1) << 4)));
         return !CLEAN || fabsf(v) < INFINITY ? v : 0.f;
     }
 };
@@ -169,7 +174,7 @@ __device__ __forceinline__ void gb_stage(const char* m, unsigned stride, int mos
     if (N < WAVES && wave >= N) return;
 #pragma unroll
     for (int u = 0; u < (N + WAVES - 1) / WAVES; ++u) {
-        const int i = wave + u * WAVES, row = RPI * i + lane / PPR, slot = lane % PPR, piece = (((slot >> 1) ^ GbTile<WT, D>::f(row)) << 1) | (slot & 1);
+        const int i = wave + u * WAVES, row = RPI * i + lane / PPR, piece = GbTile<WT, D>::swap(row, lane % PPR);
         gb_copy(src, (unsigned)min(row, most) * stride + piece * 16, tile + i * 1024);
     }
 }
@@ -369,29 +374,31 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         if constexpr (Traits<WT>::BF) {
             const Tile l = L.here();
             bf16x8 ds[2];
-            constexpr int H = STEPS / 4, N = 2 * H + NJ / 2; // chunks: K rows, V rows, K columns
+            constexpr int H = STEPS / 2, N = H + NJ / 2;     // chunks: two steps' K and V rows; four K columns
             gb_chunks<N>(
                 [&](auto n, bf16x8(&x)[4]) __attribute__((always_inline)) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        if constexpr (n < 2 * H) x[u] = __builtin_bit_cast(bf16x8, l.row(n < H ? kt : vt, 4 * (n % H) + u));
-                        else x[u] = l.template column<masked>(kt, (4 * (n - 2 * H) + u) % NJ, (4 * (n - 2 * H) + u) / NJ);
+                        if constexpr (n < H) x[u] = __builtin_bit_cast(bf16x8, l.row(u & 1 ? vt : kt, 2 * n + u / 2));
+                        else x[u] = l.template column<masked>(kt, (4 * (n - H) + u) % NJ, (4 * (n - H) + u) / NJ);
                     }
                 },
                 [&](auto n, const bf16x8(&x)[4]) __attribute__((always_inline)) {
+                    if constexpr (n < H) {
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if constexpr (n < H) {
-                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, q[0][4 * n + u]), s, 0, 0, 0);
-                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, q[PARTS - 1][4 * n + u]), s, 0, 0, 0);
-                        } else if constexpr (n < 2 * H) {
-                            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, d_o[4 * (n - H) + u]), dp, 0, 0, 0);
-                        } else {
-                            const int o = 4 * (n - 2 * H) + u;
+                        for (int u = 0; u < 2; ++u) {        // (scores and dP in turn: no MFMA takes what the one before it gives)
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[2 * u], __builtin_bit_cast(bf16x8, q[0][2 * n + u]), s, 0, 0, 0);
+                            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[2 * u + 1], __builtin_bit_cast(bf16x8, d_o[2 * n + u]), dp, 0, 0, 0);
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[2 * u], __builtin_bit_cast(bf16x8, q[PARTS - 1][2 * n + u]), s, 0, 0, 0);
+                        }
+                    } else {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int o = 4 * (n - H) + u;
                             y[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], ds[o / NJ], y[o % NJ], 0, 0, 0);
                         }
                     }
-                    if constexpr (n == 2 * H - 1) {
+                    if constexpr (n == H - 1) {
                         probabilities();
                         const GbOperand<WT> p(s);
                         ds[0] = p.b[0];
@@ -505,36 +512,35 @@ template <typename WT, int D, bool V_LDS> struct GbKeys {
         if constexpr (Traits<WT>::BF) {
             const Tile l = L.here();
             bf16x8 p[2], ds[2];
-            // chunks: rows of the queries' high and low parts; of d_out (with the values', if they stand in LDS); columns of d_out, of the parts
-            constexpr int ST = Tile::STEPS, A = 2 * ST / 4, B = A + (V_LDS ? ST / 2 : ST / 4), C = NJ / 2, N = B + 3 * C;
+            // chunks: a step's rows of the queries' high and low parts, of d_out (and of the values, if they stand in LDS); four columns of
+            // d_out, of the parts
+            constexpr int B = Tile::STEPS, C = NJ / 2, N = B + 3 * C;
+            start(stats + two, dp);
             gb_chunks<N>(
                 [&](auto n, bf16x8(&x)[4]) __attribute__((always_inline)) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        if constexpr (n < A) {
-                            x[u] = __builtin_bit_cast(bf16x8, l.row(buf + (4 * n + u) / ST * Tile::BYTES, (4 * n + u) % ST));
-                        } else if constexpr (n < B) {
-                            if constexpr (V_LDS) x[u] = __builtin_bit_cast(bf16x8, l.row(u & 1 ? v_tile : dt, 2 * (n - A) + u / 2));
-                            else x[u] = __builtin_bit_cast(bf16x8, l.row(dt, 4 * (n - A) + u));
+                        if constexpr (n < B) {
+                            if (u < 3) x[u] = __builtin_bit_cast(bf16x8, l.row(buf + u * Tile::BYTES, n));
+                            else if constexpr (V_LDS) x[u] = __builtin_bit_cast(bf16x8, l.row(v_tile, n));
                         } else {
                             const int o = 4 * ((n - B) % C) + u;
                             x[u] = l.template column<MASKED>((n - B) / C == 0 ? dt : buf + ((n - B) / C - 1) * Tile::BYTES, o % NJ, o / NJ);
                         }
                     }
-                    if constexpr (n == A) start(stats + two, dp);
                 },
                 [&](auto n, const bf16x8(&x)[4]) __attribute__((always_inline)) {
+                    if constexpr (n < B) {                   // (scores and dP in turn: no MFMA takes what the one before it gives)
+                        const bf16x8 k = __builtin_bit_cast(bf16x8, kf[n]);
+                        bf16x8 v;
+                        if constexpr (V_LDS) v = x[3];
+                        else v = __builtin_bit_cast(bf16x8, vf[n]);
+                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0], k, s, 0, 0, 0);
+                        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[2], v, dp, 0, 0, 0);
+                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[1], k, s, 0, 0, 0);
+                    } else {
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if constexpr (n < A) {
-                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, kf[(4 * n + u) % ST]), s, 0, 0, 0);
-                        } else if constexpr (n < B) {
-                            if constexpr (V_LDS) {
-                                if (u & 1) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u - 1], x[u], dp, 0, 0, 0);
-                            } else {
-                                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], __builtin_bit_cast(bf16x8, vf[4 * (n - A) + u]), dp, 0, 0, 0);
-                            }
-                        } else {
+                        for (int u = 0; u < 4; ++u) {
                             const int o = 4 * ((n - B) % C) + u;
                             if constexpr (n < B + C) dv[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], p[o / NJ], dv[o % NJ], 0, 0, 0);
                             else dk[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], ds[o / NJ], dk[o % NJ], 0, 0, 0);
