@@ -77,46 +77,38 @@ __global__ void __launch_bounds__(256) gb_prep_kernel(const GbParams P) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Tiles of 32 rows in LDS, read as rows (16 bytes of lane c's row) and as columns.  Within a row, 32-byte chunks stand at
-// chunk ^ f(row), and in rows 8 .. 15 and 24 .. 31 their halves are exchanged: the 16 rows that a quarter of a wavefront reads, and the
-// rows and chunks that half of one reads by columns, fall into different banks.  (Chunks at chunk ^ row % 8 alone: 46 % of the LDS's
-// busy cycles were conflicts, T 2048, k 4.)
+// Tiles of 32 rows in LDS, read as rows (16 bytes of lane c's row) and as columns.  A tile is cut into blocks of 64 bytes of
+// every row, row behind row; 16-byte piece i of a row's 64 bytes stands at i ^ row / 4 % 4.  So the 16 rows that a quarter of a wavefront
+// reads fall into different banks, as do the four rows of 64 bytes that half of one reads by columns, and a lane gets
+// along with two addresses for rows and two for columns: everything else is a constant of the instruction.  (Rows whole, chunks
+// exchanged by exclusive or with the row: an instruction for each address, and conflicts in up to 46 % of the LDS's busy cycles.)
 // ------------------------------------------------------------------------------------------
 template <typename WT, int D> struct GbTile {
-    static constexpr int ESZ = Traits<WT>::ESZ, ROWB = D * ESZ, BYTES = 32 * ROWB, STEPS = ROWB / 32, NJ = D / 32;
+    static constexpr int ESZ = Traits<WT>::ESZ, ROWB = D * ESZ, BYTES = 32 * ROWB, STEPS = ROWB / 32;
     static constexpr bool BF = Traits<WT>::BF;
-    static constexpr int PPR = ROWB / 16;                    // 16-byte pieces of a row
-    static __device__ __forceinline__ int f(int row) {
-        return !BF ? row & 7 : ROWB == 128 ? (row & 2) | (row >> 2 & 1) : (row & 3) << 1 | (row >> 2 & 1);
-    }
-    // the piece of a row at place i, the place of piece i
-    static __device__ __forceinline__ int swap(int row, int i) { return i ^ f(row) << 1 ^ (row >> 3 & 1); }
+    static __device__ __forceinline__ int swap(int row, int i) { return i ^ (row >> 2 & 3); }
 
-    int rd, cd;           // this lane's places: of its row (chunk 0), of its column (tile 0, keys 0 ..)
-    // the same, but the compiler does not know: what is derived from them is worked out where it is needed (an instruction each) and does
-    // not occupy registers across the loop
-    __device__ __forceinline__ GbTile here() const {
-        GbTile t = *this;
-        asm volatile("" : "+v"(t.rd), "+v"(t.cd));
-        return t;
-    }
+    int rd[2], cd[2];     // this lane's places: of its row, pieces half and 2 + half; of its column, rows 4 half .. and 8 + 4 half ..
     __device__ __forceinline__ GbTile(int lane) {
         const int c = lane & 31, half = lane >> 5;
-        rd = c * ROWB + swap(c, half) * 16;
-        if constexpr (BF) {
-            const int row = 4 * half + ((lane & 15) >> 2), vhi = (lane >> 4) & 1;
-            cd = row * ROWB + ((vhi ^ f(row)) << 5) + (lane & 3) * 8;
-        } else {
-            cd = 4 * half * ROWB + (((c >> 3) ^ f(4 * half)) << 5) + (c & 7) * 4;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            rd[i] = c * 64 + swap(c, 2 * i + half) * 16;
+            if constexpr (BF) {
+                const int row = 8 * i + 4 * half + ((lane & 15) >> 2), piece = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+                cd[i] = row * 64 + swap(row, piece) * 16 + (lane & 1) * 8;
+            } else {
+                const int row = 8 * i + 4 * half;
+                cd[i] = (c >> 4) * 2048 + row * 64 + swap(row, c >> 2 & 3) * 16 + (c & 3) * 4;
+            }
         }
     }
     // 16 bytes of the lane's row: step st's operand
-    __device__ __forceinline__ uint4 row(const char* tile, int st) const { return ld16(tile + (rd ^ (st << 5))); }
+    __device__ __forceinline__ uint4 row(const char* tile, int st) const { return ld16(tile + rd[st & 1] + (st >> 1) * 2048); }
     // columns 32 j + c, rows 16 m + 4 half + {0..3, 8..11} (bf16); with clean, values that are not finite count as zero
     template <bool CLEAN> __device__ __forceinline__ bf16x8 column(const char* tile, int j, int m) const {
-        const char* a = tile + m * 16 * ROWB + (cd ^ (j << 6));
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)a);
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + (m * 16 + 8) * ROWB + (cd ^ (j << 6) ^ 16)));
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + cd[0] + j * 2048 + m * 1024));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + cd[1] + j * 2048 + m * 1024));
         u32x4 v = __builtin_bit_cast(u32x4, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
         if constexpr (CLEAN) {
 #pragma unroll
@@ -129,15 +121,14 @@ template <typename WT, int D> struct GbTile {
     }
     // column 32 j + c of row 8 (i / 4) + i % 4 + 4 half (float32)
     template <bool CLEAN> __device__ __forceinline__ float element(const char* tile, int j, int i) const {
-        const float v = *reinterpret_cast<const float*>(tile + (8 * (i / 4) + i % 4) * ROWB + (cd ^ (j << 7) ^ ((i & 3) << 5) ^ ((i >> 2 & 1) << 4)));
+        const float v = *reinterpret_cast<const float*>(tile + cd[i >> 2 & 1] + j * 4096 + (i >> 3) * 1024 + (i & 3) * 64);
         return !CLEAN || fabsf(v) < INFINITY ? v : 0.f;
     }
 };
 
 // float32: scores += rows . own: the lane's i-th is that of row 8 (i / 4) + i % 4 + 4 half and the lane's own query or key
 template <typename WT, int D>
-__device__ __forceinline__ void gb_scores(const GbTile<WT, D>& at, const char* tile, const uint4 (&own)[GbTile<WT, D>::STEPS], f32x16& x) {
-    const GbTile<WT, D> L = at.here();
+__device__ __forceinline__ void gb_scores(const GbTile<WT, D>& L, const char* tile, const uint4 (&own)[GbTile<WT, D>::STEPS], f32x16& x) {
 #pragma unroll
     for (int st = 0; st < GbTile<WT, D>::STEPS; ++st) {
         const f32x4 u = __builtin_bit_cast(f32x4, L.row(tile, st)), w = __builtin_bit_cast(f32x4, own[st]);
@@ -147,8 +138,7 @@ __device__ __forceinline__ void gb_scores(const GbTile<WT, D>& at, const char* t
 }
 // float32: y^T += rows^T . p, p as gb_scores leaves it
 template <typename WT, int D, bool CLEAN>
-__device__ __forceinline__ void gb_products(const GbTile<WT, D>& at, const char* tile, const f32x16& p, f32x16 (&y)[D / 32]) {
-    const GbTile<WT, D> L = at.here();
+__device__ __forceinline__ void gb_products(const GbTile<WT, D>& L, const char* tile, const f32x16& p, f32x16 (&y)[D / 32]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
 #pragma unroll
@@ -166,19 +156,18 @@ template <typename WT> struct GbOperand {
 };
 typedef __attribute__((address_space(3))) void lds_void;
 __device__ __forceinline__ void gb_copy(rsrc_t from, unsigned off, char* to) { __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, 0, 0, 0); }
-// A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: this wavefront's share of WAVES, 1 KiB per request
+// A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: this wavefront's share of WAVES, 1 KiB (64 bytes of 16 rows) per request
 template <typename WT, int D, int WAVES>
 __device__ __forceinline__ void gb_stage(const char* m, unsigned stride, int most, char* tile, int wave, int lane) {
-    constexpr int ROWB = GbTile<WT, D>::ROWB, PPR = ROWB / 16, RPI = 1024 / ROWB, N = 32 / RPI;   // rows per request, requests
+    constexpr int N = GbTile<WT, D>::BYTES / 1024;
     const rsrc_t src = make_rsrc(m);
     if (N < WAVES && wave >= N) return;
 #pragma unroll
     for (int u = 0; u < (N + WAVES - 1) / WAVES; ++u) {
-        const int i = wave + u * WAVES, row = RPI * i + lane / PPR, piece = GbTile<WT, D>::swap(row, lane % PPR);
-        gb_copy(src, (unsigned)min(row, most) * stride + piece * 16, tile + i * 1024);
+        const int i = wave + u * WAVES, row = 16 * (i & 1) + lane / 4, piece = GbTile<WT, D>::swap(row, lane & 3);
+        gb_copy(src, (unsigned)min(row, most) * stride + (i >> 1) * 64 + piece * 16, tile + i * 1024);
     }
 }
-
 // bf16: a tile's work as N chunks of up to four operands from LDS and the MFMAs that take them.  A chunk's operands are asked for before the
 // MFMAs of the chunk in front of it and the compiler keeps that order: left alone it asks for one or two ahead, and an MFMA
 // waits for most of the LDS's latency.
@@ -372,15 +361,14 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
             dp[i] = delta;
         }
         if constexpr (Traits<WT>::BF) {
-            const Tile l = L.here();
             bf16x8 ds[2];
             constexpr int H = STEPS / 2, N = H + NJ / 2;     // chunks: two steps' K and V rows; four K columns
             gb_chunks<N>(
                 [&](auto n, bf16x8(&x)[4]) __attribute__((always_inline)) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        if constexpr (n < H) x[u] = __builtin_bit_cast(bf16x8, l.row(u & 1 ? vt : kt, 2 * n + u / 2));
-                        else x[u] = l.template column<masked>(kt, (4 * (n - H) + u) % NJ, (4 * (n - H) + u) / NJ);
+                        if constexpr (n < H) x[u] = __builtin_bit_cast(bf16x8, L.row(u & 1 ? vt : kt, 2 * n + u / 2));
+                        else x[u] = L.template column<masked>(kt, (4 * (n - H) + u) % NJ, (4 * (n - H) + u) / NJ);
                     }
                 },
                 [&](auto n, const bf16x8(&x)[4]) __attribute__((always_inline)) {
@@ -510,7 +498,6 @@ template <typename WT, int D, bool V_LDS> struct GbKeys {
         };
         start(stats, s);
         if constexpr (Traits<WT>::BF) {
-            const Tile l = L.here();
             bf16x8 p[2], ds[2];
             // chunks: a step's rows of the queries' high and low parts, of d_out (and of the values, if they stand in LDS); four columns of
             // d_out, of the parts
@@ -521,11 +508,11 @@ template <typename WT, int D, bool V_LDS> struct GbKeys {
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
                         if constexpr (n < B) {
-                            if (u < 3) x[u] = __builtin_bit_cast(bf16x8, l.row(buf + u * Tile::BYTES, n));
-                            else if constexpr (V_LDS) x[u] = __builtin_bit_cast(bf16x8, l.row(v_tile, n));
+                            if (u < 3) x[u] = __builtin_bit_cast(bf16x8, L.row(buf + u * Tile::BYTES, n));
+                            else if constexpr (V_LDS) x[u] = __builtin_bit_cast(bf16x8, L.row(v_tile, n));
                         } else {
                             const int o = 4 * ((n - B) % C) + u;
-                            x[u] = l.template column<MASKED>((n - B) / C == 0 ? dt : buf + ((n - B) / C - 1) * Tile::BYTES, o % NJ, o / NJ);
+                            x[u] = L.template column<MASKED>((n - B) / C == 0 ? dt : buf + ((n - B) / C - 1) * Tile::BYTES, o % NJ, o / NJ);
                         }
                     }
                 },
