@@ -156,22 +156,23 @@ template <typename WT> struct GbOperand {
 };
 typedef __attribute__((address_space(3))) void lds_void;
 __device__ __forceinline__ void gb_copy(rsrc_t from, unsigned off, char* to) { __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, 0, 0, 0); }
-// A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: this wavefront's share of WAVES, 1 KiB (64 bytes of 16 rows) per request
+// A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: its i-th KiB (64 bytes of 16 rows)
+template <typename WT, int D> __device__ __forceinline__ void gb_request(const char* m, unsigned stride, int most, char* tile, int i, int lane) {
+    const int row = 16 * (i & 1) + lane / 4, piece = GbTile<WT, D>::swap(row, lane & 3);
+    gb_copy(make_rsrc(m), (unsigned)min(row, most) * stride + (i >> 1) * 64 + piece * 16, tile + i * 1024);
+}
+// ... this wavefront's share of WAVES
 template <typename WT, int D, int WAVES>
 __device__ __forceinline__ void gb_stage(const char* m, unsigned stride, int most, char* tile, int wave, int lane) {
     constexpr int N = GbTile<WT, D>::BYTES / 1024;
-    const rsrc_t src = make_rsrc(m);
-    if (N < WAVES && wave >= N) return;
+    static_assert(N % WAVES == 0, "");
 #pragma unroll
-    for (int u = 0; u < (N + WAVES - 1) / WAVES; ++u) {
-        const int i = wave + u * WAVES, row = 16 * (i & 1) + lane / 4, piece = GbTile<WT, D>::swap(row, lane & 3);
-        gb_copy(src, (unsigned)min(row, most) * stride + (i >> 1) * 64 + piece * 16, tile + i * 1024);
-    }
+    for (int u = 0; u < N / WAVES; ++u) gb_request<WT, D>(m, stride, most, tile, wave + u * WAVES, lane);
 }
 // bf16: a tile's work as N chunks of up to four operands from LDS and the MFMAs that take them.  A chunk's operands are asked for before the
 // MFMAs of the chunk in front of it and the compiler keeps that order: left alone it asks for one or two ahead, and an MFMA
-// waits for most of the LDS's latency.
-template <int N, typename LOAD, typename MULTIPLY> __device__ __forceinline__ void gb_chunks(LOAD load, MULTIPLY multiply) {
+// waits for most of the LDS's latency.  beside(): what is done while the first chunk is multiplied (the next stage's requests).
+template <int N, typename LOAD, typename MULTIPLY, typename BESIDE> __device__ __forceinline__ void gb_chunks(LOAD load, MULTIPLY multiply, BESIDE beside) {
     bf16x8 x[2][4];
     load(std::integral_constant<int, 0>{}, x[0]);
     auto run = [&](auto self, auto n) __attribute__((always_inline)) {
@@ -180,6 +181,7 @@ template <int N, typename LOAD, typename MULTIPLY> __device__ __forceinline__ vo
             if constexpr (n + 1 < N) load(std::integral_constant<int, n + 1>{}, x[(n + 1) & 1]);
             __builtin_amdgcn_sched_barrier(0);
             multiply(n, x[n & 1]);
+            if constexpr (n == 0) beside();
             self(self, std::integral_constant<int, n + 1>{});
         }
     };
@@ -342,7 +344,7 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         for (int i = 0; i < 16; ++i) y[j][i] = 0.f;
 
     // one key tile; masked: keys lo .. hi of it (counted from 4 half) are seen
-    auto work = [&](const char* kt, auto masked, int lo, int hi) __attribute__((always_inline)) {
+    auto work = [&](const char* kt, auto masked, int lo, int hi, auto beside) __attribute__((always_inline)) {
         const char* vt = kt + Tile::BYTES;
         float lse = lse0, delta = delta0;
         asm volatile("" : "+v"(lse), "+v"(delta));          // (32 copies of them would be kept in registers across the loop)
@@ -392,8 +394,9 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
                         ds[0] = p.b[0];
                         ds[1] = p.b[1];
                     }
-                });
+                }, beside);
         } else {
+            beside();
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) gb_scores<WT, D>(L, kt, q[p], s);
             gb_scores<WT, D>(L, vt, d_o, dp);
@@ -409,7 +412,7 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
                 if (before) stage_own(r0 - 32);              // (nobody else reads these tiles)
             }
             __syncthreads();
-            if (active && (i == 0 || before)) work(mine, std::true_type{}, lo - (r0 - 32 * i), hi - (r0 - 32 * i));
+            if (active && (i == 0 || before)) work(mine, std::true_type{}, lo - (r0 - 32 * i), hi - (r0 - 32 * i), [] {});
         }
         __syncthreads();
     }
@@ -419,9 +422,9 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
     int t = 0;
     auto tile = [&](int i) __attribute__((always_inline)) { return smem + (t & 1) * BUF + i * 2 * Tile::BYTES; };
     for (const int end = active ? (wg0 + 1) / 64 : 0; t < end; ++t) {
-        if (t + 1 < n_stages) stage(t + 1);
 #pragma unroll
-        for (int i = 0; i < 2 / KW; ++i) work(tile(i * KW + kw), std::false_type{}, 0, 0);
+        for (int i = 0; i < 2 / KW; ++i)
+            work(tile(i * KW + kw), std::false_type{}, 0, 0, [&]() __attribute__((always_inline)) { if (i == 0 && t + 1 < n_stages) stage(t + 1); });
         __syncthreads();
     }
     for (; t < n_stages; ++t) {
@@ -429,7 +432,7 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
 #pragma unroll 1
         for (int i = kw; i < 2; i += KW) {
             const int first = 64 * t + 32 * i;
-            if (active && first <= wg1) work(tile(i), std::true_type{}, -first - 4 * half, qg - first - 4 * half);
+            if (active && first <= wg1) work(tile(i), std::true_type{}, -first - 4 * half, qg - first - 4 * half, [] {});
         }
         __syncthreads();
     }
@@ -475,7 +478,8 @@ template <typename WT, int D, bool V_LDS> struct GbKeys {
     }
     // buf: the tiles of the rotated queries' parts, then of d_out; stats: the 32 rows' -lse / ln 2, then (behind `two` floats) -delta; the lane's
     // key is seen by rows lo .. hi of the tile (counted from 4 half), all of them if not masked
-    template <bool MASKED> __device__ __forceinline__ void step(const Tile& L, const char* buf, const float* stats, int two, int half, int lo, int hi) {
+    template <bool MASKED, typename BESIDE>
+    __device__ __forceinline__ void step(const Tile& L, const char* buf, const float* stats, int two, int half, int lo, int hi, BESIDE beside) {
         f32x16 s, dp;
         auto start = [&](const float* x, f32x16& y) __attribute__((always_inline)) {
 #pragma unroll
@@ -538,9 +542,10 @@ template <typename WT, int D, bool V_LDS> struct GbKeys {
                         const GbOperand<WT> a(s), b(dp);
                         p[0] = a.b[0]; p[1] = a.b[1]; ds[0] = b.b[0]; ds[1] = b.b[1];
                     }
-                });
+                }, beside);
         } else {
             start(stats + two, dp);
+            beside();
             gb_scores<WT, D>(L, buf, kf, s);
             gb_scores<WT, D>(L, dt, vf, dp);
             probabilities();
@@ -610,7 +615,7 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
             stats[lane] = (lane < 32 ? P.lse2 : P.delta)[at + krow];
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");   // (the tiles have arrived, for this wavefront's own reads)
             __builtin_amdgcn_wave_barrier();
-            keys.template step<true>(L, buf, stats, 32, half, slot > 0 ? krow - first - 4 * half : 99, g * K1 + P.k - first - 4 * half);
+            keys.template step<true>(L, buf, stats, 32, half, slot > 0 ? krow - first - 4 * half : 99, g * K1 + P.k - first - 4 * half, [] {});
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
             __builtin_amdgcn_wave_barrier();
         }
@@ -622,26 +627,34 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
     const int t0 = C::KEYS * kt, w0 = t0 + 32 * kw, key = min(w0 + c, P.T - 1);   // the workgroup's and the wavefront's first token, the lane's
     const int first_row = t0 * K1, per_head = (P.rows - first_row + 63) / 64, all = per_head * P.group;
     const int i0 = (int)((long long)all * split / W.splits), i1 = (int)((long long)all * (split + 1) / W.splits);
+    // the next set of 64 rows to request: of query head hk * group + next_g, from its next_j-th on (behind the last: the last again; a branch
+    // among the products would have the compiler spill)
+    int next_g = i0 / per_head, next_j = i0 - next_g * per_head;
+    const int next_j0 = next_j;
     float stat = 0.f;
-    auto stage = [&](int i) __attribute__((always_inline)) {
-        const int g = i / per_head, h = hk * P.group + g, first = first_row + 64 * (i - g * per_head);
+    auto stage = [&](int i) __attribute__((always_inline)) {   // set i, to buffer i % 2
+        const int h = hk * P.group + next_g, first = first_row + 64 * next_j, left = P.rows - 1 - first;
         const size_t at = ((size_t)seq * P.nq + h) * P.rows + first;
         char* b = smem + (i & 1) * C::BUF;
+        constexpr int N = Tile::BYTES / 1024;
+        static_assert(2 * N % C::WAVES == 0, "");
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int from = min(32 * r, P.rows - 1 - first), most = P.rows - 1 - first - from;
+        for (int u = 0; u < 2 * N / C::WAVES; ++u) {         // the two tiles' requests together
+            const int x = wave + u * C::WAVES, r = x / N, from = min(32 * r, left), most = left - from;
+            char* to = b + r * C::SET;
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p)
-                gb_stage<WT, D, C::WAVES>(P.q_rot + p * part + (at + from) * D * ESZ, D * ESZ, most, b + r * C::SET + p * Tile::BYTES, wave, lane);
-            gb_stage<WT, D, C::WAVES>(P.d_out + (((size_t)seq * P.rows + first + from) * P.nq + h) * D * ESZ, ostride, most, b + r * C::SET + PARTS * Tile::BYTES, wave, lane);
+            for (int p = 0; p < PARTS; ++p) gb_request<WT, D>(P.q_rot + p * part + (at + from) * D * ESZ, D * ESZ, most, to + p * Tile::BYTES, x % N, lane);
+            gb_request<WT, D>(P.d_out + (((size_t)seq * P.rows + first + from) * P.nq + h) * D * ESZ, ostride, most, to + PARTS * Tile::BYTES, x % N, lane);
         }
-        // (a row beyond the last: probability 0, whatever the last row, which it repeats, holds)
-        if (wave < 2) stat = (wave ? P.delta : P.lse2)[at + min(lane, P.rows - 1 - first)];
-        if (wave == 0 && lane > P.rows - 1 - first) stat = -INFINITY;
+        // (every second wavefront's is the same; a row beyond the last: probability 0, whatever the last row, which it repeats, holds)
+        stat = (wave & 1 ? P.delta : P.lse2)[at + min(lane, left)];
+        stat = wave & 1 || lane <= left ? stat : -INFINITY;
+        next_j += i + 1 < i1;
+        const bool wrap = next_j == per_head;
+        next_j = wrap ? 0 : next_j;
+        next_g += wrap;
     };
-    auto stage_stats = [&](int i) __attribute__((always_inline)) {
-        if (wave < 2) reinterpret_cast<float*>(smem + (i & 1) * C::BUF + C::OFF_S)[64 * wave + lane] = stat;
-    };
+    auto stage_stats = [&](int i) __attribute__((always_inline)) { reinterpret_cast<float*>(smem + (i & 1) * C::BUF + C::OFF_S)[64 * (wave & 1) + lane] = stat; };
     if (i0 < i1) stage(i0);
     gb_own_rows<WT, D>(P.k_rot + (((size_t)seq * P.nkv + hk) * P.rows + (size_t)key * K1) * D * ESZ, half, keys.kf);
     if constexpr (C::V_LDS) {
@@ -653,21 +666,24 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
     }
     if (i0 < i1) stage_stats(i0);
     __syncthreads();
-    auto step = [&](int i, auto masked) __attribute__((always_inline)) {
-        if (i + 1 < i1) stage(i + 1);
+    auto step = [&](int i, int first, auto masked) __attribute__((always_inline)) {
         const char* buf = smem + (i & 1) * C::BUF;
-        const int first = first_row + 64 * (i % per_head) + 32 * rw;
-        if (!masked || (w0 < P.T && first + 31 >= w0 * K1))
-            keys.template step<masked>(L, buf + rw * C::SET, reinterpret_cast<const float*>(buf + C::OFF_S) + 32 * rw, 64, half, key * K1 - first - 4 * half, 31);
-        if (i + 1 < i1) stage_stats(i + 1);
+        const float* stats = reinterpret_cast<const float*>(buf + C::OFF_S) + 32 * rw;
+        if constexpr (masked) {
+            stage(i + 1);
+            if (w0 < P.T && first + 31 >= w0 * K1) keys.template step<true>(L, buf + rw * C::SET, stats, 64, half, key * K1 - first - 4 * half, 31, [] {});
+        } else {
+            keys.template step<false>(L, buf + rw * C::SET, stats, 64, half, 0, 31, [&]() __attribute__((always_inline)) { stage(i + 1); });
+        }
+        stage_stats(i + 1);
         __syncthreads();
     };
     // of every head the row tiles that see some of the wavefront's keys, then those that see all of them
     const int see_all = w0 < P.T ? min(max((w0 + 31) * K1 - first_row - 32 * rw + 63, 0) / 64, per_head) : per_head;
-    for (int i = i0; i < i1;) {
-        const int head0 = i / per_head * per_head;
-        for (const int end = min(i1, head0 + see_all); i < end; ++i) step(i, std::true_type{});
-        for (const int end = min(i1, head0 + per_head); i < end; ++i) step(i, std::false_type{});
+    for (int i = i0, j = next_j0; i < i1; j = 0) {
+        const int head0 = i - j;
+        for (const int end = min(i1, head0 + see_all); i < end; ++i) step(i, first_row + 64 * (i - head0) + 32 * rw, std::true_type{});
+        for (const int end = min(i1, head0 + per_head); i < end; ++i) step(i, first_row + 64 * (i - head0) + 32 * rw, std::false_type{});
     }
     // ---- the row wavefronts' sums, one gradient after the other by way of the LDS
     auto meet = [&](f32x16 (&y)[NJ]) __attribute__((always_inline)) {
