@@ -105,21 +105,23 @@ template <typename WT, int D> struct GbTile {
     }
     // 16 bytes of the lane's row: step st's operand
     __device__ __forceinline__ uint4 row(const char* tile, int st) const { return ld16(tile + rd[st & 1] + (st >> 1) * 2048); }
-    // columns 32 j + c, rows 16 m + 4 half + {0..3, 8..11} (bf16); with clean, values that are not finite count as zero
-    template <bool CLEAN> __device__ __forceinline__ bf16x8 column(const char* tile, int j, int m) const {
+    // columns 32 j + c, rows 16 m + 4 half + {0..3, 8..11} (bf16)
+    __device__ __forceinline__ bf16x8 column(const char* tile, int j, int m) const {
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + cd[0] + j * 2048 + m * 1024));
         const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + cd[1] + j * 2048 + m * 1024));
-        u32x4 v = __builtin_bit_cast(u32x4, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-        if constexpr (CLEAN) {
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // ... values that are not finite count as zero
+    static __device__ __forceinline__ bf16x8 finite(bf16x8 x) {
+        u32x4 v = __builtin_bit_cast(u32x4, x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = (v[e] & 0x7F80u) == 0x7F80u ? v[e] & 0xFFFF0000u : v[e];
-                v[e] = (v[e] & 0x7F800000u) == 0x7F800000u ? v[e] & 0xFFFFu : v[e];
-            }
+        for (int e = 0; e < 4; ++e) {
+            v[e] = (v[e] & 0x7F80u) == 0x7F80u ? v[e] & 0xFFFF0000u : v[e];
+            v[e] = (v[e] & 0x7F800000u) == 0x7F800000u ? v[e] & 0xFFFFu : v[e];
         }
         return __builtin_bit_cast(bf16x8, v);
     }
-    // column 32 j + c of row 8 (i / 4) + i % 4 + 4 half (float32)
+    // column 32 j + c of row 8 (i / 4) + i % 4 + 4 half (float32; with clean, likewise)
     template <bool CLEAN> __device__ __forceinline__ float element(const char* tile, int j, int i) const {
         const float v = *reinterpret_cast<const float*>(tile + cd[i >> 2 & 1] + j * 4096 + (i >> 3) * 1024 + (i & 3) * 64);
         return !CLEAN || fabsf(v) < INFINITY ? v : 0.f;
@@ -169,19 +171,27 @@ __device__ __forceinline__ void gb_stage(const char* m, unsigned stride, int mos
 #pragma unroll
     for (int u = 0; u < N / WAVES; ++u) gb_request<WT, D>(m, stride, most, tile, wave + u * WAVES, lane);
 }
-// bf16: a tile's work as N chunks of up to four operands from LDS and the MFMAs that take them.  A chunk's operands are asked for before the
-// MFMAs of the chunk in front of it and the compiler keeps that order: left alone it asks for one or two ahead, and an MFMA
-// waits for most of the LDS's latency.  beside(): what is done while the first chunk is multiplied (the next stage's requests).
-template <int N, typename LOAD, typename MULTIPLY, typename BESIDE> __device__ __forceinline__ void gb_chunks(LOAD load, MULTIPLY multiply, BESIDE beside) {
-    bf16x8 x[2][4];
-    load(std::integral_constant<int, 0>{}, x[0]);
+// bf16: a tile's work as N operands from LDS, one after the other, each with the MFMAs that take it (and the one before it).  Operands are
+// asked for three ahead, and the compiler keeps that order: left alone it asks for one or two, and an MFMA waits for most of the LDS's
+// latency.  (Two to six ahead take the same time; more spill.)  beside(): what is done at the start (the next stage's requests).
+constexpr int GB_SLOTS = 5;
+template <int N, typename LOAD, typename USE, typename BESIDE> __device__ __forceinline__ void gb_stream(LOAD load, USE use, BESIDE beside) {
+    constexpr int AHEAD = GB_SLOTS - 2;
+    bf16x8 x[GB_SLOTS];
+    auto first = [&](auto self, auto n) __attribute__((always_inline)) {
+        if constexpr (n < AHEAD && n < N) {
+            x[n] = load(n);
+            self(self, std::integral_constant<int, n + 1>{});
+        }
+    };
+    first(first, std::integral_constant<int, 0>{});
     auto run = [&](auto self, auto n) __attribute__((always_inline)) {
         if constexpr (n < N) {
+            if constexpr (n + AHEAD < N) x[(n + AHEAD) % GB_SLOTS] = load(std::integral_constant<int, n + AHEAD>{});
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (n + 1 < N) load(std::integral_constant<int, n + 1>{}, x[(n + 1) & 1]);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(n, x[n & 1]);
+            use(n, x[n % GB_SLOTS], x[(n + GB_SLOTS - 1) % GB_SLOTS]);
             if constexpr (n == 0) beside();
+            __builtin_amdgcn_sched_barrier(0);
             self(self, std::integral_constant<int, n + 1>{});
         }
     };
@@ -364,29 +374,23 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         }
         if constexpr (Traits<WT>::BF) {
             bf16x8 ds[2];
-            constexpr int H = STEPS / 2, N = H + NJ / 2;     // chunks: two steps' K and V rows; four K columns
-            gb_chunks<N>(
-                [&](auto n, bf16x8(&x)[4]) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if constexpr (n < H) x[u] = __builtin_bit_cast(bf16x8, L.row(u & 1 ? vt : kt, 2 * n + u / 2));
-                        else x[u] = L.template column<masked>(kt, (4 * (n - H) + u) % NJ, (4 * (n - H) + u) / NJ);
-                    }
+            constexpr int H = 2 * STEPS, N = H + 2 * NJ;     // a step's K and V rows in turn; K columns
+            gb_stream<N>(
+                [&](auto n) __attribute__((always_inline)) {
+                    if constexpr (n < H) return __builtin_bit_cast(bf16x8, L.row(n % 2 ? vt : kt, n / 2));
+                    else return L.column(kt, (n - H) % NJ, (n - H) / NJ);
                 },
-                [&](auto n, const bf16x8(&x)[4]) __attribute__((always_inline)) {
-                    if constexpr (n < H) {
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {        // (scores and dP in turn: no MFMA takes what the one before it gives)
-                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[2 * u], __builtin_bit_cast(bf16x8, q[0][2 * n + u]), s, 0, 0, 0);
-                            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[2 * u + 1], __builtin_bit_cast(bf16x8, d_o[2 * n + u]), dp, 0, 0, 0);
-                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[2 * u], __builtin_bit_cast(bf16x8, q[PARTS - 1][2 * n + u]), s, 0, 0, 0);
+                [&](auto n, bf16x8 x, bf16x8 before) __attribute__((always_inline)) {
+                    if constexpr (n < H) {                   // (scores and dP in turn: no MFMA takes what the one before it gives)
+                        if constexpr (n % 2 == 0) {
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, q[0][n / 2]), s, 0, 0, 0);
+                        } else {
+                            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, d_o[n / 2]), dp, 0, 0, 0);
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(before, __builtin_bit_cast(bf16x8, q[PARTS - 1][n / 2]), s, 0, 0, 0);
                         }
                     } else {
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            const int o = 4 * (n - H) + u;
-                            y[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], ds[o / NJ], y[o % NJ], 0, 0, 0);
-                        }
+                        constexpr int j = (n - H) % NJ;
+                        y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(masked ? Tile::finite(x) : x, ds[(n - H) / NJ], y[j], 0, 0, 0);
                     }
                     if constexpr (n == H - 1) {
                         probabilities();
@@ -503,39 +507,35 @@ template <typename WT, int D, bool V_LDS> struct GbKeys {
         start(stats, s);
         if constexpr (Traits<WT>::BF) {
             bf16x8 p[2], ds[2];
-            // chunks: a step's rows of the queries' high and low parts, of d_out (and of the values, if they stand in LDS); four columns of
-            // d_out, of the parts
-            constexpr int B = Tile::STEPS, C = NJ / 2, N = B + 3 * C;
+            // a step's rows of the queries' high part, (of the values, if they stand in LDS), of d_out and of the queries' low part; columns of d_out,
+            // of the parts
+            constexpr int U = V_LDS ? 4 : 3, B = U * Tile::STEPS, C = 2 * NJ, N = B + 3 * C;
             start(stats + two, dp);
-            gb_chunks<N>(
-                [&](auto n, bf16x8(&x)[4]) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        if constexpr (n < B) {
-                            if (u < 3) x[u] = __builtin_bit_cast(bf16x8, L.row(buf + u * Tile::BYTES, n));
-                            else if constexpr (V_LDS) x[u] = __builtin_bit_cast(bf16x8, L.row(v_tile, n));
-                        } else {
-                            const int o = 4 * ((n - B) % C) + u;
-                            x[u] = L.template column<MASKED>((n - B) / C == 0 ? dt : buf + ((n - B) / C - 1) * Tile::BYTES, o % NJ, o / NJ);
-                        }
+            gb_stream<N>(
+                [&](auto n) __attribute__((always_inline)) {
+                    if constexpr (n < B) {
+                        constexpr int u = n % U;
+                        const char* from = u == U - 1 ? buf + Tile::BYTES : u == U - 2 ? dt : u == 0 ? buf : v_tile;
+                        return __builtin_bit_cast(bf16x8, L.row(from, n / U));
+                    } else {
+                        constexpr int o = (n - B) % C;
+                        return L.column((n - B) / C == 0 ? dt : buf + ((n - B) / C - 1) * Tile::BYTES, o % NJ, o / NJ);
                     }
                 },
-                [&](auto n, const bf16x8(&x)[4]) __attribute__((always_inline)) {
+                [&](auto n, bf16x8 x, bf16x8 before) __attribute__((always_inline)) {
                     if constexpr (n < B) {                   // (scores and dP in turn: no MFMA takes what the one before it gives)
-                        const bf16x8 k = __builtin_bit_cast(bf16x8, kf[n]);
-                        bf16x8 v;
-                        if constexpr (V_LDS) v = x[3];
-                        else v = __builtin_bit_cast(bf16x8, vf[n]);
-                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0], k, s, 0, 0, 0);
-                        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[2], v, dp, 0, 0, 0);
-                        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[1], k, s, 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            const int o = 4 * ((n - B) % C) + u;
-                            if constexpr (n < B + C) dv[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], p[o / NJ], dv[o % NJ], 0, 0, 0);
-                            else dk[o % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[u], ds[o / NJ], dk[o % NJ], 0, 0, 0);
+                        constexpr int u = n % U;
+                        if constexpr (u == U - 2) {
+                            if constexpr (!V_LDS) before = __builtin_bit_cast(bf16x8, vf[n / U]);
+                            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, before, dp, 0, 0, 0);
+                        } else if constexpr (u == 0 || u == U - 1) {
+                            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, kf[n / U]), s, 0, 0, 0);
                         }
+                    } else {
+                        constexpr int o = (n - B) % C, j = o % NJ;
+                        const bf16x8 a = MASKED ? Tile::finite(x) : x;
+                        if constexpr (n < B + C) dv[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[o / NJ], dv[j], 0, 0, 0);
+                        else dk[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, ds[o / NJ], dk[j], 0, 0, 0);
                     }
                     if constexpr (n == B - 1) {
                         probabilities();
