@@ -76,21 +76,55 @@ __global__ void __launch_bounds__(GE_THREADS) ge_embed_kernel(const GeParams P) 
 // ------------------------------------------------------------------------------------------
 constexpr int GE_SORT_THREADS = 1024, GE_CHUNK_LOG = 14, GE_SMALL_LOG = 12, GE_WINDOW = 64;
 
-// the elements of one chunk in LDS, ascending: compare-and-exchange networks of strides below the size (Batcher's bitonic sort)
-__device__ __forceinline__ void ge_sort_lds(u64* s, int log_n, int tid) {
-    const int n = 1 << log_n;
-    for (int a = 1; a <= log_n; ++a)
-        for (int b = a - 1; b >= 0; --b) {
+// The elements of one chunk in LDS, ascending: compare-and-exchange networks of strides below the size (Batcher's bitonic sort).  A thread holds
+// 2^E elements and does E strides in registers between two visits to the LDS: 2^14 elements by 16 take 29 visits instead of 105.  16 a
+// thread for more than 4096 positions, 4 below, where 16 would leave few threads (203 positions 10 us by 4 and 16 by 16; 16384
+// positions, beside the partial sums, 107 by 16 and 167 with a visit per stride).
+// Element i lies at i + i / 16, so that the contiguous ones of neighbouring threads lie in other banks.
+__device__ __forceinline__ int ge_place(int i) { return i + (i >> 4); }
+__device__ __forceinline__ void ge_order(u64& x, u64& y, bool up) {
+    const u64 a = x, b = y;
+    const bool swap = (a > b) == up;
+    x = swap ? b : a;
+    y = swap ? a : b;
+}
+template <int E> __device__ __forceinline__ void ge_sort_lds(u64* s, int log_n, int tid) {
+    constexpr int N = 1 << E;
+    const bool active = tid < 1 << (log_n - E);
+    u64 x[N];
+    __syncthreads();
+    if (active) {                                            // runs of 2^E, every second one descending
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = s[ge_place(N * tid + e)];
+#pragma unroll
+        for (int a = 1; a <= E; ++a)
+#pragma unroll
+            for (int b = a - 1; b >= 0; --b)
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (!(e >> b & 1)) ge_order(x[e], x[e | 1 << b], a < E ? !(e >> a & 1) : !(tid & 1));
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[ge_place(N * tid + e)] = x[e];
+    }
+    for (int a = E + 1; a <= log_n; ++a)                     // runs of 2^a; (the last merge: all ascending)
+        for (int b = a - 1; b >= 0;) {
+            const int w = max(b - E + 1, 0), first = (tid >> w) << (w + E) | (tid & ((1 << w) - 1));   // strides 2^b .. 2^w
+            const bool up = !(first >> a & 1);
             __syncthreads();
-            for (int i = tid; i < n / 2; i += GE_SORT_THREADS) {
-                const int lo = ((i >> b) << (b + 1)) | (i & ((1 << b) - 1)), hi = lo | 1 << b;
-                const u64 x = s[lo], y = s[hi];
-                const bool up = !(lo >> a & 1);             // (the last merge: all ascending)
-                if ((x > y) == up) {
-                    s[lo] = y;
-                    s[hi] = x;
-                }
+            if (active) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) x[e] = s[ge_place(first | e << w)];
+#pragma unroll
+                for (int j = E - 1; j >= 0; --j)
+                    if (j <= b - w) {
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (!(e >> j & 1)) ge_order(x[e], x[e | 1 << j], up);
+                    }
+#pragma unroll
+                for (int e = 0; e < N; ++e) s[ge_place(first | e << w)] = x[e];
             }
+            b = w - 1;
         }
     __syncthreads();
 }
@@ -106,7 +140,7 @@ __device__ __forceinline__ void ge_mark(const GeParams& P, int i, u64 before, u6
 // (LOG: the LDS holds a chunk of up to 2^LOG elements; 0: nothing is sorted.  With 2^12 two workgroups share a compute unit.)
 template <typename WT, int LOG>
 __global__ void __launch_bounds__(GE_SORT_THREADS) ge_sort_kernel(const GeParams P) {
-    __shared__ u64 s[1 << LOG];
+    __shared__ u64 s[(1 << LOG) * 17 / 16];
     const int tid = threadIdx.x;
     if (LOG > 0 && (int)blockIdx.x < P.chunks) {
         const int ch = blockIdx.x, first = ch << P.chunk_log, size = 1 << P.chunk_log;
@@ -116,15 +150,16 @@ __global__ void __launch_bounds__(GE_SORT_THREADS) ge_sort_kernel(const GeParams
                 const int id = P.ids[first + i];
                 key = (u64)((unsigned)id < (unsigned)P.vocab ? (unsigned)id : (unsigned)P.vocab) << 32 | (unsigned)(first + i);
             }
-            s[i] = key;
+            s[ge_place(i)] = key;
         }
         for (int v = ch * GE_SORT_THREADS + tid; v < P.vocab; v += P.chunks * GE_SORT_THREADS) P.range[v] = make_int2(0, 0);
-        ge_sort_lds(s, P.chunk_log, tid);
+        ge_sort_lds<(LOG > GE_SMALL_LOG ? 4 : 2)>(s, P.chunk_log, tid);
         u64* out = P.chunks == 1 ? P.sorted : P.keys;
         const int n = min(size, P.n - first);
         for (int i = tid; i < n; i += GE_SORT_THREADS) {
-            out[first + i] = s[i];
-            if (P.chunks == 1) ge_mark(P, i, s[max(i - 1, 0)], s[i], s[min(i + 1, n - 1)]);
+            const u64 me = s[ge_place(i)];
+            out[first + i] = me;
+            if (P.chunks == 1) ge_mark(P, i, s[ge_place(max(i - 1, 0))], me, s[ge_place(min(i + 1, n - 1))]);
         }
         return;
     }
@@ -223,7 +258,7 @@ __global__ void __launch_bounds__(GE_THREADS) ge_window_kernel(const GeParams P)
         const int2 r = P.range[id];
         if (r.y - r.x <= GE_WINDOW) continue;
         float* out = P.part + ((size_t)2 * w + which) * P.pieces * GE;
-        for (int c = threadIdx.x; c < P.pieces; c += GE_THREADS) {
+        for (int c = blockIdx.y * GE_THREADS + threadIdx.x; c < P.pieces; c += gridDim.y * GE_THREADS) {
             float sum[GE];
 #pragma unroll
             for (int e = 0; e < GE; ++e) sum[e] = 0.f;
@@ -340,7 +375,7 @@ template <typename WT> int launch_grad(GeParams P, hipStream_t s) {
             hipLaunchKernelGGL(ge_rank_kernel, dim3((P.n + GE_THREADS - 1) / GE_THREADS), dim3(GE_THREADS), 0, s, P);
             hipLaunchKernelGGL(ge_range_kernel, dim3((P.n + GE_THREADS - 1) / GE_THREADS), dim3(GE_THREADS), 0, s, P);
         }
-        if (P.n > GE_WINDOW) hipLaunchKernelGGL((ge_window_kernel<WT>), dim3((P.n + GE_WINDOW - 1) / GE_WINDOW), dim3(GE_THREADS), 0, s, P);
+        if (P.n > GE_WINDOW) hipLaunchKernelGGL((ge_window_kernel<WT>), dim3((P.n + GE_WINDOW - 1) / GE_WINDOW, (P.pieces + GE_THREADS - 1) / GE_THREADS), dim3(GE_THREADS), 0, s, P);
     }
     hipLaunchKernelGGL((ge_rows_kernel<WT>), dim3(P.mask_wgs + (table ? P.vocab : 0)), dim3(GE_THREADS), 0, s, P);
     return hipGetLastError() == hipSuccess ? PS_OK : PS_ERR_DEVICE;
