@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, half = lane >> 5;
     const int rw = wave / KW, kw = wave % KW;
     // (the rows with the most keys start first; neighbours, which go to different XCDs, take different heads)
-    const int K1 = P.k + 1, blk = gridDim.y - 1 - blockIdx.y, h = blockIdx.x, seq = blockIdx.z, hk = h / P.group;
+    const int K1 = P.k + 1, y_at = blockIdx.x / P.nq, h = blockIdx.x - y_at * P.nq, blk = gridDim.x / P.nq - 1 - y_at, seq = blockIdx.y, hk = h / P.group;
     const int R0 = ROWS * blk, r0 = R0 + 32 * rw, r_last = min(R0 + ROWS, P.rows) - 1, g_last = gb_group(P, r_last);
     const bool active = r0 < P.rows;
     const int n_stages = g_last / 64 + 1;
@@ -752,17 +752,18 @@ __global__ void __launch_bounds__(D * 2) gb_merge_kernel(const GbParams P, const
     for (int u = 0; u < 4; ++u) gb_write4<WT, D>(row, which ? nullptr : P.table + (size_t)key * (D / 2), 32 * j0 + 8 * u + 4 * half, which ? 1.f : GB_LN2, a[u], b[u]);
 }
 
-// the checks are those of ps_group_attention
-ps_group_attn_args forward_args(const ps_group_attn_grad_args* a) {
+// The checks are those of ps_group_attention; and a launch's threads (256 per 128 query rows, up to 512 per tile of keys) are counted in 32 bits:
+// as many query rows fill the memory, and as many key tiles take tens of thousands of sequences of a few tokens with a hundred kv heads
+int check(const ps_group_attn_grad_args* a) {
+    if (!a) return PS_ERR_NULL;
     ps_group_attn_args f = {};
     f.seqs = a->seqs; f.tokens = a->tokens; f.k = a->k; f.n_heads = a->n_heads; f.n_kv_heads = a->n_kv_heads;
     f.head_dim = a->head_dim; f.dtype = a->dtype; f.rope_base = a->rope_base;
-    return f;
-}
-int check(const ps_group_attn_grad_args* a) {
-    if (!a) return PS_ERR_NULL;
-    const ps_group_attn_args f = forward_args(a);
-    return ga_check(&f);
+    const int st = ga_check(&f);
+    if (st != PS_OK) return st;
+    const long long rows = (long long)a->tokens * (a->k + 1), heads = (long long)a->seqs * a->n_kv_heads, gpt = 32 / (a->k + 1);
+    const long long row_wgs = (rows + GB_ROWS - 1) / GB_ROWS * a->n_heads, key_wgs = heads * ((a->tokens + 63) / 64 + (a->tokens / gpt + 4) / 4) + 1024;
+    return row_wgs >= 1 << 24 || key_wgs >= 1 << 23 ? PS_ERR_UNSUPPORTED : PS_OK;
 }
 
 // How a call is cut: wavefronts that share 32 query rows; keys of a workgroup, parts of their rows
@@ -816,7 +817,7 @@ template <typename WT, int D> int launch(const GbParams& P, const GbPlan& G, flo
     // (as ga_rope_kernel: where positions are few, several workgroups of at most one item per thread share one)
     const long long items = (long long)P.seqs * P.nkv * (D / 8) * (P.k + 1);
     hipLaunchKernelGGL((gb_prep_kernel<WT, D>), dim3(P.T + P.k, (unsigned)std::max(1LL, std::min((items + 255) / 256, 2048LL / (P.T + P.k)))), dim3(256), 0, s, P);
-    const dim3 grid(P.nq, (P.rows + GB_ROWS / G.kw - 1) / (GB_ROWS / G.kw), P.seqs);
+    const dim3 grid(P.nq * ((P.rows + GB_ROWS / G.kw - 1) / (GB_ROWS / G.kw)), P.seqs);
     if (G.kw == 2) hipLaunchKernelGGL((gb_dq_kernel<WT, D, 2>), grid, dim3(GB_THREADS), 0, s, P);
     else hipLaunchKernelGGL((gb_dq_kernel<WT, D, 1>), grid, dim3(GB_THREADS), 0, s, P);
     const GbWork W = {G.heads, G.splits, G.tiles * G.heads, P.k > 0 ? (P.T + P.gpt - 1) / P.gpt * G.heads : 0, partial};

@@ -118,3 +118,14 @@ def test_workspaces_stay_small_beside_what_they_work_on(lib):
     for T in (2048, 65536):
         a = _attn(tokens=T, n_heads=32, n_kv_heads=32, head_dim=128)
         assert TR.ps_group_attention_grad_workspace_bytes(a) < 4 * T * 5 * q
+
+
+def test_attention_gradient_launches_fit_the_grid(lib):
+    """Threads along a side of a grid are counted in 32 bits: the largest layouts are taken, larger ones refused before anything is launched."""
+    most = dict(tokens=(1 << 20) - 15, k=15, n_kv_heads=1, head_dim=64)
+    assert TR.ps_group_attention_grad_workspace_bytes(_attn(n_heads=64, **most)) > 1 << 36
+    few = dict(tokens=1, k=4, head_dim=64)
+    assert TR.ps_group_attention_grad_workspace_bytes(_attn(seqs=65535, n_heads=32, n_kv_heads=32, **few)) > 0
+    for kw in (dict(n_heads=160, **most), dict(seqs=65535, n_heads=128, n_kv_heads=128, **few), dict(seqs=65535, n_heads=65535, n_kv_heads=65535, **few)):
+        assert TR.ps_group_attention_grad_workspace_bytes(_attn(**kw)) == 0
+        assert TR.ps_group_attention_grad(_attn(**kw), None) == B.PS_ERR_UNSUPPORTED
