@@ -132,3 +132,50 @@ def test_embed_grad(dtype, seqs, T, k, hidden, vocab, scale, kind):
         assert torch.equal(alone[1], d_mask) and bool((alone[0] == 77.0).all())
     again = call(True, False)
     assert torch.equal(again[0], d_embed)
+
+
+def test_captured_calls_replayed():
+    """Embeddings and their gradients in one graph (three chunks of positions), two inputs in turn, the eager calls in between."""
+    import torch
+    seqs, T, k, hidden, vocab = 5, 8000, 1, 64, 700
+    both = []
+    for seed in (31, 32):
+        g = torch.Generator().manual_seed(seed)
+        both.append((_ids(seqs, T, vocab, g, "zipf"), torch.randn((vocab, hidden), generator=g).cuda(), torch.randn((k, hidden), generator=g).cuda(),
+                     torch.randn((seqs, T * (k + 1), hidden), generator=g).cuda()))
+
+    def calls(ids, embed, mask, dx):
+        out = [torch.full_like(t, 77.0) for t in (dx, embed, mask)]
+        e, b = TR.make_embed_args(seqs, T, k, hidden, vocab, "f32", 3.0), TR.make_embed_grad_args(seqs, T, k, hidden, vocab, "f32", 3.0)
+        e.token_ids, e.embed, e.mask_emb, e.x = ids.data_ptr(), embed.data_ptr(), mask.data_ptr(), out[0].data_ptr()
+        b.token_ids, b.d_x, b.d_embed, b.d_mask = ids.data_ptr(), dx.data_ptr(), out[1].data_ptr(), out[2].data_ptr()
+        need = TR.ps_group_embed_grad_workspace_bytes(b)
+        ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda:0")
+        b.workspace, b.workspace_bytes = (ws.data_ptr() + 255) & ~255, need
+
+        def run():
+            assert TR.ps_group_embed(e, _stream()) == B.PS_OK
+            assert TR.ps_group_embed_grad(b, _stream()) == B.PS_OK
+        return run, out, ws
+
+    want = []
+    for x in both:
+        run, out, _ws = calls(*x)
+        run()
+        torch.cuda.synchronize()
+        want.append(out)
+    buf = [t.clone() for t in both[0]]
+    run, out, _ws = calls(*buf)
+    print("case captured embeddings", flush=True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for turn in range(4):
+        for to, x in zip(buf, both[turn & 1]):
+            to.copy_(x)
+        graph.replay()
+        eager, got, _w = calls(*both[1 - (turn & 1)])
+        eager()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[turn & 1])), turn
+        assert all(torch.equal(a, b) for a, b in zip(got, want[1 - (turn & 1)])), turn

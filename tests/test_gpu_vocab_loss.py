@@ -187,3 +187,30 @@ def test_gradient_against_differences():
         step[i, j] = 1e-4
         slope = float((total(h64 + step) - total(h64 - step)) / 2e-4)
         assert abs(slope - float(d[i, j])) <= 1e-6 + 1e-5 * abs(slope)
+
+
+@pytest.mark.parametrize("rows,hidden,vocab", [(300, 512, 32000), (40, 256, 3000)])
+def test_a_captured_call_replayed(rows, hidden, vocab):
+    """One graph, two inputs in turn in the same buffers, an eager call and a synchronisation between replays."""
+    import torch
+    both = [_make(rows, hidden, vocab, "bf16", s) for s in (21, 22)]
+    want = [[t.clone() for t in _call(*x, "bf16")] for x in both]
+    buf = [t.clone() for t in both[0]]
+    loss, d = torch.zeros(rows, device="cuda:0"), torch.zeros_like(buf[0])
+    a = TR.make_loss_args(rows, hidden, vocab, "bf16")
+    a.h, a.w_lm, a.targets, a.weights, a.loss, a.d_hidden = (t.data_ptr() for t in (*buf, loss, d))
+    need = TR.ps_vocab_loss_workspace_bytes(a)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda:0")
+    a.workspace, a.workspace_bytes = (ws.data_ptr() + 255) & ~255, need
+    print("case captured loss", rows, hidden, vocab, flush=True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        assert TR.ps_vocab_loss(a, torch.cuda.current_stream().cuda_stream) == B.PS_OK
+    for turn in range(4):
+        for to, x in zip(buf, both[turn & 1]):
+            to.copy_(x)
+        graph.replay()
+        eager = _call(*both[1 - (turn & 1)], "bf16")
+        torch.cuda.synchronize()
+        assert torch.equal(loss, want[turn & 1][0]) and torch.equal(d, want[turn & 1][1]), turn
+        assert torch.equal(eager[0], want[1 - (turn & 1)][0]) and torch.equal(eager[1], want[1 - (turn & 1)][1]), turn
