@@ -13,7 +13,8 @@
 // The vocabulary is gone through in pieces; two products for each, the floor being their 4 V H operations a row:
 //   vl_score_kernel   W h^T, one tile per workgroup: exponentials to the workspace (storage type), sums of rows beside them
 //   vl_grad_kernel    exponentials . W, added to what the pieces before left, in float32
-// before the last of which vl_rows_kernel adds up the rows' sums and makes their losses and the gradients' factors.
+// The rows' sums make their losses and the gradients' factors: in vl_join_kernel, which adds up the parts of the products, or, where the last
+// product's tiles become gradients at once, in vl_rows_kernel before it.
 #include <math.h>
 
 #include "ps_train_device.h"
@@ -35,7 +36,7 @@ struct VlParams {
     float* loss;
     char* d_hidden;
     float *tl, *sums, *acc, *alone;   // target logits; sums [rows_c][nsum]; products [splits][rows_c][H]; those of rows by themselves [rows_c][H]
-    int* state;                       // rows: VL_NEAR, VL_FAR_APART (set by the scores), then VL_DONE, VL_ZERO (vl_rows_kernel)
+    int* state;                       // rows: VL_NEAR, VL_FAR_APART (set by the scores), from vl_rows_kernel on also VL_DONE, VL_ZERO
     float2* factor;                   // of a row's products, of its target's row of the LM head
     char* x;                          // exponentials [rows_c][ldx], storage type
 };
@@ -575,7 +576,7 @@ template <typename WT> __device__ __forceinline__ void vl_store_group(char* p, c
 // A row whose logits lie too far above its target's: its maximum, then sums against it, 256 tokens at a time.  Returns log2 of
 // sum_{v != t} exp(l_v - l_t); acc (of the row, float32) becomes sum_{v != t} p_v W_v.  One workgroup reads the whole LM head twice.
 template <typename WT>
-__device__ __attribute__((noinline)) float vl_row_alone(const VlParams& P, int row, int target, float* acc, float* s, int tid) {
+__device__ __forceinline__ float vl_row_alone(const VlParams& P, int row, int target, float* acc, float* s, int tid) {
     constexpr int GE = Traits<WT>::GE, ESZ = Traits<WT>::ESZ;
     const int lane = tid & 63, wave = tid >> 6;
     float m = -INFINITY, total = 0.f;
@@ -624,69 +625,78 @@ __device__ __attribute__((noinline)) float vl_row_alone(const VlParams& P, int r
     return z;
 }
 
-// The rows' losses and the factors of their gradients, a wavefront per row; then the workgroup takes rows that are far apart one by one
-template <typename WT>
-__global__ void __launch_bounds__(VL_THREADS) vl_rows_kernel(const VlParams P) {
-    constexpr int GE = Traits<WT>::GE, ESZ = Traits<WT>::ESZ;
-    __shared__ float s[VL_THREADS];
-    __shared__ int far_apart[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r0 = 4 * blockIdx.x;
+// What a row's sums make (a wavefront): its loss, written, and the factors of its products and of its target's row of the LM head, if it
+// counts and is not far apart.  sum: of its exponentials.
+struct VlRow { int state; float2 f; };
+template <typename WT> __device__ __forceinline__ float2 vl_finish(const VlParams& P, int row, float z, float scale, bool write) {
     // z: log2 of sum_{v != t} exp(l_v - l_t); the loss is log(1 + 2^z), the others' probability 2^z / (1 + 2^z)
-    auto finish = [&](int r, float z, float scale) __attribute__((always_inline)) {
-        const float weight = P.weights ? P.weights[P.row0 + r] : 1.f, e = __builtin_amdgcn_exp2f(-fabsf(z));
-        const float loss = z > 0.f ? z * VL_LN2 + log1pf(e) : log1pf(e), others = z > 0.f ? 1.f / (1.f + e) : e / (1.f + e);
-        const float2 f = make_float2(scale * weight, -weight * others);
-        if (lane == 0) {
-            P.loss[P.row0 + r] = weight * (z == z ? loss : z);
-            P.factor[r] = f;
-        }
-        return f;
-    };
-    {
-        const int r = r0 + wave, row = P.row0 + min(r, P.rows_c - 1);
-        const int state = P.state[row];
-        const bool counts = vl_counts(P, row);
-        float sum = 0.f;
-        for (int i = lane; i < P.nsum; i += 64) sum += P.sums[(size_t)(row - P.row0) * P.nsum + i];
-        sum = wave_sum(sum);
-        const bool far = r < P.rows_c && counts && state == VL_FAR_APART;
-        if (r < P.rows_c && counts && !far) finish(r, __builtin_amdgcn_logf(sum) + VL_SHIFT, 1.f / (sum + 0x1p-64f));
-        if (lane == 0) {
-            far_apart[wave] = far;
-            if (r < P.rows_c && !counts) {
-                P.loss[row] = 0.f;
-                P.factor[r] = make_float2(0.f, 0.f);
-                P.state[row] = VL_ZERO;
-            }
-        }
-    }
-    __syncthreads();
-    for (int i = 0; i < 4; ++i) {
-        if (!far_apart[i]) continue;
-        const int r = r0 + i, row = P.row0 + r, target = P.targets[row];
-        float* acc = P.alone + (size_t)r * P.H;
-        const float2 f = finish(r, vl_row_alone<WT>(P, row, target, acc, s, tid), 1.f);
-        if (tid == 0) P.state[row] = VL_DONE;
-        if (!P.d_hidden) continue;
-        for (int c = tid; c < P.H / GE; c += VL_THREADS) {
-            float sum[GE], wt[GE];
-            load_group<WT>(P.w + ((size_t)target * P.H + c * GE) * ESZ, wt);
+    const float weight = P.weights ? P.weights[row] : 1.f, e = __builtin_amdgcn_exp2f(-fabsf(z));
+    const float loss = z > 0.f ? z * VL_LN2 + log1pf(e) : log1pf(e), others = z > 0.f ? 1.f / (1.f + e) : e / (1.f + e);
+    if (write) P.loss[row] = weight * (z == z ? loss : z);
+    return make_float2(scale * weight, -weight * others);
+}
+template <typename WT> __device__ __forceinline__ VlRow vl_row(const VlParams& P, int r, int lane, bool write) {
+    const int row = P.row0 + r, state = P.state[row];
+    const bool counts = vl_counts(P, row);
+    float sum = 0.f;
+    for (int i = lane; i < P.nsum; i += 64) sum += P.sums[(size_t)r * P.nsum + i];
+    sum = wave_sum(sum);
+    VlRow y = {counts ? state : VL_ZERO, make_float2(0.f, 0.f)};
+    if (y.state == VL_NEAR) y.f = vl_finish<WT>(P, row, __builtin_amdgcn_logf(sum) + VL_SHIFT, 1.f / (sum + 0x1p-64f), write && lane == 0);
+    else if (y.state == VL_ZERO && write && lane == 0) P.loss[row] = 0.f;
+    return y;
+}
+// ... a row that is far apart (the workgroup)
+template <typename WT> __device__ __forceinline__ void vl_far_row(const VlParams& P, int r, float* s, int tid) {
+    constexpr int GE = Traits<WT>::GE, ESZ = Traits<WT>::ESZ;
+    const int row = P.row0 + r, target = P.targets[row];
+    float* acc = P.alone + (size_t)r * P.H;
+    const float2 f = vl_finish<WT>(P, row, vl_row_alone<WT>(P, row, target, acc, s, tid), 1.f, tid == 0);
+    if (!P.d_hidden) return;
+    for (int c = tid; c < P.H / GE; c += VL_THREADS) {
+        float sum[GE], wt[GE];
+        load_group<WT>(P.w + ((size_t)target * P.H + c * GE) * ESZ, wt);
 #pragma unroll
-            for (int u = 0; u < GE; ++u) sum[u] = acc[c * GE + u] * f.x + wt[u] * f.y;
-            vl_store_group<WT>(P.d_hidden + ((size_t)row * P.H + c * GE) * ESZ, sum);
-        }
+        for (int u = 0; u < GE; ++u) sum[u] = acc[c * GE + u] * f.x + wt[u] * f.y;
+        vl_store_group<WT>(P.d_hidden + ((size_t)row * P.H + c * GE) * ESZ, sum);
     }
 }
 
-// The gradient of rows whose products are in parts: a workgroup per row
+// Before products that become gradients at once, and where none are wanted: the rows' losses and factors, a wavefront per row; then the
+// workgroup takes rows that are far apart one by one
+template <typename WT>
+__global__ void __launch_bounds__(VL_THREADS) vl_rows_kernel(const VlParams P) {
+    __shared__ float s[VL_THREADS];
+    __shared__ int far_apart[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r0 = 4 * blockIdx.x, r = r0 + wave;
+    VlRow y = {VL_ZERO, make_float2(0.f, 0.f)};
+    if (r < P.rows_c) y = vl_row<WT>(P, r, lane, true);
+    if (lane == 0) {
+        far_apart[wave] = y.state == VL_FAR_APART;
+        if (r < P.rows_c) {
+            P.factor[r] = y.f;
+            P.state[P.row0 + r] = y.state == VL_FAR_APART ? VL_DONE : y.state;
+        }
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i)
+        if (far_apart[i]) vl_far_row<WT>(P, r0 + i, s, tid);
+}
+
+// The loss and the gradient of rows whose products are in parts: a workgroup per row
 template <typename WT>
 __global__ void __launch_bounds__(VL_THREADS) vl_join_kernel(const VlParams P) {
     constexpr int GE = Traits<WT>::GE, ESZ = Traits<WT>::ESZ;
-    const int r = blockIdx.x, row = P.row0 + r, state = P.state[row];
-    if (state == VL_DONE) return;
-    const float2 f = P.factor[r];
-    const char* wt = P.w + (size_t)(state == VL_NEAR ? P.targets[row] : 0) * P.H * ESZ;
-    for (int c = threadIdx.x; c < P.H / GE; c += VL_THREADS) {
+    __shared__ float s[VL_THREADS];
+    const int r = blockIdx.x, row = P.row0 + r, tid = threadIdx.x;
+    const VlRow y = vl_row<WT>(P, r, tid & 63, tid < 64);   // (every wavefront adds the sums up: the same bits)
+    if (y.state == VL_FAR_APART) {
+        vl_far_row<WT>(P, r, s, tid);
+        return;
+    }
+    const char* wt = P.w + (size_t)(y.state == VL_NEAR ? P.targets[row] : 0) * P.H * ESZ;
+    for (int c = tid; c < P.H / GE; c += VL_THREADS) {
         float sum[GE], w[GE];
 #pragma unroll
         for (int u = 0; u < GE; ++u) sum[u] = 0.f;
@@ -700,7 +710,7 @@ __global__ void __launch_bounds__(VL_THREADS) vl_join_kernel(const VlParams P) {
             }
         load_group<WT>(wt + (size_t)c * 16, w);
 #pragma unroll
-        for (int u = 0; u < GE; ++u) sum[u] = state == VL_NEAR ? sum[u] * f.x + w[u] * f.y : 0.f;
+        for (int u = 0; u < GE; ++u) sum[u] = y.state == VL_NEAR ? sum[u] * y.f.x + w[u] * y.f.y : 0.f;
         vl_store_group<WT>(P.d_hidden + ((size_t)row * P.H + c * GE) * ESZ, sum);
     }
 }
@@ -797,7 +807,7 @@ template <typename WT> int run(VlParams P, const VlPlan& L, hipStream_t s) {
             if (wide) hipLaunchKernelGGL(vl_score_wide_kernel, dim3(tokens * row_tiles), dim3(VW_THREADS), 0, s, P, tokens, row_tiles);
             else if (L.tile == 64) launch_score<WT, 64>(P, s);
             else if constexpr (Traits<WT>::BF) launch_score<WT, 128>(P, s);
-            if (last) hipLaunchKernelGGL((vl_rows_kernel<WT>), dim3((P.rows_c + 3) / 4), dim3(VL_THREADS), 0, s, P);
+            if (last && (at_once || !P.d_hidden)) hipLaunchKernelGGL((vl_rows_kernel<WT>), dim3((P.rows_c + 3) / 4), dim3(VL_THREADS), 0, s, P);
             if (!P.d_hidden) continue;
             if (last && at_once) hipLaunchKernelGGL(vl_grad_wide_kernel<true>, dim3(cols * row_tiles), dim3(VW_THREADS), 0, s, P, cols, row_tiles);
             else if (wide) hipLaunchKernelGGL(vl_grad_wide_kernel<false>, dim3(cols * row_tiles, P.splits), dim3(VW_THREADS), 0, s, P, cols, row_tiles);
