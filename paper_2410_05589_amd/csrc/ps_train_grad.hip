@@ -3,8 +3,13 @@
 // With q~, k~ rotated, s = q~ k~ / sqrt(d), P = exp(s - lse), delta_i = sum_d d_out_i out_i:
 //   dP = d_out V^T;  dS = P (dP - delta);  dV = P^T d_out;  dK~ = dS^T q~ / sqrt(d);  dQ~ = dS k~ / sqrt(d), turned back.
 // The probabilities are worked out again where they are needed, twice: by workgroups that own query rows (gb_dq_kernel) and by
-// workgroups that own keys (gb_dkv_kernel: real tokens; gb_own_kernel: [MASK] tokens, which only their own group's rows see).
-// Nobody adds to what another writes: no atomics, the same bits every time.  That is 7 products where one pass would do with 5.
+// workgroups that own keys (gb_dkv_kernel: real tokens, and [MASK] tokens, which only their own group's rows see).
+// Nobody adds to what another writes: no atomics, the same bits every time.  That is 7 products where one pass would do with 5, and 10 in bf16,
+// where the rotated queries stand as two parts (scores twice, dK~), as in the forward pass whose lse they have to match.
+//
+// Bound by the matrix cores and by waits for operands: T 2048, k 4, 32 heads x 128 takes 1065 us (5 products at the rate of a large library
+// product: 327; the 10: 654), of which keys 650 .. 710, queries 410 .. 440, rotated keys 30; 4 x T 1024, k 8, 32 / 8 heads 2376; T 203, k 5,
+// 40 heads 101; float32 2 x T 300, k 3, 8 heads x 64 84.
 //
 // All products are 32 x 32 MFMA tiles, as in ga_attn_wide_kernel: what the wavefront owns (queries, or keys) lies along the lanes,
 // so a score tile leaves the matrix core in the operand layout of the products that follow it (a lane holds 16 of the 32 rows of the other
@@ -157,6 +162,7 @@ template <typename WT> struct GbOperand {
     }
 };
 typedef __attribute__((address_space(3))) void lds_void;
+// (writes of LDS as any: a barrier's or a fence's release waits until they have arrived)
 __device__ __forceinline__ void gb_copy(rsrc_t from, unsigned off, char* to) { __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, 0, 0, 0); }
 // A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: its i-th KiB (64 bytes of 16 rows)
 template <typename WT, int D> __device__ __forceinline__ void gb_request(const char* m, unsigned stride, int most, char* tile, int i, int lane) {
@@ -413,7 +419,8 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         const int lo = qg * K1 + 1 - 4 * half, hi = qrow - 4 * half;
         for (int i = kw; i < 2; i += KW) {                   // 0: rows r0 .., 1: rows r0 - 32 ..
             if (KW == 1 && i == 1) {
-                if (before) stage_own(r0 - 32);              // (nobody else reads these tiles)
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (nobody else reads these tiles, and this wavefront's reads are back)
+                if (before) stage_own(r0 - 32);
             }
             __syncthreads();
             if (active && (i == 0 || before)) work(mine, std::true_type{}, lo - (r0 - 32 * i), hi - (r0 - 32 * i), [] {});
@@ -467,6 +474,8 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
 // at a time.  A workgroup is KW wavefronts of keys by two of rows: a stage holds two row tiles (rotated queries' parts, d_out,
 // statistics), brought in by the memory unit itself; the two row wavefronts' sums meet in the LDS at the end.
 // bf16, head_dim 128: the values' rows stay in LDS, so that two wavefronts per SIMD find room for everything else in their 256 registers.
+// (64 keys per wavefront, which halves the LDS reads per product but leaves a SIMD one wavefront: 900 us in the place of 640 at T 2048.)
+// A step takes 48 MFMAs, 88 LDS reads and 69 vector instructions; the matrix cores are busy 40 % of the time and the LDS 27 %.
 // ------------------------------------------------------------------------------------------
 template <typename WT, int D, bool V_LDS> struct GbKeys {
     typedef GbTile<WT, D> Tile;
