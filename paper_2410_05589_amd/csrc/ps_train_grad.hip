@@ -162,12 +162,28 @@ template <typename WT> struct GbOperand {
     }
 };
 typedef __attribute__((address_space(3))) void lds_void;
-// (writes of LDS as any: a barrier's or a fence's release waits until they have arrived)
-__device__ __forceinline__ void gb_copy(rsrc_t from, unsigned off, char* to) { __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, 0, 0, 0); }
+// 16 bytes per lane from base + off (base is the wavefront's) to the LDS, lane after lane from `to` on, by the memory unit itself.  The request is
+// written out because of what the compiler does with the builtin: to it both buffers of a kernel are one array, so that the first read of a
+// stage waits for the next stage's requests, which have only just been made (T 2048, k 4: 1066 us, as it is 1031).  So nobody but
+// the source waits for these: gb_arrived, before anything reads what they bring; and the source leaves the five wait states that scalars
+// restored by the vector unit need before a request reads them.
+__device__ __forceinline__ void gb_copy(const char* base, unsigned off, char* to) {
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    const u64 at = (u64)(uintptr_t)base;
+    const i32x4 from = {(int)(unsigned)at, (int)(unsigned)(at >> 32) & 0xFFFF, -1, 0x00020000};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"((unsigned)(uintptr_t)(lds_void*)to), "v"(off), "s"(from) : "memory", "m0");
+}
+// this wavefront's requests have arrived, and its own reads and writes of LDS are done
+__device__ __forceinline__ void gb_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory"); }
+// ... the workgroup's
+__device__ __forceinline__ void gb_arrived() {
+    gb_wait();
+    __syncthreads();
+}
 // A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: its i-th KiB (64 bytes of 16 rows)
 template <typename WT, int D> __device__ __forceinline__ void gb_request(const char* m, unsigned stride, int most, char* tile, int i, int lane) {
     const int row = 16 * (i & 1) + lane / 4, piece = GbTile<WT, D>::swap(row, lane & 3);
-    gb_copy(make_rsrc(m), (unsigned)min(row, most) * stride + (i >> 1) * 64 + piece * 16, tile + i * 1024);
+    gb_copy(m, (unsigned)min(row, most) * stride + (i >> 1) * 64 + piece * 16, tile + i * 1024);
 }
 // ... this wavefront's share of WAVES
 template <typename WT, int D, int WAVES>
@@ -419,24 +435,24 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         const int lo = qg * K1 + 1 - 4 * half, hi = qrow - 4 * half;
         for (int i = kw; i < 2; i += KW) {                   // 0: rows r0 .., 1: rows r0 - 32 ..
             if (KW == 1 && i == 1) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (nobody else reads these tiles, and this wavefront's reads are back)
+                gb_wait();                                   // (nobody else reads these tiles)
                 if (before) stage_own(r0 - 32);
             }
-            __syncthreads();
+            gb_arrived();
             if (active && (i == 0 || before)) work(mine, std::true_type{}, lo - (r0 - 32 * i), hi - (r0 - 32 * i), [] {});
         }
         __syncthreads();
     }
     // real tokens: stages that all of the wavefront's queries see, some of them, none
     stage(0);
-    __syncthreads();
+    gb_arrived();
     int t = 0;
     auto tile = [&](int i) __attribute__((always_inline)) { return smem + (t & 1) * BUF + i * 2 * Tile::BYTES; };
     for (const int end = active ? (wg0 + 1) / 64 : 0; t < end; ++t) {
 #pragma unroll
         for (int i = 0; i < 2 / KW; ++i)
             work(tile(i * KW + kw), std::false_type{}, 0, 0, [&]() __attribute__((always_inline)) { if (i == 0 && t + 1 < n_stages) stage(t + 1); });
-        __syncthreads();
+        gb_arrived();
     }
     for (; t < n_stages; ++t) {
         if (t + 1 < n_stages) stage(t + 1);
@@ -445,7 +461,7 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
             const int first = 64 * t + 32 * i;
             if (active && first <= wg1) work(tile(i), std::true_type{}, -first - 4 * half, qg - first - 4 * half, [] {});
         }
-        __syncthreads();
+        gb_arrived();
     }
     if constexpr (KW == 2) {
         f32x4* area = reinterpret_cast<f32x4*>(smem) + rw * NJ * 4 * 64 + lane;
@@ -622,11 +638,9 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
             for (int p = 0; p < PARTS; ++p) gb_stage<WT, D, 1>(P.q_rot + p * part + (at + first) * D * ESZ, D * ESZ, last - first, buf + p * Tile::BYTES, 0, lane);
             gb_stage<WT, D, 1>(P.d_out + (((size_t)seq * P.rows + first) * P.nq + h) * D * ESZ, ostride, last - first, buf + PARTS * Tile::BYTES, 0, lane);
             stats[lane] = (lane < 32 ? P.lse2 : P.delta)[at + krow];
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");   // (the tiles have arrived, for this wavefront's own reads)
-            __builtin_amdgcn_wave_barrier();
+            gb_wait();                                       // (for this wavefront's own reads)
             keys.template step<true>(L, buf, stats, 32, half, slot > 0 ? krow - first - 4 * half : 99, g * K1 + P.k - first - 4 * half, [] {});
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-            __builtin_amdgcn_wave_barrier();
+            gb_wait();
         }
         if (first + c <= last && slot > 0) gb_write_keys<WT, D>(P, seq, hk, krow, krow - g * P.k, half, keys.dk, keys.dv);
         return;
@@ -641,6 +655,7 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
     int next_g = i0 / per_head, next_j = i0 - next_g * per_head;
     const int next_j0 = next_j;
     float stat = 0.f;
+    bool stat_in = false;
     auto stage = [&](int i) __attribute__((always_inline)) {   // set i, to buffer i % 2
         const int h = hk * P.group + next_g, first = first_row + 64 * next_j, left = P.rows - 1 - first;
         const size_t at = ((size_t)seq * P.nq + h) * P.rows + first;
@@ -656,14 +671,15 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
             gb_request<WT, D>(P.d_out + (((size_t)seq * P.rows + first + from) * P.nq + h) * D * ESZ, ostride, most, to + PARTS * Tile::BYTES, x % N, lane);
         }
         // (every second wavefront's is the same; a row beyond the last: probability 0, whatever the last row, which it repeats, holds)
+        // (looked at where it is stored, a stage later)
         stat = (wave & 1 ? P.delta : P.lse2)[at + min(lane, left)];
-        stat = wave & 1 || lane <= left ? stat : -INFINITY;
+        stat_in = wave & 1 || lane <= left;
         next_j += i + 1 < i1;
         const bool wrap = next_j == per_head;
         next_j = wrap ? 0 : next_j;
         next_g += wrap;
     };
-    auto stage_stats = [&](int i) __attribute__((always_inline)) { reinterpret_cast<float*>(smem + (i & 1) * C::BUF + C::OFF_S)[64 * (wave & 1) + lane] = stat; };
+    auto stage_stats = [&](int i) __attribute__((always_inline)) { reinterpret_cast<float*>(smem + (i & 1) * C::BUF + C::OFF_S)[64 * (wave & 1) + lane] = stat_in ? stat : -INFINITY; };
     if (i0 < i1) stage(i0);
     gb_own_rows<WT, D>(P.k_rot + (((size_t)seq * P.nkv + hk) * P.rows + (size_t)key * K1) * D * ESZ, half, keys.kf);
     if constexpr (C::V_LDS) {
@@ -674,7 +690,11 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
         gb_own_rows<WT, D>(P.v + (((size_t)seq * P.rows + (size_t)key * K1) * P.nkv + hk) * D * ESZ, half, keys.vf);
     }
     if (i0 < i1) stage_stats(i0);
-    __syncthreads();
+    // (the compiler's own loads end here: it would wait for them in the loop, and with them for the requests that it does not know)
+    for (uint4& x : keys.kf) asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w));
+    if constexpr (!C::V_LDS)
+        for (uint4& x : keys.vf) asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w));
+    gb_arrived();
     auto step = [&](int i, int first, auto masked) __attribute__((always_inline)) {
         const char* buf = smem + (i & 1) * C::BUF;
         const float* stats = reinterpret_cast<const float*>(buf + C::OFF_S) + 32 * rw;
@@ -685,7 +705,7 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
             keys.template step<false>(L, buf + rw * C::SET, stats, 64, half, 0, 31, [&]() __attribute__((always_inline)) { stage(i + 1); });
         }
         stage_stats(i + 1);
-        __syncthreads();
+        gb_arrived();
     };
     // of every head the row tiles that see some of the wavefront's keys, then those that see all of them
     const int see_all = w0 < P.T ? min(max((w0 + 31) * K1 - first_row - 32 * rw + 63, 0) / 64, per_head) : per_head;
