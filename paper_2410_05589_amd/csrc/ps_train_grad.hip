@@ -7,9 +7,9 @@
 // Nobody adds to what another writes: no atomics, the same bits every time.  That is 7 products where one pass would do with 5, and 10 in bf16,
 // where the rotated queries stand as two parts (scores twice, dK~), as in the forward pass whose lse they have to match.
 //
-// Bound by the matrix cores and by waits for operands: T 2048, k 4, 32 heads x 128 takes 1065 us (5 products at the rate of a large library
-// product: 327; the 10: 654), of which keys 650 .. 710, queries 410 .. 440, rotated keys 30; 4 x T 1024, k 8, 32 / 8 heads 2376; T 203, k 5,
-// 40 heads 101; float32 2 x T 300, k 3, 8 heads x 64 84.
+// Bound by the matrix cores, by waits beside them and, for the [MASK] keys, by memory: T 2048, k 4, 32 heads x 128 takes 1035 us (5 products at
+// the rate of a large library product: 327; the 10: 654), of which keys 630 .. 690 ([MASK] keys 110), queries 390 .. 420, rotated keys 30; 4 x T 1024,
+// k 8, 32 / 8 heads 2320; T 203, k 5, 40 heads 102; float32 2 x T 300, k 3, 8 heads x 64 84.
 //
 // All products are 32 x 32 MFMA tiles, as in ga_attn_wide_kernel: what the wavefront owns (queries, or keys) lies along the lanes,
 // so a score tile leaves the matrix core in the operand layout of the products that follow it (a lane holds 16 of the 32 rows of the other
@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
 // statistics), brought in by the memory unit itself; the two row wavefronts' sums meet in the LDS at the end.
 // bf16, head_dim 128: the values' rows stay in LDS, so that two wavefronts per SIMD find room for everything else in their 256 registers.
 // (64 keys per wavefront, which halves the LDS reads per product but leaves a SIMD one wavefront: 900 us in the place of 640 at T 2048.)
-// A step takes 48 MFMAs, 88 LDS reads and 69 vector instructions; the matrix cores are busy 40 % of the time and the LDS 27 %.
+// A step takes 48 MFMAs, 88 LDS reads and 69 vector instructions; the matrix cores are busy 42 % of the time and the LDS 28 %.
 // ------------------------------------------------------------------------------------------
 template <typename WT, int D, bool V_LDS> struct GbKeys {
     typedef GbTile<WT, D> Tile;
