@@ -162,17 +162,8 @@ template <typename WT> struct GbOperand {
     }
 };
 typedef __attribute__((address_space(3))) void lds_void;
-// 16 bytes per lane from base + off (base is the wavefront's) to the LDS, lane after lane from `to` on, by the memory unit itself.  The request is
-// written out because of what the compiler does with the builtin: to it both buffers of a kernel are one array, so that the first read of a
-// stage waits for the next stage's requests, which have only just been made (T 2048, k 4: 1066 us, as it is 1031).  So nobody but
-// the source waits for these: gb_arrived, before anything reads what they bring; and the source leaves the five wait states that scalars
-// restored by the vector unit need before a request reads them.
-__device__ __forceinline__ void gb_copy(const char* base, unsigned off, char* to) {
-    typedef int i32x4 __attribute__((ext_vector_type(4)));
-    const u64 at = (u64)(uintptr_t)base;
-    const i32x4 from = {(int)(unsigned)at, (int)(unsigned)(at >> 32) & 0xFFFF, -1, 0x00020000};
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"((unsigned)(uintptr_t)(lds_void*)to), "v"(off), "s"(from) : "memory", "m0");
-}
+// 16 bytes per lane to the LDS, lane after lane from `to` on, by the memory unit itself
+__device__ __forceinline__ void gb_copy(rsrc_t from, unsigned off, char* to) { __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, 0, 0, 0); }
 // this wavefront's requests have arrived, and its own reads and writes of LDS are done
 __device__ __forceinline__ void gb_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory"); }
 // ... the workgroup's
@@ -183,7 +174,7 @@ __device__ __forceinline__ void gb_arrived() {
 // A tile of 32 rows, `stride` bytes apart, rows beyond `most` replaced by it: its i-th KiB (64 bytes of 16 rows)
 template <typename WT, int D> __device__ __forceinline__ void gb_request(const char* m, unsigned stride, int most, char* tile, int i, int lane) {
     const int row = 16 * (i & 1) + lane / 4, piece = GbTile<WT, D>::swap(row, lane & 3);
-    gb_copy(m, (unsigned)min(row, most) * stride + (i >> 1) * 64 + piece * 16, tile + i * 1024);
+    gb_copy(make_rsrc(m), (unsigned)min(row, most) * stride + (i >> 1) * 64 + piece * 16, tile + i * 1024);
 }
 // ... this wavefront's share of WAVES
 template <typename WT, int D, int WAVES>
@@ -297,11 +288,11 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         gb_stage<WT, D, 1>(krows + (size_t)from * D * ESZ, D * ESZ, r_last - from, b, 0, lane);
         gb_stage<WT, D, 1>(vrows + (size_t)from * vstride, vstride, r_last - from, b + Tile::BYTES, 0, lane);
     };
-    auto stage = [&](int t) __attribute__((always_inline)) {
+    auto stage = [&](int t, char* buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int first = min(64 * t + 32 * i, g_last);
-            char* b = smem + (t & 1) * BUF + i * 2 * Tile::BYTES;
+            char* b = buf + i * 2 * Tile::BYTES;
             gb_stage<WT, D, GB_WAVES>(krows + (size_t)first * K1 * D * ESZ, K1 * D * ESZ, g_last - first, b, wave, lane);
             gb_stage<WT, D, GB_WAVES>(vrows + (size_t)first * K1 * vstride, K1 * vstride, g_last - first, b + Tile::BYTES, wave, lane);
         }
@@ -444,23 +435,31 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         __syncthreads();
     }
     // real tokens: stages that all of the wavefront's queries see, some of them, none
-    stage(0);
+    stage(0, smem);
     gb_arrived();
     int t = 0;
-    auto tile = [&](int i) __attribute__((always_inline)) { return smem + (t & 1) * BUF + i * 2 * Tile::BYTES; };
-    for (const int end = active ? (wg0 + 1) / 64 : 0; t < end; ++t) {
+    // (restrict: a read of this stage need not wait for the next one's requests; to the compiler both are one array, and without it every
+    // stage's first read waits for requests that have only just been made: T 2048, k 4, both kernels, 1066 us in the place of 1031)
+    auto seen = [&](const char* __restrict mine, char* __restrict next) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2 / KW; ++i)
-            work(tile(i * KW + kw), std::false_type{}, 0, 0, [&]() __attribute__((always_inline)) { if (i == 0 && t + 1 < n_stages) stage(t + 1); });
+            work(mine + (i * KW + kw) * 2 * Tile::BYTES, std::false_type{}, 0, 0,
+                 [&]() __attribute__((always_inline)) { if (i == 0 && t + 1 < n_stages) stage(t + 1, next); });
+    };
+    for (const int end = active ? (wg0 + 1) / 64 : 0; t < end; ++t) {
+        seen(smem + (t & 1) * BUF, smem + (1 - (t & 1)) * BUF);
         gb_arrived();
     }
-    for (; t < n_stages; ++t) {
-        if (t + 1 < n_stages) stage(t + 1);
+    auto partly = [&](const char* __restrict mine, char* __restrict next) __attribute__((always_inline)) {
+        if (t + 1 < n_stages) stage(t + 1, next);
 #pragma unroll 1
         for (int i = kw; i < 2; i += KW) {
             const int first = 64 * t + 32 * i;
-            if (active && first <= wg1) work(tile(i), std::true_type{}, -first - 4 * half, qg - first - 4 * half, [] {});
+            if (active && first <= wg1) work(mine + i * 2 * Tile::BYTES, std::true_type{}, -first - 4 * half, qg - first - 4 * half, [] {});
         }
+    };
+    for (; t < n_stages; ++t) {
+        partly(smem + (t & 1) * BUF, smem + (1 - (t & 1)) * BUF);
         gb_arrived();
     }
     if constexpr (KW == 2) {
@@ -656,10 +655,9 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
     const int next_j0 = next_j;
     float stat = 0.f;
     bool stat_in = false;
-    auto stage = [&](int i) __attribute__((always_inline)) {   // set i, to buffer i % 2
+    auto stage = [&](int i, char* b) __attribute__((always_inline)) {   // set i, to a buffer
         const int h = hk * P.group + next_g, first = first_row + 64 * next_j, left = P.rows - 1 - first;
         const size_t at = ((size_t)seq * P.nq + h) * P.rows + first;
-        char* b = smem + (i & 1) * C::BUF;
         constexpr int N = Tile::BYTES / 1024;
         static_assert(2 * N % C::WAVES == 0, "");
 #pragma unroll
@@ -680,7 +678,7 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
         next_g += wrap;
     };
     auto stage_stats = [&](int i) __attribute__((always_inline)) { reinterpret_cast<float*>(smem + (i & 1) * C::BUF + C::OFF_S)[64 * (wave & 1) + lane] = stat_in ? stat : -INFINITY; };
-    if (i0 < i1) stage(i0);
+    if (i0 < i1) stage(i0, smem + (i0 & 1) * C::BUF);
     gb_own_rows<WT, D>(P.k_rot + (((size_t)seq * P.nkv + hk) * P.rows + (size_t)key * K1) * D * ESZ, half, keys.kf);
     if constexpr (C::V_LDS) {
         const int first = min(w0, P.T - 1);                  // (either row wavefront brings in half of the rows)
@@ -695,15 +693,18 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
     if constexpr (!C::V_LDS)
         for (uint4& x : keys.vf) asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w));
     gb_arrived();
-    auto step = [&](int i, int first, auto masked) __attribute__((always_inline)) {
-        const char* buf = smem + (i & 1) * C::BUF;
+    // (restrict: as in gb_dq_kernel)
+    auto products = [&](int i, int first, auto masked, const char* __restrict buf, char* __restrict next) __attribute__((always_inline)) {
         const float* stats = reinterpret_cast<const float*>(buf + C::OFF_S) + 32 * rw;
         if constexpr (masked) {
-            stage(i + 1);
+            stage(i + 1, next);
             if (w0 < P.T && first + 31 >= w0 * K1) keys.template step<true>(L, buf + rw * C::SET, stats, 64, half, key * K1 - first - 4 * half, 31, [] {});
         } else {
-            keys.template step<false>(L, buf + rw * C::SET, stats, 64, half, 0, 31, [&]() __attribute__((always_inline)) { stage(i + 1); });
+            keys.template step<false>(L, buf + rw * C::SET, stats, 64, half, 0, 31, [&]() __attribute__((always_inline)) { stage(i + 1, next); });
         }
+    };
+    auto step = [&](int i, int first, auto masked) __attribute__((always_inline)) {
+        products(i, first, masked, smem + (i & 1) * C::BUF, smem + (1 - (i & 1)) * C::BUF);
         stage_stats(i + 1);
         gb_arrived();
     };
