@@ -80,7 +80,8 @@ PS_API int ps_group_attention_lse(const ps_group_attn_args* args, float* lse, vo
  *   workspace  DEVICE, at least ps_group_attention_grad_workspace_bytes(args) bytes, 256-byte aligned, owned by the caller
  * All sums are held in float32 and added in an order that depends on the sizes alone: the same call gives the
  * same bits.  What a row holds that the mask hides from another (Inf and NaN among it) does not enter the other's d_q,
- * and d_out, q and out of rows that do not see a key do not enter the key's d_k and d_v.  The inputs must not overlap the
+ * and d_out, q and out of rows that do not see a key do not enter the key's d_k and d_v; where the mask lets Inf and NaN through, they
+ * enter as the formulas have it (a probability times Inf is Inf, also one so small that it is taken for zero).  The inputs must not overlap the
  * outputs.  (q, k, v, out, lse, d_out and the gradients need to be aligned to 4 bytes only.)  Sizes and
  * errors are those of ps_group_attention; also PS_ERR_UNSUPPORTED for rows / 128 * n_heads >= 2^24 and for 2^23 or more
  * tiles of 64 real or up to 128 [MASK] keys over all sequences and kv heads.

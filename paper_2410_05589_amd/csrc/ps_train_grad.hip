@@ -116,7 +116,7 @@ template <typename WT, int D> struct GbTile {
         const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + cd[1] + j * 2048 + m * 1024));
         return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     }
-    // ... values that are not finite count as zero
+    // ... values that are not finite count as zero (gb_add_odd makes up for it)
     static __device__ __forceinline__ bf16x8 finite(bf16x8 x) {
         u32x4 v = __builtin_bit_cast(u32x4, x);
 #pragma unroll
@@ -216,6 +216,21 @@ template <typename WT, int D> __device__ __forceinline__ void gb_own_rows(const 
     for (int st = 0; st < GbTile<WT, D>::STEPS; ++st) x[st] = ld16_q(row + st * 32 + half * 16);
 }
 constexpr float GB_LN2 = 0.6931471805599453f;
+// In tiles that the mask cuts, what is not finite counts as zero in the products (a hidden row's 0 times Inf would be NaN).  For the queries or
+// keys that do see such a row this makes up for it at the end, from memory: y[j][i], column 32 j + 8 (i / 4) + 4 half + i % 4 of the lane's sum,
+// gets the row's values that are not finite.  PROBABILITY: as they are, which is what a probability makes of them; else NaN (the
+// other factor, a dS, is NaN or Inf itself, or 0 where a key's score is -Inf).  A row may be added more than once.
+template <typename WT, int D, bool PROBABILITY> __device__ __forceinline__ void gb_add_odd(const char* row, int half, f32x16 (&y)[D / 32]) {
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const f32x4 v = load4_q<WT>(row + (32 * j + 8 * u + 4 * half) * Traits<WT>::ESZ);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!(fabsf(v[e]) < INFINITY)) y[j][4 * u + e] += PROBABILITY ? v[e] : NAN;
+        }
+}
 // columns col .. col + 3 and col + D / 2 .. of a row of a gradient, times scale; with turn, rotated back
 template <typename WT, int D> __device__ __forceinline__ void gb_write4(char* row, const float2* turn, int col, float scale, f32x4 a, f32x4 b) {
     constexpr int ESZ = Traits<WT>::ESZ;
@@ -367,12 +382,19 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         for (int i = 0; i < 16; ++i) y[j][i] = 0.f;
 
     // one key tile; masked: keys lo .. hi of it (counted from 4 half) are seen
+    bool odd = false;                                        // a key in such a tile was not finite: nor were its scores
     auto work = [&](const char* kt, auto masked, int lo, int hi, auto beside) __attribute__((always_inline)) {
         const char* vt = kt + Tile::BYTES;
         float lse = lse0, delta = delta0;
         asm volatile("" : "+v"(lse), "+v"(delta));          // (32 copies of them would be kept in registers across the loop)
         f32x16 s, dp;
         auto probabilities = [&]() __attribute__((always_inline)) {   // dS in the place of s
+            if constexpr (masked) {
+                float m = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) m = abs_max3(m, s[i], s[i + 1]);
+                odd |= __any(!(m < INFINITY)) != 0;
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int key = 8 * (i / 4) + i % 4;
@@ -461,6 +483,12 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
     for (; t < n_stages; ++t) {
         partly(smem + (t & 1) * BUF, smem + (1 - (t & 1)) * BUF);
         gb_arrived();
+    }
+    if (odd) {                                               // the lane's own [MASK] keys, the tokens behind the stages that are seen whole
+#pragma unroll 1
+        for (int r = qg * K1 + 1; r <= qrow; ++r) gb_add_odd<WT, D, false>(krows + (size_t)r * D * ESZ, half, y);
+#pragma unroll 1
+        for (int n = (wg0 + 1) / 64 * 64; n <= qg; ++n) gb_add_odd<WT, D, false>(krows + (size_t)n * K1 * D * ESZ, half, y);
     }
     if constexpr (KW == 2) {
         f32x4* area = reinterpret_cast<f32x4*>(smem) + rw * NJ * 4 * 64 + lane;
@@ -578,6 +606,20 @@ template <typename WT, int D, bool V_LDS> struct GbKeys {
         }
     }
 };
+// A query or a gradient that is not finite makes every dS of its row so, and with it the d_k of every key that it sees (of one of the wavefront's)
+template <int N> __device__ __forceinline__ bool gb_odd_rows(const f32x16 (&dk)[N]) { return __any(!(fabsf(dk[0][0]) < INFINITY)) != 0; }
+// ... what rows first .. last of the layout, which the lane's key sees, have left out: query heads of the kv head in turn
+template <typename WT, int D>
+__device__ __forceinline__ void gb_add_odd_rows(const GbParams& P, int seq, int hk, int first, int last, int half, f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32]) {
+    constexpr int ESZ = Traits<WT>::ESZ;
+#pragma unroll 1
+    for (int h = hk * P.group; h < (hk + 1) * P.group; ++h)
+#pragma unroll 1
+        for (int r = first; r <= last; ++r) {
+            gb_add_odd<WT, D, true>(P.d_out + (((size_t)seq * P.rows + r) * P.nq + h) * D * ESZ, half, dv);
+            gb_add_odd<WT, D, false>(P.q_rot + (((size_t)seq * P.nq + h) * P.rows + r) * D * ESZ, half, dk);
+        }
+}
 template <typename WT, int D>
 __device__ __forceinline__ void gb_write_keys(const GbParams& P, int seq, int hk, int row, int pos, int half, const f32x16 (&dk)[D / 32], const f32x16 (&dv)[D / 32]) {
     const size_t at = (((size_t)seq * P.rows + row) * P.nkv + hk) * D * Traits<WT>::ESZ;
@@ -641,6 +683,7 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
             keys.template step<true>(L, buf, stats, 32, half, slot > 0 ? krow - first - 4 * half : 99, g * K1 + P.k - first - 4 * half, [] {});
             gb_wait();
         }
+        if (gb_odd_rows(keys.dk)) gb_add_odd_rows<WT, D>(P, seq, hk, krow, slot > 0 ? g * K1 + P.k : -1, half, keys.dk, keys.dv);
         if (first + c <= last && slot > 0) gb_write_keys<WT, D>(P, seq, hk, krow, krow - g * P.k, half, keys.dk, keys.dv);
         return;
     }
@@ -715,6 +758,7 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
         for (const int end = min(i1, head0 + see_all); i < end; ++i) step(i, first_row + 64 * (i - head0) + 32 * rw, std::true_type{});
         for (const int end = min(i1, head0 + per_head); i < end; ++i) step(i, first_row + 64 * (i - head0) + 32 * rw, std::false_type{});
     }
+    if (gb_odd_rows(keys.dk)) gb_add_odd_rows<WT, D>(P, seq, hk, key * K1, min((w0 + 31) * K1 + 30, P.rows - 1), half, keys.dk, keys.dv);   // (the last row of a masked tile)
     // ---- the row wavefronts' sums, one gradient after the other by way of the LDS
     auto meet = [&](f32x16 (&y)[NJ]) __attribute__((always_inline)) {
         f32x4* area = reinterpret_cast<f32x4*>(smem) + kw * NJ * 4 * 64 + lane;
