@@ -292,6 +292,11 @@ typedef __attribute__((address_space(3))) void lds_void;
 __device__ __forceinline__ void vw_copy(rsrc_t from, unsigned off, unsigned soff, char* to) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)to, 16, off, soff, 0, 0);
 }
+// the workgroup's requests have arrived, and its reads and writes of LDS are done
+__device__ __forceinline__ void vw_arrived() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+}
 // 256 rows of 64 bytes, as vl_at places them
 struct VwRows {
     rsrc_t src;
@@ -361,7 +366,7 @@ __device__ __forceinline__ void vw_pipeline(int first, int steps, char* b0, char
     if (k <= last) step(k, b0, b1, x[0], x[1]);
     if (k + 1 <= last) step(k + 1, b1, b2, x[1], x[0]);
     if (k + 2 <= last) step(k + 2, b2, b3, x[0], x[1]);
-    __syncthreads();                                        // (nothing is on its way into the buffers any more)
+    vw_arrived();                                           // (nothing is on its way into the buffers any more)
 }
 
 // A tile's workgroup number -> the tile: workgroups go to the XCDs in turn; an XCD gets a stretch of the order, in which
@@ -530,7 +535,7 @@ __global__ void __launch_bounds__(VW_THREADS, 2) vl_grad_wide_kernel(const VlPar
             const char* from = P.w + (size_t)(unsigned)__float_as_int(info[rr].w) * rb + min((unsigned)ct * 2 + piece * 16, rb - 16);
             __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)from, (lds_void*)(mine + ((32 * wave + 2 * i) & 63) * 512), 16, 0, 0);
         }
-        __syncthreads();
+        vw_arrived();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             char* const at = buffer(128 * wm + 32 * i) + 32 * (i & 1) * 512 + (64 * wn + c) * 2;
