@@ -63,6 +63,21 @@ struct ps_group_attn_args;
 PS_API int ps_train_debug_launch(const struct ps_group_attn_args* args, unsigned* out);
 
 /*
+ * Host only.  How ps_group_attention_grad would cut a call (pointers are not looked at; its errors otherwise): out[3] = {wavefronts that
+ * share 32 query rows (1 or 2), keys of a workgroup, parts of their rows}.
+ */
+struct ps_group_attn_grad_args;
+PS_API int ps_train_debug_grad_plan(const struct ps_group_attn_grad_args* args, int* out);
+
+/*
+ * Host only.  How ps_vocab_loss would cut a call, with d_hidden NULL or not (the other pointers are not looked at; its errors otherwise):
+ * out[6] = {side of a tile (64, 128, 256), rows of a chunk, tokens of a piece, parts of a piece's tokens in the second product for a whole chunk and
+ * for the last one (tiles of 256 and one part: the gradients leave that product at once), workgroups of a chunk's largest launch of scores}.
+ */
+struct ps_vocab_loss_args;
+PS_API int ps_train_debug_loss_plan(const struct ps_vocab_loss_args* args, int* out);
+
+/*
  * The following steps of ctx give up a wait for data of another workgroup after `spins` polls
  * (<= 0: the default, about a second).  With 1 every wait whose data is not there at the first
  * look is given up at once: the kernel still ends normally, the step's outputs are marked

@@ -22,6 +22,7 @@
 #include <math.h>
 
 #include "ps_train_device.h"
+#include "ps_draft_debug.h"
 
 namespace {
 
@@ -849,4 +850,18 @@ extern "C" int ps_vocab_loss(const ps_vocab_loss_args* a, void* stream) {
     P.tl = (float*)(ws + L.tl); P.state = (int*)(ws + L.state); P.factor = (float2*)(ws + L.factor); P.sums = (float*)(ws + L.sums);
     P.acc = (float*)(ws + L.acc); P.alone = (float*)(ws + L.alone); P.x = a->d_hidden ? ws + L.x : nullptr;
     return a->dtype == PS_BF16 ? run<bf16_t>(P, L, (hipStream_t)stream) : run<float>(P, L, (hipStream_t)stream);
+}
+
+// see ps_draft_debug.h
+extern "C" int ps_train_debug_loss_plan(const ps_vocab_loss_args* a, int* out) {
+    const int st = check(a);
+    if (st != PS_OK) return st;
+    if (!out) return PS_ERR_NULL;
+    const VlPlan L = plan(a);
+    const int rest = a->rows % L.rows_c;
+    out[0] = L.tile; out[1] = L.rows_c; out[2] = L.piece;
+    out[3] = splits_of(L, a->hidden, L.rows_c);
+    out[4] = rest ? splits_of(L, a->hidden, rest) : out[3];
+    out[5] = (std::min(L.piece, a->vocab) + L.tile - 1) / L.tile * ((L.rows_c + L.tile - 1) / L.tile);
+    return PS_OK;
 }

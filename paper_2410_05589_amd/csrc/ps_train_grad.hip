@@ -17,6 +17,7 @@
 // -delta are the accumulators' initial values.  The other side's rows are staged in LDS once per workgroup and read both ways: as rows
 // (scores) and as columns (gradients; bf16: transposed by the LDS unit).
 #include "ps_train_device.h"
+#include "ps_draft_debug.h"
 
 namespace {
 
@@ -933,4 +934,14 @@ extern "C" int ps_group_attention_grad(const ps_group_attn_grad_args* a, void* s
     float* partial = (float*)(ws + L.partial);
     if (a->dtype == PS_BF16) return a->head_dim == 128 ? launch<bf16_t, 128>(P, G, partial, s) : launch<bf16_t, 64>(P, G, partial, s);
     return a->head_dim == 128 ? launch<float, 128>(P, G, partial, s) : launch<float, 64>(P, G, partial, s);
+}
+
+// see ps_draft_debug.h
+extern "C" int ps_train_debug_grad_plan(const ps_group_attn_grad_args* a, int* out) {
+    const int st = check(a);
+    if (st != PS_OK) return st;
+    if (!out) return PS_ERR_NULL;
+    const GbPlan L = plan(a);
+    out[0] = L.kw; out[1] = L.keys; out[2] = L.splits;
+    return PS_OK;
 }

@@ -8,7 +8,7 @@ PS_PLAN_FIELDS = 18
 PLAN_FIELD_NAMES = ("T", "Kt", "K", "rows", "kw_log", "s_log", "Gs", "per_round", "rounds", "piece_groups",
                     "npieces", "lds_bytes", "panel_off", "units", "rs", "g2_log", "ahead", "by_piece")
 EXPORTED_SYMBOLS = ("ps_draft_debug_plan", "ps_draft_debug_attn_plan", "ps_draft_debug_step_plan", "ps_draft_debug_merge_groups", "ps_draft_debug_spin_limit", "ps_draft_debug_timeline",
-                    "ps_train_debug_launch", "ps_verify_debug_exchange", "ps_measure_stream_read", "ps_measure_copy")
+                    "ps_train_debug_launch", "ps_train_debug_grad_plan", "ps_train_debug_loss_plan", "ps_verify_debug_exchange", "ps_measure_stream_read", "ps_measure_copy")
 
 _ready = False
 
@@ -33,6 +33,9 @@ def _lib():
         lib.ps_draft_debug_timeline.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
         lib.ps_train_debug_launch.restype = ctypes.c_int
         lib.ps_train_debug_launch.argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_uint)]
+        for name in ("ps_train_debug_grad_plan", "ps_train_debug_loss_plan"):
+            getattr(lib, name).restype = ctypes.c_int
+            getattr(lib, name).argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_int)]
         lib.ps_verify_debug_exchange.restype = None
         lib.ps_verify_debug_exchange.argtypes = [ctypes.c_int, ctypes.c_int]
         lib.ps_measure_stream_read.restype = ctypes.c_int
@@ -77,6 +80,20 @@ def ps_train_debug_launch(args):
     out = (ctypes.c_uint * 8)()
     st = _lib().ps_train_debug_launch(ctypes.byref(args), out)
     return st, {"kernel": out[0], "grid": tuple(out[1:4]), "threads": out[4], "rope_grid": tuple(out[5:7]), "rope_threads": out[7]}
+
+
+def ps_train_debug_grad_plan(args):
+    """Returns (status, {"kw", "keys", "parts"})."""
+    out = (ctypes.c_int * 3)()
+    st = _lib().ps_train_debug_grad_plan(ctypes.byref(args), out)
+    return st, dict(zip(("kw", "keys", "parts"), out))
+
+
+def ps_train_debug_loss_plan(args):
+    """Returns (status, {"tile", "rows", "piece", "parts", "last_parts", "workgroups"})."""
+    out = (ctypes.c_int * 6)()
+    st = _lib().ps_train_debug_loss_plan(ctypes.byref(args), out)
+    return st, dict(zip(("tile", "rows", "piece", "parts", "last_parts", "workgroups"), out))
 
 
 def ps_draft_debug_spin_limit(ctx, spins):
