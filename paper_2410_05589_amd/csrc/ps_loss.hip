@@ -735,6 +735,7 @@ int check(const ps_vocab_loss_args* a) {
 
 // How a call is cut: chunks of rows, pieces of the vocabulary, parts of a piece's tokens in the second product
 constexpr long long VL_PIECE_BYTES = 288ll << 20;            // of exponentials at a time
+constexpr long long VL_PIECE_TILES = 1ll << 22;              // a launch of scores has at most
 struct VlPlan {
     int tile, slots;      // 256 (the wide kernels), 128 or 64; workgroups of such tiles that run at a time
     int rows_c, piece, nsum;
@@ -774,7 +775,9 @@ VlPlan plan(const ps_vocab_loss_args* a) {
     // rows at a time: as many as give the second product one tile for every workgroup that can run
     L.rows_c = std::min(a->rows, std::max(1, L.slots / ((a->hidden + L.tile - 1) / L.tile)) * L.tile);
     const int vocab = (a->vocab + L.tile - 1) / L.tile * L.tile;
-    const int pieces = grad ? (int)(((long long)L.rows_c * vocab * esz + VL_PIECE_BYTES - 1) / VL_PIECE_BYTES) : 1;
+    // (losses only: nothing is kept of a piece but sums; its tiles are one launch, whose threads are counted in 32 bits)
+    const long long tiles = (long long)(vocab / L.tile) * ((L.rows_c + L.tile - 1) / L.tile);
+    const int pieces = (int)(grad ? ((long long)L.rows_c * vocab * esz + VL_PIECE_BYTES - 1) / VL_PIECE_BYTES : (tiles + VL_PIECE_TILES - 1) / VL_PIECE_TILES);
     L.piece = ((vocab + pieces - 1) / pieces + L.tile - 1) / L.tile * L.tile;
     L.nsum = vocab / (L.tile / 2);
     size_t acc = 0;                                          // of all chunks (whole ones, the last)

@@ -149,3 +149,35 @@ def test_rows_of_every_kind_side_by_side(case, plan):
 def test_a_captured_call_of_large_tiles_replayed():
     assert _loss_plan(4100, 4096, 2064)[2:] == (1, 4)
     VL.test_a_captured_call_replayed(4100, 4096, 2064)
+
+
+@pytest.mark.parametrize("rows,hidden,vocab,plan", [(5000, 1024, 20001, (64, 4096, 10048, 1, 4))])
+def test_loss_of_float32_in_pieces(rows, hidden, vocab, plan):
+    """Products that go on from what the pieces before have left, in two chunks of rows, the second one's in parts."""
+    a = TR.make_loss_args(rows, hidden, vocab, "f32")
+    a.d_hidden = 0x100000
+    st, got = DBG.ps_train_debug_loss_plan(a)
+    assert st == B.PS_OK and (got["tile"], got["rows"], got["piece"], got["parts"], got["last_parts"]) == plan, got
+    print("case loss f32", rows, hidden, vocab, plan, flush=True)
+    x = VL._make(rows, hidden, vocab, "f32", 31)
+    loss, d = VL._call(*x, "f32")
+    VL._check(*x, "f32", loss, d)
+
+
+def test_losses_of_the_largest_vocabulary():
+    """More tiles than one launch takes: losses only, 2^16 rows against 2^23 tokens, in two pieces.  Some rows are checked."""
+    import torch
+    rows, hidden, vocab = 1 << 16, 32, 1 << 23
+    a = TR.make_loss_args(rows, hidden, vocab, "bf16")
+    st, plan = DBG.ps_train_debug_loss_plan(a)
+    assert st == B.PS_OK and (plan["tile"], plan["rows"], plan["piece"]) == (256, rows, vocab // 2)
+    print("case largest vocabulary", flush=True)
+    g = torch.Generator(device="cuda:0").manual_seed(41)
+    w = (torch.randn((vocab, hidden), generator=g, device="cuda:0") * 0.05).to(torch.bfloat16)
+    h = torch.randn((rows, hidden), generator=g, device="cuda:0").to(torch.bfloat16)
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda:0").to(torch.int32)
+    t[0], t[1], t[rows - 1] = vocab - 1, vocab // 2, 0
+    loss, _ = VL._call(h, w, t, None, "bf16", grad=False)
+    assert bool(torch.isfinite(loss).all())
+    some = torch.tensor([0, 1, 255, 256, 4097, 65279, rows - 1], device="cuda:0")
+    VL._check(h[some], w, t[some], None, "bf16", loss[some], None, grad=False)

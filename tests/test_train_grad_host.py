@@ -129,3 +129,17 @@ def test_attention_gradient_launches_fit_the_grid(lib):
     for kw in (dict(n_heads=160, **most), dict(seqs=65535, n_heads=128, n_kv_heads=128, **few), dict(seqs=65535, n_heads=65535, n_kv_heads=65535, **few)):
         assert TR.ps_group_attention_grad_workspace_bytes(_attn(**kw)) == 0
         assert TR.ps_group_attention_grad(_attn(**kw), None) == B.PS_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("grad", [None, 0x100000])
+def test_loss_launches_fit_the_grid(lib, grad):
+    """The threads of a launch are counted in 32 bits, 512 for a tile of 256 x 256: the sizes that are taken stay within."""
+    from paper_2410_05589_amd import debug as DBG
+    for rows in (1, 97, 65536, 1 << 22):
+        for hidden in (32, 256, 288, 4096, 1 << 16):
+            for vocab in (1, 32000, 128256, (1 << 23) - 300, 1 << 23):
+                st, plan = DBG.ps_train_debug_loss_plan(_loss(rows=rows, hidden=hidden, vocab=vocab, d_hidden=grad))
+                assert st == B.PS_OK
+                if plan["tile"] == 256:
+                    assert plan["workgroups"] * 512 < 1 << 32, (rows, hidden, vocab, plan)
+    assert DBG.ps_train_debug_loss_plan(_loss(vocab=(1 << 23) + 1))[0] == B.PS_ERR_UNSUPPORTED
