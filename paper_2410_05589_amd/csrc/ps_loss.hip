@@ -640,6 +640,8 @@ __device__ __forceinline__ float vl_row_alone(const VlParams& P, int row, int ta
 struct VlRow { int state; float2 f; };
 template <typename WT> __device__ __forceinline__ float2 vl_finish(const VlParams& P, int row, float z, float scale, bool write) {
     // z: log2 of sum_{v != t} exp(l_v - l_t); the loss is log(1 + 2^z), the others' probability 2^z / (1 + 2^z)
+    // (a target's logit of Inf or NaN leaves no sum to compare it with: NaN; of -Inf, an infinite loss)
+    if (!(fabsf(P.tl[row]) < INFINITY) && z != INFINITY) z = NAN;
     const float weight = P.weights ? P.weights[row] : 1.f, e = __builtin_amdgcn_exp2f(-fabsf(z));
     const float loss = z > 0.f ? z * VL_LN2 + log1pf(e) : log1pf(e), others = z > 0.f ? 1.f / (1.f + e) : e / (1.f + e);
     if (write) P.loss[row] = weight * (z == z ? loss : z);

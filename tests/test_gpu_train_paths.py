@@ -181,3 +181,25 @@ def test_losses_of_the_largest_vocabulary():
     assert bool(torch.isfinite(loss).all())
     some = torch.tensor([0, 1, 255, 256, 4097, 65279, rows - 1], device="cuda:0")
     VL._check(h[some], w, t[some], None, "bf16", loss[some], None, grad=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,hidden,vocab", [(70, 64, 1), (70, 64, 2), (300, 64, 900), (4200, 4096, 2064)])
+def test_targets_whose_logit_is_not_finite(dtype, rows, hidden, vocab):
+    """log(sum exp) - l_t where l_t is Inf or NaN: NaN, unless every other logit is finite or Inf and l_t -Inf (Inf); never a loss of zero."""
+    import torch
+    h, w, t, _ = VL._make(rows, hidden, vocab, dtype, 51)
+    w[:, 7] = w[:, 7].float().clamp(max=-1e-3).to(w.dtype)   # (the row's others: -Inf, so that nothing but the target's logit shows it)
+    t[:] = vocab - 1
+    w[vocab - 1, 7] = 0.03
+    print("case target not finite", dtype, rows, hidden, vocab, flush=True)
+    want, want_d = VL._call(h, w, t, None, dtype)
+    h[rows // 2, 7], h[rows - 1, 7] = float("inf"), float("nan")
+    for grad in (True, False):
+        loss, d = VL._call(h, w, t, None, dtype, grad=grad)
+        hit = torch.zeros(rows, dtype=torch.bool, device="cuda:0")
+        hit[[rows // 2, rows - 1]] = True
+        assert bool(torch.isnan(loss[hit]).all()), loss[hit]
+        assert torch.equal(loss[~hit], want[~hit])
+        if grad:
+            assert bool(torch.isnan(d[hit]).all()) and torch.equal(d[~hit], want_d[~hit])
