@@ -203,3 +203,27 @@ def test_targets_whose_logit_is_not_finite(dtype, rows, hidden, vocab):
         assert torch.equal(loss[~hit], want[~hit])
         if grad:
             assert bool(torch.isnan(d[hit]).all()) and torch.equal(d[~hit], want_d[~hit])
+
+
+FORWARD = [  # dtype, seqs, T, k, heads, kv heads, head_dim; kernel, as ps_train_debug_launch numbers it
+    (("bf16", 1, 1, 4, 2, 1, 128), 1), (("bf16", 1, 5, 4, 2, 1, 128), 1), (("bf16", 1, 3, 4, 4, 2, 64), 1), (("bf16", 2, 16, 8, 4, 2, 64), 1), (("bf16", 2, 16, 8, 4, 2, 128), 1),
+    (("bf16", 1, 70, 0, 2, 1, 128), 2), (("f32", 1, 1000, 3, 8, 8, 64), 3), (("f32", 1, 700, 3, 8, 4, 64), 4), (("f32", 1, 400, 4, 8, 4, 128), 0),
+]
+
+
+@pytest.mark.parametrize("length", [1.0, 30.0])
+@pytest.mark.parametrize("case,kernel", FORWARD)
+def test_log_sums_of_every_forward_kernel(case, kernel, length):
+    """Also of queries 30 times as long (log sums up to hundreds): float32 leaves 2^-18 (1 + reach), a rotated bf16 key e_s (see the gradients' tests)."""
+    import torch
+    dtype, seqs, T, k, nq, nkv, d = case
+    st, launch = DBG.ps_train_debug_launch(TR.make_args(seqs, T, k, nq, nkv, d, dtype, 10000.0))
+    assert st == B.PS_OK and launch["kernel"] == kernel
+    print("case log sums", case, length, flush=True)
+    x = AG.make(seqs, T, k, nq, nkv, d, dtype, 61, length)
+    out, lse = AG.forward(x, T, k)
+    plain, _ = AG.forward(x, T, k, lse=False)
+    assert torch.equal(out, plain)
+    _, _, out64, lse64, reach = AG.reference(x, T, k)
+    flip = 2.0 ** -7 * 25.0 * length / d ** 0.5 if dtype == "bf16" else 0.0
+    assert float((lse - lse64).abs().max()) <= 2.0 ** -18 * (1 + reach) + flip
