@@ -11,13 +11,15 @@
 // out again one by one, against their maximum.
 //
 // The vocabulary is gone through in pieces; two products for each, the floor being their 4 V H operations a row:
-//   vl_score_kernel   W h^T, one tile per workgroup: exponentials to the workspace (storage type), sums of rows beside them
+//   vl_score_kernel   W h^T, one tile per workgroup: exponentials to the workspace, sums of rows (of the unrounded) beside them.  In bf16 they are
+//                     rounded once, half a step 2^-8 each: they are operands of the next product's MFMAs, and a gradient adds up many, so that its
+//                     error stays that of its own rounding (relative 2-norm 0.0017 with them and with float32 exponentials)
 //   vl_grad_kernel    exponentials . W, added to what the pieces before left, in float32
 // The rows' sums make their losses and the gradients' factors: in vl_join_kernel, which adds up the parts of the products, or, where the last
 // product's tiles become gradients at once, in vl_rows_kernel before it.
 //
-// Bound by the matrix cores: 10240 rows, H 4096, V 32000 take 4300 us, 1.25 PFLOP/s of a large library product's 1.32 (4070 us); 9216 rows, V 128256
-// 15690 (14700); 1218 rows, H 5120, V 32000 785 (605); the cores are busy 74 % of the scores' time and 84 % of the gradients'.  Small calls
+// Bound by the matrix cores: 10240 rows, H 4096, V 32000 take 4240 .. 4440 us, 1.21 .. 1.27 PFLOP/s of a large library product's 1.32 (4070 us); 9216 rows,
+// V 128256 15650 .. 15990 (14700); 1218 rows, H 5120, V 32000 800 (605); the cores are busy 74 % of the scores' time and 84 % of the gradients'.  Small calls
 // are a chain of four launches: 200 rows, H 256, V 1024 in float32 25 us.
 #include <math.h>
 
@@ -740,7 +742,7 @@ struct VlPlan {
 };
 // Where a chunk's tiles of the second product leave workgroups idle, several share a tile's tokens: the fewest that leave the
 // least time, counted in rounds of all workgroups over the share of the tokens.  A part costs about as much as more tokens would: its sums
-// are written, read and added.  (Counting 1000, 2000 or 5000 in the place of 3000: within 2 %.  500 rows, V 32000: 1 part 318 us, 8 274.)
+// are written, read and added.  (Counting 1000, 2000 or 5000 in the place of 3000: within 2 %.  500 rows, V 32000: 713 us in one part, 445 in 2, 317 in 4, 263 in 8.)
 int splits_of(const VlPlan& L, int hidden, int rows) {
     const int tiles = (rows + L.tile - 1) / L.tile * ((hidden + L.tile - 1) / L.tile), part = L.tile == VW_TILE ? 3000 : 64;
     const int fewest = L.tile == VW_TILE ? 512 : 128;
@@ -760,10 +762,11 @@ VlPlan plan(const ps_vocab_loss_args* a) {
     const bool grad = a->d_hidden != nullptr;
     VlPlan L;
     // Tiles.  The wide kernels where they have a tile for about half of the compute units: us, wide / 128 at H 4096, V 32000: 130 rows (125
-    // tiles) 196 / 212, 300 rows 247 / 313; V 128256, 130 rows 527 / 903; H 512, V 2064: 5000 rows (180 tiles) 78 / 84, 1500 (54) 57 / 51.
-    // But a tile of few rows: 65 rows 173 / 157 (V 128256, 501 tiles: 501 / 545, 30 rows 481 / 506).
-    // 64 / 128: 30 rows 130 / 140 (V 128256 549 / 522), 130 rows 266 / 211; H 512, V 2064: 500 rows 32 / 43.  float32, which is
-    // bound by its matrix rate and by few workgroups: 64 always (H 256, V 1024: 30 rows 29 / 56, 5000 88 / 116; H 512, V 2064, 2000 rows 112 / 153).
+    // tiles) 184 / 217, 300 rows 239 / 307; V 128256, 130 rows 512 / 889; H 512, V 2064: 5000 rows (180 tiles) 67 / 71, 1500 (54) 50 / 44.
+    // But a tile of few rows: 65 rows 166 / 148 (V 128256, 501 tiles: 489 / 546, 30 rows 483 / 498).
+    // 64 / 128: 30 rows 124 / 136 (V 128256 550 / 498), 130 rows 277 / 217; H 512, V 2064: 500 rows 28 / 38.  float32, which is
+    // bound by its matrix rate and by few workgroups: 64 always (64 / 128 with kernels as they first were, the latter no longer built: H 256, V 1024: 30
+    // rows 29 / 56, 5000 88 / 116; H 512, V 2064, 2000 rows 112 / 153; the first and the last now 25 and 105).
     const bool bf = a->dtype == PS_BF16;
     const long long tiles128 = (long long)((a->vocab + 127) / 128) * ((a->rows + 127) / 128), tiles256 = (long long)((a->vocab + 255) / 256) * ((a->rows + 255) / 256);
     if (bf && tiles256 >= 120 && (a->rows > 96 || tiles256 >= 400)) L.tile = VW_TILE, L.slots = 256;

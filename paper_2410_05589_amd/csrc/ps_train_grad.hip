@@ -7,9 +7,9 @@
 // Nobody adds to what another writes: no atomics, the same bits every time.  That is 7 products where one pass would do with 5, and 10 in bf16,
 // where the rotated queries stand as two parts (scores twice, dK~), as in the forward pass whose lse they have to match.
 //
-// Bound by the matrix cores, by waits beside them and, for the [MASK] keys, by memory: T 2048, k 4, 32 heads x 128 takes 1035 us (5 products at
-// the rate of a large library product: 327; the 10: 654), of which keys 630 .. 690 ([MASK] keys 110), queries 390 .. 420, rotated keys 30; 4 x T 1024,
-// k 8, 32 / 8 heads 2320; T 203, k 5, 40 heads 102; float32 2 x T 300, k 3, 8 heads x 64 84.
+// Bound by the matrix cores, by waits beside them and, for the [MASK] keys, by memory: T 2048, k 4, 32 heads x 128 takes 1036 .. 1053 us (5 products
+// at the rate of a large library product: 327; the 10: 654), of which keys 640 .. 710 ([MASK] keys 110), queries 395 .. 430, rotated keys 30; 4 x T 1024,
+// k 8, 32 / 8 heads 2320; T 203, k 5, 40 heads 104 (112 with other calls in between); float32 2 x T 300, k 3, 8 heads x 64 84.
 //
 // All products are 32 x 32 MFMA tiles, as in ga_attn_wide_kernel: what the wavefront owns (queries, or keys) lies along the lanes,
 // so a score tile leaves the matrix core in the operand layout of the products that follow it (a lane holds 16 of the 32 rows of the other
@@ -152,7 +152,10 @@ __device__ __forceinline__ void gb_products(const GbTile<WT, D>& L, const char* 
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) y[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(L.template element<CLEAN>(tile, j, i), p[i], y[j], 0, 0, 0);
 }
-// bf16: p as operand of the two MFMAs over its 32 rows (rounded)
+// bf16: p (P, or dS) as operand of the two MFMAs over its 32 rows, rounded to bf16 once.  The forward pass holds P in two parts; here a second part
+// would be 3 products more in the keys' kernel (dV, dK with either part of dS) and one in the queries', 14 in the place of 10, for an error of 0.0017 of the
+// gradients' 2-norm, which the results' own rounding leaves, in the place of 0.0024: the rounding of P and dS weighs as much as that of the
+// results.  The queries' low parts are another matter: they belong to the scores, whose lse the forward pass made with them.
 template <typename WT> struct GbOperand {
     bf16x8 b[2];
     __device__ __forceinline__ GbOperand(const f32x16& p) {
@@ -847,19 +850,19 @@ GbPlan plan(const ps_group_attn_grad_args* a) {
     GbPlan L;
     const bool bf = a->dtype == PS_BF16, d128 = a->head_dim == 128;
     // Two wavefronts for 32 query rows where four rows' workgroups would leave compute units without one.  Whole calls, us, one / two:
-    // T 64, k 4, 8 heads x 64 (24 workgroups) 31 / 29, T 1000, k 2 (192) 69 / 62, float32 2 x T 300, k 3 (160) 90 / 83; but 8 x T 128, k 3, 8 heads x 128
-    // (256) 76 / 79, T 203, k 5, 40 heads (400) 122 / 131
+    // T 64, k 4, 8 heads x 64 (24 workgroups) 30 / 29, T 1000, k 2 (192) 63 / 56, float32 2 x T 300, k 3 (160) 89 / 85; but 8 x T 128, k 3, 8 heads x 128
+    // (256) 64 / 68, T 203, k 5, 40 heads (400) 101 / 109
     const long long row_blocks = ((long long)a->tokens * (a->k + 1) + GB_ROWS - 1) / GB_ROWS * a->n_heads * a->seqs;
     L.kw = row_blocks < 256 ? 2 : 1;
     // 128 keys per workgroup at head_dim 128 in bf16; 64 where two wavefronts per SIMD do not fit (float32), or, at head_dim 64, where there are few
-    // (64 / 128: T 1000, k 2, 8 heads 57 / 61, float32 2 x T 300 83 / 92)
+    // (64 / 128: T 1000, k 2, 8 heads 56 / 59, float32 2 x T 300 84 / 94)
     L.heads = a->n_kv_heads * a->seqs;
     L.keys = d128 ? (bf ? 128 : 64) : (long long)((a->tokens + 127) / 128) * L.heads >= 256 ? 128 : 64;
     L.tiles = (a->tokens + L.keys - 1) / L.keys;
     // Parts of a key tile's rows, for a workgroup on every compute unit (two where the LDS takes two) as long as a part has a few stages of 64
     // rows, for twice as many where parts stay long: a causal call's key tiles are unlike each other.  Whole calls, us, parts 1 / 2 / 3 / 4 / 8:
-    // T 2048, k 4, 32 heads (512 tiles) 1134 / 1191 / 1229 / 1248 / 1371; 4 x T 1024, k 8, 32 / 8 heads (256) 2880 / 2538 / 2533 / 2559 / 2658; T 203, k 5,
-    // 40 heads (80) 142 / 117 / 113 / 120 / 132; T 512, k 4, 32 / 8 heads (32) 559 / 330 / 269 / 217 / 172
+    // T 2048, k 4, 32 heads (512 tiles) 1042 / 1067 / 1123 / 1140 / 1283; 4 x T 1024, k 8, 32 / 8 heads (256) 2470 / 2311 / 2333 / 2351 / 2436; T 203, k 5,
+    // 40 heads (80) 123 / 104 / 103 / 108 / 120; T 512, k 4, 32 / 8 heads (32) 455 / 270 / 223 / 181 / 156
     const long long units = (long long)L.tiles * L.heads, places = d128 || L.keys == 128 ? 256 : 512;
     const long long stages = ((long long)a->tokens * (a->k + 1) + 63) / 64 * (a->n_heads / a->n_kv_heads);
     L.splits = (int)std::max(1LL, std::max(std::min(places / units, stages / (bf && d128 ? 4 : 2)), std::min(2 * places / units, stages / 64)));

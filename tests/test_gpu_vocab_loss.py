@@ -91,10 +91,11 @@ CASES = [  # dtype, rows, hidden, vocab
     ("f32", 1, 16, 1), ("bf16", 1, 32, 1), ("bf16", 1, 32, 2), ("f32", 3, 48, 129),
     ("f32", 130, 256, 1024), ("bf16", 5, 512, 2064), ("bf16", 127, 96, 127), ("bf16", 129, 160, 1000), ("bf16", 257, 288, 4099),
     ("f32", 300, 80, 513), ("bf16", 1218, 1056, 3001), ("bf16", 64, 4096, 32000), ("bf16", 700, 512, 20000), ("f32", 33, 512, 2064),
-    # tiles of 256 x 256: one row and one token more than a tile, half a stage at the end, one stage and less, several chunks of rows, pieces
+    # one row and one token more and less than a tile, half a stage at the end, one stage, several chunks of rows (tiles of 64); the last: tiles
+    # of 256, two pieces, many parts (those whose gradients leave the product at once: tests/test_gpu_train_paths.py)
     ("bf16", 513, 64, 257), ("bf16", 511, 32, 255), ("bf16", 300, 2080, 770), ("bf16", 1030, 4096, 1000), ("bf16", 4200, 4096, 600),
     ("bf16", 2500, 8192, 700), ("bf16", 1400, 256, 128256),
-    # tiles of 128: a row more than 64, an odd number of tokens; tiles of 256 with few rows and many tokens
+    # tiles of 128: a row more than 64, an odd number of tokens (the third: tiles of 256 with few rows and many tokens; the last: of 64, float32)
     ("bf16", 65, 96, 26001), ("bf16", 90, 128, 40001), ("bf16", 3, 64, 102400), ("bf16", 200, 160, 30100), ("f32", 65, 64, 20001)]
 
 
