@@ -7,7 +7,7 @@
 // Nobody adds to what another writes: no atomics, the same bits every time.  That is 7 products where one pass would do with 5, and 10 in bf16,
 // where the rotated queries stand as two parts (scores twice, dK~), as in the forward pass whose lse they have to match.
 //
-// Bound by the matrix cores, by waits beside them and, for the [MASK] keys, by memory: T 2048, k 4, 32 heads x 128 takes 1036 .. 1053 us (5 products
+// Bound by the matrix cores, by waits beside them and, for the [MASK] keys, by memory: T 2048, k 4, 32 heads x 128 takes 1036 .. 1063 us (5 products
 // at the rate of a large library product: 327; the 10: 654), of which keys 640 .. 710 ([MASK] keys 110), queries 395 .. 430, rotated keys 30; 4 x T 1024,
 // k 8, 32 / 8 heads 2320; T 203, k 5, 40 heads 104 (112 with other calls in between); float32 2 x T 300, k 3, 8 heads x 64 84.
 //
@@ -234,6 +234,15 @@ template <typename WT, int D, bool PROBABILITY> __device__ __forceinline__ void 
             for (int e = 0; e < 4; ++e)
                 if (!(fabsf(v[e]) < INFINITY)) y[j][4 * u + e] += PROBABILITY ? v[e] : NAN;
         }
+}
+// whether there is nothing left to add: a call whose values are all NaN would walk all rows for it (T 2048, k 4 3.3 ms in the place of 1.1)
+template <int N> __device__ __forceinline__ bool gb_all_nan(const f32x16 (&y)[N]) {
+    bool all = true;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) all &= y[j][i] != y[j][i];
+    return all;
 }
 // columns col .. col + 3 and col + D / 2 .. of a row of a gradient, times scale; with turn, rotated back
 template <typename WT, int D> __device__ __forceinline__ void gb_write4(char* row, const float2* turn, int col, float scale, f32x4 a, f32x4 b) {
@@ -488,11 +497,11 @@ __global__ void __launch_bounds__(GB_THREADS, D * Traits<WT>::ESZ > 256 ? 1 : 2)
         partly(smem + (t & 1) * BUF, smem + (1 - (t & 1)) * BUF);
         gb_arrived();
     }
-    if (odd) {                                               // the lane's own [MASK] keys, the tokens behind the stages that are seen whole
+    if (__builtin_expect(odd, 0)) {                          // the lane's own [MASK] keys, the tokens behind the stages that are seen whole
 #pragma unroll 1
-        for (int r = qg * K1 + 1; r <= qrow; ++r) gb_add_odd<WT, D, false>(krows + (size_t)r * D * ESZ, half, y);
+        for (int r = qg * K1 + 1; r <= qrow && !gb_all_nan(y); ++r) gb_add_odd<WT, D, false>(krows + (size_t)r * D * ESZ, half, y);
 #pragma unroll 1
-        for (int n = (wg0 + 1) / 64 * 64; n <= qg; ++n) gb_add_odd<WT, D, false>(krows + (size_t)n * K1 * D * ESZ, half, y);
+        for (int n = (wg0 + 1) / 64 * 64; n <= qg && !gb_all_nan(y); ++n) gb_add_odd<WT, D, false>(krows + (size_t)n * K1 * D * ESZ, half, y);
     }
     if constexpr (KW == 2) {
         f32x4* area = reinterpret_cast<f32x4*>(smem) + rw * NJ * 4 * 64 + lane;
@@ -619,7 +628,7 @@ __device__ __forceinline__ void gb_add_odd_rows(const GbParams& P, int seq, int 
 #pragma unroll 1
     for (int h = hk * P.group; h < (hk + 1) * P.group; ++h)
 #pragma unroll 1
-        for (int r = first; r <= last; ++r) {
+        for (int r = first; r <= last && !gb_all_nan(dv); ++r) {   // (a d_v of NaN alone: P or d_out was, and so is d_k)
             gb_add_odd<WT, D, true>(P.d_out + (((size_t)seq * P.rows + r) * P.nq + h) * D * ESZ, half, dv);
             gb_add_odd<WT, D, false>(P.q_rot + (((size_t)seq * P.nq + h) * P.rows + r) * D * ESZ, half, dk);
         }
@@ -687,7 +696,7 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
             keys.template step<true>(L, buf, stats, 32, half, slot > 0 ? krow - first - 4 * half : 99, g * K1 + P.k - first - 4 * half, [] {});
             gb_wait();
         }
-        if (gb_odd_rows(keys.dk)) gb_add_odd_rows<WT, D>(P, seq, hk, krow, slot > 0 ? g * K1 + P.k : -1, half, keys.dk, keys.dv);
+        if (__builtin_expect(gb_odd_rows(keys.dk), 0)) gb_add_odd_rows<WT, D>(P, seq, hk, krow, slot > 0 ? g * K1 + P.k : -1, half, keys.dk, keys.dv);
         if (first + c <= last && slot > 0) gb_write_keys<WT, D>(P, seq, hk, krow, krow - g * P.k, half, keys.dk, keys.dv);
         return;
     }
@@ -762,7 +771,7 @@ __global__ void __launch_bounds__((GbDkv<WT, D, KW>::WAVES * 64), (GbDkv<WT, D, 
         for (const int end = min(i1, head0 + see_all); i < end; ++i) step(i, first_row + 64 * (i - head0) + 32 * rw, std::true_type{});
         for (const int end = min(i1, head0 + per_head); i < end; ++i) step(i, first_row + 64 * (i - head0) + 32 * rw, std::false_type{});
     }
-    if (gb_odd_rows(keys.dk)) gb_add_odd_rows<WT, D>(P, seq, hk, key * K1, min((w0 + 31) * K1 + 30, P.rows - 1), half, keys.dk, keys.dv);   // (the last row of a masked tile)
+    if (__builtin_expect(gb_odd_rows(keys.dk), 0)) gb_add_odd_rows<WT, D>(P, seq, hk, key * K1, min((w0 + 31) * K1 + 30, P.rows - 1), half, keys.dk, keys.dv);   // (the last row of a masked tile)
     // ---- the row wavefronts' sums, one gradient after the other by way of the LDS
     auto meet = [&](f32x16 (&y)[NJ]) __attribute__((always_inline)) {
         f32x4* area = reinterpret_cast<f32x4*>(smem) + kw * NJ * 4 * 64 + lane;
