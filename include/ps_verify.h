@@ -1,7 +1,9 @@
 /*
  * ps_verify.h - C ABI of the steps that follow the parallel draft step in Algorithm 1:
- * building the draft token tree from the drafter's top-k output, and the acceptance walk
- * over that tree against the target model's distributions.  Same library as ps_draft.h
+ * building the draft token tree from the drafter's top-k output, what the target model needs
+ * around its pass over that tree (its KV cache in 8 bits, the attention of the tree's rows over
+ * it, its distributions from its logits), and the acceptance walk over the tree against those
+ * distributions.  Same library as ps_draft.h
  * (libps_draft.so), same conventions: extern "C", plain pointers and sizes, int status
  * (ps_status of ps_draft.h: 0 = OK, negative = error), nothing is enqueued on an error,
  * no allocation, no host synchronisation, asynchronous on the given hipStream_t.
@@ -115,6 +117,171 @@ PS_API size_t ps_verify_workspace_bytes(int32_t batch, int32_t vocab);
  * The first call on a device asks the runtime for the array's address: make it outside graph capture.
  */
 PS_API int ps_verify_walk_static(const ps_tree_shape* tree, const ps_verify_args* args, void* stream);
+
+/*
+ * The target's KV cache in 8 bits.  The unit is a block: 32 consecutive positions of one kv head, whose keys share one scale and
+ * whose values share another, a power of two each; an element is an e4m3 number (4 exponent and 3 fraction bits, largest 448, no
+ * infinities, 0x7F and 0xFF are NaN) and stands for code * scale.  The scale is the least 2^e, e >= -100, with which the block's
+ * largest finite magnitude is at most 448; Inf and NaN are stored as NaN and do not count for the scale.
+ *   k_codes, v_codes  DEVICE [blocks][n_kv_heads][32 * head_dim], 16-byte aligned.  A block is laid out as the attention's matrix
+ *                     instructions take it: dim j of position t (0..31) is byte
+ *                       keys    ((j/32 * 2 + j/16 % 2) * 32 + t) * 16 + j % 16
+ *                       values  ((j/32 * 2 + t/4 % 2) * 32 + j % 32) * 16 + t/8 * 4 + t % 4
+ *   k_scale, v_scale  DEVICE [blocks][n_kv_heads] float32
+ *   kv_offsets        HOST [batch+1], in positions as in ps_draft_step_args, multiples of 32: sequence b owns the blocks
+ *                     kv_offsets[b] / 32 .. kv_offsets[b+1] / 32 - 1
+ * Nothing has to be initialised: a block is valid from the first position of it that is written.  Supported: head_dim 64 or 128,
+ * batch 1..PS_CACHE_MAX_BATCH, kv_offsets below 2^36.
+ */
+#define PS_CACHE_BLOCK 32
+#define PS_CACHE_MAX_BATCH 64
+typedef struct ps_cache {
+    int32_t n_kv_heads, head_dim;
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    float* k_scale;
+    float* v_scale;
+    const int64_t* kv_offsets;
+} ps_cache;
+
+/*
+ * Writes rows of keys (after the rotary embedding) and values behind the kv_len[b] positions that sequence b has.
+ *   k_rows, v_rows  DEVICE [batch][rows][n_kv_heads][head_dim], dtype
+ *   row_stride      elements between consecutive rows, >= n_kv_heads * head_dim (0 stands for that): rows of a fused projection
+ *                   are taken where they are; sequence b starts rows * row_stride elements after sequence b - 1
+ *   kv_len          HOST [batch]: valid positions before the call;  kv_len_dev  DEVICE [batch] or NULL: the lengths themselves,
+ *                   kv_len then holds upper bounds (a length outside 0..kv_len[b] counts as the nearer of the two)
+ *   n_seq           HOST [batch] or NULL: only the first n_seq[b] rows (0..rows) of sequence b are written
+ *   n_accepted, path  DEVICE [batch] and [batch][path_rows] int32, both or neither, not with n_seq: what ps_verify_walk left.  The
+ *                   rows are then a tree's, and node 0 and the accepted nodes path[b][0 .. n_accepted[b]-1] are written, in that
+ *                   order.  A path ends before an entry outside [0, rows); nothing is written where n_accepted[b] < 0.
+ *                   1 <= path_rows < PS_TREE_MAX_NODES (more nodes than that are on no path); n_accepted[b] counts as at most path_rows
+ *   len_out         DEVICE [batch] int32 or NULL, written: the new lengths.  May be kv_len_dev itself
+ * In a block that has positions already the scale only grows; when it does, the codes that are there are rounded again to the new
+ * scale.  Positions of the last block written that are behind the new length become zero codes; blocks behind it stay as they are.
+ * Calls that write the same sequence must not overlap in time, and no other call may read what one writes.
+ * Errors: PS_ERR_NULL; PS_ERR_SHAPE; PS_ERR_OFFSETS (kv_offsets negative, decreasing or no multiples of 32); PS_ERR_KV_CAPACITY
+ * (kv_len[b] and the most rows that can follow exceed the sequence's blocks); PS_ERR_UNSUPPORTED (head_dim, batch, alignment: rows
+ * and row_stride to 4 bytes); PS_ERR_DEVICE.
+ */
+typedef struct ps_cache_write_args {
+    int32_t batch, rows, dtype;
+    const ps_cache* cache;
+    const void* k_rows;
+    const void* v_rows;
+    int64_t row_stride;
+    const int32_t* kv_len;
+    const int32_t* kv_len_dev;
+    const int32_t* n_seq;
+    const int32_t* n_accepted;
+    const int32_t* path;
+    int32_t path_rows;
+    int32_t* len_out;
+} ps_cache_write_args;
+PS_API int ps_cache_write(const ps_cache_write_args* args, void* stream);
+
+/*
+ * Reads positions start[b] .. start[b] + n_seq[b] - 1 of every sequence back: code * scale in dtype (exact in both types;
+ * what rounds to 2^128 when it is written is Inf).
+ *   k_rows, v_rows  DEVICE [batch][rows][n_kv_heads][head_dim], dtype, written; one of them may be NULL; row_stride as above.
+ *                   Rows from n_seq[b] on and what lies between rows stay as they were
+ *   start           HOST [batch] or NULL: 0;  n_seq  HOST [batch] or NULL: rows
+ * Errors: as ps_cache_write.
+ */
+typedef struct ps_cache_read_args {
+    int32_t batch, rows, dtype;
+    const ps_cache* cache;
+    void* k_rows;
+    void* v_rows;
+    int64_t row_stride;
+    const int32_t* start;
+    const int32_t* n_seq;
+} ps_cache_read_args;
+PS_API int ps_cache_read(const ps_cache_read_args* args, void* stream);
+
+/*
+ * Tree attention over that cache (Section 3, token tree verification: each token attends to its ancestors only): row s of a
+ * sequence, node s of the tree, attends to the sequence's kv_len[b] cached positions, to itself and to its ancestors among the rows;
+ *   out = softmax(scale * q k^T) v per head, query head h uses kv head h / (n_heads / n_kv_heads).
+ * A single token is the tree of one node, a chain of rows the tree with parent[s] = s - 1 (tree->rank is not used).
+ *   q               DEVICE [batch][n_nodes][n_heads][head_dim], dtype, after the rotary embedding
+ *   k_rows, v_rows  DEVICE [batch][n_nodes][n_kv_heads][head_dim], dtype: the rows' own keys and values, used as they are (they reach
+ *                   the cache when the walk has accepted them).  Both NULL: the rows attend to the cached positions only
+ *   q_stride, kv_stride  elements between consecutive rows of q, and of k_rows and v_rows (0: no gap), as row_stride above
+ *   scale           0 stands for 1 / sqrt(head_dim)
+ *   out             DEVICE [batch][n_nodes][n_heads][head_dim], dtype, written
+ *   lse             DEVICE [batch][n_nodes][n_heads] float32 or NULL, written: log of the sum of exp(scale * q k)
+ *   kv_len, kv_len_dev  as for ps_cache_write
+ *   workspace       DEVICE, ps_tree_attention_workspace_bytes bytes, 256-byte aligned (NULL where that is 0); its contents do not
+ *                   matter before or after the call.  Calls that overlap in time need one each
+ * A row that sees nothing (no cached position, no own rows) has out = 0 and lse = -Inf.  A value row that is hidden from a row does
+ * not enter that row's result, whatever it holds; a key row that is not finite leaves the rows that see it undefined, no others.
+ * Scores, softmax and sums are float32.  bf16: probabilities are rounded to bf16 before they are multiplied with the values.
+ * Errors: PS_ERR_NULL; PS_ERR_SHAPE (also a malformed tree, a scale that is negative or not finite); PS_ERR_OFFSETS;
+ * PS_ERR_KV_CAPACITY (kv_len[b] exceeds the sequence's blocks); PS_ERR_WORKSPACE; PS_ERR_UNSUPPORTED (head_dim, batch, alignment
+ * to 4 bytes, n_heads > 1024, kv_len above 2^30); PS_ERR_DEVICE.
+ */
+typedef struct ps_tree_attn_args {
+    int32_t batch, n_heads, dtype;
+    float scale;
+    const ps_cache* cache;
+    const void* q;
+    const void* k_rows;
+    const void* v_rows;
+    int64_t q_stride, kv_stride;
+    void* out;
+    float* lse;
+    const int32_t* kv_len;
+    const int32_t* kv_len_dev;
+    void* workspace;
+    size_t workspace_bytes;
+} ps_tree_attn_args;
+PS_API int ps_tree_attention(const ps_tree_shape* tree, const ps_tree_attn_args* args, void* stream);
+
+/* Bytes of device scratch that call needs (0: none, or bad arguments).  Host only; reads no device pointer. */
+PS_API size_t ps_tree_attention_workspace_bytes(const ps_tree_shape* tree, const ps_tree_attn_args* args);
+
+/*
+ * The target's distributions, as ps_verify_walk takes them (p), from its logits, and draws from them.  Per row, with the settings of
+ * its sequence:  x_i = logits_i / temperature, e_i = exp(x_i - max x); kept are the top_k largest logits (of equal ones those with
+ * the lowest ids), of these, in the same order, the shortest prefix whose sum of e is at least top_p times the sum over all of them,
+ * and of these the ones with e_i >= min_p; at least the first one is kept.  probs_i = e_i / (sum of the kept e), 0 for the others.
+ *   logits       DEVICE [batch][rows][vocab], dtype
+ *   temperature  DEVICE [batch] float32 or NULL: 1.  Not above 0 (or NaN): greedy, all mass on the first of the largest logits
+ *   top_k        DEVICE [batch] int32 or NULL: all.  Below 1: all
+ *   top_p        DEVICE [batch] float32 or NULL: 1.  1 and above, or NaN: all
+ *   min_p        DEVICE [batch] float32 or NULL: 0.  Above 1 counts as 1; NaN as 0
+ *   r            DEVICE [batch][rows] float32 uniform numbers in [0, 1); needed with ids
+ *   probs        DEVICE [batch][rows][vocab] float32 or NULL, written
+ *   ids          DEVICE [batch][rows] int32 or NULL, written: drawn by inversion, the number of ids whose cumulative sum of kept
+ *                e (in id order) is <= r * sum, at most the last kept id
+ *   id_probs     DEVICE [batch][rows] float32 or NULL (needs ids), written: the drawn id's probability
+ *   workspace    DEVICE, ps_target_probs_workspace_bytes bytes, 256-byte aligned (NULL where that is 0); its contents do not matter
+ *                before or after the call.  Calls that overlap in time need one each
+ * Which tokens are kept and which one is drawn is decided with exponentials and sums that carry more than 40 bits.  A logit of -Inf
+ * has no mass; a row without any mass (all -Inf) has probs 0 and id -1, a row with a NaN or +Inf has probs NaN and id -1, id_probs
+ * likewise.  Supported: vocab <= 2^20, batch * rows <= 2^20.
+ * Errors: PS_ERR_NULL (args, logits, ids without r, neither probs nor ids); PS_ERR_SHAPE; PS_ERR_WORKSPACE; PS_ERR_UNSUPPORTED
+ * (sizes; alignment: logits to their type, everything else to 4 bytes); PS_ERR_DEVICE.
+ */
+typedef struct ps_target_probs_args {
+    int32_t batch, rows, vocab, dtype;
+    const void* logits;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    const float* r;
+    float* probs;
+    int32_t* ids;
+    float* id_probs;
+    void* workspace;
+    size_t workspace_bytes;
+} ps_target_probs_args;
+PS_API int ps_target_probs(const ps_target_probs_args* args, void* stream);
+
+/* Bytes of device scratch that call needs (0: none, or bad arguments).  Host only; reads no device pointer. */
+PS_API size_t ps_target_probs_workspace_bytes(const ps_target_probs_args* args);
 
 #ifdef __cplusplus
 }

@@ -10,10 +10,12 @@ LIB_PATH = os.path.join(PKG_DIR, "libps_draft.so")
 CSRC = os.path.join(PKG_DIR, "csrc")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 HEADERS = [os.path.join(CSRC, "ps_internal.h"), os.path.join(CSRC, "ps_device.h"), os.path.join(CSRC, "ps_train_device.h"),
+           os.path.join(CSRC, "ps_cache_device.h"),
            os.path.join(ROOT, "include", "ps_draft.h"), os.path.join(ROOT, "include", "ps_verify.h"),
            os.path.join(ROOT, "include", "ps_draft_debug.h"), os.path.join(ROOT, "include", "ps_train.h")]
 # sources that are compiled once each (ps_inst.hip: once per instance)
-UNITS = ("ps_host", "ps_verify", "ps_measure", "ps_train", "ps_train_grad", "ps_embed", "ps_loss")
+UNITS = ("ps_host", "ps_verify", "ps_measure", "ps_train", "ps_train_grad", "ps_embed", "ps_loss",
+         "ps_cache", "ps_tree_attn", "ps_probs")
 SOURCES = [os.path.join(CSRC, n + ".hip") for n in UNITS + ("ps_inst",)]
 # the device code is instantiated once per (storage type, head_dim)
 INSTANCES = [("f32_d64", 0, 64), ("f32_d128", 0, 128), ("bf16_d64", 1, 64), ("bf16_d128", 1, 128)]

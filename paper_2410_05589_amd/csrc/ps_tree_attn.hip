@@ -1,0 +1,530 @@
+// Attention of a draft tree's rows over the target's 8-bit cache and over the tree's own keys and values (see include/ps_verify.h).
+//
+//   S = scale q K^T,  P = exp(S - m),  out = P V / sum P,  K = k_scale code, V = v_scale code per block of 32 positions
+//
+// e4m3 codes are bf16 numbers, so both products run on v_mfma_f32_32x32x16_bf16 with exact keys and values; the scales, powers of two,
+// join the scores' constant and the exponent of P.  Queries stand along the lanes: S^T = K Q^T leaves a lane (query c, half h) the
+// scores of positions 8 a + 4 h + b, and out^T = V^T P^T takes them from there as its operand: the cache keeps values in just that order, so
+// codes go from memory to the matrix cores through a conversion (two codes an instruction), with no exchange between lanes and no LDS.
+// The running maximum is raised only when a score passes it by 2^8 (sums stay far inside float32), so sums are rarely rescaled.
+//
+// Work: a sequence's blocks are cut into splits of `per` blocks; a workgroup of four wavefronts takes a split of one kv head for 32 ... 256 rows
+// (a row is a node and one of the heads that share the kv head).  Its wavefronts divide rows (WR) and blocks (4 / WR); those that share
+// rows meet in LDS, splits in the workspace and a second kernel.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ps_cache_device.h"
+
+namespace {
+
+constexpr int TA_WAVES = 4, TA_TILE = 32;
+constexpr float TA_LAZY = 8.f;      // how far (in powers of two) scores may pass the maximum that they are taken against
+
+struct TaParams {
+    const char *q, *k, *v;
+    char* out;
+    float *lse, *part;
+    const uint8_t *k_codes, *v_codes;
+    const float *k_scale, *v_scale;
+    long long q_row, kv_row;        // bytes between rows
+    int n_heads, heads, grp, nodes, rows, tiles;   // rows = nodes * grp; tiles of 32 of them
+    int batch, per;                 // blocks per split
+    float c;                        // scale * log2(e)
+    const int* len_dev;
+    unsigned first[PC_SEQS];
+    int len[PC_SEQS];
+    int split0[PC_SEQS + 1];        // the sequence's first split
+    u64 sees[PS_TREE_MAX_NODES];    // bit t: node t is the node itself or an ancestor
+};
+
+template <int D> struct Tile { uint4 k[D / 32], v[D / 32]; };
+
+// 8 codes as bf16
+__device__ __forceinline__ bf16x8 widen8(unsigned lo, unsigned hi) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+    const b2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ unsigned word(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// 8 floats as NP bf16 parts (three: all 24 bits)
+template <int NP> __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&out)[NP]) {
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = pack_bf16x2(rest[2 * i], rest[2 * i + 1]);
+            rest[2 * i] -= __uint_as_float(w[i] << 16);
+            rest[2 * i + 1] -= __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+        out[p] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+}
+// 8 consecutive elements of a row
+template <typename WT, int NP> __device__ __forceinline__ void load_parts(const char* p, bool valid, bf16x8 (&out)[NP]) {
+    if constexpr (Traits<WT>::BF) {
+        out[0] = __builtin_bit_cast(bf16x8, valid ? ld16_q(p) : make_uint4(0, 0, 0, 0));
+    } else {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const f32x4 v = valid ? load4_q<WT>(p + 16 * i) : f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * i + e] = v[e];
+        }
+        split8(x, out);
+    }
+}
+template <typename WT> __device__ __forceinline__ float load1(const char* p) {
+    if constexpr (Traits<WT>::BF) return bf16_to_f32(*reinterpret_cast<const uint16_t*>(p));
+    else return *reinterpret_cast<const float*>(p);
+}
+
+// the other half's value (lane ^ 32)
+__device__ __forceinline__ float other_half(float v) {
+    const unsigned u = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
+}
+
+// What a wavefront has of one tile of 32 rows: lane (row c, half h) has of every 32 dims the dims 8 a + 4 h + b as o[.][4 a + b]
+template <int D> struct RowState {
+    f32x16 o[D / 32];
+    float m, l;                     // maximum (in powers of two), this half's sum
+};
+
+// One tile of 32 keys: scores (raw products) to probabilities against the running maximum.  c: what makes products powers of two; lv: log2 of
+// the values' scale, which the probabilities that meet codes carry
+template <int D> __device__ __forceinline__ void softmax_tile(RowState<D>& R, f32x16& s, float c, float lv, float inv_vs) {
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    mx = fmaxf(mx, other_half(mx)) * c;
+    if (__ballot(mx > R.m + TA_LAZY)) {
+        const float m = fmaxf(R.m, mx), alpha = m > R.m ? __builtin_amdgcn_exp2f(R.m - m) : 1.f;
+        R.m = m;
+        R.l *= alpha;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) R.o[j] *= alpha;
+    }
+    const float off = (R.m == -__builtin_inff() ? 0.f : R.m) - lv;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -off));
+        sum += s[i];
+    }
+    R.l = __builtin_fmaf(sum, inv_vs, R.l);
+}
+template <int NP> __device__ __forceinline__ void prob_parts(const f32x16& s, bf16x8 (&p)[2][NP]) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[8 * st + e];
+        split8(x, p[st]);
+    }
+}
+
+// other's sums into mine
+template <int D> __device__ __forceinline__ void merge(RowState<D>& R, float m2, float l2, const f32x16 (&o2)[D / 32]) {
+    const float m = fmaxf(R.m, m2);
+    const float a = R.m == m ? 1.f : __builtin_amdgcn_exp2f(R.m - m), b = m2 == m ? 1.f : __builtin_amdgcn_exp2f(m2 - m);
+    R.m = m;
+    R.l = R.l * a + l2 * b;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) R.o[j] = R.o[j] * a + o2[j] * b;
+}
+
+// a finished tile: lane's row (node and head) of one sequence, dims 32 j ..
+template <typename WT, int D> __device__ __forceinline__ void store_row(const TaParams& P, int b, int h, int row, int j, const f32x16& o, float m, float l) {
+    if (row >= P.rows) return;
+    const int half = (threadIdx.x >> 5) & 1, node = row / P.grp, head = h * P.grp + row % P.grp;
+    const size_t at = ((size_t)b * P.nodes + node) * P.n_heads + head;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+        const f32x4 x = f32x4{o[4 * a], o[4 * a + 1], o[4 * a + 2], o[4 * a + 3]} * inv;
+        char* p = P.out + (at * D + 32 * j + 8 * a + 4 * half) * Traits<WT>::ESZ;
+        if constexpr (Traits<WT>::BF) *reinterpret_cast<u32x2_q*>(p) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+        else *reinterpret_cast<f32x4_q*>(p) = x;
+    }
+    if (P.lse && j == 0 && half == 0) P.lse[at] = l == 0.f ? -__builtin_inff() : 0.69314718055994530942f * (m + __log2f(l));
+}
+
+// floats of one tile's part in the workspace: sums, then maxima and row sums
+template <int D> constexpr int part_floats() { return TA_TILE * D + 2 * 64; }
+
+template <typename WT, int D, int RT, int WR>
+__global__ __launch_bounds__(64 * TA_WAVES, RT == 2 ? 1 : 2) void tree_attn_kernel(const TaParams P) {
+    constexpr int WK = TA_WAVES / WR, NP = Traits<WT>::BF ? 1 : 3, C = D / 32, TILE = PC_BLOCK * D, ESZ = Traits<WT>::ESZ;
+    __shared__ __attribute__((aligned(16))) float s_meet[WK > 1 ? (TA_WAVES / 2) * RT * part_floats<D>() : 4];
+    __shared__ float s_p[TA_WAVES][PC_BLOCK * TA_TILE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, lc = lane & 31;
+    const int wr = wave % WR, wk = wave / WR, h = blockIdx.y;
+    int b = 0;
+    while ((int)blockIdx.x >= P.split0[b + 1]) ++b;
+    const int split = blockIdx.x - P.split0[b], splits = P.split0[b + 1] - P.split0[b];
+    const int len = pc_length(P.len_dev, b, P.len[b]), blocks = (len + 31) >> 5, tail = len & 31;
+    const int tile0 = ((int)blockIdx.z * WR + wr) * RT;      // this wavefront's first tile of rows
+    const bool active = tile0 < P.tiles;
+
+    bf16x8 q[RT][2 * C][NP];
+    RowState<D> R[RT];
+    u64 sees[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = (tile0 + rt) * TA_TILE + lc;
+        const bool valid = row < P.rows;
+        const int node = valid ? row / P.grp : 0, head = h * P.grp + (valid ? row % P.grp : 0);
+        const char* from = P.q + ((long long)b * P.nodes + node) * P.q_row + (long long)head * D * ESZ;
+#pragma unroll
+        for (int i = 0; i < 2 * C; ++i) load_parts<WT, NP>(from + (32 * (i >> 1) + 16 * half + 8 * (i & 1)) * ESZ, valid, q[rt][i]);
+        sees[rt] = P.sees[node];
+        R[rt].m = -__builtin_inff();
+        R[rt].l = 0.f;
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) R[rt].o[j][i] = 0.f;
+    }
+
+    const int end = min(blocks, (split + 1) * P.per);
+    const size_t seq0 = (size_t)P.first[b] * P.heads + h;
+    auto fetch = [&](int i, Tile<D>& t) {
+        const size_t at = (seq0 + (size_t)i * P.heads) * TILE + lane * 16;
+#pragma unroll
+        for (int c = 0; c < C; ++c) t.k[c] = ld16(P.k_codes + at + c * 1024);
+#pragma unroll
+        for (int c = 0; c < C; ++c) t.v[c] = ld16(P.v_codes + at + c * 1024);
+    };
+    Tile<D> next;
+    int i = split * P.per + wk;
+    if (active && i < end) fetch(i, next);
+    if (active)
+        for (; i < end; i += WK) {
+            Tile<D> t = next;
+            if (i + WK < end) fetch(i + WK, next);
+            const size_t sat = seq0 + (size_t)i * P.heads;
+            const float ks = P.k_scale[sat], vs = P.v_scale[sat];
+            const bool cut = tail && i == blocks - 1;
+            f32x16 s[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[rt][e] = 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const bf16x8 kf = widen8(word(t.k[c], 2 * u), word(t.k[c], 2 * u + 1));
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int p = NP - 1; p >= 0; --p) s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[rt][2 * c + u][p], s[rt], 0, 0, 0);
+                }
+            if (cut) {                                       // positions behind the end: hidden, and their codes no numbers that count
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[rt][e] = 8 * (e >> 2) + 4 * half + (e & 3) < tail ? s[rt][e] : -__builtin_inff();
+                unsigned keep[4];
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const int n = min(max(tail - 8 * a - 4 * half, 0), 4);
+                    keep[a] = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
+                }
+#pragma unroll
+                for (int c = 0; c < C; ++c) t.v[c] = make_uint4(t.v[c].x & keep[0], t.v[c].y & keep[1], t.v[c].z & keep[2], t.v[c].w & keep[3]);
+            }
+            const float lv = (float)((int)(__float_as_uint(vs) >> 23) - 127), inv_vs = 1.f / vs, cs = P.c * ks;
+            bf16x8 p[RT][2][NP];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                softmax_tile<D>(R[rt], s[rt], cs, lv, inv_vs);
+                prob_parts<NP>(s[rt], p[rt]);
+            }
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const bf16x8 vf = widen8(word(t.v[j], 2 * st), word(t.v[j], 2 * st + 1));
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int n = NP - 1; n >= 0; --n) R[rt].o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[rt][st][n], R[rt].o[j], 0, 0, 0);
+                }
+        }
+
+    // the tree's own rows, in the sequence's last split: tiles of 32 nodes
+    if (active && P.k && split == splits - 1)
+        for (int kt = wk; kt * 32 < P.nodes; kt += WK) {
+            const char* own_k = P.k + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
+            const char* own_v = P.v + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
+            f32x16 s[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[rt][e] = 0.f;
+            const int key = kt * 32 + lc;
+#pragma unroll
+            for (int f = 0; f < 2 * C; ++f) {
+                bf16x8 kf[NP];
+                load_parts<WT, NP>(own_k + (long long)key * P.kv_row + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, key < P.nodes, kf);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int x = NP - 1; x >= 0; --x)        // (parts whose product is below 2^-24 of the whole are left out)
+#pragma unroll
+                        for (int y = NP - 1 - x; y >= 0; --y) s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], q[rt][f][y], s[rt], 0, 0, 0);
+            }
+            bf16x8 p[RT][2][NP];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const unsigned seen = (unsigned)(sees[rt] >> (32 * kt));
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[rt][e] = (seen >> (8 * (e >> 2) + 4 * half + (e & 3))) & 1 ? s[rt][e] : -__builtin_inff();
+                softmax_tile<D>(R[rt], s[rt], P.c, 0.f, 1.f);
+                prob_parts<NP>(s[rt], p[rt]);
+            }
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                bool odd = false;                            // Inf or NaN among them: zeros in the products, added below for the rows that see them
+                float x[2][8];
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int node = kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3);
+                        const float v = node < P.nodes ? load1<WT>(own_v + (long long)node * P.kv_row + (32 * j + lc) * ESZ) : 0.f;
+                        const bool fine = __builtin_fabsf(v) < __builtin_inff();
+                        odd |= !fine;
+                        x[st][e] = fine ? v : 0.f;
+                    }
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    bf16x8 vf[NP];
+                    split8(x[st], vf);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int a = NP - 1; a >= 0; --a)
+#pragma unroll
+                            for (int c = NP - 1 - a; c >= 0; --c) R[rt].o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[rt][st][c], R[rt].o[j], 0, 0, 0);
+                }
+                if (__ballot(odd)) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        float* sp = s_p[wave];               // probabilities by node
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[rt][e];
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+                        const unsigned seen = (unsigned)(sees[rt] >> (32 * kt));
+                        for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
+                            const float pt = sp[t * TA_TILE + lc];
+                            const bool see = (seen >> t) & 1;
+#pragma unroll
+                            for (int i2 = 0; i2 < 16; ++i2) {
+                                const float v = load1<WT>(own_v + (long long)(kt * 32 + t) * P.kv_row + (32 * j + 8 * (i2 >> 2) + 4 * half + (i2 & 3)) * ESZ);
+                                if (see && !(__builtin_fabsf(v) < __builtin_inff())) R[rt].o[j][i2] += pt * v;
+                            }
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+                    }
+                }
+            }
+        }
+
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) R[rt].l += other_half(R[rt].l);
+    // wavefronts that share rows: the upper half of them leaves its sums in LDS, the lower half adds them
+    if constexpr (WK > 1) {
+        for (int n = WK / 2; n >= 1; n >>= 1) {
+            if (n < WK / 2) __syncthreads();
+            if (wk >= n && wk < 2 * n) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    float* to = s_meet + (((wk - n) * WR + wr) * RT + rt) * part_floats<D>();
+#pragma unroll
+                    for (int j = 0; j < C; ++j)
+#pragma unroll
+                        for (int a = 0; a < 4; ++a)
+                            *reinterpret_cast<f32x4*>(to + ((j * 4 + a) * 64 + lane) * 4) = f32x4{R[rt].o[j][4 * a], R[rt].o[j][4 * a + 1], R[rt].o[j][4 * a + 2], R[rt].o[j][4 * a + 3]};
+                    to[TA_TILE * D + lane] = R[rt].m;
+                    to[TA_TILE * D + 64 + lane] = R[rt].l;
+                }
+            }
+            __syncthreads();
+            if (wk < n) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float* from = s_meet + ((wk * WR + wr) * RT + rt) * part_floats<D>();
+                    f32x16 o2[C];
+#pragma unroll
+                    for (int j = 0; j < C; ++j)
+#pragma unroll
+                        for (int a = 0; a < 4; ++a) {
+                            const f32x4 x = *reinterpret_cast<const f32x4*>(from + ((j * 4 + a) * 64 + lane) * 4);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o2[j][4 * a + e] = x[e];
+                        }
+                    merge<D>(R[rt], from[TA_TILE * D + lane], from[TA_TILE * D + 64 + lane], o2);
+                }
+            }
+        }
+        if (wk > 0) return;
+    }
+    if (!active) return;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int tile = tile0 + rt;
+        if (tile >= P.tiles) continue;
+        if (splits == 1) {
+#pragma unroll
+            for (int j = 0; j < C; ++j) store_row<WT, D>(P, b, h, tile * TA_TILE + lc, j, R[rt].o[j], R[rt].m, R[rt].l);
+        } else {
+            float* to = P.part + (((size_t)blockIdx.x * P.heads + h) * P.tiles + tile) * part_floats<D>();
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+                    *reinterpret_cast<f32x4*>(to + ((j * 4 + a) * 64 + lane) * 4) = f32x4{R[rt].o[j][4 * a], R[rt].o[j][4 * a + 1], R[rt].o[j][4 * a + 2], R[rt].o[j][4 * a + 3]};
+            to[TA_TILE * D + lane] = R[rt].m;
+            to[TA_TILE * D + 64 + lane] = R[rt].l;
+        }
+    }
+}
+
+// The splits of one tile, 32 dims of it per wavefront
+template <typename WT, int D>
+__global__ __launch_bounds__(D * 2) void tree_attn_join_kernel(const TaParams P) {
+    const int lane = threadIdx.x & 63, j = threadIdx.x >> 6, tile = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const int s0 = P.split0[b], s1 = P.split0[b + 1];
+    if (s1 - s0 == 1) return;
+    const size_t step = (size_t)P.heads * P.tiles * part_floats<D>();
+    const float* from = P.part + (((size_t)s0 * P.heads + h) * P.tiles + tile) * part_floats<D>();
+    float m = -__builtin_inff();
+    for (int s = s0; s < s1; ++s) m = fmaxf(m, from[(s - s0) * step + TA_TILE * D + lane]);
+    const float base = m == -__builtin_inff() ? 0.f : m;
+    float l = 0.f;
+    f32x16 o;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = 0.f;
+    for (int s = s0; s < s1; ++s, from += step) {
+        const float w = __builtin_amdgcn_exp2f(from[TA_TILE * D + lane] - base);
+        l += from[TA_TILE * D + 64 + lane] * w;
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(from + ((j * 4 + a) * 64 + lane) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[4 * a + e] += x[e] * w;
+        }
+    }
+    store_row<WT, D>(P, b, h, tile * TA_TILE + (lane & 31), j, o, m, l);
+}
+
+// ------------------------------------------------------------------------------------------ host
+struct TaPlan { int rt, wr, groups; size_t bytes; };
+
+int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaPlan& L) {
+    if (!a || !tree || !tree->parent || !a->kv_len) return PS_ERR_NULL;
+    const int st = pc_check(a->cache, a->batch);
+    if (st != PS_OK) return st;
+    const int N = tree->n_nodes, heads = a->cache->n_kv_heads, d = a->cache->head_dim;
+    if (N < 1 || N > PS_TREE_MAX_NODES || tree->parent[0] != -1) return PS_ERR_SHAPE;
+    P.sees[0] = 1;
+    for (int s = 1; s < N; ++s) {
+        const int pa = tree->parent[s];
+        if (pa < 0 || pa >= s) return PS_ERR_SHAPE;
+        P.sees[s] = P.sees[pa] | 1ull << s;
+    }
+    if (a->n_heads < 1 || a->n_heads % heads != 0) return PS_ERR_SHAPE;
+    if (a->dtype != PS_F32 && a->dtype != PS_BF16) return PS_ERR_SHAPE;
+    if (!(a->scale >= 0.f) || !(a->scale < __builtin_inff())) return PS_ERR_SHAPE;
+    if (a->n_heads > 1024) return PS_ERR_UNSUPPORTED;
+    P.batch = a->batch; P.n_heads = a->n_heads; P.heads = heads; P.grp = a->n_heads / heads; P.nodes = N; P.rows = N * P.grp;
+    P.tiles = (P.rows + TA_TILE - 1) / TA_TILE;
+    P.c = (float)((a->scale > 0.f ? (double)a->scale : 1.0 / __builtin_sqrt((double)d)) * 1.4426950408889634074);
+    long long total = 0;
+    for (int b = 0; b < a->batch; ++b) {
+        P.first[b] = (unsigned)(a->cache->kv_offsets[b] / PC_BLOCK);
+        P.len[b] = a->kv_len[b];
+        if (P.len[b] < 0) return PS_ERR_SHAPE;
+        if (P.len[b] > a->cache->kv_offsets[b + 1] - a->cache->kv_offsets[b]) return PS_ERR_KV_CAPACITY;
+        if (P.len[b] > 1 << 30) return PS_ERR_UNSUPPORTED;
+        total += (P.len[b] + PC_BLOCK - 1) / PC_BLOCK;
+    }
+    L.rt = a->dtype == PS_BF16 && P.tiles >= 2 ? 2 : 1;
+    const int waves = (P.tiles + L.rt - 1) / L.rt;
+    L.wr = waves >= 3 ? 4 : waves;
+    L.groups = (waves + L.wr - 1) / L.wr;
+    const long long units = (long long)heads * L.groups;
+    const int wk = TA_WAVES / L.wr;
+    P.per = (int)std::max<long long>(2 * wk, (total * units + 767) / 768);
+    P.split0[0] = 0;
+    bool one = true;
+    for (int b = 0; b < a->batch; ++b) {
+        const int blocks = (P.len[b] + PC_BLOCK - 1) / PC_BLOCK;
+        const int n = std::max(1, (blocks + P.per - 1) / P.per);
+        P.split0[b + 1] = P.split0[b] + n;
+        one &= n == 1;
+    }
+    L.bytes = one ? 0 : a256((size_t)P.split0[a->batch] * heads * P.tiles * (size_t)(d == 128 ? part_floats<128>() : part_floats<64>()) * sizeof(float));
+    return PS_OK;
+}
+
+template <typename WT, int D, int RT> void go(const TaParams& P, const TaPlan& L, hipStream_t s) {
+    const dim3 grid(P.split0[P.batch], P.heads, L.groups), block(64 * TA_WAVES);
+    if (L.wr == 4) hipLaunchKernelGGL((tree_attn_kernel<WT, D, RT, 4>), grid, block, 0, s, P);
+    else if (L.wr == 2) hipLaunchKernelGGL((tree_attn_kernel<WT, D, RT, 2>), grid, block, 0, s, P);
+    else hipLaunchKernelGGL((tree_attn_kernel<WT, D, RT, 1>), grid, block, 0, s, P);
+    if (L.bytes) hipLaunchKernelGGL((tree_attn_join_kernel<WT, D>), dim3(P.tiles, P.heads, P.batch), dim3(2 * D), 0, s, P);
+}
+
+}   // namespace
+
+extern "C" size_t ps_tree_attention_workspace_bytes(const ps_tree_shape* tree, const ps_tree_attn_args* a) {
+    TaParams P = {};
+    TaPlan L = {};
+    return plan(tree, a, P, L) == PS_OK ? L.bytes : 0;
+}
+
+extern "C" int ps_tree_attention(const ps_tree_shape* tree, const ps_tree_attn_args* a, void* stream) {
+    if (!a || !a->q || !a->out || !a->k_rows != !a->v_rows) return PS_ERR_NULL;
+    TaParams P = {};
+    TaPlan L = {};
+    const int st = plan(tree, a, P, L);
+    if (st != PS_OK) return st;
+    if (!aligned4(a->q) || !aligned4(a->k_rows) || !aligned4(a->v_rows) || !aligned4(a->out) || !aligned4(a->lse) || !aligned4(a->kv_len_dev))
+        return PS_ERR_UNSUPPORTED;
+    int64_t bytes = 0;
+    const int d = a->cache->head_dim;
+    int sst = pc_stride(a->q_stride, (int64_t)a->n_heads * d, a->dtype, &bytes);
+    P.q_row = bytes;
+    if (sst == PS_OK && a->k_rows) {
+        sst = pc_stride(a->kv_stride, (int64_t)P.heads * d, a->dtype, &bytes);
+        P.kv_row = bytes;
+    }
+    if (sst != PS_OK) return sst;
+    if (L.bytes && (!a->workspace || a->workspace_bytes < L.bytes || ((uintptr_t)a->workspace & 255))) return a->workspace ? PS_ERR_WORKSPACE : PS_ERR_NULL;
+    P.q = (const char*)a->q; P.k = (const char*)a->k_rows; P.v = (const char*)a->v_rows;
+    P.out = (char*)a->out; P.lse = a->lse; P.part = (float*)a->workspace;
+    P.k_codes = a->cache->k_codes; P.v_codes = a->cache->v_codes; P.k_scale = a->cache->k_scale; P.v_scale = a->cache->v_scale;
+    P.len_dev = a->kv_len_dev;
+    const hipStream_t s = (hipStream_t)stream;
+    if (a->dtype == PS_BF16) {
+        if (d == 128) { if (L.rt == 2) go<bf16_t, 128, 2>(P, L, s); else go<bf16_t, 128, 1>(P, L, s); }
+        else if (L.rt == 2) go<bf16_t, 64, 2>(P, L, s);
+        else go<bf16_t, 64, 1>(P, L, s);
+    } else if (d == 128) go<float, 128, 1>(P, L, s);
+    else go<float, 64, 1>(P, L, s);
+    return hipGetLastError() == hipSuccess ? PS_OK : PS_ERR_DEVICE;
+}
