@@ -4,13 +4,13 @@
 //
 // c_i = (logit, descending; id, ascending) as one whole number puts the tokens in the order in which top-k and top-p take them, so what
 // either keeps is everything up to one token, the bound, and min_p is a bound too.  Nothing is sorted:
-//   top-k, small k   the k-th largest of the threads' own maxima is a lower limit; the few tokens above it are listed in LDS
+//   top-k, small k   a histogram of the threads' own maxima gives a lower limit that k tokens reach; the few tokens above it are listed in LDS
 //   top-p, large k   a histogram of y in steps of 1/32 (sums of e, or counts) says which step the bound lies in; that step's tokens are listed
-//   the list         ordered by c eleven bits at a time, from the highest bit in which its tokens differ
+//   the list         up to 64 tokens by comparing all with all in a wavefront, more by eleven bits of c at a time, from the highest that differs
 // e is a whole number of 2^-F (F = 62 - log2 V, at most 51), from a double: sums are exact in any order, whoever adds them, and
-// their error is far below what decides a draw.
+// their error is far below what decides a draw.  (Doubles cost no more instructions here than floats, a histogram no more than its additions.)
 //
-// One workgroup of 1024 threads per row, two of them on a compute unit; the row is read again by each pass, from the caches.
+// One workgroup per row; the row is read again by each pass, from the caches.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -18,13 +18,13 @@
 
 namespace {
 
-constexpr int TP_THREADS = 1024, TP_WAVES = TP_THREADS / 64;
 constexpr int TP_BINS = 2048;                      // steps of 1/32 in y: 64 powers of two, what is below has no mass in F <= 51 bits
-constexpr int TP_LIST = 2 * TP_THREADS;            // tokens that are ordered in LDS
+constexpr int TP_LIST = 2048;                      // tokens that are ordered in LDS
 constexpr int TP_SMALL_K = 512;                    // top-k by the threads' maxima
 constexpr int TP_MAX_LOG = 20;                     // vocab <= 2^20: an id takes 20 bits of c
 constexpr int TP_MAX_CELLS = 4096;                 // wavefronts' shares of a row: 2^20 / (64 * 4)
-constexpr int TP_TABLE = 64;                       // 2^(j/64)
+constexpr int TP_TABLE_LOG = 8, TP_TABLE = 1 << TP_TABLE_LOG;   // 2^(j/256)
+constexpr int TP_K_PER_STEP_LOG = TP_TABLE_LOG - 5;
 
 struct TpParams {
     const char* logits;
@@ -66,27 +66,31 @@ template <typename LT> __device__ __forceinline__ u32x4 load_vec(const char* row
     return v;
 }
 
-// The place up to which tokens are kept
-struct Bound {
-    float l;
-    unsigned id;
-    __device__ __forceinline__ bool keeps(float x, unsigned i) const { return x > l || (x == l && i <= id); }
-};
-
-// the token's place: descending logit (0 and -0 are equal), ascending id
-__device__ __forceinline__ u64 place(float l, int id) {
-    const unsigned u = __float_as_uint(l + 0.f);
-    const unsigned key = u >> 31 ? u : ~u & 0x7FFFFFFFu;
-    return (u64)key << TP_MAX_LOG | (unsigned)id;
-}
-__device__ __forceinline__ Bound bound_of(u64 c) {
-    const unsigned key = (unsigned)(c >> TP_MAX_LOG);
-    return {__uint_as_float(key >> 31 ? key : ~key & 0x7FFFFFFFu), (unsigned)c & ((1u << TP_MAX_LOG) - 1)};
-}
-
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
 __device__ __forceinline__ double uniform(double v) {
     return __hiloint2double(__builtin_amdgcn_readfirstlane(__double2hiint(v)), __builtin_amdgcn_readfirstlane(__double2loint(v)));
+}
+__device__ __forceinline__ u64 lane_u64(u64 v, int lane) {
+    return (u64)(unsigned)__builtin_amdgcn_readlane((unsigned)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((unsigned)v, lane);
+}
+template <int CTRL, int ROW_MASK> __device__ __forceinline__ u64 dpp_u64(u64 self, u64 v) {
+    const unsigned lo = __builtin_amdgcn_update_dpp((int)self, (int)v, CTRL, ROW_MASK, 0xF, false);
+    const unsigned hi = __builtin_amdgcn_update_dpp((int)(self >> 32), (int)(v >> 32), CTRL, ROW_MASK, 0xF, false);
+    return (u64)hi << 32 | lo;
+}
+// inclusive prefix sums over a row of 16 lanes, over the wavefront
+__device__ __forceinline__ u64 row_scan(u64 v) {
+    v += dpp_u64<0x111, 0xF>(0, v);    // row_shr:1, 2, 4, 8
+    v += dpp_u64<0x112, 0xF>(0, v);
+    v += dpp_u64<0x114, 0xF>(0, v);
+    v += dpp_u64<0x118, 0xF>(0, v);
+    return v;
+}
+__device__ __forceinline__ u64 wave_scan(u64 v) {
+    v = row_scan(v);
+    v += dpp_u64<0x142, 0xA>(0, v);    // row_bcast:15 into rows 1 and 3
+    v += dpp_u64<0x143, 0xC>(0, v);    // row_bcast:31 into rows 2 and 3
+    return v;
 }
 
 struct Shared {
@@ -96,91 +100,81 @@ struct Shared {
         u64 cell[TP_MAX_CELLS];
     };
     u64 list[TP_LIST];
-    u64 red[TP_WAVES], red2[TP_WAVES];
+    u64 red[16], red2[16];
     u64 found_before;
-    unsigned red32[TP_WAVES];
+    unsigned red32[16];
     int found, n_list;
 };
 
 struct Row {
-    double max, c;                                 // the largest logit, 64 log2(e) / temperature
-    int frac;
-    const double* table;
-    // e = 2^(k / 64) * (1 + ...): k = rint(64 y), the rest by Taylor's series to the 4th power (the next is 4e-14).  Below 2^-80, and for -Inf: 2^-80
-    __device__ __forceinline__ double part(float l, int& k) const {
-        constexpr double big = 6755399441055744.0, q = 0.69314718055994530942 / TP_TABLE;   // 1.5 * 2^52: the sum's low word is the rounded number
-        const double u = __builtin_fmax(((double)l - max) * c, -80.0 * TP_TABLE), t = u + big, r = u - (t - big);
+    double max, c;                                 // the largest logit, 256 log2(e) / temperature
+    const double* table;                           // 2^(j/256 + frac)
+    // k = rint(256 y); below -80 * 256, and for -Inf: that
+    __device__ __forceinline__ double split(float l, int& k) const {
+        constexpr double big = 6755399441055744.0;  // 1.5 * 2^52: the sum's low word is the rounded number
+        const double u = __builtin_fmax(((double)l - max) * c, -80.0 * TP_TABLE), t = u + big;
         k = __double2loint(t);
-        double p = fma(r, q * q * q * q / 24, q * q * q / 6);
-        p = fma(p, r, q * q / 2);
+        return u - (t - big);
+    }
+    // e 2^frac = 2^(k / 256 + frac) * (1 + ...): the rest by Taylor's series to the third power (the next is 1.4e-13)
+    __device__ __forceinline__ double scaled(float l, int& k) const {
+        constexpr double q = 0.69314718055994530942 / TP_TABLE;
+        const double r = split(l, k);
+        double p = fma(r, q * q * q / 6, q * q / 2);
         p = fma(p, r, q);
-        p = fma(p, r, 1.0);
-        return p * table[k & (TP_TABLE - 1)];
+        p = fma(p, r, 1.0) * table[k & (TP_TABLE - 1)];
+        return __hiloint2double(__double2hiint(p) + ((k >> TP_TABLE_LOG) << 20), __double2loint(p));
     }
-    __device__ __forceinline__ double e(float l) const {
-        int k;
-        const double p = part(l, k);
-        return ldexp(p, k >> 6);
-    }
-    // e as a whole number of 2^-frac, below 2^52
+    // as a whole number, below 2^52
     __device__ __forceinline__ u64 mass(float l, int& k) const {
-        const double p = part(l, k), x = ldexp(p, (k >> 6) + frac) + 4503599627370496.0;
+        const double x = scaled(l, k) + 4503599627370496.0;
         return (u64)(unsigned)(__double2hiint(x) - 0x43300000) << 32 | (unsigned)__double2loint(x);
     }
     __device__ __forceinline__ u64 mass(float l) const { int k; return mass(l, k); }
     __device__ __forceinline__ int step(float l) const {
-        constexpr double big = 6755399441055744.0;
-        const double u = __builtin_fmax(((double)l - max) * c, -80.0 * TP_TABLE);
-        return step_of(__double2loint(u + big));
+        int k;
+        split(l, k);
+        return step_of(k);
     }
-    static __device__ __forceinline__ int step_of(int k) { return min(-k >> 1, TP_BINS - 1); }
+    static __device__ __forceinline__ int step_of(int k) { return min(-k >> TP_K_PER_STEP_LOG, TP_BINS - 1); }
 };
 
-__device__ __forceinline__ u64 shfl_up64(u64 v, int d) {
-    return (u64)__shfl_up((unsigned)(v >> 32), d) << 32 | __shfl_up((unsigned)v, d);
+// The token's place: descending logit (0 and -0 are equal), ascending id; and the place up to which tokens are kept
+__device__ __forceinline__ unsigned key_of(float l) {
+    const unsigned u = __float_as_uint(l + 0.f);
+    return u >> 31 ? u : ~u & 0x7FFFFFFFu;
 }
-__device__ __forceinline__ u64 shfl_xor64(u64 v, int d) {
-    return (u64)__shfl_xor((unsigned)(v >> 32), d) << 32 | __shfl_xor((unsigned)v, d);
+__device__ __forceinline__ float logit_of(unsigned key) { return __uint_as_float(key >> 31 ? key : ~key & 0x7FFFFFFFu); }
+__device__ __forceinline__ u64 place(float l, int id) { return (u64)key_of(l) << TP_MAX_LOG | (unsigned)id; }
+struct Bound {
+    float l;
+    unsigned id;
+    __device__ __forceinline__ bool keeps(float x, unsigned i) const { return x > l || (x == l && i <= id); }
+};
+__device__ __forceinline__ Bound bound_of(u64 c) {
+    return {uniform(logit_of((unsigned)(c >> TP_MAX_LOG))), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)c & ((1u << TP_MAX_LOG) - 1))};
 }
-__device__ __forceinline__ u64 wave_scan_u64(u64 v) {       // inclusive
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const u64 o = shfl_up64(v, d);
-        if ((int)(threadIdx.x & 63) >= d) v += o;
+// The least float, at most `max`, for which `pred` holds; it holds for max and for everything between.  Wavefronts do it alike
+template <typename F> __device__ __forceinline__ float least_float(float max, F pred) {
+    unsigned a = key_of(max), b = 0xFF800000u;              // holds at a; b: one behind the last (-Inf: not asked)
+    while (b - a > 1) {
+        const unsigned stride = (b - a + 63) >> 6, at = a + (threadIdx.x & 63) * stride;
+        const u64 yes = __ballot(at < b && pred(logit_of(at)));
+        const int n = ~yes ? __builtin_ctzll(~yes) : 64;    // (at least one: a itself)
+        a += (unsigned)(n - 1) * stride;
+        b = min(b, a + stride);
     }
-    return v;
-}
-// lane 0 has the sum
-__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += shfl_xor64(v, d);
-    return v;
-}
-// inclusive scan over the threads; total to every thread.  Synchronises before and after
-__device__ __forceinline__ u64 block_scan_u64(u64 v, Shared& S, u64& total) {
-    const int wave = threadIdx.x >> 6;
-    v = wave_scan_u64(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) S.red[wave] = v;
-    __syncthreads();
-    u64 base = 0;
-    total = 0;
-    for (int w = 0; w < TP_WAVES; ++w) {
-        if (w < wave) base += S.red[w];
-        total += S.red[w];
-    }
-    __syncthreads();
-    return base + v;
+    return uniform(logit_of(a));
 }
 
-template <typename LT> struct Logits {
+template <typename LT, int T> struct Logits {               // T threads
     const char* row;
     int vocab, nvec;
     // f(vector, its number), by whole wavefronts: what is behind the row's end is -Inf
     template <typename F> __device__ __forceinline__ void each(F f) const {
-        u32x4 x = load_vec<LT>(row, (int)threadIdx.x, vocab), next = load_vec<LT>(row, TP_THREADS + (int)threadIdx.x, vocab);
-        for (int i = 0; i < nvec; i += TP_THREADS) {        // two vectors ahead
-            const u32x4 after = load_vec<LT>(row, i + 2 * TP_THREADS + (int)threadIdx.x, vocab);
+        u32x4 x = load_vec<LT>(row, (int)threadIdx.x, vocab), next = load_vec<LT>(row, T + (int)threadIdx.x, vocab);
+        for (int i = 0; i < nvec; i += T) {                 // two vectors ahead
+            const u32x4 after = load_vec<LT>(row, i + 2 * T + (int)threadIdx.x, vocab);
             f(x, i + (int)threadIdx.x);
             x = next;
             next = after;
@@ -198,22 +192,37 @@ template <typename LT> struct Logits {
     }
 };
 
+__device__ __forceinline__ void lds_add(u64* p, u64 v) { __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void lds_add(unsigned* p, unsigned v) { __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void list_add(Shared& S, u64 c) {
     const int at = __hip_atomic_fetch_add(&S.n_list, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     if (at < TP_LIST) S.list[at] = c;
 }
 
-// The histogram's first entry with which the sum, `before` in front of it, reaches `want`; S.found, S.found_before to every thread
-__device__ __forceinline__ u64 find_in_bins(Shared& S, u64 before, u64 want, double of_all) {
-    constexpr int PER = TP_BINS / TP_THREADS;
+// inclusive prefix sums over the threads; total to every thread.  Synchronises once, behind which S.red may be used again only after another barrier
+template <int T> __device__ __forceinline__ u64 block_scan(u64 v, Shared& S, u64& total) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    v = wave_scan(v);
+    if (lane == 63) S.red[wave] = v;
+    __syncthreads();
+    const u64 w = row_scan((lane & 15) < T / 64 ? S.red[lane & 15] : 0);
+    total = lane_u64(w, 15);
+    const u64 upto = lane_u64(w, __builtin_amdgcn_readfirstlane(max(wave - 1, 0)));
+    return v + (wave > 0 ? upto : 0);
+}
+
+// The histogram's first entry with which the sum, `before` in front of it, reaches `want`; S.found, S.found_before to every thread.  of_all >= 0: want is that
+// share of the whole.  Takes and leaves synchronised
+template <int T> __device__ __forceinline__ u64 find_in_bins(Shared& S, u64 before, u64 want, double of_all) {
+    constexpr int PER = TP_BINS / T;
     u64 own[PER], sum = 0, total;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         own[i] = S.h.mass[threadIdx.x * PER + i];
         sum += own[i];
     }
-    u64 upto = block_scan_u64(sum, S, total) - sum + before;
-    if (of_all >= 0.0) {                                    // (a share of the whole)
+    u64 upto = block_scan<T>(sum, S, total) - sum + before;
+    if (of_all >= 0.0) {
         const double t = ceil(of_all * (double)total);
         want = t >= 1.0 ? min((u64)t, total) : 1;
     }
@@ -227,58 +236,85 @@ __device__ __forceinline__ u64 find_in_bins(Shared& S, u64 before, u64 want, dou
 }
 
 // Of the list's n tokens, with weights w(logit): the first, in the order of places, with which the sum (`before` in front of them) reaches `want`.
-// of_all: as above.  Takes and leaves synchronised; S.found_before: the sum up to and with that token
-template <typename W> __device__ __forceinline__ u64 find_in_list(Shared& S, int n, u64 before, u64 want, double of_all, W w) {
+// with: the sum up to and with that token.  Takes and leaves synchronised
+template <int T, typename W> __device__ __forceinline__ u64 find_in_list(Shared& S, int n, u64 before, u64 want, double of_all, u64& with, W w) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    u64 c[2], m[2];
-    bool live[2];
+    if (n <= 64) {                                          // every wavefront by itself
+        const u64 c = lane < n ? S.list[lane] : ~0ull, m = lane < n ? w(logit_of((unsigned)(c >> TP_MAX_LOG))) : 0;
+        if (of_all >= 0.0) {
+            const u64 total = lane_u64(wave_scan(m), 63);
+            const double t = ceil(of_all * (double)total);
+            want = t >= 1.0 ? min((u64)t, total) : 1;
+        }
+        u64 upto = before;                                  // with everything up to the lane's own token
+        for (int j = 0; j < n; ++j) {
+            const u64 cj = lane_u64(c, j), mj = lane_u64(m, j);
+            upto += cj <= c ? mj : 0;
+        }
+        const u64 hit = __ballot(upto >= want && upto - m < want && m);
+        __syncthreads();                                    // (the list may be written again)
+        if (!hit) return ~0ull;
+        const int at = __builtin_ctzll(hit);
+        with = lane_u64(upto, at);
+        return lane_u64(c, at);
+    }
+    constexpr int PER = TP_LIST / T;
+    u64 c[PER], m[PER];
+    unsigned live = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        live[i] = tid + i * TP_THREADS < n;
-        c[i] = live[i] ? S.list[tid + i * TP_THREADS] : 0;
-        m[i] = live[i] ? w(bound_of(c[i]).l) : 0;
+    for (int i = 0; i < PER; ++i) {
+        const bool is = tid + i * T < n;
+        c[i] = is ? S.list[tid + i * T] : 0;
+        m[i] = is ? w(logit_of((unsigned)(c[i] >> TP_MAX_LOG))) : 0;
+        if (m[i]) live |= 1u << i;
     }
     for (int round = 0; round < 6; ++round) {               // (52 bits, eleven and more at a time)
-        u64 all = ~0ull, any = 0;                           // bits that every one has, that one has at least
+        u64 none = 0, any = 0;                              // bits that one lacks, that one has
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (live[i]) { all &= c[i]; any |= c[i]; }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) { all &= shfl_xor64(all, d); any |= shfl_xor64(any, d); }
-        if (lane == 0) { S.red[wave] = all; S.red2[wave] = any; }
-        for (int i = tid; i < TP_BINS; i += TP_THREADS) S.h.mass[i] = 0;
+        for (int i = 0; i < PER; ++i)
+            if (live >> i & 1) { none |= ~c[i]; any |= c[i]; }
+#define TP_OR(CTRL, RM) { none |= dpp_u64<CTRL, RM>(0, none); any |= dpp_u64<CTRL, RM>(0, any); }
+        PS_DPP_STEPS(TP_OR)
+#undef TP_OR
+        if (lane == 63) { S.red[wave] = none; S.red2[wave] = any; }
+        for (int i = tid; i < TP_BINS; i += T) S.h.mass[i] = 0;
         __syncthreads();
-        for (int i = 0; i < TP_WAVES; ++i) { all &= S.red[i]; any |= S.red2[i]; }
-        const u64 differ = all ^ any;
+        none = (lane & 15) < T / 64 ? S.red[lane & 15] : 0;
+        any = (lane & 15) < T / 64 ? S.red2[lane & 15] : 0;
+#define TP_OR(CTRL, RM) { none |= dpp_u64<CTRL, RM>(0, none); any |= dpp_u64<CTRL, RM>(0, any); }
+        PS_DPP_ROW_STEPS(TP_OR)
+#undef TP_OR
+        any = lane_u64(any, 0);
+        const u64 differ = any & lane_u64(none, 0);
         const int shift = differ ? max(0, 63 - __builtin_clzll(differ) - 10) : 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (live[i] && m[i]) __hip_atomic_fetch_add(&S.h.mass[(c[i] >> shift) & (TP_BINS - 1)], m[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        for (int i = 0; i < PER; ++i)
+            if (live >> i & 1) lds_add(&S.h.mass[(c[i] >> shift) & (TP_BINS - 1)], m[i]);
         __syncthreads();
-        want = find_in_bins(S, before, want, of_all);
+        want = find_in_bins<T>(S, before, want, of_all);
         of_all = -1.0;
         const int digit = S.found;
         before = S.found_before;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) live[i] = live[i] && (int)((c[i] >> shift) & (TP_BINS - 1)) == digit;
         if (differ >> 11 == 0) {                            // these eleven bits were the last ones
-            const u64 at = (any & ~(u64)(TP_BINS - 1)) | digit;
-            if (tid == 0) S.found_before = before + S.h.mass[digit];
+            with = before + S.h.mass[digit];
             __syncthreads();
-            return at;
+            return (any & ~(u64)(TP_BINS - 1)) | (unsigned)digit;
         }
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if ((int)((c[i] >> shift) & (TP_BINS - 1)) != digit) live &= ~(1u << i);
         __syncthreads();
     }
-    return 0;
+    return ~0ull;
 }
 
 // The bound of the row's tokens that `within` keeps: the first token with which the sum of e (BY_MASS) reaches top_p of their sum, or the
-// top_k-th.  S.found_before: the sum up to and with it
-template <bool BY_MASS, typename LT>
-__device__ __forceinline__ u64 find_in_row(const Logits<LT>& L, const Row& R, Shared& S, Bound within, u64 want, double of_all) {
+// top_k-th.  with: the sum up to and with it
+template <bool BY_MASS, typename LT, int T>
+__device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R, float mx, Shared& S, Bound within, u64 want, double of_all, u64& with) {
     const int tid = threadIdx.x;
     auto weight = [&](float l) { return BY_MASS ? R.mass(l) : (u64)1; };
-    for (int i = tid; i < TP_BINS; i += TP_THREADS) S.h.mass[i] = 0;
+    for (int i = tid; i < TP_BINS; i += T) S.h.mass[i] = 0;
     if (tid == 0) S.n_list = 0;
     __syncthreads();
     L.tokens([&](float l, int id) {
@@ -286,90 +322,89 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT>& L, const Row& R, Sh
         if constexpr (BY_MASS) {
             int k;
             const u64 m = R.mass(l, k);
-            __hip_atomic_fetch_add(&S.h.mass[R.step_of(k)], m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        } else __hip_atomic_fetch_add((unsigned*)&S.h.mass[R.step(l)], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            lds_add(&S.h.mass[R.step_of(k)], m);
+        } else lds_add((unsigned*)&S.h.mass[R.step(l)], 1u);
     });
     __syncthreads();
-    want = find_in_bins(S, 0, want, of_all);
+    want = find_in_bins<T>(S, 0, want, of_all);
     const int step = S.found;
     u64 before = S.found_before;
+    // the step's logits: least <= l < above
+    const float least = step < TP_BINS - 1 ? least_float(mx, [&](float l) { return R.step(l) <= step; }) : -__builtin_inff();
+    const float above = step > 0 ? least_float(mx, [&](float l) { return R.step(l) < step; }) : __builtin_inff();
     L.tokens([&](float l, int id) {
-        if (R.step(l) == step && within.keeps(l, id)) list_add(S, place(l, id));
+        if (l >= least && l < above && within.keeps(l, id)) list_add(S, place(l, id));
     });
     __syncthreads();
-    if (S.n_list <= TP_LIST) return find_in_list(S, S.n_list, before, want, -1.0, weight);
+    if (S.n_list <= TP_LIST) return find_in_list<T>(S, S.n_list, before, want, -1.0, with, weight);
     // more tokens than the list holds (equal or nearly equal logits): eleven bits of the place at a time, until few enough are left
     u64 prefix = 0;
     for (int shift = 44;; shift -= 11) {
         __syncthreads();
-        for (int i = tid; i < TP_BINS; i += TP_THREADS) { S.h.mass[i] = 0; S.h.count[i] = 0; }
+        for (int i = tid; i < TP_BINS; i += T) { S.h.mass[i] = 0; S.h.count[i] = 0; }
         if (tid == 0) S.n_list = 0;
         __syncthreads();
         L.tokens([&](float l, int id) {
             const u64 c = place(l, id);
-            if (R.step(l) != step || !within.keeps(l, id) || c >> (shift + 11) != prefix) return;
+            if (!(l >= least && l < above && within.keeps(l, id)) || c >> (shift + 11) != prefix) return;
             const int digit = (int)(c >> shift) & (TP_BINS - 1);
-            __hip_atomic_fetch_add(&S.h.count[digit], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-            __hip_atomic_fetch_add(&S.h.mass[digit], weight(l), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            lds_add(&S.h.count[digit], 1u);
+            lds_add(&S.h.mass[digit], weight(l));
         });
         __syncthreads();
-        find_in_bins(S, before, want, -1.0);
+        find_in_bins<T>(S, before, want, -1.0);
         prefix = prefix << 11 | (unsigned)S.found;
         before = S.found_before;
         if (S.h.count[S.found] > TP_LIST && shift > 0) continue;   // (at the last digit it is one token)
         L.tokens([&](float l, int id) {
             const u64 c = place(l, id);
-            if (c >> shift == prefix && R.step(l) == step && within.keeps(l, id)) list_add(S, c);
+            if (c >> shift == prefix && within.keeps(l, id)) list_add(S, c);
         });
         __syncthreads();
-        return find_in_list(S, S.n_list, before, want, -1.0, weight);
+        return find_in_list<T>(S, S.n_list, before, want, -1.0, with, weight);
     }
 }
 
-template <typename LT>
-__global__ __launch_bounds__(TP_THREADS, 4) void target_probs_kernel(const TpParams P) {
-    constexpr int N = Vec<LT>::N;
+template <typename LT, int T>
+__global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
+    constexpr int N = Vec<LT>::N, WAVES = T / 64;
     __shared__ Shared S;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = P.vocab;
     const size_t row = blockIdx.x;
     const int b = (int)(row / (unsigned)P.rows);
-    Logits<LT> L;
+    Logits<LT, T> L;
     L.row = P.logits + row * V * Traits<LT>::ESZ; L.vocab = V; L.nvec = (V + N - 1) / N;
     const float t_in = P.temperature ? P.temperature[b] : 1.f;
     const bool greedy = !(t_in > 0.f);
     const int k_in = P.top_k ? P.top_k[b] : 0;
     const int k = greedy ? 1 : k_in < 1 || k_in > V ? V : k_in;
     const float p_in = P.top_p ? P.top_p[b] : 1.f, m_in = P.min_p ? P.min_p[b] : 0.f, min_p = m_in > 0.f ? fminf(m_in, 1.f) : 0.f;
-    if (tid < TP_TABLE) S.table[tid] = ga_exp2(tid * (1.0 / TP_TABLE));
+    if (tid < TP_TABLE) S.table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
 
-    // the largest logit, and whether any is NaN or +Inf; each thread's first of its largest
+    // the largest logit, and whether any is NaN or +Inf
     float mx = -__builtin_inff();
-    unsigned first = 0;
     bool bad = false;
-    L.each([&](const u32x4& x, int at) {
+    L.each([&](const u32x4& x, int) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float l = Vec<LT>::get(x, e);
             bad |= !(l < __builtin_inff());
-            if (l > mx) { mx = l; first = at * N + e; }
+            mx = fmaxf(mx, l);
         }
     });
     const float mine = mx;
     mx = __ballot(bad) ? __builtin_nanf("") : wave_max(mx);
     if (lane == 0) S.red32[wave] = __float_as_uint(mx);
-    if (tid == 0) S.n_list = 0;
+    if (tid == 0) { S.n_list = 0; S.found = V; }
+    for (int i = tid; i < TP_BINS; i += T) S.h.mass[i] = 0;
     __syncthreads();
-    mx = -__builtin_inff();
-    bad = false;
-    for (int w = 0; w < TP_WAVES; ++w) {
-        const float m = __uint_as_float(S.red32[w]);
-        bad |= m != m;
-        mx = fmaxf(mx, m);
-    }
+    mx = __uint_as_float(S.red32[lane % WAVES]);
+    bad = __ballot(mx != mx);
+    mx = uniform(row_max(mx));
     float* out = P.probs ? P.probs + row * V : nullptr;
     if (bad || mx == -__builtin_inff()) {
         const float fill = bad ? __builtin_nanf("") : 0.f;
-        if (out) for (int i = tid; i < V; i += TP_THREADS) out[i] = fill;
+        if (out) for (int i = tid; i < V; i += T) out[i] = fill;
         if (P.ids && tid == 0) {
             P.ids[row] = -1;
             if (P.id_probs) P.id_probs[row] = fill;
@@ -377,65 +412,62 @@ __global__ __launch_bounds__(TP_THREADS, 4) void target_probs_kernel(const TpPar
         return;
     }
     Row R;
-    R.max = uniform(mx); R.c = uniform(1.4426950408889634074 * TP_TABLE / (greedy ? 1.0 : (double)t_in)); R.frac = P.frac; R.table = S.table;
+    R.max = mx; R.c = uniform(1.4426950408889634074 * TP_TABLE / (greedy ? 1.0 : (double)t_in)); R.table = S.table;
     Bound bound = {-__builtin_inff(), ~0u};
     u64 total = 0;                                          // the sum of the kept e, where it is known
     auto mass = [&](float l) { return R.mass(l); };
     auto one = [](float) { return (u64)1; };
     if (k == 1) {                                           // the first of the largest
-        unsigned id = mine == mx ? first : ~0u;
-        id = ~wave_max_u32(~id);
+        L.tokens([&](float l, int id) { if (l == mx) __hip_atomic_fetch_min(&S.found, id, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); });
         __syncthreads();
-        if (lane == 0) S.red32[wave] = id;
-        __syncthreads();
-        for (int w = 0; w < TP_WAVES; ++w) id = min(id, S.red32[w]);
-        bound = {mx, id};
+        bound = {mx, (unsigned)S.found};
         total = R.mass(mx);
     } else {
         bool listed = false, all = k == V;                  // all: no top-k, or one that only drops tokens at -Inf
-        if (k <= TP_SMALL_K && k < L.nvec) {
-            // every one of the k threads with the largest maxima has a token at or above the k-th of them: so have the k largest tokens
-            S.list[tid] = place(mine, first);
+        u64 with = 0;
+        if (k <= TP_SMALL_K && k <= min(T, L.nvec)) {
+            // k threads' maxima are at or above some step: so are the k largest tokens
+            if (tid < L.nvec) lds_add((unsigned*)&S.h.mass[R.step(mine)], 1u);
             __syncthreads();
-            const Bound least = bound_of(find_in_list(S, TP_THREADS, 0, (u64)k, -1.0, one));
-            if (least.l == -__builtin_inff()) all = true;
-            else {
-                L.tokens([&](float l, int id) { if (least.keeps(l, id)) list_add(S, place(l, id)); });
+            find_in_bins<T>(S, 0, (u64)k, -1.0);
+            const int step = S.found;
+            if (step < TP_BINS - 1) {
+                const float least = least_float(mx, [&](float l) { return R.step(l) <= step; });
+                L.tokens([&](float l, int id) { if (l >= least) list_add(S, place(l, id)); });
                 __syncthreads();
                 listed = S.n_list <= TP_LIST;
             }
         }
         if (listed) {
             const int n = S.n_list;
-            bound = bound_of(find_in_list(S, n, 0, (u64)k, -1.0, one));
+            bound = bound_of(find_in_list<T>(S, n, 0, (u64)k, -1.0, with, one));
             u64 m = 0;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (tid + i * TP_THREADS < n) {             // tokens behind the bound leave the list: the last place, without mass
-                    const Bound at = bound_of(S.list[tid + i * TP_THREADS]);
-                    if (bound.keeps(at.l, at.id)) m += R.mass(at.l);
-                    else S.list[tid + i * TP_THREADS] = place(-__builtin_inff(), at.id);
-                }
-            block_scan_u64(m, S, total);
-            if (p_in < 1.f) {
-                bound = bound_of(find_in_list(S, n, 0, 0, fmax((double)p_in, 0.0), mass));
-                total = S.found_before;
+            for (int i = tid; i < n; i += T) {              // tokens behind the bound leave the list: the last place, without mass
+                const u64 c = S.list[i];
+                const float l = logit_of((unsigned)(c >> TP_MAX_LOG));
+                const unsigned id = (unsigned)c & ((1u << TP_MAX_LOG) - 1);
+                if (bound.keeps(l, id)) m += R.mass(l);
+                else S.list[i] = place(-__builtin_inff(), id);
             }
-        } else {
-            if (!all) bound = bound_of(find_in_row<false>(L, R, S, bound, (u64)k, -1.0));
+            block_scan<T>(m, S, total);
             if (p_in < 1.f) {
                 __syncthreads();
-                bound = bound_of(find_in_row<true>(L, R, S, bound, 0, fmax((double)p_in, 0.0)));
-                total = S.found_before;
+                bound = bound_of(find_in_list<T>(S, n, 0, 0, fmax((double)p_in, 0.0), with, mass));
+                total = with;
+            }
+        } else {
+            if (!all) bound = bound_of(find_in_row<false>(L, R, mx, S, bound, (u64)k, -1.0, with));
+            if (p_in < 1.f) {
+                __syncthreads();
+                bound = bound_of(find_in_row<true>(L, R, mx, S, bound, 0, fmax((double)p_in, 0.0), with));
+                total = with;
             }
         }
     }
-    if (min_p > 0.f && R.c > 0.0) {                         // the least logit with e >= min_p: near max + log2(min_p) / c, tried out
-        const float near = (float)(R.max + log2((double)min_p) * TP_TABLE / R.c);
-        const unsigned key = (unsigned)(place(near, 0) >> TP_MAX_LOG) + 31 - lane;   // ascending logits along the lanes
-        const float l = bound_of((u64)key << TP_MAX_LOG).l;
-        const u64 fine = __ballot(R.e(l) >= (double)min_p && l <= mx);
-        const float least = fminf(mx, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l), fine ? __builtin_ctzll(fine) : 63)));
+    if (min_p > 0.f) {
+        const double least_e = ldexp((double)min_p, P.frac);
+        int kk;
+        const float least = least_float(mx, [&](float l) { return R.scaled(l, kk) >= least_e; });
         if (least > bound.l) { bound = {least, ~0u}; total = 0; }
     }
 
@@ -448,48 +480,49 @@ __global__ __launch_bounds__(TP_THREADS, 4) void target_probs_kernel(const TpPar
             for (int e = 0; e < N; ++e) {
                 const float l = Vec<LT>::get(x, e);
                 if (at * N + e < V && bound.keeps(l, at * N + e)) m += R.mass(l);
+                if (e & 1) __builtin_amdgcn_sched_barrier(0);
             }
-            if (__ballot(m != 0)) m = wave_sum_u64(m);
-            if (lane == 0) S.cell[at / 64] = m;
+            if (__ballot(m != 0)) m = wave_scan(m);
+            if (lane == 63) S.cell[at >> 6] = m;
         });
         __syncthreads();
-        constexpr int PER = TP_MAX_CELLS / TP_THREADS;
-        const int cells = (L.nvec + TP_THREADS - 1) / TP_THREADS * TP_WAVES;
-        u64 own[PER], sum = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            own[i] = tid * PER + i < cells ? S.cell[tid * PER + i] : 0;
-            sum += own[i];
-        }
-        u64 upto = block_scan_u64(sum, S, total) - sum;
+        constexpr int PER = TP_MAX_CELLS / T;
+        const int cells = (L.nvec + T - 1) / T * WAVES;
+        u64 sum = 0;
+        for (int i = 0; i < PER; ++i) sum += tid * PER + i < cells ? S.cell[tid * PER + i] : 0;
+        u64 upto = block_scan<T>(sum, S, total) - sum;
         if (P.ids) {
             const double t = (double)P.r[row] * (double)total;
             const u64 want = t >= 1.0 ? min((u64)t, total - 1) : 0;   // the drawn token is the first with which the sum passes it
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                if (upto <= want && upto + own[i] > want) { S.found = tid * PER + i; S.found_before = upto; }
-                upto += own[i];
-            }
+            if (upto <= want && upto + sum > want)
+                for (int i = 0; i < PER; ++i) {
+                    const u64 own = tid * PER + i < cells ? S.cell[tid * PER + i] : 0;
+                    if (upto <= want && upto + own > want) { S.found = tid * PER + i; S.found_before = upto; }
+                    upto += own;
+                }
             __syncthreads();
             if (wave == 0) {
                 const int at = S.found * 64 + lane;
                 const u32x4 x = load_vec<LT>(L.row, at, V);
-                u64 m[N], all = 0;
+                u64 all = 0;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float l = Vec<LT>::get(x, e);
-                    m[e] = at * N + e < V && bound.keeps(l, at * N + e) ? R.mass(l) : 0;
-                    all += m[e];
+                    if (at * N + e < V && bound.keeps(l, at * N + e)) all += R.mass(l);
                 }
-                u64 to = S.found_before + wave_scan_u64(all) - all;
+                u64 to = S.found_before + wave_scan(all) - all;
+                if (to <= want && to + all > want)
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    if (to <= want && to + m[e] > want) {
-                        P.ids[row] = at * N + e;
-                        if (P.id_probs) P.id_probs[row] = (float)(R.e(Vec<LT>::get(x, e)) / ldexp((double)total, -P.frac));
+                    for (int e = 0; e < N; ++e) {
+                        const float l = Vec<LT>::get(x, e);
+                        const u64 m = at * N + e < V && bound.keeps(l, at * N + e) ? R.mass(l) : 0;
+                        if (to <= want && to + m > want) {
+                            P.ids[row] = at * N + e;
+                            int kk;
+                            if (P.id_probs) P.id_probs[row] = (float)(R.scaled(l, kk) / (double)total);
+                        }
+                        to += m;
                     }
-                    to += m[e];
-                }
             }
         }
     }
@@ -506,6 +539,7 @@ __global__ __launch_bounds__(TP_THREADS, 4) void target_probs_kernel(const TpPar
                 const double y = __builtin_fmax(((double)l - R.max) * cy, -1000.0), n = rint(y);
                 p[e] = ldexpf(__builtin_amdgcn_exp2f((float)(y - n)) * inv, (int)n);
             }
+            if (e & 1) __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int q = 0; q < N; q += 4) {
@@ -519,7 +553,8 @@ __global__ __launch_bounds__(TP_THREADS, 4) void target_probs_kernel(const TpPar
 }
 
 template <typename LT> void go(const TpParams& P, int total, hipStream_t s) {
-    hipLaunchKernelGGL((target_probs_kernel<LT>), dim3(total), dim3(TP_THREADS), 0, s, P);
+    if (total <= 256) hipLaunchKernelGGL((target_probs_kernel<LT, 1024>), dim3(total), dim3(1024), 0, s, P);
+    else hipLaunchKernelGGL((target_probs_kernel<LT, 512>), dim3(total), dim3(512), 0, s, P);
 }
 
 int check(const ps_target_probs_args* a) {
