@@ -8,9 +8,9 @@
 // codes go from memory to the matrix cores through a conversion (two codes an instruction), with no exchange between lanes and no LDS.
 // The running maximum is raised only when a score passes it by 2^8 (sums stay far inside float32), so sums are rarely rescaled.
 //
-// Work: a sequence's blocks are cut into splits of `per` blocks; a workgroup of four wavefronts takes a split of one kv head for 32 ... 256 rows
-// (a row is a node and one of the heads that share the kv head).  Its wavefronts divide rows (WR) and blocks (4 / WR); those that share
-// rows meet in LDS, splits in the workspace and a second kernel.
+// Work: a sequence's blocks are cut into splits of `per` blocks; a workgroup takes a split of one kv head for up to 256 rows
+// (a row is a node and one of the heads that share the kv head), a wavefront 32 of them.  Its wavefronts divide rows (WR) and blocks (WK); those
+// that share rows meet in LDS, splits in the workspace and a second kernel.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -18,7 +18,9 @@
 
 namespace {
 
-constexpr int TA_WAVES = 4, TA_TILE = 32;
+constexpr int TA_TILE = 32;
+// wavefronts of a workgroup: two per SIMD, so that one's matrix instructions run beside the other's exponentials; float32 has three parts of every query
+template <typename WT> constexpr int ta_waves() { return Traits<WT>::BF ? 8 : 4; }
 constexpr float TA_LAZY = 8.f;      // how far (in powers of two) scores may pass the maximum that they are taken against
 
 struct TaParams {
@@ -142,61 +144,34 @@ template <int D> __device__ __forceinline__ void merge(RowState<D>& R, float m2,
     for (int j = 0; j < D / 32; ++j) R.o[j] = R.o[j] * a + o2[j] * b;
 }
 
-// a finished tile: lane's row (node and head) of one sequence, dims 32 j ..
-template <typename WT, int D> __device__ __forceinline__ void store_row(const TaParams& P, int b, int h, int row, int j, const f32x16& o, float m, float l) {
-    if (row >= P.rows) return;
-    const int half = (threadIdx.x >> 5) & 1, node = row / P.grp, head = h * P.grp + row % P.grp;
-    const size_t at = ((size_t)b * P.nodes + node) * P.n_heads + head;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int a = 0; a < 4; ++a) {
-        const f32x4 x = f32x4{o[4 * a], o[4 * a + 1], o[4 * a + 2], o[4 * a + 3]} * inv;
-        char* p = P.out + (at * D + 32 * j + 8 * a + 4 * half) * Traits<WT>::ESZ;
-        if constexpr (Traits<WT>::BF) *reinterpret_cast<u32x2_q*>(p) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-        else *reinterpret_cast<f32x4_q*>(p) = x;
-    }
-    if (P.lse && j == 0 && half == 0) P.lse[at] = l == 0.f ? -__builtin_inff() : 0.69314718055994530942f * (m + __log2f(l));
+template <typename WT> __device__ __forceinline__ void store4_out(char* p, f32x4 x) {
+    if constexpr (Traits<WT>::BF) *reinterpret_cast<u32x2_q*>(p) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+    else *reinterpret_cast<f32x4_q*>(p) = x;
 }
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -__builtin_inff() : 0.69314718055994530942f * (m + __log2f(l)); }
 
-// floats of one tile's part in the workspace: sums, then maxima and row sums
+// floats that a wavefront leaves in LDS: sums, then maxima and row sums
 template <int D> constexpr int part_floats() { return TA_TILE * D + 2 * 64; }
 
-template <typename WT, int D, int RT, int WR>
-__global__ __launch_bounds__(64 * TA_WAVES, RT == 2 ? 1 : 2) void tree_attn_kernel(const TaParams P) {
-    constexpr int WK = TA_WAVES / WR, NP = Traits<WT>::BF ? 1 : 3, C = D / 32, TILE = PC_BLOCK * D, ESZ = Traits<WT>::ESZ;
-    __shared__ __attribute__((aligned(16))) float s_meet[WK > 1 ? (TA_WAVES / 2) * RT * part_floats<D>() : 4];
-    __shared__ float s_p[TA_WAVES][PC_BLOCK * TA_TILE];
+template <typename WT, int D, int WR>
+__global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_attn_kernel(const TaParams P) {
+    constexpr int W = ta_waves<WT>(), WK = W / WR, NP = Traits<WT>::BF ? 1 : 3, C = D / 32, TILE = PC_BLOCK * D, ESZ = Traits<WT>::ESZ;
+    __shared__ __attribute__((aligned(16))) float s_meet[WK > 1 ? (W / 2) * part_floats<D>() : 4];
+    __shared__ float s_p[W][PC_BLOCK * TA_TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, lc = lane & 31;
     const int wr = wave % WR, wk = wave / WR, h = blockIdx.y;
     int b = 0;
     while ((int)blockIdx.x >= P.split0[b + 1]) ++b;
     const int split = blockIdx.x - P.split0[b], splits = P.split0[b + 1] - P.split0[b];
     const int len = pc_length(P.len_dev, b, P.len[b]), blocks = (len + 31) >> 5, tail = len & 31;
-    const int tile0 = ((int)blockIdx.z * WR + wr) * RT;      // this wavefront's first tile of rows
-    const bool active = tile0 < P.tiles;
-
-    bf16x8 q[RT][2 * C][NP];
-    RowState<D> R[RT];
-    u64 sees[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int row = (tile0 + rt) * TA_TILE + lc;
-        const bool valid = row < P.rows;
-        const int node = valid ? row / P.grp : 0, head = h * P.grp + (valid ? row % P.grp : 0);
-        const char* from = P.q + ((long long)b * P.nodes + node) * P.q_row + (long long)head * D * ESZ;
-#pragma unroll
-        for (int i = 0; i < 2 * C; ++i) load_parts<WT, NP>(from + (32 * (i >> 1) + 16 * half + 8 * (i & 1)) * ESZ, valid, q[rt][i]);
-        sees[rt] = P.sees[node];
-        R[rt].m = -__builtin_inff();
-        R[rt].l = 0.f;
-#pragma unroll
-        for (int j = 0; j < C; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) R[rt].o[j][i] = 0.f;
-    }
-
-    const int end = min(blocks, (split + 1) * P.per);
+    const int tile = (int)blockIdx.z * WR + wr;              // this wavefront's rows
+    const bool active = tile < P.tiles;
+    const int begin = split * P.per, end = min(blocks, begin + P.per);
     const size_t seq0 = (size_t)P.first[b] * P.heads + h;
+    const int row = tile * TA_TILE + lc;
+    const bool valid = row < P.rows;
+    const int node = valid ? row / P.grp : 0, head = h * P.grp + (valid ? row % P.grp : 0);
+
     auto fetch = [&](int i, Tile<D>& t) {
         const size_t at = (seq0 + (size_t)i * P.heads) * TILE + lane * 16;
 #pragma unroll
@@ -204,36 +179,61 @@ __global__ __launch_bounds__(64 * TA_WAVES, RT == 2 ? 1 : 2) void tree_attn_kern
 #pragma unroll
         for (int c = 0; c < C; ++c) t.v[c] = ld16(P.v_codes + at + c * 1024);
     };
+    // the scales of this wavefront's next 64 blocks, one a lane
+    float k_scales = 0.f, v_scales = 0.f;
+    auto fetch_scales = [&](int i) {
+        const int mine = i + lane * WK;
+        if (mine < end) {
+            const size_t at = seq0 + (size_t)mine * P.heads;
+            k_scales = P.k_scale[at];
+            v_scales = P.v_scale[at];
+        }
+    };
     Tile<D> next;
-    int i = split * P.per + wk;
-    if (active && i < end) fetch(i, next);
-    if (active)
+    int i = begin + wk;
+    const bool any = active && i < end;
+    if (any) {
+        fetch_scales(i);
+        fetch(i, next);
+    }
+    bf16x8 q[2 * C][NP];
+    RowState<D> R;
+    {
+        const char* from = P.q + ((long long)b * P.nodes + node) * P.q_row + (long long)head * D * ESZ;
+#pragma unroll
+        for (int f = 0; f < 2 * C; ++f) load_parts<WT, NP>(from + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, active && valid, q[f]);
+        R.m = -__builtin_inff();
+        R.l = 0.f;
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) R.o[j][e] = 0.f;
+    }
+    if (any) {
+        int turn = 0;
         for (; i < end; i += WK) {
             Tile<D> t = next;
-            if (i + WK < end) fetch(i + WK, next);
-            const size_t sat = seq0 + (size_t)i * P.heads;
-            const float ks = P.k_scale[sat], vs = P.v_scale[sat];
-            const bool cut = tail && i == blocks - 1;
-            f32x16 s[RT];
+            const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), turn));
+            const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), turn));
+            if (i + WK < end) {
+                fetch(i + WK, next);
+                turn = (turn + 1) & 63;
+                if (turn == 0) fetch_scales(i + WK);
+            }
+            f32x16 s;
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[rt][e] = 0.f;
+            for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const bf16x8 kf = widen8(word(t.k[c], 2 * u), word(t.k[c], 2 * u + 1));
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int p = NP - 1; p >= 0; --p) s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[rt][2 * c + u][p], s[rt], 0, 0, 0);
+                    for (int p = NP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[2 * c + u][p], s, 0, 0, 0);
                 }
-            if (cut) {                                       // positions behind the end: hidden, and their codes no numbers that count
+            if (tail && i == blocks - 1) {                   // positions behind the end: hidden, and their codes no numbers that count
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) s[rt][e] = 8 * (e >> 2) + 4 * half + (e & 3) < tail ? s[rt][e] : -__builtin_inff();
+                for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + 4 * half + (e & 3) < tail ? s[e] : -__builtin_inff();
                 unsigned keep[4];
 #pragma unroll
                 for (int a = 0; a < 4; ++a) {
@@ -243,56 +243,48 @@ __global__ __launch_bounds__(64 * TA_WAVES, RT == 2 ? 1 : 2) void tree_attn_kern
 #pragma unroll
                 for (int c = 0; c < C; ++c) t.v[c] = make_uint4(t.v[c].x & keep[0], t.v[c].y & keep[1], t.v[c].z & keep[2], t.v[c].w & keep[3]);
             }
-            const float lv = (float)((int)(__float_as_uint(vs) >> 23) - 127), inv_vs = 1.f / vs, cs = P.c * ks;
-            bf16x8 p[RT][2][NP];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                softmax_tile<D>(R[rt], s[rt], cs, lv, inv_vs);
-                prob_parts<NP>(s[rt], p[rt]);
-            }
+            const float lv = (float)((int)(__float_as_uint(vs) >> 23) - 127);
+            softmax_tile<D>(R, s, P.c * ks, lv, __uint_as_float((254u << 23) - __float_as_uint(vs)));   // (1 / vs: a power of two)
+            bf16x8 p[2][NP];
+            prob_parts<NP>(s, p);
 #pragma unroll
             for (int j = 0; j < C; ++j)
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
                     const bf16x8 vf = widen8(word(t.v[j], 2 * st), word(t.v[j], 2 * st + 1));
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int n = NP - 1; n >= 0; --n) R[rt].o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[rt][st][n], R[rt].o[j], 0, 0, 0);
+                    for (int n = NP - 1; n >= 0; --n) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[st][n], R.o[j], 0, 0, 0);
                 }
         }
+    }
 
-    // the tree's own rows, in the sequence's last split: tiles of 32 nodes
-    if (active && P.k && split == splits - 1)
-        for (int kt = wk; kt * 32 < P.nodes; kt += WK) {
+    // the tree's own rows, in the sequence's last split: tiles of 32 nodes, which take their turn behind its blocks
+    if (active && P.k && split == splits - 1) {
+        const u64 sees = P.sees[node];
+        const int behind = max(end - begin, 0);
+        for (int kt = 0; kt * 32 < P.nodes; ++kt) {
+            if ((behind + kt) % WK != wk) continue;
             const char* own_k = P.k + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
             const char* own_v = P.v + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
-            f32x16 s[RT];
+            f32x16 s;
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[rt][e] = 0.f;
+            for (int e = 0; e < 16; ++e) s[e] = 0.f;
             const int key = kt * 32 + lc;
 #pragma unroll
             for (int f = 0; f < 2 * C; ++f) {
                 bf16x8 kf[NP];
                 load_parts<WT, NP>(own_k + (long long)key * P.kv_row + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, key < P.nodes, kf);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
+                for (int x = NP - 1; x >= 0; --x)            // (parts whose product is below 2^-24 of the whole are left out)
 #pragma unroll
-                    for (int x = NP - 1; x >= 0; --x)        // (parts whose product is below 2^-24 of the whole are left out)
-#pragma unroll
-                        for (int y = NP - 1 - x; y >= 0; --y) s[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], q[rt][f][y], s[rt], 0, 0, 0);
+                    for (int y = NP - 1 - x; y >= 0; --y) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], q[f][y], s, 0, 0, 0);
             }
-            bf16x8 p[RT][2][NP];
+            const unsigned seen = (unsigned)(sees >> (32 * kt));
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const unsigned seen = (unsigned)(sees[rt] >> (32 * kt));
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[rt][e] = (seen >> (8 * (e >> 2) + 4 * half + (e & 3))) & 1 ? s[rt][e] : -__builtin_inff();
-                softmax_tile<D>(R[rt], s[rt], P.c, 0.f, 1.f);
-                prob_parts<NP>(s[rt], p[rt]);
-            }
+            for (int e = 0; e < 16; ++e) s[e] = (seen >> (8 * (e >> 2) + 4 * half + (e & 3))) & 1 ? s[e] : -__builtin_inff();
+            softmax_tile<D>(R, s, P.c, 0.f, 1.f);
+            bf16x8 p[2][NP];
+            prob_parts<NP>(s, p);
 #pragma unroll
             for (int j = 0; j < C; ++j) {
                 bool odd = false;                            // Inf or NaN among them: zeros in the products, added below for the rows that see them
@@ -301,138 +293,173 @@ __global__ __launch_bounds__(64 * TA_WAVES, RT == 2 ? 1 : 2) void tree_attn_kern
                 for (int st = 0; st < 2; ++st)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const int node = kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3);
-                        const float v = node < P.nodes ? load1<WT>(own_v + (long long)node * P.kv_row + (32 * j + lc) * ESZ) : 0.f;
-                        const bool fine = __builtin_fabsf(v) < __builtin_inff();
-                        odd |= !fine;
-                        x[st][e] = fine ? v : 0.f;
+                        const int at = kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3);
+                        x[st][e] = at < P.nodes ? load1<WT>(own_v + (long long)at * P.kv_row + (32 * j + lc) * ESZ) : 0.f;
                     }
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool fine = __builtin_fabsf(x[st][e]) < __builtin_inff();
+                        odd |= !fine;
+                        x[st][e] = fine ? x[st][e] : 0.f;
+                    }
                     bf16x8 vf[NP];
                     split8(x[st], vf);
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
+                    for (int a = NP - 1; a >= 0; --a)
 #pragma unroll
-                        for (int a = NP - 1; a >= 0; --a)
-#pragma unroll
-                            for (int c = NP - 1 - a; c >= 0; --c) R[rt].o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[rt][st][c], R[rt].o[j], 0, 0, 0);
+                        for (int c = NP - 1 - a; c >= 0; --c) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[st][c], R.o[j], 0, 0, 0);
                 }
                 if (__ballot(odd)) {
+                    float* sp = s_p[wave];                   // probabilities by node
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        float* sp = s_p[wave];               // probabilities by node
+                    for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[e];
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
+                        const float pt = sp[t * TA_TILE + lc];
+                        const bool see = (seen >> t) & 1;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[rt][e];
-                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                        __builtin_amdgcn_wave_barrier();
-                        const unsigned seen = (unsigned)(sees[rt] >> (32 * kt));
-                        for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
-                            const float pt = sp[t * TA_TILE + lc];
-                            const bool see = (seen >> t) & 1;
-#pragma unroll
-                            for (int i2 = 0; i2 < 16; ++i2) {
-                                const float v = load1<WT>(own_v + (long long)(kt * 32 + t) * P.kv_row + (32 * j + 8 * (i2 >> 2) + 4 * half + (i2 & 3)) * ESZ);
-                                if (see && !(__builtin_fabsf(v) < __builtin_inff())) R[rt].o[j][i2] += pt * v;
-                            }
+                        for (int e = 0; e < 16; ++e) {
+                            const float v = load1<WT>(own_v + (long long)(kt * 32 + t) * P.kv_row + (32 * j + 8 * (e >> 2) + 4 * half + (e & 3)) * ESZ);
+                            if (see && !(__builtin_fabsf(v) < __builtin_inff())) R.o[j][e] += pt * v;
                         }
-                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                        __builtin_amdgcn_wave_barrier();
                     }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
                 }
             }
         }
+    }
 
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) R[rt].l += other_half(R[rt].l);
+    R.l += other_half(R.l);
     // wavefronts that share rows: the upper half of them leaves its sums in LDS, the lower half adds them
     if constexpr (WK > 1) {
         for (int n = WK / 2; n >= 1; n >>= 1) {
             if (n < WK / 2) __syncthreads();
             if (wk >= n && wk < 2 * n) {
+                float* to = s_meet + ((wk - n) * WR + wr) * part_floats<D>();
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    float* to = s_meet + (((wk - n) * WR + wr) * RT + rt) * part_floats<D>();
+                for (int j = 0; j < C; ++j)
 #pragma unroll
-                    for (int j = 0; j < C; ++j)
-#pragma unroll
-                        for (int a = 0; a < 4; ++a)
-                            *reinterpret_cast<f32x4*>(to + ((j * 4 + a) * 64 + lane) * 4) = f32x4{R[rt].o[j][4 * a], R[rt].o[j][4 * a + 1], R[rt].o[j][4 * a + 2], R[rt].o[j][4 * a + 3]};
-                    to[TA_TILE * D + lane] = R[rt].m;
-                    to[TA_TILE * D + 64 + lane] = R[rt].l;
-                }
+                    for (int a = 0; a < 4; ++a)
+                        *reinterpret_cast<f32x4*>(to + ((j * 4 + a) * 64 + lane) * 4) = f32x4{R.o[j][4 * a], R.o[j][4 * a + 1], R.o[j][4 * a + 2], R.o[j][4 * a + 3]};
+                to[TA_TILE * D + lane] = R.m;
+                to[TA_TILE * D + 64 + lane] = R.l;
             }
             __syncthreads();
             if (wk < n) {
+                const float* from = s_meet + (wk * WR + wr) * part_floats<D>();
+                f32x16 o2[C];
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const float* from = s_meet + ((wk * WR + wr) * RT + rt) * part_floats<D>();
-                    f32x16 o2[C];
+                for (int j = 0; j < C; ++j)
 #pragma unroll
-                    for (int j = 0; j < C; ++j)
+                    for (int a = 0; a < 4; ++a) {
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(from + ((j * 4 + a) * 64 + lane) * 4);
 #pragma unroll
-                        for (int a = 0; a < 4; ++a) {
-                            const f32x4 x = *reinterpret_cast<const f32x4*>(from + ((j * 4 + a) * 64 + lane) * 4);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o2[j][4 * a + e] = x[e];
-                        }
-                    merge<D>(R[rt], from[TA_TILE * D + lane], from[TA_TILE * D + 64 + lane], o2);
-                }
+                        for (int e = 0; e < 4; ++e) o2[j][4 * a + e] = x[e];
+                    }
+                merge<D>(R, from[TA_TILE * D + lane], from[TA_TILE * D + 64 + lane], o2);
             }
         }
         if (wk > 0) return;
     }
-    if (!active) return;
+    if (!active || !valid) return;
+    if (splits == 1) {
+        const size_t at = ((size_t)b * P.nodes + node) * P.n_heads + head;
+        const float inv = R.l == 0.f ? 0.f : 1.f / R.l;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int tile = tile0 + rt;
-        if (tile >= P.tiles) continue;
-        if (splits == 1) {
+        for (int j = 0; j < C; ++j)
 #pragma unroll
-            for (int j = 0; j < C; ++j) store_row<WT, D>(P, b, h, tile * TA_TILE + lc, j, R[rt].o[j], R[rt].m, R[rt].l);
-        } else {
-            float* to = P.part + (((size_t)blockIdx.x * P.heads + h) * P.tiles + tile) * part_floats<D>();
+            for (int a = 0; a < 4; ++a)
+                store4_out<WT>(P.out + (at * D + 32 * j + 8 * a + 4 * half) * ESZ, f32x4{R.o[j][4 * a], R.o[j][4 * a + 1], R.o[j][4 * a + 2], R.o[j][4 * a + 3]} * inv);
+        if (P.lse && half == 0) P.lse[at] = log_sum(R.m, R.l);
+    } else {
+        float* to = P.part + (((size_t)blockIdx.x * P.heads + h) * P.rows + row) * (D + 4);
 #pragma unroll
-            for (int j = 0; j < C; ++j)
+        for (int j = 0; j < C; ++j)
 #pragma unroll
-                for (int a = 0; a < 4; ++a)
-                    *reinterpret_cast<f32x4*>(to + ((j * 4 + a) * 64 + lane) * 4) = f32x4{R[rt].o[j][4 * a], R[rt].o[j][4 * a + 1], R[rt].o[j][4 * a + 2], R[rt].o[j][4 * a + 3]};
-            to[TA_TILE * D + lane] = R[rt].m;
-            to[TA_TILE * D + 64 + lane] = R[rt].l;
-        }
+            for (int a = 0; a < 4; ++a)
+                *reinterpret_cast<f32x4*>(to + 32 * j + 8 * a + 4 * half) = f32x4{R.o[j][4 * a], R.o[j][4 * a + 1], R.o[j][4 * a + 2], R.o[j][4 * a + 3]};
+        if (half == 0) { to[D] = R.m; to[D + 1] = R.l; }
     }
 }
 
-// The splits of one tile, 32 dims of it per wavefront
+// The splits of one row of one head: a wavefront takes every fourth split, a lane D / 64 dims
 template <typename WT, int D>
-__global__ __launch_bounds__(D * 2) void tree_attn_join_kernel(const TaParams P) {
-    const int lane = threadIdx.x & 63, j = threadIdx.x >> 6, tile = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-    const int s0 = P.split0[b], s1 = P.split0[b + 1];
-    if (s1 - s0 == 1) return;
-    const size_t step = (size_t)P.heads * P.tiles * part_floats<D>();
-    const float* from = P.part + (((size_t)s0 * P.heads + h) * P.tiles + tile) * part_floats<D>();
-    float m = -__builtin_inff();
-    for (int s = s0; s < s1; ++s) m = fmaxf(m, from[(s - s0) * step + TA_TILE * D + lane]);
-    const float base = m == -__builtin_inff() ? 0.f : m;
-    float l = 0.f;
-    f32x16 o;
+__global__ __launch_bounds__(256) void tree_attn_join_kernel(const TaParams P) {
+    constexpr int E = D / 64;
+    __shared__ float s_o[3][D], s_m[3], s_l[3];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const int s0 = P.split0[b], splits = P.split0[b + 1] - s0;
+    if (splits == 1) return;
+    const size_t step = (size_t)P.heads * P.rows * (D + 4);
+    const float* from = P.part + (((size_t)s0 * P.heads + h) * P.rows + row) * (D + 4);
+    float m = -__builtin_inff(), l = 0.f, o[E] = {};
+    // sixteen of this wavefront's splits at a time: all their sums are asked for before the first is used
+    for (int s = wave; s < splits; s += 64) {
+        float ms[16], ls[16], x[16][E];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[e] = 0.f;
-    for (int s = s0; s < s1; ++s, from += step) {
-        const float w = __builtin_amdgcn_exp2f(from[TA_TILE * D + lane] - base);
-        l += from[TA_TILE * D + 64 + lane] * w;
+        for (int u = 0; u < 16; ++u) {
+            const bool is = s + 4 * u < splits;
+            const float* at = from + (size_t)(is ? s + 4 * u : s) * step;
+            ms[u] = is ? at[D] : -__builtin_inff();
+            ls[u] = is ? at[D + 1] : 0.f;
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(from + ((j * 4 + a) * 64 + lane) * 4);
+            for (int e = 0; e < E; ++e) x[u][e] = is ? at[lane * E + e] : 0.f;
+        }
+        float top = m;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[4 * a + e] += x[e] * w;
+        for (int u = 0; u < 16; ++u) top = fmaxf(top, ms[u]);
+        const float base = top == -__builtin_inff() ? 0.f : top, w0 = __builtin_amdgcn_exp2f(m - base);
+        m = top;
+        l *= w0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= w0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            const float w = __builtin_amdgcn_exp2f(ms[u] - base);
+            l = __builtin_fmaf(ls[u], w, l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(x[u][e], w, o[e]);
         }
     }
-    store_row<WT, D>(P, b, h, tile * TA_TILE + (lane & 31), j, o, m, l);
+    if (wave) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) s_o[wave - 1][lane * E + e] = o[e];
+        if (lane == 0) { s_m[wave - 1] = m; s_l[wave - 1] = l; }
+    }
+    __syncthreads();
+    if (wave) return;
+    float top = m;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) top = fmaxf(top, s_m[w]);
+    const float base = top == -__builtin_inff() ? 0.f : top, w0 = __builtin_amdgcn_exp2f(m - base);
+    l *= w0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= w0;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) {
+        const float f = __builtin_amdgcn_exp2f(s_m[w] - base);
+        l = __builtin_fmaf(s_l[w], f, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(s_o[w][lane * E + e], f, o[e]);
+    }
+    const size_t at = ((size_t)b * P.nodes + row / P.grp) * P.n_heads + h * P.grp + row % P.grp;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if constexpr (Traits<WT>::BF) {
+        if constexpr (E == 2) *reinterpret_cast<unsigned*>(P.out + (at * D + lane * 2) * 2) = pack_bf16x2(o[0] * inv, o[1] * inv);
+        else reinterpret_cast<uint16_t*>(P.out)[at * D + lane] = (uint16_t)pack_bf16x2(o[0] * inv, 0.f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) reinterpret_cast<float*>(P.out)[at * D + lane * E + e] = o[e] * inv;
+    }
+    if (P.lse && lane == 0) P.lse[at] = log_sum(top, l);
 }
 
 // ------------------------------------------------------------------------------------------ host
-struct TaPlan { int rt, wr, groups; size_t bytes; };
+struct TaPlan { int wr, groups; size_t bytes; };
 
 int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaPlan& L) {
     if (!a || !tree || !tree->parent || !a->kv_len) return PS_ERR_NULL;
@@ -462,13 +489,13 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
         if (P.len[b] > 1 << 30) return PS_ERR_UNSUPPORTED;
         total += (P.len[b] + PC_BLOCK - 1) / PC_BLOCK;
     }
-    L.rt = a->dtype == PS_BF16 && P.tiles >= 2 ? 2 : 1;
-    const int waves = (P.tiles + L.rt - 1) / L.rt;
-    L.wr = waves >= 3 ? 4 : waves;
-    L.groups = (waves + L.wr - 1) / L.wr;
+    const int waves = a->dtype == PS_BF16 ? ta_waves<bf16_t>() : ta_waves<float>();
+    L.wr = 1;
+    while (L.wr < P.tiles && L.wr < waves) L.wr *= 2;
+    L.groups = (P.tiles + L.wr - 1) / L.wr;
+    // a workgroup for every compute unit (256), each with at least two blocks per wavefront
     const long long units = (long long)heads * L.groups;
-    const int wk = TA_WAVES / L.wr;
-    P.per = (int)std::max<long long>(2 * wk, (total * units + 767) / 768);
+    P.per = (int)std::max<long long>(2 * (waves / L.wr), (total * units + 255) / 256);
     P.split0[0] = 0;
     bool one = true;
     for (int b = 0; b < a->batch; ++b) {
@@ -477,16 +504,17 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
         P.split0[b + 1] = P.split0[b] + n;
         one &= n == 1;
     }
-    L.bytes = one ? 0 : a256((size_t)P.split0[a->batch] * heads * P.tiles * (size_t)(d == 128 ? part_floats<128>() : part_floats<64>()) * sizeof(float));
+    L.bytes = one ? 0 : a256((size_t)P.split0[a->batch] * heads * P.rows * (d + 4) * sizeof(float));
     return PS_OK;
 }
 
-template <typename WT, int D, int RT> void go(const TaParams& P, const TaPlan& L, hipStream_t s) {
-    const dim3 grid(P.split0[P.batch], P.heads, L.groups), block(64 * TA_WAVES);
-    if (L.wr == 4) hipLaunchKernelGGL((tree_attn_kernel<WT, D, RT, 4>), grid, block, 0, s, P);
-    else if (L.wr == 2) hipLaunchKernelGGL((tree_attn_kernel<WT, D, RT, 2>), grid, block, 0, s, P);
-    else hipLaunchKernelGGL((tree_attn_kernel<WT, D, RT, 1>), grid, block, 0, s, P);
-    if (L.bytes) hipLaunchKernelGGL((tree_attn_join_kernel<WT, D>), dim3(P.tiles, P.heads, P.batch), dim3(2 * D), 0, s, P);
+template <typename WT, int D> void go(const TaParams& P, const TaPlan& L, hipStream_t s) {
+    const dim3 grid(P.split0[P.batch], P.heads, L.groups), block(64 * ta_waves<WT>());
+    if (L.wr == 1) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 1>), grid, block, 0, s, P);
+    else if (L.wr == 2) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 2>), grid, block, 0, s, P);
+    else if (L.wr == 4) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 4>), grid, block, 0, s, P);
+    else if constexpr (ta_waves<WT>() == 8) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 8>), grid, block, 0, s, P);
+    if (L.bytes) hipLaunchKernelGGL((tree_attn_join_kernel<WT, D>), dim3(P.rows, P.heads, P.batch), dim3(256), 0, s, P);
 }
 
 }   // namespace
@@ -520,11 +548,8 @@ extern "C" int ps_tree_attention(const ps_tree_shape* tree, const ps_tree_attn_a
     P.k_codes = a->cache->k_codes; P.v_codes = a->cache->v_codes; P.k_scale = a->cache->k_scale; P.v_scale = a->cache->v_scale;
     P.len_dev = a->kv_len_dev;
     const hipStream_t s = (hipStream_t)stream;
-    if (a->dtype == PS_BF16) {
-        if (d == 128) { if (L.rt == 2) go<bf16_t, 128, 2>(P, L, s); else go<bf16_t, 128, 1>(P, L, s); }
-        else if (L.rt == 2) go<bf16_t, 64, 2>(P, L, s);
-        else go<bf16_t, 64, 1>(P, L, s);
-    } else if (d == 128) go<float, 128, 1>(P, L, s);
-    else go<float, 64, 1>(P, L, s);
+    if (a->dtype == PS_BF16) { if (d == 128) go<bf16_t, 128>(P, L, s); else go<bf16_t, 64>(P, L, s); }
+    else if (d == 128) go<float, 128>(P, L, s);
+    else go<float, 64>(P, L, s);
     return hipGetLastError() == hipSuccess ? PS_OK : PS_ERR_DEVICE;
 }
