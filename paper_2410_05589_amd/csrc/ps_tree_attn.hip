@@ -153,11 +153,63 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -
 // floats that a wavefront leaves in LDS: sums, then maxima and row sums
 template <int D> constexpr int part_floats() { return TA_TILE * D + 2 * 64; }
 
+// One block: the products with its keys, the softmax, the products with its values.  tail: positions of it that count (0: all)
+template <typename WT, int D, int NP> __device__ __forceinline__ void attend_block(RowState<D>& R, const bf16x8 (&q)[D / 16][NP], Tile<D>& t, float cs, float vs, int tail) {
+    constexpr int C = D / 32;
+    const int half = (threadIdx.x >> 5) & 1;
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const bf16x8 kf = widen8(word(t.k[c], 2 * u), word(t.k[c], 2 * u + 1));
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[2 * c + u][p], s, 0, 0, 0);
+        }
+    if (tail) {                                              // positions behind the end: hidden, and their codes no numbers that count
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + 4 * half + (e & 3) < tail ? s[e] : -__builtin_inff();
+        unsigned keep[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int n = min(max(tail - 8 * a - 4 * half, 0), 4);
+            keep[a] = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) t.v[c] = make_uint4(t.v[c].x & keep[0], t.v[c].y & keep[1], t.v[c].z & keep[2], t.v[c].w & keep[3]);
+    }
+    const float lv = (float)((int)(__float_as_uint(vs) >> 23) - 127);
+    softmax_tile<D>(R, s, cs, lv, __uint_as_float((254u << 23) - __float_as_uint(vs)));   // (1 / vs: a power of two)
+    bf16x8 p[2][NP];
+    prob_parts<NP>(s, p);
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            const bf16x8 vf = widen8(word(t.v[j], 2 * st), word(t.v[j], 2 * st + 1));
+#pragma unroll
+            for (int n = NP - 1; n >= 0; --n) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[st][n], R.o[j], 0, 0, 0);
+        }
+}
+
+// Four or eight tiles of rows (WR): the wavefronts read the same blocks, which come to LDS by way of the memory unit, 1 KiB per request, three steps of
+// TA_STEP blocks ahead in four buffers (arrays of their own: a read from one need not wait for what is on its way into another).
+// Each wavefront asks for an eighth of a step (and, so that all wait for as many requests, for scales: those of the first two are read).
+constexpr int TA_STEP = 2;
+typedef __attribute__((address_space(3))) void lds_void;
+template <int D> struct Stage {
+    char codes[TA_STEP * 2 * PC_BLOCK * D];
+    float scales[8][64];
+};
+
 template <typename WT, int D, int WR>
 __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_attn_kernel(const TaParams P) {
     constexpr int W = ta_waves<WT>(), WK = W / WR, NP = Traits<WT>::BF ? 1 : 3, C = D / 32, TILE = PC_BLOCK * D, ESZ = Traits<WT>::ESZ;
-    __shared__ __attribute__((aligned(16))) float s_meet[WK > 1 ? (W / 2) * part_floats<D>() : 4];
-    __shared__ float s_p[W][PC_BLOCK * TA_TILE];
+    constexpr bool STAGED = W == 8 && WR >= 4;
+    // where wavefronts that share rows meet, and before that a wavefront's probabilities of its own rows
+    __shared__ __attribute__((aligned(16))) float s_meet[WK > 1 && (W / 2) * part_floats<D>() > W * PC_BLOCK * TA_TILE ? (W / 2) * part_floats<D>() : W * PC_BLOCK * TA_TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, lc = lane & 31;
     const int wr = wave % WR, wk = wave / WR, h = blockIdx.y;
     int b = 0;
@@ -172,33 +224,48 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
     const bool valid = row < P.rows;
     const int node = valid ? row / P.grp : 0, head = h * P.grp + (valid ? row % P.grp : 0);
 
-    auto fetch = [&](int i, Tile<D>& t) {
-        const size_t at = (seq0 + (size_t)i * P.heads) * TILE + lane * 16;
+    // the tree's own values, where this workgroup takes them: in LDS by node, zeros in the place of Inf and NaN (s_odd: there were any)
+    constexpr int OWN_PITCH = D * ESZ + 4 * ESZ;
+    __shared__ __attribute__((aligned(16))) char s_own[PS_TREE_MAX_NODES * OWN_PITCH];
+    __shared__ int s_odd;
+    const bool own = P.k && split == splits - 1;
+    const char* own_k = P.k + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
+    const char* own_v = P.v + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
+    auto stage_own = [&]() __attribute__((always_inline)) {
+        if (threadIdx.x == 0) s_odd = 0;
+        __syncthreads();
+        bool odd = false;
+        const int pieces = (P.nodes + 31) / 32 * 32 * (D / 8);   // (8 elements each; nodes up to the tile's end: zeros)
+        for (int i = threadIdx.x; i < pieces; i += 64 * W) {
+            const int at = i / (D / 8), part = i % (D / 8);
+            float x[8] = {};
+            if (at < P.nodes) {
+                const char* from = own_v + (long long)at * P.kv_row + part * 8 * ESZ;
+                const f32x4 lo = load4_q<WT>(from), hi = load4_q<WT>(from + 4 * ESZ);
 #pragma unroll
-        for (int c = 0; c < C; ++c) t.k[c] = ld16(P.k_codes + at + c * 1024);
-#pragma unroll
-        for (int c = 0; c < C; ++c) t.v[c] = ld16(P.v_codes + at + c * 1024);
-    };
-    // the scales of this wavefront's next 64 blocks, one a lane
-    float k_scales = 0.f, v_scales = 0.f;
-    auto fetch_scales = [&](int i) {
-        const int mine = i + lane * WK;
-        if (mine < end) {
-            const size_t at = seq0 + (size_t)mine * P.heads;
-            k_scales = P.k_scale[at];
-            v_scales = P.v_scale[at];
+                for (int e = 0; e < 8; ++e) {
+                    const float v = e < 4 ? lo[e & 3] : hi[e & 3];
+                    const bool fine = __builtin_fabsf(v) < __builtin_inff();
+                    odd |= !fine;
+                    x[e] = fine ? v : 0.f;
+                }
+            }
+            char* to = s_own + at * OWN_PITCH + part * 8 * ESZ;
+            if constexpr (Traits<WT>::BF) {
+                *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+                *reinterpret_cast<u32x2*>(to + 8) = u32x2{pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+            } else {
+                *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
+                *reinterpret_cast<f32x4*>(to + 16) = f32x4{x[4], x[5], x[6], x[7]};
+            }
         }
+        if (odd) s_odd = 1;
     };
-    Tile<D> next;
-    int i = begin + wk;
-    const bool any = active && i < end;
-    if (any) {
-        fetch_scales(i);
-        fetch(i, next);
-    }
+    const u64 sees = own ? P.sees[node] : 0;
+
     bf16x8 q[2 * C][NP];
     RowState<D> R;
-    {
+    auto load_rows = [&]() __attribute__((always_inline)) {
         const char* from = P.q + ((long long)b * P.nodes + node) * P.q_row + (long long)head * D * ESZ;
 #pragma unroll
         for (int f = 0; f < 2 * C; ++f) load_parts<WT, NP>(from + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, active && valid, q[f]);
@@ -208,64 +275,114 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
         for (int j = 0; j < C; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) R.o[j][e] = 0.f;
-    }
-    if (any) {
-        int turn = 0;
-        for (; i < end; i += WK) {
-            Tile<D> t = next;
-            const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), turn));
-            const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), turn));
-            if (i + WK < end) {
-                fetch(i + WK, next);
-                turn = (turn + 1) & 63;
-                if (turn == 0) fetch_scales(i + WK);
+    };
+    if constexpr (STAGED) {
+        __shared__ __attribute__((aligned(16))) Stage<D> b0, b1, b2, b3;
+        constexpr int PIECES = TA_STEP * 2 * C / W;          // requests of 1 KiB per wavefront and step
+        const int steps = (end - begin + TA_STEP - 1) / TA_STEP;
+        // (offsets inside a split are 32 bits: the plan sees to that)
+        const size_t at0 = seq0 + (size_t)begin * P.heads;
+        const rsrc_t from_k = make_rsrc(P.k_codes + at0 * TILE), from_v = make_rsrc(P.v_codes + at0 * TILE);
+        const rsrc_t from_ks = make_rsrc(P.k_scale + at0), from_vs = make_rsrc(P.v_scale + at0);
+        auto request = [&](int step, Stage<D>& to) __attribute__((always_inline)) {
+            const int first = step * TA_STEP, most = end - begin - 1;
+#pragma unroll
+            for (int r = 0; r < PIECES; ++r) {
+                const int piece = wave * PIECES + r, block = min(first + piece / (2 * C), most), part = piece % (2 * C);   // keys' C pieces, then values'
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(part < C ? from_k : from_v, (lds_void*)(to.codes + piece * 1024), 16, lane * 16,
+                                                         (unsigned)block * P.heads * TILE + (part % C) * 1024, 0, 0);
             }
-            f32x16 s;
+            const unsigned off = (unsigned)min(first + lane, most) * P.heads * 4;   // (lane i: the step's block i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wave & 1 ? from_vs : from_ks, (lds_void*)to.scales[wave], 4, off, 0, 0, 0);
+        };
+        auto step = [&](int k, Stage<D>& mine, Stage<D>& last) __attribute__((always_inline)) {
+            // this step's requests have arrived (the two steps' behind it may be on their way), and everyone is done with the last one's buffer
+            if constexpr (PIECES == 2) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
+            static_assert(PIECES == 1 || PIECES == 2, "two steps of PIECES + 1 requests");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            request(k + 3, last);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = 0.f;
+            for (int turn = 0; turn < TA_STEP / WK; ++turn) {
+                const int u = turn * WK + wk, i = begin + k * TA_STEP + u;
+                if (!active || i >= end) continue;
+                Tile<D> t;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c) t.k[c] = ld16(mine.codes + (u * 2 * C + c) * 1024 + lane * 16);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const bf16x8 kf = widen8(word(t.k[c], 2 * u), word(t.k[c], 2 * u + 1));
-#pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[2 * c + u][p], s, 0, 0, 0);
-                }
-            if (tail && i == blocks - 1) {                   // positions behind the end: hidden, and their codes no numbers that count
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + 4 * half + (e & 3) < tail ? s[e] : -__builtin_inff();
-                unsigned keep[4];
-#pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    const int n = min(max(tail - 8 * a - 4 * half, 0), 4);
-                    keep[a] = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
-                }
-#pragma unroll
-                for (int c = 0; c < C; ++c) t.v[c] = make_uint4(t.v[c].x & keep[0], t.v[c].y & keep[1], t.v[c].z & keep[2], t.v[c].w & keep[3]);
+                for (int c = 0; c < C; ++c) t.v[c] = ld16(mine.codes + (u * 2 * C + C + c) * 1024 + lane * 16);
+                attend_block<WT, D, NP>(R, q, t, P.c * mine.scales[0][u], mine.scales[1][u], i == blocks - 1 ? tail : 0);
             }
-            const float lv = (float)((int)(__float_as_uint(vs) >> 23) - 127);
-            softmax_tile<D>(R, s, P.c * ks, lv, __uint_as_float((254u << 23) - __float_as_uint(vs)));   // (1 / vs: a power of two)
-            bf16x8 p[2][NP];
-            prob_parts<NP>(s, p);
+        };
+        if (steps > 0) {
+            request(0, b0);
+            request(1, b1);
+            request(2, b2);
+        }
+        load_rows();
+        if (own) stage_own();
+        for (int k = 0; k < steps;) {
+            step(k, b0, b3);
+            if (++k >= steps) break;
+            step(k, b1, b0);
+            if (++k >= steps) break;
+            step(k, b2, b1);
+            if (++k >= steps) break;
+            step(k, b3, b2);
+            ++k;
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (nothing is on its way to LDS any more)
+    } else {
+        // a wavefront's block after the current one is on its way to its registers
+        auto fetch = [&](int i, Tile<D>& t) {
+            const size_t at = (seq0 + (size_t)i * P.heads) * TILE + lane * 16;
 #pragma unroll
-            for (int j = 0; j < C; ++j)
+            for (int c = 0; c < C; ++c) t.k[c] = ld16(P.k_codes + at + c * 1024);
 #pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    const bf16x8 vf = widen8(word(t.v[j], 2 * st), word(t.v[j], 2 * st + 1));
-#pragma unroll
-                    for (int n = NP - 1; n >= 0; --n) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[st][n], R.o[j], 0, 0, 0);
+            for (int c = 0; c < C; ++c) t.v[c] = ld16(P.v_codes + at + c * 1024);
+        };
+        // the scales of its next 64 blocks, one a lane
+        float k_scales = 0.f, v_scales = 0.f;
+        auto fetch_scales = [&](int i) {
+            const int mine = i + lane * WK;
+            if (mine < end) {
+                const size_t at = seq0 + (size_t)mine * P.heads;
+                k_scales = P.k_scale[at];
+                v_scales = P.v_scale[at];
+            }
+        };
+        Tile<D> next;
+        int i = begin + wk;
+        const bool any = active && i < end;
+        if (any) {
+            fetch_scales(i);
+            fetch(i, next);
+        }
+        load_rows();
+        if (own) stage_own();
+        if (any) {
+            int turn = 0;
+            for (; i < end; i += WK) {
+                Tile<D> t = next;
+                const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), turn));
+                const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), turn));
+                if (i + WK < end) {
+                    fetch(i + WK, next);
+                    turn = (turn + 1) & 63;
+                    if (turn == 0) fetch_scales(i + WK);
                 }
+                attend_block<WT, D, NP>(R, q, t, P.c * ks, vs, i == blocks - 1 ? tail : 0);
+            }
         }
     }
 
     // the tree's own rows, in the sequence's last split: tiles of 32 nodes, which take their turn behind its blocks
-    if (active && P.k && split == splits - 1) {
-        const u64 sees = P.sees[node];
+    if (own) __syncthreads();
+    if (active && own) {
         const int behind = max(end - begin, 0);
         for (int kt = 0; kt * 32 < P.nodes; ++kt) {
             if ((behind + kt) % WK != wk) continue;
-            const char* own_k = P.k + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
-            const char* own_v = P.v + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
             f32x16 s;
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -286,49 +403,38 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
             bf16x8 p[2][NP];
             prob_parts<NP>(s, p);
 #pragma unroll
-            for (int j = 0; j < C; ++j) {
-                bool odd = false;                            // Inf or NaN among them: zeros in the products, added below for the rows that see them
-                float x[2][8];
-#pragma unroll
-                for (int st = 0; st < 2; ++st)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int at = kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3);
-                        x[st][e] = at < P.nodes ? load1<WT>(own_v + (long long)at * P.kv_row + (32 * j + lc) * ESZ) : 0.f;
-                    }
+            for (int j = 0; j < C; ++j)
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
+                    float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool fine = __builtin_fabsf(x[st][e]) < __builtin_inff();
-                        odd |= !fine;
-                        x[st][e] = fine ? x[st][e] : 0.f;
-                    }
+                    for (int e = 0; e < 8; ++e) x[e] = load1<WT>(s_own + (kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3)) * OWN_PITCH + (32 * j + lc) * ESZ);
                     bf16x8 vf[NP];
-                    split8(x[st], vf);
+                    split8(x, vf);
 #pragma unroll
                     for (int a = NP - 1; a >= 0; --a)
 #pragma unroll
                         for (int c = NP - 1 - a; c >= 0; --c) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[st][c], R.o[j], 0, 0, 0);
                 }
-                if (__ballot(odd)) {
-                    float* sp = s_p[wave];                   // probabilities by node
+            if (s_odd) {                                     // what is Inf or NaN, for the rows that see it
+                float* sp = s_meet + wave * PC_BLOCK * TA_TILE;   // probabilities by node
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[e];
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
-                    for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
-                        const float pt = sp[t * TA_TILE + lc];
-                        const bool see = (seen >> t) & 1;
+                for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[e];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
+                    const float pt = sp[t * TA_TILE + lc];
+                    const bool see = (seen >> t) & 1;
+#pragma unroll
+                    for (int j = 0; j < C; ++j)
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const float v = load1<WT>(own_v + (long long)(kt * 32 + t) * P.kv_row + (32 * j + 8 * (e >> 2) + 4 * half + (e & 3)) * ESZ);
                             if (see && !(__builtin_fabsf(v) < __builtin_inff())) R.o[j][e] += pt * v;
                         }
-                    }
-                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                    __builtin_amdgcn_wave_barrier();
                 }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
             }
         }
     }
@@ -337,7 +443,7 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
     // wavefronts that share rows: the upper half of them leaves its sums in LDS, the lower half adds them
     if constexpr (WK > 1) {
         for (int n = WK / 2; n >= 1; n >>= 1) {
-            if (n < WK / 2) __syncthreads();
+            __syncthreads();
             if (wk >= n && wk < 2 * n) {
                 float* to = s_meet + ((wk - n) * WR + wr) * part_floats<D>();
 #pragma unroll
@@ -493,14 +599,26 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
     L.wr = 1;
     while (L.wr < P.tiles && L.wr < waves) L.wr *= 2;
     L.groups = (P.tiles + L.wr - 1) / L.wr;
-    // a workgroup for every compute unit (256), each with at least two blocks per wavefront
+    // at most one workgroup for every compute unit (256) where a split has at least two blocks per wavefront: the least `per` that gives that.
+    // (Sequences of 4099 ... 12288 in one batch: with the mean of all blocks as `per` 288 workgroups, two rounds)
     const long long units = (long long)heads * L.groups;
-    P.per = (int)std::max<long long>(2 * (waves / L.wr), (total * units + 255) / 256);
+    auto count = [&](long long per) {
+        long long n = 0;
+        for (int b = 0; b < a->batch; ++b) n += std::max<long long>(1, ((P.len[b] + PC_BLOCK - 1) / PC_BLOCK + per - 1) / per);
+        return n * units;
+    };
+    // (a split's codes stay below 2 GiB)
+    long long lo = 2 * (waves / L.wr), hi = (1LL << 31) / ((long long)heads * PC_BLOCK * d);
+    const long long most = std::max<long long>(256, count(hi));
+    while (lo < hi) {
+        const long long mid = (lo + hi) / 2;
+        if (count(mid) <= most) hi = mid; else lo = mid + 1;
+    }
+    P.per = (int)lo;
     P.split0[0] = 0;
     bool one = true;
     for (int b = 0; b < a->batch; ++b) {
-        const int blocks = (P.len[b] + PC_BLOCK - 1) / PC_BLOCK;
-        const int n = std::max(1, (blocks + P.per - 1) / P.per);
+        const int n = std::max(1, ((P.len[b] + PC_BLOCK - 1) / PC_BLOCK + P.per - 1) / P.per);
         P.split0[b + 1] = P.split0[b] + n;
         one &= n == 1;
     }
