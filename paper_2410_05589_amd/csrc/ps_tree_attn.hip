@@ -212,8 +212,7 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
     __shared__ __attribute__((aligned(16))) float s_meet[WK > 1 && (W / 2) * part_floats<D>() > W * PC_BLOCK * TA_TILE ? (W / 2) * part_floats<D>() : W * PC_BLOCK * TA_TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, lc = lane & 31;
     const int wr = wave % WR, wk = wave / WR, h = blockIdx.y;
-    int b = 0;
-    while ((int)blockIdx.x >= P.split0[b + 1]) ++b;
+    const int b = __popcll(__ballot(lane < P.batch && P.split0[lane + 1] <= (int)blockIdx.x));   // the sequence whose split this is
     const int split = blockIdx.x - P.split0[b], splits = P.split0[b + 1] - P.split0[b];
     const int len = pc_length(P.len_dev, b, P.len[b]), blocks = (len + 31) >> 5, tail = len & 31;
     const int tile = (int)blockIdx.z * WR + wr;              // this wavefront's rows
@@ -276,6 +275,73 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
 #pragma unroll
             for (int e = 0; e < 16; ++e) R.o[j][e] = 0.f;
     };
+    // the tree's own rows, in the sequence's last split, while the first blocks are on their way: tiles of 32 nodes, from the last wavefront on
+    auto own_rows = [&]() __attribute__((always_inline)) {
+        bf16x8 k0[2 * C][NP];
+        auto load_keys = [&](int kt) __attribute__((always_inline)) {
+            const int key = kt * 32 + lc;
+#pragma unroll
+            for (int f = 0; f < 2 * C; ++f)
+                load_parts<WT, NP>(own_k + (long long)key * P.kv_row + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, key < P.nodes, k0[f]);
+        };
+        const int first = (WK - 1 - wk) % WK;
+        load_keys(first);
+        stage_own();
+        __syncthreads();
+        if (!active) return;
+        for (int kt = first; kt * 32 < P.nodes; kt += WK) {
+            if (kt != first) load_keys(kt);
+            f32x16 s;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+            for (int f = 0; f < 2 * C; ++f)
+#pragma unroll
+                for (int x = NP - 1; x >= 0; --x)            // (parts whose product is below 2^-24 of the whole are left out)
+#pragma unroll
+                    for (int y = NP - 1 - x; y >= 0; --y) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0[f][x], q[f][y], s, 0, 0, 0);
+            const unsigned seen = (unsigned)(sees >> (32 * kt));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = (seen >> (8 * (e >> 2) + 4 * half + (e & 3))) & 1 ? s[e] : -__builtin_inff();
+            softmax_tile<D>(R, s, P.c, 0.f, 1.f);
+            bf16x8 p[2][NP];
+            prob_parts<NP>(s, p);
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = load1<WT>(s_own + (kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3)) * OWN_PITCH + (32 * j + lc) * ESZ);
+                    bf16x8 vf[NP];
+                    split8(x, vf);
+#pragma unroll
+                    for (int a = NP - 1; a >= 0; --a)
+#pragma unroll
+                        for (int c = NP - 1 - a; c >= 0; --c) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[st][c], R.o[j], 0, 0, 0);
+                }
+            if (s_odd) {                                     // what is Inf or NaN, for the rows that see it
+                float* sp = s_meet + wave * PC_BLOCK * TA_TILE;   // probabilities by node
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[e];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
+                    const float pt = sp[t * TA_TILE + lc];
+                    const bool see = (seen >> t) & 1;
+#pragma unroll
+                    for (int j = 0; j < C; ++j)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float v = load1<WT>(own_v + (long long)(kt * 32 + t) * P.kv_row + (32 * j + 8 * (e >> 2) + 4 * half + (e & 3)) * ESZ);
+                            if (see && !(__builtin_fabsf(v) < __builtin_inff())) R.o[j][e] += pt * v;
+                        }
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+    };
     if constexpr (STAGED) {
         __shared__ __attribute__((aligned(16))) Stage<D> b0, b1, b2, b3;
         constexpr int PIECES = TA_STEP * 2 * C / W;          // requests of 1 KiB per wavefront and step
@@ -321,7 +387,7 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
             request(2, b2);
         }
         load_rows();
-        if (own) stage_own();
+        if (own) own_rows();
         for (int k = 0; k < steps;) {
             step(k, b0, b3);
             if (++k >= steps) break;
@@ -338,9 +404,9 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
         auto fetch = [&](int i, Tile<D>& t) {
             const size_t at = (seq0 + (size_t)i * P.heads) * TILE + lane * 16;
 #pragma unroll
-            for (int c = 0; c < C; ++c) t.k[c] = ld16(P.k_codes + at + c * 1024);
+            for (int c = 0; c < C; ++c) t.k[c] = WR == 1 ? ldg_stream16(P.k_codes + at + c * 1024) : ld16(P.k_codes + at + c * 1024);
 #pragma unroll
-            for (int c = 0; c < C; ++c) t.v[c] = ld16(P.v_codes + at + c * 1024);
+            for (int c = 0; c < C; ++c) t.v[c] = WR == 1 ? ldg_stream16(P.v_codes + at + c * 1024) : ld16(P.v_codes + at + c * 1024);
         };
         // the scales of its next 64 blocks, one a lane
         float k_scales = 0.f, v_scales = 0.f;
@@ -360,7 +426,7 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
             fetch(i, next);
         }
         load_rows();
-        if (own) stage_own();
+        if (own) own_rows();
         if (any) {
             int turn = 0;
             for (; i < end; i += WK) {
@@ -377,74 +443,12 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
         }
     }
 
-    // the tree's own rows, in the sequence's last split: tiles of 32 nodes, which take their turn behind its blocks
-    if (own) __syncthreads();
-    if (active && own) {
-        const int behind = max(end - begin, 0);
-        for (int kt = 0; kt * 32 < P.nodes; ++kt) {
-            if ((behind + kt) % WK != wk) continue;
-            f32x16 s;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = 0.f;
-            const int key = kt * 32 + lc;
-#pragma unroll
-            for (int f = 0; f < 2 * C; ++f) {
-                bf16x8 kf[NP];
-                load_parts<WT, NP>(own_k + (long long)key * P.kv_row + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, key < P.nodes, kf);
-#pragma unroll
-                for (int x = NP - 1; x >= 0; --x)            // (parts whose product is below 2^-24 of the whole are left out)
-#pragma unroll
-                    for (int y = NP - 1 - x; y >= 0; --y) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], q[f][y], s, 0, 0, 0);
-            }
-            const unsigned seen = (unsigned)(sees >> (32 * kt));
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = (seen >> (8 * (e >> 2) + 4 * half + (e & 3))) & 1 ? s[e] : -__builtin_inff();
-            softmax_tile<D>(R, s, P.c, 0.f, 1.f);
-            bf16x8 p[2][NP];
-            prob_parts<NP>(s, p);
-#pragma unroll
-            for (int j = 0; j < C; ++j)
-#pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = load1<WT>(s_own + (kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3)) * OWN_PITCH + (32 * j + lc) * ESZ);
-                    bf16x8 vf[NP];
-                    split8(x, vf);
-#pragma unroll
-                    for (int a = NP - 1; a >= 0; --a)
-#pragma unroll
-                        for (int c = NP - 1 - a; c >= 0; --c) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[st][c], R.o[j], 0, 0, 0);
-                }
-            if (s_odd) {                                     // what is Inf or NaN, for the rows that see it
-                float* sp = s_meet + wave * PC_BLOCK * TA_TILE;   // probabilities by node
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[e];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
-                    const float pt = sp[t * TA_TILE + lc];
-                    const bool see = (seen >> t) & 1;
-#pragma unroll
-                    for (int j = 0; j < C; ++j)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float v = load1<WT>(own_v + (long long)(kt * 32 + t) * P.kv_row + (32 * j + 8 * (e >> 2) + 4 * half + (e & 3)) * ESZ);
-                            if (see && !(__builtin_fabsf(v) < __builtin_inff())) R.o[j][e] += pt * v;
-                        }
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
-        }
-    }
-
     R.l += other_half(R.l);
     // wavefronts that share rows: the upper half of them leaves its sums in LDS, the lower half adds them
     if constexpr (WK > 1) {
         for (int n = WK / 2; n >= 1; n >>= 1) {
             __syncthreads();
-            if (wk >= n && wk < 2 * n) {
+            if (wk >= n && wk < 2 * n && valid) {
                 float* to = s_meet + ((wk - n) * WR + wr) * part_floats<D>();
 #pragma unroll
                 for (int j = 0; j < C; ++j)
@@ -455,7 +459,7 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
                 to[TA_TILE * D + 64 + lane] = R.l;
             }
             __syncthreads();
-            if (wk < n) {
+            if (wk < n && valid) {
                 const float* from = s_meet + (wk * WR + wr) * part_floats<D>();
                 f32x16 o2[C];
 #pragma unroll
@@ -492,65 +496,41 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
     }
 }
 
-// The splits of one row of one head: a wavefront takes every fourth split, a lane D / 64 dims
+// The splits of one row of one head: a wavefront, a lane has D / 64 dims
 template <typename WT, int D>
 __global__ __launch_bounds__(256) void tree_attn_join_kernel(const TaParams P) {
-    constexpr int E = D / 64;
-    __shared__ float s_o[3][D], s_m[3], s_l[3];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    constexpr int E = D / 64, AHEAD = 8;
+    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y, b = blockIdx.z;
     const int s0 = P.split0[b], splits = P.split0[b + 1] - s0;
-    if (splits == 1) return;
+    if (splits == 1 || row >= P.rows) return;
     const size_t step = (size_t)P.heads * P.rows * (D + 4);
     const float* from = P.part + (((size_t)s0 * P.heads + h) * P.rows + row) * (D + 4);
     float m = -__builtin_inff(), l = 0.f, o[E] = {};
-    // sixteen of this wavefront's splits at a time: all their sums are asked for before the first is used
-    for (int s = wave; s < splits; s += 64) {
-        float ms[16], ls[16], x[16][E];
+    for (int s = 0; s < splits; s += AHEAD) {               // (as many splits' sums at a time: all asked for before the first is used)
+        float ms[AHEAD], ls[AHEAD], x[AHEAD][E];
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            const bool is = s + 4 * u < splits;
-            const float* at = from + (size_t)(is ? s + 4 * u : s) * step;
-            ms[u] = is ? at[D] : -__builtin_inff();
-            ls[u] = is ? at[D + 1] : 0.f;
+        for (int u = 0; u < AHEAD; ++u) {
+            const float* at = from + (size_t)min(s + u, splits - 1) * step;
+            ms[u] = at[D];
+            ls[u] = at[D + 1];
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[u][e] = is ? at[lane * E + e] : 0.f;
+            for (int e = 0; e < E; ++e) x[u][e] = at[lane * E + e];
         }
         float top = m;
 #pragma unroll
-        for (int u = 0; u < 16; ++u) top = fmaxf(top, ms[u]);
+        for (int u = 0; u < AHEAD; ++u) top = fmaxf(top, ms[u]);
         const float base = top == -__builtin_inff() ? 0.f : top, w0 = __builtin_amdgcn_exp2f(m - base);
         m = top;
         l *= w0;
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] *= w0;
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
-            const float w = __builtin_amdgcn_exp2f(ms[u] - base);
+        for (int u = 0; u < AHEAD; ++u) {
+            const float w = s + u < splits ? __builtin_amdgcn_exp2f(ms[u] - base) : 0.f;
             l = __builtin_fmaf(ls[u], w, l);
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(x[u][e], w, o[e]);
         }
-    }
-    if (wave) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) s_o[wave - 1][lane * E + e] = o[e];
-        if (lane == 0) { s_m[wave - 1] = m; s_l[wave - 1] = l; }
-    }
-    __syncthreads();
-    if (wave) return;
-    float top = m;
-#pragma unroll
-    for (int w = 0; w < 3; ++w) top = fmaxf(top, s_m[w]);
-    const float base = top == -__builtin_inff() ? 0.f : top, w0 = __builtin_amdgcn_exp2f(m - base);
-    l *= w0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] *= w0;
-#pragma unroll
-    for (int w = 0; w < 3; ++w) {
-        const float f = __builtin_amdgcn_exp2f(s_m[w] - base);
-        l = __builtin_fmaf(s_l[w], f, l);
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(s_o[w][lane * E + e], f, o[e]);
     }
     const size_t at = ((size_t)b * P.nodes + row / P.grp) * P.n_heads + h * P.grp + row % P.grp;
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -561,7 +541,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(const TaParams P) {
 #pragma unroll
         for (int e = 0; e < E; ++e) reinterpret_cast<float*>(P.out)[at * D + lane * E + e] = o[e] * inv;
     }
-    if (P.lse && lane == 0) P.lse[at] = log_sum(top, l);
+    if (P.lse && lane == 0) P.lse[at] = log_sum(m, l);
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -632,7 +612,7 @@ template <typename WT, int D> void go(const TaParams& P, const TaPlan& L, hipStr
     else if (L.wr == 2) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 2>), grid, block, 0, s, P);
     else if (L.wr == 4) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 4>), grid, block, 0, s, P);
     else if constexpr (ta_waves<WT>() == 8) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 8>), grid, block, 0, s, P);
-    if (L.bytes) hipLaunchKernelGGL((tree_attn_join_kernel<WT, D>), dim3(P.rows, P.heads, P.batch), dim3(256), 0, s, P);
+    if (L.bytes) hipLaunchKernelGGL((tree_attn_join_kernel<WT, D>), dim3((P.rows + 3) / 4, P.heads, P.batch), dim3(256), 0, s, P);
 }
 
 }   // namespace
