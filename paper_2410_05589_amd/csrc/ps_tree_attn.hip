@@ -8,7 +8,7 @@
 // codes go from memory to the matrix cores through a conversion (two codes an instruction), with no exchange between lanes and no LDS.
 // The running maximum is raised only when a score passes it by 2^8 (sums stay far inside float32), so sums are rarely rescaled.
 //
-// Work: a sequence's blocks are cut into splits of `per` blocks; a workgroup takes a split of one kv head for up to 256 rows
+// Work: a sequence's blocks are cut into splits of `per` blocks; a workgroup takes a split of one kv head for up to 128 rows
 // (a row is a node and one of the heads that share the kv head), a wavefront 32 of them.  Its wavefronts divide rows (WR) and blocks (WK); those
 // that share rows meet in LDS, splits in the workspace and a second kernel.
 #include <hip/hip_runtime.h>
@@ -19,8 +19,9 @@
 namespace {
 
 constexpr int TA_TILE = 32;
-// wavefronts of a workgroup: two per SIMD, so that one's matrix instructions run beside the other's exponentials; float32 has three parts of every query
-template <typename WT> constexpr int ta_waves() { return Traits<WT>::BF ? 8 : 4; }
+// wavefronts of a workgroup.  bf16: two per SIMD, so that one's matrix instructions run beside the other's exponentials, of one workgroup or, where
+// wavefronts wait for each other's requests (WR 4), of two; float32 has three parts of every query and one wavefront per SIMD
+template <typename WT, int WR> constexpr int ta_waves() { return Traits<WT>::BF && WR < 4 ? 8 : 4; }
 constexpr float TA_LAZY = 8.f;      // how far (in powers of two) scores may pass the maximum that they are taken against
 
 struct TaParams {
@@ -32,6 +33,7 @@ struct TaParams {
     long long q_row, kv_row;        // bytes between rows
     int n_heads, heads, grp, nodes, rows, tiles;   // rows = nodes * grp; tiles of 32 of them
     int batch, per;                 // blocks per split
+    int stream;                     // codes pass the caches by
     float c;                        // scale * log2(e)
     const int* len_dev;
     unsigned first[PC_SEQS];
@@ -103,11 +105,16 @@ template <int D> struct RowState {
 
 // One tile of 32 keys: scores (raw products) to probabilities against the running maximum.  c: what makes products powers of two; lv: log2 of
 // the values' scale, which the probabilities that meet codes carry
-template <int D> __device__ __forceinline__ void softmax_tile(RowState<D>& R, f32x16& s, float c, float lv, float inv_vs) {
-    float mx = s[0];
+template <int D, int NB> __device__ __forceinline__ void raise_maximum(RowState<D>& R, const f32x16 (&s)[NB], const float (&c)[NB]) {
+    float mx = -__builtin_inff();
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    mx = fmaxf(mx, other_half(mx)) * c;
+    for (int n = 0; n < NB; ++n) {
+        float x = s[n][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) x = fmaxf(x, s[n][i]);
+        mx = fmaxf(mx, x * c[n]);
+    }
+    mx = fmaxf(mx, other_half(mx));
     if (__ballot(mx > R.m + TA_LAZY)) {
         const float m = fmaxf(R.m, mx), alpha = m > R.m ? __builtin_amdgcn_exp2f(R.m - m) : 1.f;
         R.m = m;
@@ -115,6 +122,8 @@ template <int D> __device__ __forceinline__ void softmax_tile(RowState<D>& R, f3
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) R.o[j] *= alpha;
     }
+}
+template <int D> __device__ __forceinline__ void exponentials(RowState<D>& R, f32x16& s, float c, float lv, float inv_vs) {
     const float off = (R.m == -__builtin_inff() ? 0.f : R.m) - lv;
     float sum = 0.f;
 #pragma unroll
@@ -153,63 +162,95 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -
 // floats that a wavefront leaves in LDS: sums, then maxima and row sums
 template <int D> constexpr int part_floats() { return TA_TILE * D + 2 * 64; }
 
-// One block: the products with its keys, the softmax, the products with its values.  tail: positions of it that count (0: all)
-template <typename WT, int D, int NP> __device__ __forceinline__ void attend_block(RowState<D>& R, const bf16x8 (&q)[D / 16][NP], Tile<D>& t, float cs, float vs, int tail) {
-    constexpr int C = D / 32;
-    const int half = (threadIdx.x >> 5) & 1;
-    f32x16 s;
+// The parts of a block's attention: products with its keys, ...
+template <int D, int NP> __device__ __forceinline__ void key_products(const bf16x8 (&q)[D / 16][NP], const uint4 (&k)[D / 32], f32x16& s) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const bf16x8 kf = widen8(word(t.k[c], 2 * u), word(t.k[c], 2 * u + 1));
+            const bf16x8 kf = widen8(word(k[c], 2 * u), word(k[c], 2 * u + 1));
 #pragma unroll
             for (int p = NP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[2 * c + u][p], s, 0, 0, 0);
         }
-    if (tail) {                                              // positions behind the end: hidden, and their codes no numbers that count
+}
+// ... positions from `tail` on hidden, and their codes, which may be no numbers, zero, ...
+template <int D> __device__ __forceinline__ void hide(f32x16& s, uint4 (&v)[D / 32], int tail) {
+    const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + 4 * half + (e & 3) < tail ? s[e] : -__builtin_inff();
-        unsigned keep[4];
+    for (int e = 0; e < 16; ++e) s[e] = 8 * (e >> 2) + 4 * half + (e & 3) < tail ? s[e] : -__builtin_inff();
+    unsigned keep[4];
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const int n = min(max(tail - 8 * a - 4 * half, 0), 4);
-            keep[a] = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
-        }
-#pragma unroll
-        for (int c = 0; c < C; ++c) t.v[c] = make_uint4(t.v[c].x & keep[0], t.v[c].y & keep[1], t.v[c].z & keep[2], t.v[c].w & keep[3]);
+    for (int a = 0; a < 4; ++a) {
+        const int n = min(max(tail - 8 * a - 4 * half, 0), 4);
+        keep[a] = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
     }
-    const float lv = (float)((int)(__float_as_uint(vs) >> 23) - 127);
-    softmax_tile<D>(R, s, cs, lv, __uint_as_float((254u << 23) - __float_as_uint(vs)));   // (1 / vs: a power of two)
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) v[c] = make_uint4(v[c].x & keep[0], v[c].y & keep[1], v[c].z & keep[2], v[c].w & keep[3]);
+}
+// ... products with its values
+template <int D, int NP> __device__ __forceinline__ void value_products(RowState<D>& R, const f32x16& s, const uint4 (&v)[D / 32]) {
     bf16x8 p[2][NP];
     prob_parts<NP>(s, p);
 #pragma unroll
-    for (int j = 0; j < C; ++j)
+    for (int j = 0; j < D / 32; ++j)
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-            const bf16x8 vf = widen8(word(t.v[j], 2 * st), word(t.v[j], 2 * st + 1));
+            const bf16x8 vf = widen8(word(v[j], 2 * st), word(v[j], 2 * st + 1));
 #pragma unroll
             for (int n = NP - 1; n >= 0; --n) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[st][n], R.o[j], 0, 0, 0);
         }
 }
+__device__ __forceinline__ float log2_of(float scale) { return (float)((int)(__float_as_uint(scale) >> 23) - 127); }   // (powers of two)
+__device__ __forceinline__ float one_over(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }
 
-// Four or eight tiles of rows (WR): the wavefronts read the same blocks, which come to LDS by way of the memory unit, 1 KiB per request, three steps of
-// TA_STEP blocks ahead in four buffers (arrays of their own: a read from one need not wait for what is on its way into another).
-// Each wavefront asks for an eighth of a step (and, so that all wait for as many requests, for scales: those of the first two are read).
+// Three tiles of rows and more: four wavefronts read the same blocks, which come to LDS by way of the memory unit, 1 KiB per request, two steps of
+// TA_STEP blocks ahead in three buffers (arrays of their own: a read from one need not wait for what is on its way into another).  A step's
+// blocks are taken together: two chains of products, one look at the maximum.  Each wavefront asks for a quarter of a step
+// (and, so that all wait for as many requests, for scales: those of the first two are read).
 constexpr int TA_STEP = 2;
 typedef __attribute__((address_space(3))) void lds_void;
 template <int D> struct Stage {
     char codes[TA_STEP * 2 * PC_BLOCK * D];
-    float scales[8][64];
+    float scales[4][64];
 };
 
+// the sums of a tile to and from LDS
+template <int D> __device__ __forceinline__ void leave(float* to, const RowState<D>& R) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+            *reinterpret_cast<f32x4*>(to + ((j * 4 + a) * 64 + lane) * 4) = f32x4{R.o[j][4 * a], R.o[j][4 * a + 1], R.o[j][4 * a + 2], R.o[j][4 * a + 3]};
+    to[TA_TILE * D + lane] = R.m;
+    to[TA_TILE * D + 64 + lane] = R.l;
+}
+template <int D> __device__ __forceinline__ void join(RowState<D>& R, const float* from) {
+    const int lane = threadIdx.x & 63;
+    f32x16 o2[D / 32];
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(from + ((j * 4 + a) * 64 + lane) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o2[j][4 * a + e] = x[e];
+        }
+    merge<D>(R, from[TA_TILE * D + lane], from[TA_TILE * D + 64 + lane], o2);
+}
+
 template <typename WT, int D, int WR>
-__global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_attn_kernel(const TaParams P) {
-    constexpr int W = ta_waves<WT>(), WK = W / WR, NP = Traits<WT>::BF ? 1 : 3, C = D / 32, TILE = PC_BLOCK * D, ESZ = Traits<WT>::ESZ;
-    constexpr bool STAGED = W == 8 && WR >= 4;
-    // where wavefronts that share rows meet, and before that a wavefront's probabilities of its own rows
-    __shared__ __attribute__((aligned(16))) float s_meet[WK > 1 && (W / 2) * part_floats<D>() > W * PC_BLOCK * TA_TILE ? (W / 2) * part_floats<D>() : W * PC_BLOCK * TA_TILE];
+__global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)) void tree_attn_kernel(const TaParams P) {
+    constexpr int W = ta_waves<WT, WR>(), WK = W / WR, NP = Traits<WT>::BF ? 1 : 3, C = D / 32, TILE = PC_BLOCK * D, ESZ = Traits<WT>::ESZ;
+    constexpr bool STAGED = Traits<WT>::BF && WR == 4;
+    // where wavefronts that share rows meet, and before that a wavefront's probabilities of its own rows (staged, where it is large enough: the
+    // buffer that is requested last)
+    constexpr bool OWN_IN_BUFFER = STAGED && sizeof(Stage<D>::codes) >= W * PC_BLOCK * TA_TILE * 4;
+    constexpr int MEET = WK > 1 ? (W / 2) * part_floats<D>() : 4, OWN_P = OWN_IN_BUFFER ? 4 : W * PC_BLOCK * TA_TILE;
+    __shared__ __attribute__((aligned(16))) float s_meet[MEET > OWN_P ? MEET : OWN_P];
+    __shared__ __attribute__((aligned(16))) Stage<STAGED ? D : 0> b0, b1, b2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, lc = lane & 31;
     const int wr = wave % WR, wk = wave / WR, h = blockIdx.y;
     const int b = __popcll(__ballot(lane < P.batch && P.split0[lane + 1] <= (int)blockIdx.x));   // the sequence whose split this is
@@ -219,15 +260,16 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
     const bool active = tile < P.tiles;
     const int begin = split * P.per, end = min(blocks, begin + P.per);
     const size_t seq0 = (size_t)P.first[b] * P.heads + h;
+    const bool own = P.k && split == splits - 1;             // the tree's own rows are this workgroup's
     const int row = tile * TA_TILE + lc;
     const bool valid = row < P.rows;
     const int node = valid ? row / P.grp : 0, head = h * P.grp + (valid ? row % P.grp : 0);
+    const u64 sees = own ? P.sees[node] : 0;
 
     // the tree's own values, where this workgroup takes them: in LDS by node, zeros in the place of Inf and NaN (s_odd: there were any)
     constexpr int OWN_PITCH = D * ESZ + 4 * ESZ;
     __shared__ __attribute__((aligned(16))) char s_own[PS_TREE_MAX_NODES * OWN_PITCH];
     __shared__ int s_odd;
-    const bool own = P.k && split == splits - 1;
     const char* own_k = P.k + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
     const char* own_v = P.v + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
     auto stage_own = [&]() __attribute__((always_inline)) {
@@ -260,14 +302,13 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
         }
         if (odd) s_odd = 1;
     };
-    const u64 sees = own ? P.sees[node] : 0;
 
     bf16x8 q[2 * C][NP];
     RowState<D> R;
     auto load_rows = [&]() __attribute__((always_inline)) {
         const char* from = P.q + ((long long)b * P.nodes + node) * P.q_row + (long long)head * D * ESZ;
 #pragma unroll
-        for (int f = 0; f < 2 * C; ++f) load_parts<WT, NP>(from + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, active && valid, q[f]);
+        for (int f = 0; f < 2 * C; ++f) load_parts<WT, NP>(from + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, valid, q[f]);
         R.m = -__builtin_inff();
         R.l = 0.f;
 #pragma unroll
@@ -291,59 +332,63 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
         if (!active) return;
         for (int kt = first; kt * 32 < P.nodes; kt += WK) {
             if (kt != first) load_keys(kt);
-            f32x16 s;
+            {
+                f32x16 s;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = 0.f;
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-            for (int f = 0; f < 2 * C; ++f)
+                for (int f = 0; f < 2 * C; ++f)
 #pragma unroll
-                for (int x = NP - 1; x >= 0; --x)            // (parts whose product is below 2^-24 of the whole are left out)
+                    for (int x = NP - 1; x >= 0; --x)        // (parts whose product is below 2^-24 of the whole are left out)
 #pragma unroll
-                    for (int y = NP - 1 - x; y >= 0; --y) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0[f][x], q[f][y], s, 0, 0, 0);
-            const unsigned seen = (unsigned)(sees >> (32 * kt));
+                        for (int y = NP - 1 - x; y >= 0; --y) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0[f][x], q[f][y], s, 0, 0, 0);
+                const unsigned seen = (unsigned)(sees >> (32 * kt));
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = (seen >> (8 * (e >> 2) + 4 * half + (e & 3))) & 1 ? s[e] : -__builtin_inff();
-            softmax_tile<D>(R, s, P.c, 0.f, 1.f);
-            bf16x8 p[2][NP];
-            prob_parts<NP>(s, p);
+                for (int e = 0; e < 16; ++e) s[e] = (seen >> (8 * (e >> 2) + 4 * half + (e & 3))) & 1 ? s[e] : -__builtin_inff();
+                f32x16 one[1] = {s};
+                const float c1[1] = {P.c};
+                raise_maximum<D, 1>(R, one, c1);
+                exponentials<D>(R, s, P.c, 0.f, 1.f);
+                bf16x8 p[2][NP];
+                prob_parts<NP>(s, p);
 #pragma unroll
-            for (int j = 0; j < C; ++j)
+                for (int j = 0; j < C; ++j)
 #pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    float x[8];
+                    for (int st = 0; st < 2; ++st) {
+                        float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = load1<WT>(s_own + (kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3)) * OWN_PITCH + (32 * j + lc) * ESZ);
-                    bf16x8 vf[NP];
-                    split8(x, vf);
+                        for (int e = 0; e < 8; ++e) x[e] = load1<WT>(s_own + (kt * 32 + 8 * (2 * st + (e >> 2)) + 4 * half + (e & 3)) * OWN_PITCH + (32 * j + lc) * ESZ);
+                        bf16x8 vf[NP];
+                        split8(x, vf);
 #pragma unroll
-                    for (int a = NP - 1; a >= 0; --a)
+                        for (int a = NP - 1; a >= 0; --a)
 #pragma unroll
-                        for (int c = NP - 1 - a; c >= 0; --c) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[st][c], R.o[j], 0, 0, 0);
+                            for (int c = NP - 1 - a; c >= 0; --c) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[st][c], R.o[j], 0, 0, 0);
+                    }
+                if (s_odd) {                                 // what is Inf or NaN, for the rows that see it
+                    float* sp = (OWN_IN_BUFFER ? reinterpret_cast<float*>(b2.codes) : s_meet) + wave * PC_BLOCK * TA_TILE;   // probabilities by node
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[e];
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                    for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
+                        const float pt = sp[t * TA_TILE + lc];
+                        const bool see = (seen >> t) & 1;
+#pragma unroll
+                        for (int j = 0; j < C; ++j)
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const float v = load1<WT>(own_v + (long long)(kt * 32 + t) * P.kv_row + (32 * j + 8 * (e >> 2) + 4 * half + (e & 3)) * ESZ);
+                                if (see && !(__builtin_fabsf(v) < __builtin_inff())) R.o[j][e] += pt * v;
+                            }
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
                 }
-            if (s_odd) {                                     // what is Inf or NaN, for the rows that see it
-                float* sp = s_meet + wave * PC_BLOCK * TA_TILE;   // probabilities by node
-#pragma unroll
-                for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[e];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                for (int t = 0; t < 32 && kt * 32 + t < P.nodes; ++t) {
-                    const float pt = sp[t * TA_TILE + lc];
-                    const bool see = (seen >> t) & 1;
-#pragma unroll
-                    for (int j = 0; j < C; ++j)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float v = load1<WT>(own_v + (long long)(kt * 32 + t) * P.kv_row + (32 * j + 8 * (e >> 2) + 4 * half + (e & 3)) * ESZ);
-                            if (see && !(__builtin_fabsf(v) < __builtin_inff())) R.o[j][e] += pt * v;
-                        }
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
             }
         }
     };
     if constexpr (STAGED) {
-        __shared__ __attribute__((aligned(16))) Stage<D> b0, b1, b2, b3;
         constexpr int PIECES = TA_STEP * 2 * C / W;          // requests of 1 KiB per wavefront and step
         const int steps = (end - begin + TA_STEP - 1) / TA_STEP;
         // (offsets inside a split are 32 bits: the plan sees to that)
@@ -362,40 +407,56 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
             __builtin_amdgcn_raw_ptr_buffer_load_lds(wave & 1 ? from_vs : from_ks, (lds_void*)to.scales[wave], 4, off, 0, 0, 0);
         };
         auto step = [&](int k, Stage<D>& mine, Stage<D>& last) __attribute__((always_inline)) {
-            // this step's requests have arrived (the two steps' behind it may be on their way), and everyone is done with the last one's buffer
-            if constexpr (PIECES == 2) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)" ::: "memory");
-            else asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
-            static_assert(PIECES == 1 || PIECES == 2, "two steps of PIECES + 1 requests");
+            // this step's requests have arrived (the step's behind it may be on their way), and everyone is done with the last one's buffer
+            static_assert(PIECES == 2 || PIECES == 4, "one step of PIECES + 1 requests");
+            if constexpr (PIECES == 4) asm volatile("s_waitcnt vmcnt(5) lgkmcnt(0)" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(3) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
-            request(k + 3, last);
+            request(k + 2, last);
+            const int i = begin + k * TA_STEP;
+            if (!active) return;
+            f32x16 x[2];
+            uint4 t[2][C];
+            float cs[2], vs[2];
 #pragma unroll
-            for (int turn = 0; turn < TA_STEP / WK; ++turn) {
-                const int u = turn * WK + wk, i = begin + k * TA_STEP + u;
-                if (!active || i >= end) continue;
-                Tile<D> t;
+            for (int n = 0; n < 2; ++n) {
 #pragma unroll
-                for (int c = 0; c < C; ++c) t.k[c] = ld16(mine.codes + (u * 2 * C + c) * 1024 + lane * 16);
+                for (int c = 0; c < C; ++c) t[n][c] = ld16(mine.codes + (n * 2 * C + c) * 1024 + lane * 16);
+                cs[n] = P.c * mine.scales[0][n];
+                vs[n] = mine.scales[1][n];
+            }
 #pragma unroll
-                for (int c = 0; c < C; ++c) t.v[c] = ld16(mine.codes + (u * 2 * C + C + c) * 1024 + lane * 16);
-                attend_block<WT, D, NP>(R, q, t, P.c * mine.scales[0][u], mine.scales[1][u], i == blocks - 1 ? tail : 0);
+            for (int n = 0; n < 2; ++n) key_products<D, NP>(q, t[n], x[n]);
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int c = 0; c < C; ++c) t[n][c] = ld16(mine.codes + (n * 2 * C + C + c) * 1024 + lane * 16);
+            if (i + 2 >= end) {                              // (the second one may be behind the split's end, either the sequence's last)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                    if (i + n >= end) hide<D>(x[n], t[n], 0);
+                    else if (tail && i + n == blocks - 1) hide<D>(x[n], t[n], tail);
+            }
+            raise_maximum<D, 2>(R, x, cs);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                exponentials<D>(R, x[n], cs[n], log2_of(vs[n]), one_over(vs[n]));
+                value_products<D, NP>(R, x[n], t[n]);
             }
         };
         if (steps > 0) {
             request(0, b0);
             request(1, b1);
-            request(2, b2);
         }
         load_rows();
         if (own) own_rows();
         for (int k = 0; k < steps;) {
-            step(k, b0, b3);
+            step(k, b0, b2);
             if (++k >= steps) break;
             step(k, b1, b0);
             if (++k >= steps) break;
             step(k, b2, b1);
-            if (++k >= steps) break;
-            step(k, b3, b2);
             ++k;
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (nothing is on its way to LDS any more)
@@ -403,10 +464,17 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
         // a wavefront's block after the current one is on its way to its registers
         auto fetch = [&](int i, Tile<D>& t) {
             const size_t at = (seq0 + (size_t)i * P.heads) * TILE + lane * 16;
+            if (P.stream) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) t.k[c] = WR == 1 ? ldg_stream16(P.k_codes + at + c * 1024) : ld16(P.k_codes + at + c * 1024);
+                for (int c = 0; c < C; ++c) t.k[c] = ldg_stream16(P.k_codes + at + c * 1024);
 #pragma unroll
-            for (int c = 0; c < C; ++c) t.v[c] = WR == 1 ? ldg_stream16(P.v_codes + at + c * 1024) : ld16(P.v_codes + at + c * 1024);
+                for (int c = 0; c < C; ++c) t.v[c] = ldg_stream16(P.v_codes + at + c * 1024);
+            } else {
+#pragma unroll
+                for (int c = 0; c < C; ++c) t.k[c] = ld16(P.k_codes + at + c * 1024);
+#pragma unroll
+                for (int c = 0; c < C; ++c) t.v[c] = ld16(P.v_codes + at + c * 1024);
+            }
         };
         // the scales of its next 64 blocks, one a lane
         float k_scales = 0.f, v_scales = 0.f;
@@ -438,7 +506,13 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
                     turn = (turn + 1) & 63;
                     if (turn == 0) fetch_scales(i + WK);
                 }
-                attend_block<WT, D, NP>(R, q, t, P.c * ks, vs, i == blocks - 1 ? tail : 0);
+                f32x16 x[1];
+                key_products<D, NP>(q, t.k, x[0]);
+                if (tail && i == blocks - 1) hide<D>(x[0], t.v, tail);
+                const float cs[1] = {P.c * ks};
+                raise_maximum<D, 1>(R, x, cs);
+                exponentials<D>(R, x[0], cs[0], log2_of(vs), one_over(vs));
+                value_products<D, NP>(R, x[0], t.v);
             }
         }
     }
@@ -448,34 +522,13 @@ __global__ __launch_bounds__(64 * ta_waves<WT>(), ta_waves<WT>() / 4) void tree_
     if constexpr (WK > 1) {
         for (int n = WK / 2; n >= 1; n >>= 1) {
             __syncthreads();
-            if (wk >= n && wk < 2 * n && valid) {
-                float* to = s_meet + ((wk - n) * WR + wr) * part_floats<D>();
-#pragma unroll
-                for (int j = 0; j < C; ++j)
-#pragma unroll
-                    for (int a = 0; a < 4; ++a)
-                        *reinterpret_cast<f32x4*>(to + ((j * 4 + a) * 64 + lane) * 4) = f32x4{R.o[j][4 * a], R.o[j][4 * a + 1], R.o[j][4 * a + 2], R.o[j][4 * a + 3]};
-                to[TA_TILE * D + lane] = R.m;
-                to[TA_TILE * D + 64 + lane] = R.l;
-            }
+            if (wk >= n && wk < 2 * n && valid) leave<D>(s_meet + ((wk - n) * WR + wr) * part_floats<D>(), R);
             __syncthreads();
-            if (wk < n && valid) {
-                const float* from = s_meet + (wk * WR + wr) * part_floats<D>();
-                f32x16 o2[C];
-#pragma unroll
-                for (int j = 0; j < C; ++j)
-#pragma unroll
-                    for (int a = 0; a < 4; ++a) {
-                        const f32x4 x = *reinterpret_cast<const f32x4*>(from + ((j * 4 + a) * 64 + lane) * 4);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o2[j][4 * a + e] = x[e];
-                    }
-                merge<D>(R, from[TA_TILE * D + lane], from[TA_TILE * D + 64 + lane], o2);
-            }
+            if (wk < n && valid) join<D>(R, s_meet + (wk * WR + wr) * part_floats<D>());
         }
         if (wk > 0) return;
     }
-    if (!active || !valid) return;
+    if (!valid) return;
     if (splits == 1) {
         const size_t at = ((size_t)b * P.nodes + node) * P.n_heads + head;
         const float inv = R.l == 0.f ? 0.f : 1.f / R.l;
@@ -545,7 +598,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(const TaParams P) {
 }
 
 // ------------------------------------------------------------------------------------------ host
-struct TaPlan { int wr, groups; size_t bytes; };
+struct TaPlan { int wr, waves, groups; size_t bytes; };
 
 int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaPlan& L) {
     if (!a || !tree || !tree->parent || !a->kv_len) return PS_ERR_NULL;
@@ -575,12 +628,15 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
         if (P.len[b] > 1 << 30) return PS_ERR_UNSUPPORTED;
         total += (P.len[b] + PC_BLOCK - 1) / PC_BLOCK;
     }
-    const int waves = a->dtype == PS_BF16 ? ta_waves<bf16_t>() : ta_waves<float>();
-    L.wr = 1;
-    while (L.wr < P.tiles && L.wr < waves) L.wr *= 2;
+    L.wr = P.tiles >= 3 ? 4 : P.tiles;
+    L.waves = a->dtype == PS_BF16 && L.wr < 4 ? 8 : 4;
     L.groups = (P.tiles + L.wr - 1) / L.wr;
-    // at most one workgroup for every compute unit (256) where a split has at least two blocks per wavefront: the least `per` that gives that.
-    // (Sequences of 4099 ... 12288 in one batch: with the mean of all blocks as `per` 288 workgroups, two rounds)
+    // codes that are read once and are more than the memory-side cache (256 MB) holds pass the caches by (one row tile, 32 x 2048 positions of 32 heads, 537 MB:
+    // 114 -> 97 us; of 8 heads, 134 MB: 26.7 -> 28.1)
+    P.stream = P.tiles == 1 && total * heads * PC_BLOCK * d * 2 > 192LL << 20;
+    // as many workgroups as run at once (256 compute units, two workgroups of four bf16 wavefronts on each) where a split has at least two blocks per wavefront:
+    // the least `per` that gives no more.  (Sequences of 4099 ... 12288 in one batch, one workgroup each: with the mean of all blocks as `per` 288, two rounds)
+    const int at_once = a->dtype == PS_BF16 && L.waves == 4 ? 512 : 256;
     const long long units = (long long)heads * L.groups;
     auto count = [&](long long per) {
         long long n = 0;
@@ -588,8 +644,8 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
         return n * units;
     };
     // (a split's codes stay below 2 GiB)
-    long long lo = 2 * (waves / L.wr), hi = (1LL << 31) / ((long long)heads * PC_BLOCK * d);
-    const long long most = std::max<long long>(256, count(hi));
+    long long lo = 2 * (L.waves / L.wr), hi = (1LL << 31) / ((long long)heads * PC_BLOCK * d);
+    const long long most = std::max<long long>(at_once, count(hi));
     while (lo < hi) {
         const long long mid = (lo + hi) / 2;
         if (count(mid) <= most) hi = mid; else lo = mid + 1;
@@ -607,11 +663,10 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
 }
 
 template <typename WT, int D> void go(const TaParams& P, const TaPlan& L, hipStream_t s) {
-    const dim3 grid(P.split0[P.batch], P.heads, L.groups), block(64 * ta_waves<WT>());
+    const dim3 grid(P.split0[P.batch], P.heads, L.groups), block(64 * L.waves);
     if (L.wr == 1) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 1>), grid, block, 0, s, P);
     else if (L.wr == 2) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 2>), grid, block, 0, s, P);
-    else if (L.wr == 4) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 4>), grid, block, 0, s, P);
-    else if constexpr (ta_waves<WT>() == 8) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 8>), grid, block, 0, s, P);
+    else hipLaunchKernelGGL((tree_attn_kernel<WT, D, 4>), grid, block, 0, s, P);
     if (L.bytes) hipLaunchKernelGGL((tree_attn_join_kernel<WT, D>), dim3((P.rows + 3) / 4, P.heads, P.batch), dim3(256), 0, s, P);
 }
 
