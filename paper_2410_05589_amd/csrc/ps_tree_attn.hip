@@ -316,7 +316,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
 #pragma unroll
             for (int e = 0; e < 16; ++e) R.o[j][e] = 0.f;
     };
-    // the tree's own rows, in the sequence's last split, while the first blocks are on their way: tiles of 32 nodes, from the last wavefront on
+    // the tree's own rows, in the sequence's last split, while the first blocks are on their way: tiles of 32 nodes
     auto own_rows = [&]() __attribute__((always_inline)) {
         bf16x8 k0[2 * C][NP];
         auto load_keys = [&](int kt) __attribute__((always_inline)) {
@@ -325,7 +325,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             for (int f = 0; f < 2 * C; ++f)
                 load_parts<WT, NP>(own_k + (long long)key * P.kv_row + (32 * (f >> 1) + 16 * half + 8 * (f & 1)) * ESZ, key < P.nodes, k0[f]);
         };
-        const int first = (WK - 1 - wk) % WK;
+        const int first = wk;
         load_keys(first);
         stage_own();
         __syncthreads();
@@ -487,7 +487,8 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             }
         };
         Tile<D> next;
-        int i = begin + wk;
+        // (blocks in turn; where there are own rows, behind the wavefronts that have those)
+        int i = begin + (own ? (wk + WK - (P.nodes + 31) / 32 % WK) % WK : wk);
         const bool any = active && i < end;
         if (any) {
             fetch_scales(i);
