@@ -35,6 +35,8 @@ struct TpParams {
     int* ids;
     float* id_probs;
     int rows, vocab, frac;                         // F
+    int parts, part_vecs;                          // workgroups per row, vectors of each
+    char* work;                                    // of each row: see Work
 };
 
 typedef unsigned u32x4_h __attribute__((ext_vector_type(4), aligned(2)));
@@ -169,11 +171,12 @@ template <typename F> __device__ __forceinline__ float least_float(float max, F 
 
 template <typename LT, int T> struct Logits {               // T threads
     const char* row;
-    int vocab, nvec;
+    int vocab, nvec;                                        // tokens of the row; vectors up to the end of
+    int begin = 0;                                          // this workgroup's part, which begins here
     // f(vector, its number), by whole wavefronts: what is behind the row's end is -Inf
     template <typename F> __device__ __forceinline__ void each(F f) const {
-        u32x4 x = load_vec<LT>(row, (int)threadIdx.x, vocab), next = load_vec<LT>(row, T + (int)threadIdx.x, vocab);
-        for (int i = 0; i < nvec; i += T) {                 // two vectors ahead
+        u32x4 x = load_vec<LT>(row, begin + (int)threadIdx.x, vocab), next = load_vec<LT>(row, begin + T + (int)threadIdx.x, vocab);
+        for (int i = begin; i < nvec; i += T) {             // two vectors ahead
             const u32x4 after = load_vec<LT>(row, i + 2 * T + (int)threadIdx.x, vocab);
             f(x, i + (int)threadIdx.x);
             x = next;
@@ -365,6 +368,109 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
     }
 }
 
+// the sums of the kept e of the wavefronts' vectors, in id order (S.cell), and of all
+template <int T, typename LT> __device__ __forceinline__ u64 sum_cells(const Logits<LT, T>& L, const Row& R, Shared& S, Bound bound) {
+    constexpr int N = Vec<LT>::N, PER = TP_MAX_CELLS / T;
+    const int tid = threadIdx.x, lane = tid & 63;
+    L.each([&](const u32x4& x, int at) {
+        u64 m = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float l = Vec<LT>::get(x, e);
+            if (at * N + e < L.vocab && bound.keeps(l, at * N + e)) m += R.mass(l);
+            if (e & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        if (__ballot(m != 0)) m = wave_scan(m);
+        if (lane == 63) S.cell[(at - L.begin) >> 6] = m;
+    });
+    __syncthreads();
+    const int cells = (L.nvec - L.begin + T - 1) / T * (T / 64);
+    u64 sum = 0, total;
+    for (int i = 0; i < PER; ++i) sum += tid * PER + i < cells ? S.cell[tid * PER + i] : 0;
+    block_scan<T>(sum, S, total);
+    return total;
+}
+// The mass up to which the draw goes: the drawn token is the first with which the sum passes it
+__device__ __forceinline__ u64 drawn_mass(float r, u64 total) {
+    const double t = (double)r * (double)total;
+    return t >= 1.0 ? min((u64)t, total - 1) : 0;
+}
+// The token with which the sum, `before` in front of the part, passes `want`; takes S.cell
+template <int T, typename LT>
+__device__ __forceinline__ void draw_from_cells(const TpParams& P, const Logits<LT, T>& L, const Row& R, Shared& S, Bound bound, size_t row, u64 before, u64 want, u64 total) {
+    constexpr int N = Vec<LT>::N, PER = TP_MAX_CELLS / T;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int cells = (L.nvec - L.begin + T - 1) / T * (T / 64);
+    u64 sum = 0, all;
+    for (int i = 0; i < PER; ++i) sum += tid * PER + i < cells ? S.cell[tid * PER + i] : 0;
+    __syncthreads();
+    u64 upto = before + block_scan<T>(sum, S, all) - sum;
+    if (upto <= want && upto + sum > want)
+        for (int i = 0; i < PER; ++i) {
+            const u64 own = tid * PER + i < cells ? S.cell[tid * PER + i] : 0;
+            if (upto <= want && upto + own > want) { S.found = tid * PER + i; S.found_before = upto; }
+            upto += own;
+        }
+    __syncthreads();
+    if (tid >= 64) return;
+    const int at = L.begin + S.found * 64 + lane;
+    const u32x4 x = load_vec<LT>(L.row, at, L.vocab);
+    u64 mine = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float l = Vec<LT>::get(x, e);
+        if (at * N + e < L.vocab && bound.keeps(l, at * N + e)) mine += R.mass(l);
+    }
+    u64 to = S.found_before + wave_scan(mine) - mine;
+    if (to <= want && to + mine > want)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float l = Vec<LT>::get(x, e);
+            const u64 m = at * N + e < L.vocab && bound.keeps(l, at * N + e) ? R.mass(l) : 0;
+            if (to <= want && to + m > want) {
+                P.ids[row] = at * N + e;
+                int kk;
+                if (P.id_probs) P.id_probs[row] = (float)(R.scaled(l, kk) / (double)total);
+            }
+            to += m;
+        }
+}
+template <int T, typename LT>
+__device__ __forceinline__ void draw(const TpParams& P, const Logits<LT, T>& L, const Row& R, Shared& S, Bound bound, size_t row, u64 before, u64 want, u64 total) {
+    sum_cells<T>(L, R, S, bound);
+    draw_from_cells<T>(P, L, R, S, bound, row, before, want, total);
+}
+template <int T, typename LT>
+__device__ __forceinline__ void write_probs(const TpParams& P, const Logits<LT, T>& L, const Row& R, Bound bound, size_t row, u64 total) {
+    constexpr int N = Vec<LT>::N;
+    const int V = L.vocab;
+    float* out = P.probs + row * V;
+    const double cy = R.c / TP_TABLE;
+    const float inv = (float)(1.0 / ldexp((double)total, -P.frac));
+    L.each([&](const u32x4& x, int at) {
+        if (at >= L.nvec) return;                           // (the next part's)
+        float p[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float l = Vec<LT>::get(x, e);
+            p[e] = 0.f;
+            if (bound.keeps(l, at * N + e) && l > -__builtin_inff()) {
+                const double y = __builtin_fmax(((double)l - R.max) * cy, -1000.0), n = rint(y);
+                p[e] = ldexpf(__builtin_amdgcn_exp2f((float)(y - n)) * inv, (int)n);
+            }
+            if (e & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int q = 0; q < N; q += 4) {
+            if (at * N + q + 4 <= V) *reinterpret_cast<f32x4_q*>(out + (size_t)at * N + q) = f32x4{p[q], p[q + 1], p[q + 2], p[q + 3]};
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at * N + q + e < V) out[(size_t)at * N + q + e] = p[q + e];
+        }
+    });
+}
+
 template <typename LT, int T>
 __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
     constexpr int N = Vec<LT>::N, WAVES = T / 64;
@@ -471,90 +577,282 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
         if (least > bound.l) { bound = {least, ~0u}; total = 0; }
     }
 
-    // the sum of the kept e, by the wavefronts' shares in id order, where it is not known or a token is drawn
+    // the sum of the kept e, where it is not known or a token is drawn
     if (P.ids || total == 0) {
         __syncthreads();
-        L.each([&](const u32x4& x, int at) {
-            u64 m = 0;
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float l = Vec<LT>::get(x, e);
-                if (at * N + e < V && bound.keeps(l, at * N + e)) m += R.mass(l);
-                if (e & 1) __builtin_amdgcn_sched_barrier(0);
-            }
-            if (__ballot(m != 0)) m = wave_scan(m);
-            if (lane == 63) S.cell[at >> 6] = m;
-        });
-        __syncthreads();
-        constexpr int PER = TP_MAX_CELLS / T;
-        const int cells = (L.nvec + T - 1) / T * WAVES;
-        u64 sum = 0;
-        for (int i = 0; i < PER; ++i) sum += tid * PER + i < cells ? S.cell[tid * PER + i] : 0;
-        u64 upto = block_scan<T>(sum, S, total) - sum;
-        if (P.ids) {
-            const double t = (double)P.r[row] * (double)total;
-            const u64 want = t >= 1.0 ? min((u64)t, total - 1) : 0;   // the drawn token is the first with which the sum passes it
-            if (upto <= want && upto + sum > want)
-                for (int i = 0; i < PER; ++i) {
-                    const u64 own = tid * PER + i < cells ? S.cell[tid * PER + i] : 0;
-                    if (upto <= want && upto + own > want) { S.found = tid * PER + i; S.found_before = upto; }
-                    upto += own;
-                }
-            __syncthreads();
-            if (wave == 0) {
-                const int at = S.found * 64 + lane;
-                const u32x4 x = load_vec<LT>(L.row, at, V);
-                u64 all = 0;
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float l = Vec<LT>::get(x, e);
-                    if (at * N + e < V && bound.keeps(l, at * N + e)) all += R.mass(l);
-                }
-                u64 to = S.found_before + wave_scan(all) - all;
-                if (to <= want && to + all > want)
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const float l = Vec<LT>::get(x, e);
-                        const u64 m = at * N + e < V && bound.keeps(l, at * N + e) ? R.mass(l) : 0;
-                        if (to <= want && to + m > want) {
-                            P.ids[row] = at * N + e;
-                            int kk;
-                            if (P.id_probs) P.id_probs[row] = (float)(R.scaled(l, kk) / (double)total);
-                        }
-                        to += m;
-                    }
-            }
-        }
+        total = sum_cells<T>(L, R, S, bound);
+        if (P.ids) draw_from_cells<T>(P, L, R, S, bound, row, 0, drawn_mass(P.r[row], total), total);
     }
-    if (!out) return;
-    const double cy = R.c / TP_TABLE;
-    const float inv = (float)(1.0 / ldexp((double)total, -P.frac));
-    L.each([&](const u32x4& x, int at) {
-        float p[N];
+    if (P.probs) write_probs(P, L, R, bound, row, total);
+}
+
+// ------------------------------------------------------------------------------------------
+// Few rows of a large vocabulary: several workgroups per row, a kernel for each pass.  What a row's workgroups tell each other is in the workspace.
+// ------------------------------------------------------------------------------------------
+constexpr int TP_PART = 16384;                     // tokens per workgroup
+constexpr int TP_SPLIT_ROWS = 128;                 // rows up to which they are cut up
+constexpr int TP_MAX_PARTS = (1 << TP_MAX_LOG) / TP_PART;
+struct Work {
+    u64 hist[TP_BINS];
+    u64 list[TP_LIST];
+    u64 sum[TP_MAX_PARTS];                         // the parts' sums of the kept e
+    float max[TP_MAX_PARTS];                       // their largest logits, NaN where one is NaN or +Inf
+    u64 total;                                     // the sum over the row where it is known
+    Bound bound;
+    int n_list;
+};
+
+// A row's settings and its largest logit (every lane the same); false: nothing to be searched for (bad: NaN or +Inf; max -Inf: no mass)
+struct Setting {
+    float max, top_p, min_p;
+    int k;
+    bool bad;
+    double c;
+    __device__ __forceinline__ bool plain() const { return bad || max == -__builtin_inff(); }
+};
+__device__ __forceinline__ Setting setting_of(const TpParams& P, const Work& W, int b) {
+    Setting s;
+    const float t = P.temperature ? P.temperature[b] : 1.f;
+    const bool greedy = !(t > 0.f);
+    const int k = P.top_k ? P.top_k[b] : 0;
+    s.k = greedy ? 1 : k < 1 || k > P.vocab ? P.vocab : k;
+    s.top_p = P.top_p ? P.top_p[b] : 1.f;
+    const float m = P.min_p ? P.min_p[b] : 0.f;
+    s.min_p = m > 0.f ? fminf(m, 1.f) : 0.f;
+    const int lane = threadIdx.x & 63;
+    const float x = lane < P.parts ? W.max[lane] : -__builtin_inff();
+    s.bad = __ballot(x != x);
+    s.max = wave_max(x);
+    s.c = uniform(1.4426950408889634074 * TP_TABLE / (greedy ? 1.0 : (double)t));
+    return s;
+}
+static_assert(TP_MAX_PARTS <= 64, "a lane for each part");
+
+template <typename LT> __device__ __forceinline__ Logits<LT, 1024> part_of(const TpParams& P, size_t row, int part) {
+    Logits<LT, 1024> L;
+    constexpr int N = Vec<LT>::N;
+    L.row = P.logits + row * P.vocab * Traits<LT>::ESZ;
+    L.vocab = P.vocab;
+    L.begin = part * P.part_vecs;
+    L.nvec = min((P.vocab + N - 1) / N, L.begin + P.part_vecs);
+    return L;
+}
+
+template <typename LT> __global__ __launch_bounds__(1024) void part_max_kernel(const TpParams P) {
+    __shared__ float s_max[16];
+    const int tid = threadIdx.x, lane = tid & 63, part = blockIdx.x;
+    const size_t row = blockIdx.y;
+    Work& W = reinterpret_cast<Work*>(P.work)[row];
+    for (int i = part * 1024 + tid; i < TP_BINS; i += P.parts * 1024) W.hist[i] = 0;
+    if (part == 0 && tid == 0) W.n_list = 0;
+    float mx = -__builtin_inff();
+    bool bad = false;
+    part_of<LT>(P, row, part).each([&](const u32x4& x, int) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
+        for (int e = 0; e < Vec<LT>::N; ++e) {
             const float l = Vec<LT>::get(x, e);
-            p[e] = 0.f;
-            if (bound.keeps(l, at * N + e) && l > -__builtin_inff()) {
-                const double y = __builtin_fmax(((double)l - R.max) * cy, -1000.0), n = rint(y);
-                p[e] = ldexpf(__builtin_amdgcn_exp2f((float)(y - n)) * inv, (int)n);
-            }
-            if (e & 1) __builtin_amdgcn_sched_barrier(0);
+            bad |= !(l < __builtin_inff());
+            mx = fmaxf(mx, l);
         }
-#pragma unroll
-        for (int q = 0; q < N; q += 4) {
-            if (at * N + q + 4 <= V) *reinterpret_cast<f32x4_q*>(out + (size_t)at * N + q) = f32x4{p[q], p[q + 1], p[q + 2], p[q + 3]};
-            else
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (at * N + q + e < V) out[(size_t)at * N + q + e] = p[q + e];
-        }
+    });
+    mx = __ballot(bad) ? __builtin_nanf("") : wave_max(mx);
+    if (lane == 0) s_max[tid >> 6] = mx;
+    __syncthreads();
+    mx = s_max[lane & 15];
+    bad = __ballot(mx != mx);
+    mx = row_max(mx);
+    if (tid == 0) W.max[part] = bad ? __builtin_nanf("") : mx;
+}
+
+// the histogram that the row's setting asks for: counts for top-k, else sums of e for top-p
+template <typename LT> __global__ __launch_bounds__(1024, 4) void part_hist_kernel(const TpParams P) {
+    __shared__ double s_table[TP_TABLE];
+    __shared__ u64 s_hist[TP_BINS];
+    const int tid = threadIdx.x;
+    const size_t row = blockIdx.y;
+    Work& W = reinterpret_cast<Work*>(P.work)[row];
+    const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
+    if (s.plain() || (s.k == P.vocab && !(s.top_p < 1.f))) return;
+    if (tid < TP_TABLE) s_table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
+    for (int i = tid; i < TP_BINS; i += 1024) s_hist[i] = 0;
+    __syncthreads();
+    const Row R = {s.max, s.c, s_table};
+    const auto L = part_of<LT>(P, row, blockIdx.x);
+    if (s.k < P.vocab) L.tokens([&](float l, int) { lds_add((unsigned*)&s_hist[R.step(l)], 1u); });
+    else L.tokens([&](float l, int) {
+        int k;
+        const u64 m = R.mass(l, k);
+        lds_add(&s_hist[R.step_of(k)], m);
+    });
+    __syncthreads();
+    for (int i = tid; i < TP_BINS; i += 1024)
+        if (s_hist[i]) __hip_atomic_fetch_add(&W.hist[i], s_hist[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The step that the bound lies in, from the row's histogram, and the range of logits whose tokens are listed: top-k everything down to that step, top-p the step
+struct Range { float least, above; u64 before, want; };
+__device__ __forceinline__ Range range_of(const TpParams& P, const Work& W, const Setting& s, const Row& R, Shared& S) {
+    for (int i = threadIdx.x; i < TP_BINS; i += 1024) S.h.mass[i] = W.hist[i];
+    __syncthreads();
+    const bool count = s.k < P.vocab;
+    Range r;
+    r.want = find_in_bins<1024>(S, 0, (u64)s.k, count ? -1.0 : fmax((double)s.top_p, 0.0));
+    const int step = S.found;
+    r.before = count ? 0 : S.found_before;
+    r.least = step < TP_BINS - 1 ? least_float(s.max, [&](float l) { return R.step(l) <= step; }) : -__builtin_inff();
+    r.above = !count && step > 0 ? least_float(s.max, [&](float l) { return R.step(l) < step; }) : __builtin_inff();
+    return r;
+}
+
+template <typename LT> __global__ __launch_bounds__(1024, 4) void part_list_kernel(const TpParams P) {
+    __shared__ Shared S;
+    const size_t row = blockIdx.y;
+    Work& W = reinterpret_cast<Work*>(P.work)[row];
+    const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
+    if (s.plain() || (s.k == P.vocab && !(s.top_p < 1.f))) return;
+    const Row R = {s.max, s.c, S.table};
+    const Range r = range_of(P, W, s, R, S);
+    part_of<LT>(P, row, blockIdx.x).tokens([&](float l, int id) {
+        if (!(l >= r.least && l < r.above)) return;
+        const int at = __hip_atomic_fetch_add(&W.n_list, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (at < TP_LIST) W.list[at] = place(l, id);
     });
 }
 
+// the row's bound, by one workgroup
+template <typename LT> __global__ __launch_bounds__(1024, 4) void row_bound_kernel(const TpParams P) {
+    __shared__ Shared S;
+    const int tid = threadIdx.x;
+    const size_t row = blockIdx.x;
+    Work& W = reinterpret_cast<Work*>(P.work)[row];
+    const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
+    if (s.plain()) return;
+    if (tid < TP_TABLE) S.table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
+    __syncthreads();
+    const Row R = {s.max, s.c, S.table};
+    Bound bound = {-__builtin_inff(), ~0u};
+    u64 total = 0, with = 0;
+    auto mass = [&](float l) { return R.mass(l); };
+    if (s.k < P.vocab || s.top_p < 1.f) {
+        const int n = W.n_list;
+        if (n <= TP_LIST) {
+            const Range r = range_of(P, W, s, R, S);
+            for (int i = tid; i < n; i += 1024) S.list[i] = W.list[i];
+            __syncthreads();
+            if (s.k < P.vocab) {
+                bound = bound_of(find_in_list<1024>(S, n, 0, (u64)s.k, -1.0, with, [](float) { return (u64)1; }));
+                u64 m = 0;
+                for (int i = tid; i < n; i += 1024) {       // tokens behind the bound leave the list: the last place, without mass
+                    const u64 c = S.list[i];
+                    const float l = logit_of((unsigned)(c >> TP_MAX_LOG));
+                    const unsigned id = (unsigned)c & ((1u << TP_MAX_LOG) - 1);
+                    if (bound.keeps(l, id)) m += R.mass(l);
+                    else S.list[i] = place(-__builtin_inff(), id);
+                }
+                block_scan<1024>(m, S, total);
+                if (s.top_p < 1.f) {
+                    __syncthreads();
+                    bound = bound_of(find_in_list<1024>(S, n, 0, 0, fmax((double)s.top_p, 0.0), with, mass));
+                    total = with;
+                }
+            } else {
+                bound = bound_of(find_in_list<1024>(S, n, r.before, r.want, -1.0, with, mass));
+                total = with;
+            }
+        } else {                                            // more tokens than the list holds: the whole row, by this workgroup
+            Logits<LT, 1024> L;
+            L.row = P.logits + row * P.vocab * Traits<LT>::ESZ; L.vocab = P.vocab; L.nvec = (P.vocab + Vec<LT>::N - 1) / Vec<LT>::N;
+            if (s.k < P.vocab) bound = bound_of(find_in_row<false>(L, R, s.max, S, bound, (u64)s.k, -1.0, with));
+            if (s.top_p < 1.f) {
+                __syncthreads();
+                bound = bound_of(find_in_row<true>(L, R, s.max, S, bound, 0, fmax((double)s.top_p, 0.0), with));
+                total = with;
+            }
+        }
+    }
+    if (s.min_p > 0.f) {
+        const double least_e = ldexp((double)s.min_p, P.frac);
+        int kk;
+        const float least = least_float(s.max, [&](float l) { return R.scaled(l, kk) >= least_e; });
+        if (least > bound.l) { bound = {least, ~0u}; total = 0; }
+    }
+    if (tid == 0) { W.bound = bound; W.total = total; }
+}
+
+// the parts' sums of the kept e, where the row's is not known or a token is drawn
+template <typename LT> __global__ __launch_bounds__(1024, 4) void part_sum_kernel(const TpParams P) {
+    __shared__ double s_table[TP_TABLE];
+    __shared__ u64 s_sum[16];
+    const int tid = threadIdx.x;
+    const size_t row = blockIdx.y;
+    Work& W = reinterpret_cast<Work*>(P.work)[row];
+    const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
+    if (s.plain() || (W.total && !P.ids)) return;
+    if (tid < TP_TABLE) s_table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
+    __syncthreads();
+    const Row R = {s.max, s.c, s_table};
+    const Bound bound = W.bound;
+    u64 m = 0;
+    part_of<LT>(P, row, blockIdx.x).tokens([&](float l, int id) { if (bound.keeps(l, id)) m += R.mass(l); });
+    m = wave_scan(m);
+    if ((tid & 63) == 63) s_sum[tid >> 6] = m;
+    __syncthreads();
+    m = row_scan(s_sum[tid & 15]);
+    if (tid == 15) W.sum[blockIdx.x] = m;
+}
+
+// the part's probabilities, and the drawn token where it is the part's
+template <typename LT> __global__ __launch_bounds__(1024, 4) void part_out_kernel(const TpParams P) {
+    __shared__ Shared S;
+    const int tid = threadIdx.x, lane = tid & 63, part = blockIdx.x;
+    const size_t row = blockIdx.y;
+    Work& W = reinterpret_cast<Work*>(P.work)[row];
+    const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
+    const auto L = part_of<LT>(P, row, part);
+    if (s.plain()) {
+        const float fill = s.bad ? __builtin_nanf("") : 0.f;
+        if (P.probs) for (int i = L.begin * Vec<LT>::N + tid; i < min(P.vocab, L.nvec * Vec<LT>::N); i += 1024) P.probs[row * P.vocab + i] = fill;
+        if (P.ids && part == 0 && tid == 0) {
+            P.ids[row] = -1;
+            if (P.id_probs) P.id_probs[row] = fill;
+        }
+        return;
+    }
+    if (tid < TP_TABLE) S.table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
+    __syncthreads();
+    const Row R = {s.max, s.c, S.table};
+    const Bound bound = W.bound;
+    u64 total = W.total;
+    if (P.ids || total == 0) {
+        const u64 own = lane < P.parts ? W.sum[lane] : 0, upto = wave_scan(own);
+        total = lane_u64(upto, 63);
+        if (P.ids) {
+            const u64 want = drawn_mass(P.r[row], total);
+            if (lane_u64(upto, part) > want && lane_u64(upto - own, part) <= want)
+                draw<1024>(P, L, R, S, bound, row, lane_u64(upto - own, part), want, total);
+        }
+    }
+    if (P.probs) write_probs(P, L, R, bound, row, total);
+}
+
 template <typename LT> void go(const TpParams& P, int total, hipStream_t s) {
-    if (total <= 256) hipLaunchKernelGGL((target_probs_kernel<LT, 1024>), dim3(total), dim3(1024), 0, s, P);
+    if (P.parts > 1) {
+        const dim3 grid(P.parts, total), block(1024);
+        hipLaunchKernelGGL((part_max_kernel<LT>), grid, block, 0, s, P);
+        if (P.temperature || P.top_k || P.top_p) {          // (greedy rows have a bound, too)
+            hipLaunchKernelGGL((part_hist_kernel<LT>), grid, block, 0, s, P);
+            hipLaunchKernelGGL((part_list_kernel<LT>), grid, block, 0, s, P);
+        }
+        hipLaunchKernelGGL((row_bound_kernel<LT>), dim3(total), block, 0, s, P);
+        hipLaunchKernelGGL((part_sum_kernel<LT>), grid, block, 0, s, P);
+        hipLaunchKernelGGL((part_out_kernel<LT>), grid, block, 0, s, P);
+    } else if (total <= 256) hipLaunchKernelGGL((target_probs_kernel<LT, 1024>), dim3(total), dim3(1024), 0, s, P);
     else hipLaunchKernelGGL((target_probs_kernel<LT, 512>), dim3(total), dim3(512), 0, s, P);
+}
+
+// workgroups per row
+int parts_of(const ps_target_probs_args* a) {
+    return a->vocab >= 4 * TP_PART && a->batch * a->rows <= TP_SPLIT_ROWS ? (a->vocab + TP_PART - 1) / TP_PART : 1;
 }
 
 int check(const ps_target_probs_args* a) {
@@ -568,7 +866,7 @@ int check(const ps_target_probs_args* a) {
 }   // namespace
 
 extern "C" size_t ps_target_probs_workspace_bytes(const ps_target_probs_args* a) {
-    return check(a) == PS_OK ? 0 : 0;
+    return check(a) == PS_OK && parts_of(a) > 1 ? a256((size_t)a->batch * a->rows * sizeof(Work)) : 0;
 }
 
 extern "C" int ps_target_probs(const ps_target_probs_args* a, void* stream) {
@@ -578,8 +876,14 @@ extern "C" int ps_target_probs(const ps_target_probs_args* a, void* stream) {
     if ((uintptr_t)a->logits & (a->dtype == PS_BF16 ? 1 : 3)) return PS_ERR_UNSUPPORTED;
     if (!aligned4(a->temperature) || !aligned4(a->top_k) || !aligned4(a->top_p) || !aligned4(a->min_p) || !aligned4(a->r) || !aligned4(a->probs) ||
         !aligned4(a->ids) || !aligned4(a->id_probs)) return PS_ERR_UNSUPPORTED;
+    const size_t need = ps_target_probs_workspace_bytes(a);
+    if (need && !a->workspace) return PS_ERR_NULL;
+    if (need && (a->workspace_bytes < need || ((uintptr_t)a->workspace & 255))) return PS_ERR_WORKSPACE;
     TpParams P = {};
     P.logits = (const char*)a->logits; P.temperature = a->temperature; P.top_k = a->top_k; P.top_p = a->top_p; P.min_p = a->min_p; P.r = a->r;
+    P.parts = parts_of(a);
+    P.part_vecs = TP_PART / (a->dtype == PS_BF16 ? 8 : 4);
+    P.work = (char*)a->workspace;
     P.probs = a->probs; P.ids = a->ids; P.id_probs = a->id_probs; P.rows = a->rows; P.vocab = a->vocab;
     int log = 0;
     while (1 << log < a->vocab) ++log;
