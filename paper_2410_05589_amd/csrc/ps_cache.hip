@@ -34,25 +34,19 @@ __device__ __forceinline__ void wave_sync() {   // LDS written by a wavefront's 
     __builtin_amdgcn_wave_barrier();
 }
 
-// 8 elements of a row as floats
-template <typename WT> __device__ __forceinline__ void load8(const char* p, float (&x)[8]) {
-    if constexpr (Traits<WT>::BF) {
-        const uint4 v = ld16_q(p);
-        const unsigned w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const f32x4 v = load4_q<WT>(p + 16 * i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * i + e] = v[e];
-        }
-    }
-}
+// 8 elements of a row as they are, and as floats
+template <typename WT> struct Eight;
+template <> struct Eight<bf16_t> {
+    uint4 v;
+    __device__ __forceinline__ void load(const char* p) { v = ld16_q(p); }
+    __device__ __forceinline__ unsigned word(int i) const { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+    __device__ __forceinline__ float get(int e) const { return __uint_as_float(e & 1 ? word(e >> 1) & 0xFFFF0000u : word(e >> 1) << 16); }
+};
+template <> struct Eight<float> {
+    f32x4 lo, hi;
+    __device__ __forceinline__ void load(const char* p) { lo = load4_q<float>(p); hi = load4_q<float>(p + 16); }
+    __device__ __forceinline__ float get(int e) const { return e < 4 ? lo[e & 3] : hi[e & 3]; }
+};
 template <typename WT> __device__ __forceinline__ void store8(char* p, const float (&x)[8]) {
     if constexpr (Traits<WT>::BF) {
         *reinterpret_cast<u32x4_q*>(p) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
@@ -83,8 +77,8 @@ __global__ __launch_bounds__(64 * PC_WAVES) void cache_write_kernel(const PcPara
     const int len = pc_length(P.len_dev, b, P.len[b]);
     int count = P.n[b], node = 0;
     if (P.n_accepted) {                                     // lane i + 1: the path's entry i; lane 0: node 0
+        node = lane > 0 && lane <= P.path_rows ? P.path[(size_t)b * P.path_rows + lane - 1] : 0;
         const int acc = min(P.n_accepted[b], P.path_rows);
-        node = lane > 0 && lane <= acc ? P.path[(size_t)b * P.path_rows + lane - 1] : 0;
         const u64 good = __ballot(lane <= acc && (unsigned)node < (unsigned)P.rows);
         count = ~good ? __builtin_ctzll(~good) : 64;
     }
@@ -103,27 +97,37 @@ __global__ __launch_bounds__(64 * PC_WAVES) void cache_write_kernel(const PcPara
     unsigned char* tile = (value ? P.v_codes : P.k_codes) + at * TILE;
     float* scale = (value ? P.v_scale : P.k_scale) + at;
     const float was = t0 ? *scale : 0.f;
+    uint4 old[D / 32];                                      // the codes that are there (asked for together with the rows)
+    if (t0)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) old[c] = ld16(tile + c * 1024 + lane * 16);
     const int li = lane % LR, lr = lane / LR;
 
-    float x[PASSES][8];
-    unsigned amax = 0;
+    Eight<WT> x[PASSES] = {};
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
         const int t = i * RP + lr, row = from + t - t0;
-        const bool mine = t >= t0 && t < t0 + n;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
         const int src = P.n_accepted ? __shfl(node, row & 63) : row;
-        if (mine) load8<WT>(rows + (long long)src * P.row_bytes + li * 8 * Traits<WT>::ESZ, x[i]);
+        if (t >= t0 && t < t0 + n) x[i].load(rows + (long long)src * P.row_bytes + li * 8 * Traits<WT>::ESZ);
     }
+    unsigned amax = 0;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const unsigned m = __float_as_uint(x[i][e]) & 0x7FFFFFFFu;
-            amax = max(amax, m < 0x7F800000u ? m : 0u);
-        }
+        for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(x[i].get(e)) & 0x7FFFFFFFu);
     amax = wave_max_u32(amax);
+    const bool odd = amax >= 0x7F800000u;                   // Inf or NaN among them: they do not count for the scale
+    if (odd) {
+        amax = 0;
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const unsigned m = __float_as_uint(x[i].get(e)) & 0x7FFFFFFFu;
+                amax = max(amax, m < 0x7F800000u ? m : 0u);
+            }
+        amax = wave_max_u32(amax);
+    }
     const float s = fmaxf(scale_for(amax), was), inv = 1.f / s;   // (powers of two: exact)
 
     unsigned char* mem = s_tile[wave];
@@ -132,7 +136,10 @@ __global__ __launch_bounds__(64 * PC_WAVES) void cache_write_kernel(const PcPara
         const int t = i * RP + lr;
         float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (__float_as_uint(x[i][e]) & 0x7FFFFFFFu) < 0x7F800000u ? x[i][e] * inv : __uint_as_float(0x7FC00000u);
+        for (int e = 0; e < 8; ++e) y[e] = x[i].get(e) * inv;
+        if (odd)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = __builtin_fabsf(x[i].get(e)) < __builtin_inff() ? y[e] : __uint_as_float(0x7FC00000u);
         if (t >= t0) *reinterpret_cast<uint2*>(mem + t * PITCH + li * 8) = make_uint2(pack_e4m3x4(y[0], y[1], y[2], y[3]), pack_e4m3x4(y[4], y[5], y[6], y[7]));
     }
     if (t0) {
@@ -141,7 +148,7 @@ __global__ __launch_bounds__(64 * PC_WAVES) void cache_write_kernel(const PcPara
         const int r = lane & 31, half = lane >> 5;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
-            uint4 v = ld16(tile + c * 1024 + lane * 16);
+            uint4 v = old[c];
             if (grown) v = make_uint4(again(v.x, ratio), again(v.y, ratio), again(v.z, ratio), again(v.w, ratio));
             if (!value) {
                 if (r < t0) *reinterpret_cast<uint4*>(mem + r * PITCH + c * 32 + half * 16) = v;

@@ -139,6 +139,9 @@ struct Row {
         return step_of(k);
     }
     static __device__ __forceinline__ int step_of(int k) { return min(-k >> TP_K_PER_STEP_LOG, TP_BINS - 1); }
+    // about the least logit of a step
+    __device__ __forceinline__ float end_of(int step) const { return (float)(max - (((step + 1) << TP_K_PER_STEP_LOG) - 0.5) / c); }
+    __device__ __forceinline__ float near_e(float e) const { return (float)(max + log2((double)e) * TP_TABLE / c); }
 };
 
 // The token's place: descending logit (0 and -0 are equal), ascending id; and the place up to which tokens are kept
@@ -156,9 +159,16 @@ struct Bound {
 __device__ __forceinline__ Bound bound_of(u64 c) {
     return {uniform(logit_of((unsigned)(c >> TP_MAX_LOG))), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)c & ((1u << TP_MAX_LOG) - 1))};
 }
-// The least float, at most `max`, for which `pred` holds; it holds for max and for everything between.  Wavefronts do it alike
-template <typename F> __device__ __forceinline__ float least_float(float max, F pred) {
+// The least float, at most `max`, for which `pred` holds; it holds for max and for everything between.  near: about where.  Wavefronts do it alike
+template <typename F> __device__ __forceinline__ float least_float(float max, float near, F pred) {
     unsigned a = key_of(max), b = 0xFF800000u;              // holds at a; b: one behind the last (-Inf: not asked)
+    {
+        const unsigned first = key_of(near) - 32, at = first + (threadIdx.x & 63);
+        if (first >= a && first < b - 64) {                 // (the 64 floats around `near`: one look where it changes among them)
+            const u64 yes = __ballot(pred(logit_of(at)));
+            if ((yes & 1) && ~yes) return uniform(logit_of(first + (unsigned)__builtin_ctzll(~yes) - 1));
+        }
+    }
     while (b - a > 1) {
         const unsigned stride = (b - a + 63) >> 6, at = a + (threadIdx.x & 63) * stride;
         const u64 yes = __ballot(at < b && pred(logit_of(at)));
@@ -333,8 +343,8 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
     const int step = S.found;
     u64 before = S.found_before;
     // the step's logits: least <= l < above
-    const float least = step < TP_BINS - 1 ? least_float(mx, [&](float l) { return R.step(l) <= step; }) : -__builtin_inff();
-    const float above = step > 0 ? least_float(mx, [&](float l) { return R.step(l) < step; }) : __builtin_inff();
+    const float least = step < TP_BINS - 1 ? least_float(mx, R.end_of(step), [&](float l) { return R.step(l) <= step; }) : -__builtin_inff();
+    const float above = step > 0 ? least_float(mx, R.end_of(step - 1), [&](float l) { return R.step(l) < step; }) : __builtin_inff();
     L.tokens([&](float l, int id) {
         if (l >= least && l < above && within.keeps(l, id)) list_add(S, place(l, id));
     });
@@ -538,7 +548,7 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
             find_in_bins<T>(S, 0, (u64)k, -1.0);
             const int step = S.found;
             if (step < TP_BINS - 1) {
-                const float least = least_float(mx, [&](float l) { return R.step(l) <= step; });
+                const float least = least_float(mx, R.end_of(step), [&](float l) { return R.step(l) <= step; });
                 L.tokens([&](float l, int id) { if (l >= least) list_add(S, place(l, id)); });
                 __syncthreads();
                 listed = S.n_list <= TP_LIST;
@@ -573,7 +583,7 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
     if (min_p > 0.f) {
         const double least_e = ldexp((double)min_p, P.frac);
         int kk;
-        const float least = least_float(mx, [&](float l) { return R.scaled(l, kk) >= least_e; });
+        const float least = least_float(mx, R.near_e(min_p), [&](float l) { return R.scaled(l, kk) >= least_e; });
         if (least > bound.l) { bound = {least, ~0u}; total = 0; }
     }
 
@@ -598,6 +608,7 @@ struct Work {
     u64 sum[TP_MAX_PARTS];                         // the parts' sums of the kept e
     float max[TP_MAX_PARTS];                       // their largest logits, NaN where one is NaN or +Inf
     u64 total;                                     // the sum over the row where it is known
+    u64 before, want;                              // top-p: the sum in front of the listed step, the sum to be reached
     Bound bound;
     int n_list;
 };
@@ -699,8 +710,8 @@ __device__ __forceinline__ Range range_of(const TpParams& P, const Work& W, cons
     r.want = find_in_bins<1024>(S, 0, (u64)s.k, count ? -1.0 : fmax((double)s.top_p, 0.0));
     const int step = S.found;
     r.before = count ? 0 : S.found_before;
-    r.least = step < TP_BINS - 1 ? least_float(s.max, [&](float l) { return R.step(l) <= step; }) : -__builtin_inff();
-    r.above = !count && step > 0 ? least_float(s.max, [&](float l) { return R.step(l) < step; }) : __builtin_inff();
+    r.least = step < TP_BINS - 1 ? least_float(s.max, R.end_of(step), [&](float l) { return R.step(l) <= step; }) : -__builtin_inff();
+    r.above = !count && step > 0 ? least_float(s.max, R.end_of(step - 1), [&](float l) { return R.step(l) < step; }) : __builtin_inff();
     return r;
 }
 
@@ -712,6 +723,7 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void part_list_kern
     if (s.plain() || (s.k == P.vocab && !(s.top_p < 1.f))) return;
     const Row R = {s.max, s.c, S.table};
     const Range r = range_of(P, W, s, R, S);
+    if (blockIdx.x == 0 && threadIdx.x == 0) { W.before = r.before; W.want = r.want; }
     part_of<LT>(P, row, blockIdx.x).tokens([&](float l, int id) {
         if (!(l >= r.least && l < r.above)) return;
         const int at = __hip_atomic_fetch_add(&W.n_list, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -736,7 +748,6 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void row_bound_kern
     if (s.k < P.vocab || s.top_p < 1.f) {
         const int n = W.n_list;
         if (n <= TP_LIST) {
-            const Range r = range_of(P, W, s, R, S);
             for (int i = tid; i < n; i += 1024) S.list[i] = W.list[i];
             __syncthreads();
             if (s.k < P.vocab) {
@@ -756,7 +767,7 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void row_bound_kern
                     total = with;
                 }
             } else {
-                bound = bound_of(find_in_list<1024>(S, n, r.before, r.want, -1.0, with, mass));
+                bound = bound_of(find_in_list<1024>(S, n, W.before, W.want, -1.0, with, mass));
                 total = with;
             }
         } else {                                            // more tokens than the list holds: the whole row, by this workgroup
@@ -773,7 +784,7 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void row_bound_kern
     if (s.min_p > 0.f) {
         const double least_e = ldexp((double)s.min_p, P.frac);
         int kk;
-        const float least = least_float(s.max, [&](float l) { return R.scaled(l, kk) >= least_e; });
+        const float least = least_float(s.max, R.near_e(s.min_p), [&](float l) { return R.scaled(l, kk) >= least_e; });
         if (least > bound.l) { bound = {least, ~0u}; total = 0; }
     }
     if (tid == 0) { W.bound = bound; W.total = total; }
