@@ -39,12 +39,14 @@ template <typename WT> struct Eight;
 template <> struct Eight<bf16_t> {
     uint4 v;
     __device__ __forceinline__ void load(const char* p) { v = ld16_q(p); }
+    __device__ __forceinline__ void keep() { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }   // (its floats are made again, not kept: registers)
     __device__ __forceinline__ unsigned word(int i) const { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
     __device__ __forceinline__ float get(int e) const { return __uint_as_float(e & 1 ? word(e >> 1) & 0xFFFF0000u : word(e >> 1) << 16); }
 };
 template <> struct Eight<float> {
     f32x4 lo, hi;
     __device__ __forceinline__ void load(const char* p) { lo = load4_q<float>(p); hi = load4_q<float>(p + 16); }
+    __device__ __forceinline__ void keep() {}
     __device__ __forceinline__ float get(int e) const { return e < 4 ? lo[e & 3] : hi[e & 3]; }
 };
 template <typename WT> __device__ __forceinline__ void store8(char* p, const float (&x)[8]) {
@@ -118,6 +120,8 @@ __global__ __launch_bounds__(64 * PC_WAVES) void cache_write_kernel(const PcPara
     amax = wave_max_u32(amax);
     const bool odd = amax >= 0x7F800000u;                   // Inf or NaN among them: they do not count for the scale
     if (odd) {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) x[i].keep();
         amax = 0;
 #pragma unroll
         for (int i = 0; i < PASSES; ++i)
@@ -135,6 +139,7 @@ __global__ __launch_bounds__(64 * PC_WAVES) void cache_write_kernel(const PcPara
     for (int i = 0; i < PASSES; ++i) {
         const int t = i * RP + lr;
         float y[8];
+        x[i].keep();
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = x[i].get(e) * inv;
         if (odd)

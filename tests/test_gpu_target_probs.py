@@ -248,3 +248,43 @@ def test_two_streams_at_once():
                 got.append(call(x, settings, r, keep=keep))
     torch.cuda.synchronize()
     assert all(p.equal(q) for g in got for p, q in zip(g, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_masked_and_broken_rows_of_a_large_vocabulary(dtype):
+    """The same where several workgroups share a row: what one of them sees decides for all."""
+    import torch
+    V = 65536 + 11
+    x, r = language(1, 8, V, dtype, 5)
+    x[0, 0, ::3] = -math.inf
+    x[0, 1] = -math.inf
+    x[0, 1, V - 1] = -2.0
+    x[0, 2] = -math.inf
+    x[0, 3, V - 1] = math.nan
+    x[0, 4, 20000] = math.inf
+    x[0, 5, 5:] = torch.finfo(x.dtype).min
+    x[0, 6] = 0.25
+    x[0, 7, :V - 300] = -math.inf
+    odd = [1, 2, 3, 4, 5, 7]
+    for settings in (None, dict(top_k=[100], top_p=[0.9]), dict(top_p=[0.99], min_p=[0.01]), dict(top_k=[40000]), dict(temperature=[0.0])):
+        out, ids, id_p = call(x, settings, r)
+        check(x, settings, r, out, ids, id_p, at=[0] + odd)
+        _, ids2, id_p2 = call(x, settings, r, probs=False)
+        assert ids2.equal(ids) and torch.equal(id_p2.nan_to_num(7.0), id_p.nan_to_num(7.0))
+        alone, _, _ = call(x, settings)
+        assert torch.equal(alone.nan_to_num(7.0), out.nan_to_num(7.0))
+    out, ids, _ = call(x, dict(top_k=[70000], top_p=[0.5]), r)
+    n = math.ceil(V / 2)
+    assert (out[0, 6, :n] > 0).all() and (out[0, 6, n:] == 0).all() and int(ids[0, 6]) == min(int(float(r[0, 6]) * n), n - 1)
+
+
+def test_a_row_is_the_same_alone_and_among_others():
+    """One workgroup per row (many rows) or several: the same bits."""
+    import torch
+    x, r = language(1, 300, 70000, "bf16", 6)
+    settings = dict(temperature=[0.9], top_p=[0.9])
+    out, ids, id_p = call(x, settings, r)
+    one, one_id, one_p = call(x[:, :100].contiguous(), settings, r[:, :100].contiguous())
+    assert one.equal(out[:, :100]) and one_id.equal(ids[:, :100]) and one_p.equal(id_p[:, :100])
+    few, few_id, few_p = call(x[:, 7:9].contiguous(), settings, r[:, 7:9].contiguous())
+    assert few.equal(out[:, 7:9]) and few_id.equal(ids[:, 7:9]) and few_p.equal(id_p[:, 7:9])
