@@ -155,6 +155,23 @@ struct Bound {
     float l;
     unsigned id;
     __device__ __forceinline__ bool keeps(float x, unsigned i) const { return x > l || (x == l && i <= id); }
+    __device__ __forceinline__ bool all() const { return l == -__builtin_inff() && id == ~0u; }
+    // of a vector's logits, ids from `first` on, the ones that are kept (most vectors have no logit like the bound's)
+    template <int N> __device__ __forceinline__ unsigned kept(const float (&x)[N], unsigned first) const {
+        unsigned yes = 0, same = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            yes |= x[e] > l ? 1u << e : 0;
+            same |= x[e] == l ? 1u << e : 0;
+        }
+        if (__ballot(same != 0)) {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (first + e > id) same &= ~(1u << e);
+            yes |= same;
+        }
+        return yes;
+    }
 };
 __device__ __forceinline__ Bound bound_of(u64 c) {
     return {uniform(logit_of((unsigned)(c >> TP_MAX_LOG))), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)c & ((1u << TP_MAX_LOG) - 1))};
@@ -193,12 +210,12 @@ template <typename LT, int T> struct Logits {               // T threads
             next = after;
         }
     }
-    // f(logit, id) of the row's tokens
+    // f(logit, id) of the row's tokens, and of some behind its end at -Inf
     template <typename F> __device__ __forceinline__ void tokens(F f) const {
         each([&](const u32x4& x, int at) {
 #pragma unroll
             for (int e = 0; e < Vec<LT>::N; ++e) {
-                if (at * Vec<LT>::N + e < vocab) f(Vec<LT>::get(x, e), at * Vec<LT>::N + e);
+                f(Vec<LT>::get(x, e), at * Vec<LT>::N + e);
                 if (e & 1) __builtin_amdgcn_sched_barrier(0);   // (two at a time: registers)
             }
         });
@@ -207,7 +224,8 @@ template <typename LT, int T> struct Logits {               // T threads
 
 __device__ __forceinline__ void lds_add(u64* p, u64 v) { __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void lds_add(unsigned* p, unsigned v) { __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
-__device__ __forceinline__ void list_add(Shared& S, u64 c) {
+__device__ __forceinline__ void list_add(Shared& S, u64 c, int vocab) {
+    if (((unsigned)c & ((1u << TP_MAX_LOG) - 1)) >= (unsigned)vocab) return;
     const int at = __hip_atomic_fetch_add(&S.n_list, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     if (at < TP_LIST) S.list[at] = c;
 }
@@ -330,14 +348,16 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
     for (int i = tid; i < TP_BINS; i += T) S.h.mass[i] = 0;
     if (tid == 0) S.n_list = 0;
     __syncthreads();
-    L.tokens([&](float l, int id) {
-        if (!within.keeps(l, id)) return;
+    auto count = [&](float l) {
         if constexpr (BY_MASS) {
             int k;
             const u64 m = R.mass(l, k);
             lds_add(&S.h.mass[R.step_of(k)], m);
         } else lds_add((unsigned*)&S.h.mass[R.step(l)], 1u);
-    });
+    };
+    // (what is behind the row's end has no mass, and counts in the last step, behind all that is wanted)
+    if (within.all()) L.tokens([&](float l, int) { count(l); });
+    else L.tokens([&](float l, int id) { if (within.keeps(l, id)) count(l); });
     __syncthreads();
     want = find_in_bins<T>(S, 0, want, of_all);
     const int step = S.found;
@@ -346,7 +366,7 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
     const float least = step < TP_BINS - 1 ? least_float(mx, R.end_of(step), [&](float l) { return R.step(l) <= step; }) : -__builtin_inff();
     const float above = step > 0 ? least_float(mx, R.end_of(step - 1), [&](float l) { return R.step(l) < step; }) : __builtin_inff();
     L.tokens([&](float l, int id) {
-        if (l >= least && l < above && within.keeps(l, id)) list_add(S, place(l, id));
+        if (l >= least && l < above && within.keeps(l, id)) list_add(S, place(l, id), L.vocab);
     });
     __syncthreads();
     if (S.n_list <= TP_LIST) return find_in_list<T>(S, S.n_list, before, want, -1.0, with, weight);
@@ -359,7 +379,7 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
         __syncthreads();
         L.tokens([&](float l, int id) {
             const u64 c = place(l, id);
-            if (!(l >= least && l < above && within.keeps(l, id)) || c >> (shift + 11) != prefix) return;
+            if (!(l >= least && l < above && within.keeps(l, id)) || c >> (shift + 11) != prefix || id >= L.vocab) return;
             const int digit = (int)(c >> shift) & (TP_BINS - 1);
             lds_add(&S.h.count[digit], 1u);
             lds_add(&S.h.mass[digit], weight(l));
@@ -371,7 +391,7 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
         if (S.h.count[S.found] > TP_LIST && shift > 0) continue;   // (at the last digit it is one token)
         L.tokens([&](float l, int id) {
             const u64 c = place(l, id);
-            if (c >> shift == prefix && within.keeps(l, id)) list_add(S, c);
+            if (c >> shift == prefix && within.keeps(l, id)) list_add(S, c, L.vocab);
         });
         __syncthreads();
         return find_in_list<T>(S, S.n_list, before, want, -1.0, with, weight);
@@ -382,13 +402,22 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
 template <int T, typename LT> __device__ __forceinline__ u64 sum_cells(const Logits<LT, T>& L, const Row& R, Shared& S, Bound bound) {
     constexpr int N = Vec<LT>::N, PER = TP_MAX_CELLS / T;
     const int tid = threadIdx.x, lane = tid & 63;
+    const bool all = bound.all();
     L.each([&](const u32x4& x, int at) {
         u64 m = 0;
+        if (all) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float l = Vec<LT>::get(x, e);
-            if (at * N + e < L.vocab && bound.keeps(l, at * N + e)) m += R.mass(l);
-            if (e & 1) __builtin_amdgcn_sched_barrier(0);
+            for (int e = 0; e < N; ++e) {
+                m += R.mass(Vec<LT>::get(x, e));
+                if (e & 1) __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float l = Vec<LT>::get(x, e);
+                if (bound.keeps(l, at * N + e)) m += R.mass(l);
+                if (e & 1) __builtin_amdgcn_sched_barrier(0);
+            }
         }
         if (__ballot(m != 0)) m = wave_scan(m);
         if (lane == 63) S.cell[(at - L.begin) >> 6] = m;
@@ -429,14 +458,14 @@ __device__ __forceinline__ void draw_from_cells(const TpParams& P, const Logits<
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         const float l = Vec<LT>::get(x, e);
-        if (at * N + e < L.vocab && bound.keeps(l, at * N + e)) mine += R.mass(l);
+        if (bound.keeps(l, at * N + e)) mine += R.mass(l);
     }
     u64 to = S.found_before + wave_scan(mine) - mine;
     if (to <= want && to + mine > want)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float l = Vec<LT>::get(x, e);
-            const u64 m = at * N + e < L.vocab && bound.keeps(l, at * N + e) ? R.mass(l) : 0;
+            const u64 m = bound.keeps(l, at * N + e) ? R.mass(l) : 0;
             if (to <= want && to + m > want) {
                 P.ids[row] = at * N + e;
                 int kk;
@@ -455,20 +484,35 @@ __device__ __forceinline__ void write_probs(const TpParams& P, const Logits<LT, 
     constexpr int N = Vec<LT>::N;
     const int V = L.vocab;
     float* out = P.probs + row * V;
+    const bool all = bound.all();
     const double cy = R.c / TP_TABLE;
     const float inv = (float)(1.0 / ldexp((double)total, -P.frac));
     L.each([&](const u32x4& x, int at) {
         if (at >= L.nvec) return;                           // (the next part's)
-        float p[N];
+        float p[N], l[N];
+        auto prob = [&](float l) {
+            const double y = __builtin_fmax(((double)l - R.max) * cy, -1000.0), t = y + 6755399441055744.0;   // (1.5 * 2^52: the low word is rint(y))
+            return ldexpf(__builtin_amdgcn_exp2f((float)(y - (t - 6755399441055744.0))) * inv, __double2loint(t));
+        };
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float l = Vec<LT>::get(x, e);
-            p[e] = 0.f;
-            if (bound.keeps(l, at * N + e) && l > -__builtin_inff()) {
-                const double y = __builtin_fmax(((double)l - R.max) * cy, -1000.0), n = rint(y);
-                p[e] = ldexpf(__builtin_amdgcn_exp2f((float)(y - n)) * inv, (int)n);
+        for (int e = 0; e < N; ++e) l[e] = Vec<LT>::get(x, e);
+        if (all) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                p[e] = prob(l[e]);                          // (-Inf: 2^-1000 is 0)
+                if (e & 1) __builtin_amdgcn_sched_barrier(0);
             }
-            if (e & 1) __builtin_amdgcn_sched_barrier(0);
+        } else {
+            const unsigned kept = bound.kept(l, at * N);
+#pragma unroll
+            for (int e = 0; e < N; ++e) p[e] = 0.f;
+            if (__ballot(kept != 0)) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (kept >> e & 1) p[e] = prob(l[e]);
+                    if (e & 1) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
 #pragma unroll
         for (int q = 0; q < N; q += 4) {
@@ -549,7 +593,7 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
             const int step = S.found;
             if (step < TP_BINS - 1) {
                 const float least = least_float(mx, R.end_of(step), [&](float l) { return R.step(l) <= step; });
-                L.tokens([&](float l, int id) { if (l >= least) list_add(S, place(l, id)); });
+                L.tokens([&](float l, int id) { if (l >= least) list_add(S, place(l, id), L.vocab); });
                 __syncthreads();
                 listed = S.n_list <= TP_LIST;
             }
@@ -725,7 +769,7 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void part_list_kern
     const Range r = range_of(P, W, s, R, S);
     if (blockIdx.x == 0 && threadIdx.x == 0) { W.before = r.before; W.want = r.want; }
     part_of<LT>(P, row, blockIdx.x).tokens([&](float l, int id) {
-        if (!(l >= r.least && l < r.above)) return;
+        if (!(l >= r.least && l < r.above) || id >= P.vocab) return;
         const int at = __hip_atomic_fetch_add(&W.n_list, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (at < TP_LIST) W.list[at] = place(l, id);
     });
@@ -804,7 +848,9 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void part_sum_kerne
     const Row R = {s.max, s.c, s_table};
     const Bound bound = W.bound;
     u64 m = 0;
-    part_of<LT>(P, row, blockIdx.x).tokens([&](float l, int id) { if (bound.keeps(l, id)) m += R.mass(l); });
+    const auto L = part_of<LT>(P, row, blockIdx.x);
+    if (bound.all()) L.tokens([&](float l, int) { m += R.mass(l); });
+    else L.tokens([&](float l, int id) { if (bound.keeps(l, id)) m += R.mass(l); });
     m = wave_scan(m);
     if ((tid & 63) == 63) s_sum[tid >> 6] = m;
     __syncthreads();
