@@ -103,7 +103,7 @@ struct Shared {
     };
     u64 list[TP_LIST];
     u64 red[16], red2[16];
-    u64 found_before;
+    u64 found_before, found_at;
     unsigned red32[16];
     int found, n_list;
 };
@@ -270,24 +270,29 @@ template <int T> __device__ __forceinline__ u64 find_in_bins(Shared& S, u64 befo
 // with: the sum up to and with that token.  Takes and leaves synchronised
 template <int T, typename W> __device__ __forceinline__ u64 find_in_list(Shared& S, int n, u64 before, u64 want, double of_all, u64& with, W w) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (n <= 64) {                                          // every wavefront by itself
-        const u64 c = lane < n ? S.list[lane] : ~0ull, m = lane < n ? w(logit_of((unsigned)(c >> TP_MAX_LOG))) : 0;
-        if (of_all >= 0.0) {
-            const u64 total = lane_u64(wave_scan(m), 63);
-            const double t = ceil(of_all * (double)total);
-            want = t >= 1.0 ? min((u64)t, total) : 1;
+    if (n <= 64) {                                          // one wavefront
+        if (wave == 0) {
+            const u64 c = lane < n ? S.list[lane] : ~0ull, m = lane < n ? w(logit_of((unsigned)(c >> TP_MAX_LOG))) : 0;
+            if (of_all >= 0.0) {
+                const u64 total = lane_u64(wave_scan(m), 63);
+                const double t = ceil(of_all * (double)total);
+                want = t >= 1.0 ? min((u64)t, total) : 1;
+            }
+            u64 upto = before;                              // with everything up to the lane's own token
+            for (int j = 0; j < n; ++j) {
+                const u64 cj = lane_u64(c, j), mj = lane_u64(m, j);
+                upto += cj <= c ? mj : 0;
+            }
+            const u64 hit = __ballot(upto >= want && upto - m < want && m);
+            const int at = hit ? __builtin_ctzll(hit) : 0;
+            S.found_at = lane_u64(c, at);
+            S.found_before = lane_u64(upto, at);
         }
-        u64 upto = before;                                  // with everything up to the lane's own token
-        for (int j = 0; j < n; ++j) {
-            const u64 cj = lane_u64(c, j), mj = lane_u64(m, j);
-            upto += cj <= c ? mj : 0;
-        }
-        const u64 hit = __ballot(upto >= want && upto - m < want && m);
-        __syncthreads();                                    // (the list may be written again)
-        if (!hit) return ~0ull;
-        const int at = __builtin_ctzll(hit);
-        with = lane_u64(upto, at);
-        return lane_u64(c, at);
+        __syncthreads();
+        with = S.found_before;
+        const u64 at = S.found_at;
+        __syncthreads();                                    // (both may be written again)
+        return at;
     }
     constexpr int PER = TP_LIST / T;
     u64 c[PER], m[PER];
