@@ -131,7 +131,8 @@ PS_API int ps_verify_walk_static(const ps_tree_shape* tree, const ps_verify_args
  *   kv_offsets        HOST [batch+1], in positions as in ps_draft_step_args, multiples of 32: sequence b owns the blocks
  *                     kv_offsets[b] / 32 .. kv_offsets[b+1] / 32 - 1
  * Nothing has to be initialised: a block is valid from the first position of it that is written.  Supported: head_dim 64 or 128,
- * batch 1..PS_CACHE_MAX_BATCH, kv_offsets below 2^36.
+ * n_kv_heads up to 1024, batch 1..PS_CACHE_MAX_BATCH, kv_offsets below 2^36.
+ * For this and all that follows: the stream and the device pointers belong to the current device, outputs overlap nothing else.
  */
 #define PS_CACHE_BLOCK 32
 #define PS_CACHE_MAX_BATCH 64
@@ -208,7 +209,7 @@ PS_API int ps_cache_read(const ps_cache_read_args* args, void* stream);
  *   k_rows, v_rows  DEVICE [batch][n_nodes][n_kv_heads][head_dim], dtype: the rows' own keys and values, used as they are (they reach
  *                   the cache when the walk has accepted them).  Both NULL: the rows attend to the cached positions only
  *   q_stride, kv_stride  elements between consecutive rows of q, and of k_rows and v_rows (0: no gap), as row_stride above
- *   scale           0 stands for 1 / sqrt(head_dim)
+ *   scale           0 stands for 1 / sqrt(head_dim); else 2^-20 .. 2^20
  *   out             DEVICE [batch][n_nodes][n_heads][head_dim], dtype, written
  *   lse             DEVICE [batch][n_nodes][n_heads] float32 or NULL, written: log of the sum of exp(scale * q k)
  *   kv_len, kv_len_dev  as for ps_cache_write
@@ -219,7 +220,7 @@ PS_API int ps_cache_read(const ps_cache_read_args* args, void* stream);
  * Scores, softmax and sums are float32.  bf16: probabilities are rounded to bf16 before they are multiplied with the values.
  * Errors: PS_ERR_NULL; PS_ERR_SHAPE (also a malformed tree, a scale that is negative or not finite); PS_ERR_OFFSETS;
  * PS_ERR_KV_CAPACITY (kv_len[b] exceeds the sequence's blocks); PS_ERR_WORKSPACE; PS_ERR_UNSUPPORTED (head_dim, batch, alignment
- * to 4 bytes, n_heads > 1024, kv_len above 2^30); PS_ERR_DEVICE.
+ * to 4 bytes, n_heads > 1024, scale, kv_len above 2^30); PS_ERR_DEVICE.
  */
 typedef struct ps_tree_attn_args {
     int32_t batch, n_heads, dtype;

@@ -616,7 +616,8 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
     if (a->n_heads < 1 || a->n_heads % heads != 0) return PS_ERR_SHAPE;
     if (a->dtype != PS_F32 && a->dtype != PS_BF16) return PS_ERR_SHAPE;
     if (!(a->scale >= 0.f) || !(a->scale < __builtin_inff())) return PS_ERR_SHAPE;
-    if (a->n_heads > 1024) return PS_ERR_UNSUPPORTED;
+    // (with a block's scale, 2^-100 and more, the scores' constant stays a normal number: a hidden key's -Inf times 0 would be NaN)
+    if (a->n_heads > 1024 || (a->scale > 0.f && (a->scale < 0x1p-20f || a->scale > 0x1p20f))) return PS_ERR_UNSUPPORTED;
     P.batch = a->batch; P.n_heads = a->n_heads; P.heads = heads; P.grp = a->n_heads / heads; P.nodes = N; P.rows = N * P.grp;
     P.tiles = (P.rows + TA_TILE - 1) / TA_TILE;
     P.c = (float)((a->scale > 0.f ? (double)a->scale : 1.0 / __builtin_sqrt((double)d)) * 1.4426950408889634074);

@@ -282,3 +282,64 @@ def test_two_streams_at_once():
                 got.append(call(cache, fanout(4, 2), q, k, v, [6000, 50], "bf16", keep=keep)[0])
     torch.cuda.synchronize()
     assert all(g.equal(want) for g in got)
+
+
+def _whole(cache, parent, q, k, v, lens, heads):
+    """out and lse of some kv heads in float64 on the GPU, from the codes."""
+    import torch
+    values, d, nq = torch.from_numpy(orc.VALUES).cuda(), cache.d, q.shape[2]
+    grp, n = nq // cache.heads, len(parent)
+    sees = torch.eye(n, dtype=torch.bool, device="cuda:0")
+    for s in range(1, n):
+        sees[s] |= sees[parent[s]]
+    for b, length in enumerate(lens):
+        blocks = slice(cache.offsets[b] // 32, cache.offsets[b] // 32 + (length + 31) // 32)
+        for h in heads:
+            kv = []
+            for name, own in (("k", k), ("v", v)):
+                at = torch.from_numpy(TU.places(name, d)).cuda()
+                x = values[cache.codes[name][blocks, h].long()[:, at]].reshape(-1, 32, d) * cache.scales[name][blocks, h].double()[:, None, None]
+                kv.append(torch.cat((x.reshape(-1, d)[:length], own[b, :, h].double())))
+            x = q[b, :, h * grp:(h + 1) * grp].double().transpose(0, 1).reshape(grp * n, d) @ kv[0].t() / math.sqrt(d)
+            x[:, length:].masked_fill_(~sees.repeat(grp, 1), -math.inf)
+            lse = torch.logsumexp(x, 1)
+            p = torch.exp(x - lse[:, None])
+            yield b, h, *(y.reshape(grp, n, -1).transpose(0, 1) for y in (p @ kv[1], p @ kv[1].abs(), lse))
+
+
+def _check_whole(cache, parent, q, k, v, lens, heads, out, lse):
+    grp = q.shape[2] // cache.heads
+    for b, h, want, size, want_lse in _whole(cache, parent, q, k, v, lens, heads):
+        mine = slice(h * grp, (h + 1) * grp)
+        # (the formula of the file's head for bf16, with Q <= 16 for these inputs: scores are N(0, 1) up to their keys' rounding)
+        n = lens[b] + len(parent)
+        tol = (2 * (cache.d + 4) * 2.0 ** -24 * 16 + 2 * n * 2.0 ** -24 + 2.0 ** -19 + 2.0 ** -8) * size + 2.0 ** -8 * want.abs()
+        assert ((out[b, :, mine].double() - want).abs() <= tol).all(), (b, h)
+        assert ((lse[b, :, mine].double() - want_lse[..., 0]).abs() <= (cache.d + 4) * 2.0 ** -24 * 16 + n * 2.0 ** -24 + 2.0 ** -18).all()
+
+
+def test_codes_that_pass_the_caches_by():
+    """One tile of rows over more than 192 MB of codes."""
+    lens, heads = (20000,), 40
+    cache, q, k, v = make("bf16", heads, heads, 128, lens, 1, seed=9)
+    out, lse = call(cache, [-1], q, k, v, list(lens), "bf16")
+    _check_whole(cache, [-1], q, k, v, lens, (0, 17, heads - 1), out, lse)
+
+
+@pytest.mark.parametrize("parent", [[-1], fanout(3), fanout(4, 2, 2, 1, 1)], ids=lambda p: "%d nodes" % len(p))
+def test_codes_beyond_32_bits_of_bytes(parent):
+    """Sequences whose codes lie more than 4 GiB behind the cache's start."""
+    import torch
+    heads, d, lens = 16, 128, (95, 700)
+    blocks = (1 << 32) // (heads * 32 * d) + 1
+    cache = TU.Cache(1, d, [32])
+    cache.heads, cache.offsets = heads, [32 * blocks, 32 * (blocks + 3), 32 * (blocks + 25)]
+    cache.codes = {n: torch.full(((blocks + 26), heads, 32 * d), 0x7F, dtype=torch.uint8, device="cuda:0") for n in "kv"}
+    cache.scales = {n: torch.full((blocks + 26, heads), float("nan"), device="cuda:0") for n in "kv"}
+    cache.struct = VF.make_cache(heads, d, cache.codes["k"].data_ptr(), cache.codes["v"].data_ptr(), cache.scales["k"].data_ptr(), cache.scales["v"].data_ptr(), cache.offsets)
+    x = [TU.normal((2, 700, heads, d), i, "bf16") for i in range(2)]
+    cache.write(x[0], x[1], [0, 0], "bf16", n_seq=lens)
+    q = TU.normal((2, len(parent), 2 * heads, d), 5, "bf16")
+    k, v = (TU.normal((2, len(parent), heads, d), 6 + i, "bf16") for i in range(2))
+    out, lse = call(cache, parent, q, k, v, list(lens), "bf16")
+    _check_whole(cache, parent, q, k, v, lens, (0, heads - 1), out, lse)

@@ -124,7 +124,7 @@ def test_bad_reads_are_refused(status, kw):
     (B.PS_ERR_SHAPE, dict(n_heads=3)), (B.PS_ERR_SHAPE, dict(n_heads=0)), (B.PS_ERR_SHAPE, dict(dtype=2)), (B.PS_ERR_SHAPE, dict(scale=-1.0)),
     (B.PS_ERR_SHAPE, dict(scale=float("nan"))), (B.PS_ERR_SHAPE, dict(scale=float("inf"))), (B.PS_ERR_SHAPE, dict(kv_len=(-1, 0))),
     (B.PS_ERR_SHAPE, dict(q_stride=255)), (B.PS_ERR_SHAPE, dict(kv_stride=127)), (B.PS_ERR_UNSUPPORTED, dict(q_stride=257)),
-    (B.PS_ERR_UNSUPPORTED, dict(n_heads=2048)), (B.PS_ERR_UNSUPPORTED, dict(out=0x100002)), (B.PS_ERR_UNSUPPORTED, dict(lse=0x100001)),
+    (B.PS_ERR_UNSUPPORTED, dict(n_heads=2048)), (B.PS_ERR_UNSUPPORTED, dict(scale=2.0 ** -21)), (B.PS_ERR_UNSUPPORTED, dict(scale=2.0 ** 21)), (B.PS_ERR_UNSUPPORTED, dict(out=0x100002)), (B.PS_ERR_UNSUPPORTED, dict(lse=0x100001)),
     (B.PS_ERR_KV_CAPACITY, dict(kv_len=(65, 0))), (B.PS_ERR_KV_CAPACITY, dict(kv_len=(0, 97))),
 ])
 def test_bad_attention_calls_are_refused(status, kw):
@@ -158,6 +158,19 @@ def _probs(batch=2, rows=3, vocab=100, dtype=B.PS_F32, **kw):
     a = VF.ps_target_probs_args()
     a.batch, a.rows, a.vocab, a.dtype = batch, rows, vocab, dtype
     return _set(a, ("logits", "probs", "ids", "r"), kw)
+
+
+def test_distribution_workspace():
+    need = VF.ps_target_probs_workspace_bytes(_probs(batch=8, rows=1, vocab=128256))
+    assert need > 0 and need % 256 == 0                      # (several workgroups per row)
+    assert VF.ps_target_probs_workspace_bytes(_probs(batch=8, rows=61, vocab=128256)) == 0 == VF.ps_target_probs_workspace_bytes(_probs(vocab=32000))
+    assert VF.ps_target_probs_workspace_bytes(_probs(vocab=0)) == 0
+    a = _probs(batch=8, rows=1, vocab=128256, workspace=0x100000, workspace_bytes=need - 1)
+    assert VF.ps_target_probs(a, None) == B.PS_ERR_WORKSPACE
+    a.workspace_bytes, a.workspace = need, 0x100080
+    assert VF.ps_target_probs(a, None) == B.PS_ERR_WORKSPACE
+    a.workspace = None
+    assert VF.ps_target_probs(a, None) == B.PS_ERR_NULL
 
 
 @pytest.mark.parametrize("status,kw", [
