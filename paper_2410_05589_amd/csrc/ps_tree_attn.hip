@@ -621,38 +621,59 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
     P.batch = a->batch; P.n_heads = a->n_heads; P.heads = heads; P.grp = a->n_heads / heads; P.nodes = N; P.rows = N * P.grp;
     P.tiles = (P.rows + TA_TILE - 1) / TA_TILE;
     P.c = (float)((a->scale > 0.f ? (double)a->scale : 1.0 / __builtin_sqrt((double)d)) * 1.4426950408889634074);
-    long long total = 0;
+    long long total = 0, blocks_of_longest = 0;
     for (int b = 0; b < a->batch; ++b) {
         P.first[b] = (unsigned)(a->cache->kv_offsets[b] / PC_BLOCK);
         P.len[b] = a->kv_len[b];
         if (P.len[b] < 0) return PS_ERR_SHAPE;
         if (P.len[b] > a->cache->kv_offsets[b + 1] - a->cache->kv_offsets[b]) return PS_ERR_KV_CAPACITY;
         if (P.len[b] > 1 << 30) return PS_ERR_UNSUPPORTED;
-        total += (P.len[b] + PC_BLOCK - 1) / PC_BLOCK;
+        const int blocks = (P.len[b] + PC_BLOCK - 1) / PC_BLOCK;
+        total += blocks;
+        blocks_of_longest = std::max<long long>(blocks_of_longest, blocks);
     }
-    L.wr = P.tiles >= 3 ? 4 : P.tiles;
-    L.waves = a->dtype == PS_BF16 && L.wr < 4 ? 8 : 4;
-    L.groups = (P.tiles + L.wr - 1) / L.wr;
     // codes that are read once and are more than the memory-side cache (256 MB) holds pass the caches by (one row tile, 32 x 2048 positions of 32 heads, 537 MB:
     // 114 -> 97 us; of 8 heads, 134 MB: 26.7 -> 28.1)
     P.stream = P.tiles == 1 && total * heads * PC_BLOCK * d * 2 > 192LL << 20;
-    // as many workgroups as run at once (256 compute units, two workgroups of four bf16 wavefronts on each) where a split has at least two blocks per wavefront:
-    // the least `per` that gives no more.  (Sequences of 4099 ... 12288 in one batch, one workgroup each: with the mean of all blocks as `per` 288, two rounds)
-    const int at_once = a->dtype == PS_BF16 && L.waves == 4 ? 512 : 256;
-    const long long units = (long long)heads * L.groups;
-    auto count = [&](long long per) {
-        long long n = 0;
-        for (int b = 0; b < a->batch; ++b) n += std::max<long long>(1, ((P.len[b] + PC_BLOCK - 1) / PC_BLOCK + per - 1) / per);
-        return n * units;
+
+    const bool bf = a->dtype == PS_BF16;
+    // How rows and blocks are cut: two or four tiles of rows per workgroup, about 256 workgroups or 512, whichever is estimated to take least time.  (bf16, us,
+    // four tiles and 512 always / as estimated: 61 nodes, 32 heads that share 8, 2048 positions: 27.3 / 17.8, 8 x 2048: 44.1 / 29.5, 16 x 2048: 68.8 / 54.7 (two tiles:
+    // 61), 32 x 2048: 93.6 / 89.3 (two tiles: 133), 64 x 1000: 105.5 / 107.9 (168); float32, four / two: 2048 33.3 / 26.7, 64 x 1000 298 / 312)
+    auto cut = [&](int wr, int waves, long long at_once) {  // the least `per` that gives no more workgroups than that, where a split has two blocks per wavefront
+        const long long units = (long long)heads * ((P.tiles + wr - 1) / wr);
+        auto count = [&](long long per) {
+            long long n = 0;
+            for (int b = 0; b < a->batch; ++b) n += std::max<long long>(1, ((P.len[b] + PC_BLOCK - 1) / PC_BLOCK + per - 1) / per);
+            return n * units;
+        };
+        // (a split's codes stay below 2 GiB)
+        long long lo = 2 * (waves / wr), hi = (1LL << 31) / ((long long)heads * PC_BLOCK * d);
+        const long long most = std::max<long long>(at_once, count(hi));
+        while (lo < hi) {
+            const long long mid = (lo + hi) / 2;
+            if (count(mid) <= most) hi = mid; else lo = mid + 1;
+        }
+        const long long groups = count(lo), splits = groups / units, longest = std::min<long long>(lo, blocks_of_longest);
+        // us: 10 for what comes before and after a workgroup's blocks, 0.17 per block and tile of rows on a compute unit (float32: 0.5), rounds of 256
+        // workgroups; two staged ones are on a compute unit, which shares its matrix cores among them; the join, at 4.5 TB/s
+        const double block = (bf ? 0.17 : 0.5) * wr;
+        const long long rounds = (groups + 255) / 256;
+        double t = (bf && wr == 4 ? (groups + 511) / 512 : rounds) * 10 + rounds * longest * block;
+        if (splits > a->batch) t += 4 + (double)splits * heads * P.rows * (d + 4) * 8 / 4.5e6;
+        return std::pair<double, long long>(t, lo);
     };
-    // (a split's codes stay below 2 GiB)
-    long long lo = 2 * (L.waves / L.wr), hi = (1LL << 31) / ((long long)heads * PC_BLOCK * d);
-    const long long most = std::max<long long>(at_once, count(hi));
-    while (lo < hi) {
-        const long long mid = (lo + hi) / 2;
-        if (count(mid) <= most) hi = mid; else lo = mid + 1;
-    }
-    P.per = (int)lo;
+    double best = 0;
+    for (int wr = std::min(P.tiles, 2); wr <= (P.tiles >= 3 ? 4 : std::min(P.tiles, 2)); wr *= 2)
+        for (int at_once = 256; at_once <= (wr == 1 ? 256 : 512); at_once *= 2) {
+            const int waves = bf && wr < 4 ? 8 : 4;
+            const auto c = cut(wr, waves, at_once);
+            if (best > 0 && !(c.first < best)) continue;
+            best = c.first;
+            L.wr = wr; L.waves = waves;
+            P.per = (int)c.second;
+        }
+    L.groups = (P.tiles + L.wr - 1) / L.wr;
     P.split0[0] = 0;
     bool one = true;
     for (int b = 0; b < a->batch; ++b) {
