@@ -10,7 +10,9 @@
 // e is a whole number of 2^-F (F = 62 - log2 V, at most 51), from a double: sums are exact in any order, whoever adds them, and
 // their error is far below what decides a draw.  (Doubles cost no more instructions here than floats, a histogram no more than its additions.)
 //
-// One workgroup per row; the row is read again by each pass, from the caches.
+// One workgroup per row (few rows of a large vocabulary: several, see below); the row is read again by each pass, from the caches.  What bounds it: a pass over a row
+// that makes masses is 25 instructions per token (V 128256: 12 us on one compute unit), one that only compares is a read.  Measured (us; V 32000 float32, 61 rows,
+// top-k 50 and top-p 0.95, probabilities: 20, 3 of them the bytes at a copy's rate; V 128256 bf16, 488 rows, a setting per sequence: 142, bytes 73).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,7 +22,8 @@ namespace {
 
 constexpr int TP_BINS = 2048;                      // steps of 1/32 in y: 64 powers of two, what is below has no mass in F <= 51 bits
 constexpr int TP_LIST = 2048;                      // tokens that are ordered in LDS
-constexpr int TP_SMALL_K = 512;                    // top-k by the threads' maxima
+// top-k by the threads' maxima.  (V 32000, 64 rows, us, by maxima / by the histogram of all: k 50 17.2 / 24.6, k 300 23.0 / 28.0; 512 threads have no more maxima)
+constexpr int TP_SMALL_K = 512;
 constexpr int TP_MAX_LOG = 20;                     // vocab <= 2^20: an id takes 20 bits of c
 constexpr int TP_MAX_CELLS = 4096;                 // wavefronts' shares of a row: 2^20 / (64 * 4)
 constexpr int TP_TABLE_LOG = 8, TP_TABLE = 1 << TP_TABLE_LOG;   // 2^(j/256)
@@ -530,6 +533,20 @@ __device__ __forceinline__ void write_probs(const TpParams& P, const Logits<LT, 
     });
 }
 
+// a row without mass (bad: with a NaN or +Inf)
+__device__ __forceinline__ void no_token(const TpParams& P, size_t row, bool bad) {
+    P.ids[row] = -1;
+    if (P.id_probs) P.id_probs[row] = bad ? __builtin_nanf("") : 0.f;
+}
+// min_p's bound, where it is above `bound`
+__device__ __forceinline__ void apply_min_p(const TpParams& P, const Row& R, float min_p, Bound& bound, u64& total) {
+    if (!(min_p > 0.f)) return;
+    const double least_e = ldexp((double)min_p, P.frac);
+    int kk;
+    const float least = least_float((float)R.max, R.near_e(min_p), [&](float l) { return R.scaled(l, kk) >= least_e; });
+    if (least > bound.l) { bound = {least, ~0u}; total = 0; }
+}
+
 template <typename LT, int T>
 __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
     constexpr int N = Vec<LT>::N, WAVES = T / 64;
@@ -568,12 +585,8 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
     mx = uniform(row_max(mx));
     float* out = P.probs ? P.probs + row * V : nullptr;
     if (bad || mx == -__builtin_inff()) {
-        const float fill = bad ? __builtin_nanf("") : 0.f;
-        if (out) for (int i = tid; i < V; i += T) out[i] = fill;
-        if (P.ids && tid == 0) {
-            P.ids[row] = -1;
-            if (P.id_probs) P.id_probs[row] = fill;
-        }
+        if (out) for (int i = tid; i < V; i += T) out[i] = bad ? __builtin_nanf("") : 0.f;
+        if (P.ids && tid == 0) no_token(P, row, bad);
         return;
     }
     Row R;
@@ -629,12 +642,7 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
             }
         }
     }
-    if (min_p > 0.f) {
-        const double least_e = ldexp((double)min_p, P.frac);
-        int kk;
-        const float least = least_float(mx, R.near_e(min_p), [&](float l) { return R.scaled(l, kk) >= least_e; });
-        if (least > bound.l) { bound = {least, ~0u}; total = 0; }
-    }
+    apply_min_p(P, R, min_p, bound, total);
 
     // the sum of the kept e, where it is not known or a token is drawn
     if (P.ids || total == 0) {
@@ -648,26 +656,33 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
 // ------------------------------------------------------------------------------------------
 // Few rows of a large vocabulary: several workgroups per row, a kernel for each pass.  What a row's workgroups tell each other is in the workspace.
 // ------------------------------------------------------------------------------------------
-constexpr int TP_PART = 16384;                     // tokens per workgroup
-constexpr int TP_SPLIT_ROWS = 128;                 // rows up to which they are cut up
-constexpr int TP_MAX_PARTS = (1 << TP_MAX_LOG) / TP_PART;
+// A workgroup's tokens are a multiple of TP_PART (a pass of 1024 threads over bf16).  Up to TP_SPLIT_ROWS rows: masses of a row take one workgroup long, but every kernel reads
+// the row once more.  (V 128256 bf16, us, cut up / one workgroup per row: 8 rows top-p 35 / 78, no filter 20 / 48, top-k 50 27 / 31; 64 rows top-p 53 / 82, top-k 50
+// 41 / 34; 128 rows top-p 75 / 82, no filter 47 / 54, top-k 50 54 / 37.  So calls with top-k and no top-p, which have masses of a few tokens only, are cut up to a quarter of
+// the rows: 16 rows 28 / 31, 32 rows 33 / 32.  8 rows of V 64000: top-p 35 / 46, no filter 21 / 27, top-k 28 / 21, of V 32000: 36 / 30, 21 / 17, 30 / 16)
+constexpr int TP_PART = 8192;
+constexpr int TP_SPLIT_ROWS = 64;                  // rows up to which they are cut up,
+constexpr int TP_SPLIT_VOCAB = 65536;              // from this vocabulary on
+constexpr int TP_MAX_PARTS = 64;
 struct Work {
     u64 hist[TP_BINS];
     u64 list[TP_LIST];
     u64 sum[TP_MAX_PARTS];                         // the parts' sums of the kept e
     float max[TP_MAX_PARTS];                       // their largest logits, NaN where one is NaN or +Inf
+    int first[TP_MAX_PARTS];                       // the first token of theirs that has it
     u64 total;                                     // the sum over the row where it is known
-    u64 before, want;                              // top-p: the sum in front of the listed step, the sum to be reached
     Bound bound;
+    u64 before, want;                              // top-p: the sum in front of the listed step, the sum to be reached
     int n_list;
 };
 
 // A row's settings and its largest logit (every lane the same); false: nothing to be searched for (bad: NaN or +Inf; max -Inf: no mass)
 struct Setting {
     float max, top_p, min_p;
-    int k;
+    int k, first;                                  // first: the first token that has the largest logit
     bool bad;
     double c;
+    bool search;                                   // top-k of more than one or top-p leave something out: the bound is in the workspace
     __device__ __forceinline__ bool plain() const { return bad || max == -__builtin_inff(); }
 };
 __device__ __forceinline__ Setting setting_of(const TpParams& P, const Work& W, int b) {
@@ -679,14 +694,18 @@ __device__ __forceinline__ Setting setting_of(const TpParams& P, const Work& W, 
     s.top_p = P.top_p ? P.top_p[b] : 1.f;
     const float m = P.min_p ? P.min_p[b] : 0.f;
     s.min_p = m > 0.f ? fminf(m, 1.f) : 0.f;
+    s.search = s.k != 1 && (s.k < P.vocab || s.top_p < 1.f);
     const int lane = threadIdx.x & 63;
     const float x = lane < P.parts ? W.max[lane] : -__builtin_inff();
     s.bad = __ballot(x != x);
     s.max = wave_max(x);
+    const u64 at = __ballot(x == s.max);                    // (parts in order: the first one has the first token)
+    s.first = W.first[at ? __builtin_ctzll(at) : 0];
     s.c = uniform(1.4426950408889634074 * TP_TABLE / (greedy ? 1.0 : (double)t));
     return s;
 }
 static_assert(TP_MAX_PARTS <= 64, "a lane for each part");
+static_assert(TP_PART % (1024 * Vec<bf16_t>::N) == 0, "parts end where passes of 1024 threads do");
 
 template <typename LT> __device__ __forceinline__ Logits<LT, 1024> part_of(const TpParams& P, size_t row, int part) {
     Logits<LT, 1024> L;
@@ -700,28 +719,49 @@ template <typename LT> __device__ __forceinline__ Logits<LT, 1024> part_of(const
 
 template <typename LT> __global__ __launch_bounds__(1024) void part_max_kernel(const TpParams P) {
     __shared__ float s_max[16];
+    __shared__ int s_first;
     const int tid = threadIdx.x, lane = tid & 63, part = blockIdx.x;
     const size_t row = blockIdx.y;
     Work& W = reinterpret_cast<Work*>(P.work)[row];
     for (int i = part * 1024 + tid; i < TP_BINS; i += P.parts * 1024) W.hist[i] = 0;
     if (part == 0 && tid == 0) W.n_list = 0;
+    if (tid == 0) s_first = P.vocab;
     float mx = -__builtin_inff();
+    int first = 0;
     bool bad = false;
-    part_of<LT>(P, row, part).each([&](const u32x4& x, int) {
+    part_of<LT>(P, row, part).each([&](const u32x4& x, int at) {
 #pragma unroll
         for (int e = 0; e < Vec<LT>::N; ++e) {
             const float l = Vec<LT>::get(x, e);
             bad |= !(l < __builtin_inff());
+            first = l > mx ? at * Vec<LT>::N + e : first;
             mx = fmaxf(mx, l);
         }
     });
+    const float mine = mx;
     mx = __ballot(bad) ? __builtin_nanf("") : wave_max(mx);
     if (lane == 0) s_max[tid >> 6] = mx;
     __syncthreads();
     mx = s_max[lane & 15];
     bad = __ballot(mx != mx);
     mx = row_max(mx);
-    if (tid == 0) W.max[part] = bad ? __builtin_nanf("") : mx;
+    if (mine == mx) __hip_atomic_fetch_min(&s_first, first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    __syncthreads();
+    if (tid == 0) {
+        W.max[part] = bad ? __builtin_nanf("") : mx;
+        W.first[part] = s_first;
+    }
+}
+
+// the row's bound and, where it is known, the sum of what it keeps
+__device__ __forceinline__ void bound_of_row(const TpParams& P, const Work& W, const Setting& s, const Row& R, Bound& bound, u64& total) {
+    if (s.search) { bound = W.bound; total = W.total; }
+    else if (s.k == 1) { bound = {s.max, (unsigned)s.first}; total = R.mass(s.max); }
+    else {
+        bound = {-__builtin_inff(), ~0u};
+        total = 0;
+        apply_min_p(P, R, s.min_p, bound, total);
+    }
 }
 
 // the histogram that the row's setting asks for: counts for top-k, else sums of e for top-p
@@ -732,7 +772,7 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void part_hist_kern
     const size_t row = blockIdx.y;
     Work& W = reinterpret_cast<Work*>(P.work)[row];
     const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
-    if (s.plain() || (s.k == P.vocab && !(s.top_p < 1.f))) return;
+    if (s.plain() || !s.search) return;
     if (tid < TP_TABLE) s_table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
     for (int i = tid; i < TP_BINS; i += 1024) s_hist[i] = 0;
     __syncthreads();
@@ -766,13 +806,14 @@ __device__ __forceinline__ Range range_of(const TpParams& P, const Work& W, cons
 
 template <typename LT> __global__ __launch_bounds__(1024, 4) void part_list_kernel(const TpParams P) {
     __shared__ Shared S;
+    const int tid = threadIdx.x;
     const size_t row = blockIdx.y;
     Work& W = reinterpret_cast<Work*>(P.work)[row];
     const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
-    if (s.plain() || (s.k == P.vocab && !(s.top_p < 1.f))) return;
+    if (s.plain() || !s.search) return;
     const Row R = {s.max, s.c, S.table};
     const Range r = range_of(P, W, s, R, S);
-    if (blockIdx.x == 0 && threadIdx.x == 0) { W.before = r.before; W.want = r.want; }
+    if (blockIdx.x == 0 && tid == 0) { W.before = r.before; W.want = r.want; }
     part_of<LT>(P, row, blockIdx.x).tokens([&](float l, int id) {
         if (!(l >= r.least && l < r.above) || id >= P.vocab) return;
         const int at = __hip_atomic_fetch_add(&W.n_list, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -787,55 +828,48 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void row_bound_kern
     const size_t row = blockIdx.x;
     Work& W = reinterpret_cast<Work*>(P.work)[row];
     const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
-    if (s.plain()) return;
-    if (tid < TP_TABLE) S.table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
-    __syncthreads();
+    if (s.plain() || !s.search) return;
     const Row R = {s.max, s.c, S.table};
+    if (tid < TP_TABLE) S.table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
     Bound bound = {-__builtin_inff(), ~0u};
     u64 total = 0, with = 0;
     auto mass = [&](float l) { return R.mass(l); };
-    if (s.k < P.vocab || s.top_p < 1.f) {
-        const int n = W.n_list;
-        if (n <= TP_LIST) {
-            for (int i = tid; i < n; i += 1024) S.list[i] = W.list[i];
-            __syncthreads();
-            if (s.k < P.vocab) {
-                bound = bound_of(find_in_list<1024>(S, n, 0, (u64)s.k, -1.0, with, [](float) { return (u64)1; }));
-                u64 m = 0;
-                for (int i = tid; i < n; i += 1024) {       // tokens behind the bound leave the list: the last place, without mass
-                    const u64 c = S.list[i];
-                    const float l = logit_of((unsigned)(c >> TP_MAX_LOG));
-                    const unsigned id = (unsigned)c & ((1u << TP_MAX_LOG) - 1);
-                    if (bound.keeps(l, id)) m += R.mass(l);
-                    else S.list[i] = place(-__builtin_inff(), id);
-                }
-                block_scan<1024>(m, S, total);
-                if (s.top_p < 1.f) {
-                    __syncthreads();
-                    bound = bound_of(find_in_list<1024>(S, n, 0, 0, fmax((double)s.top_p, 0.0), with, mass));
-                    total = with;
-                }
-            } else {
-                bound = bound_of(find_in_list<1024>(S, n, W.before, W.want, -1.0, with, mass));
-                total = with;
+    const int n = W.n_list;
+    if (n <= TP_LIST) {
+        for (int i = tid; i < n; i += 1024) S.list[i] = W.list[i];
+        __syncthreads();
+        if (s.k < P.vocab) {
+            bound = bound_of(find_in_list<1024>(S, n, 0, (u64)s.k, -1.0, with, [](float) { return (u64)1; }));
+            u64 m = 0;
+            for (int i = tid; i < n; i += 1024) {           // tokens behind the bound leave the list: the last place, without mass
+                const u64 c = S.list[i];
+                const float l = logit_of((unsigned)(c >> TP_MAX_LOG));
+                const unsigned id = (unsigned)c & ((1u << TP_MAX_LOG) - 1);
+                if (bound.keeps(l, id)) m += R.mass(l);
+                else S.list[i] = place(-__builtin_inff(), id);
             }
-        } else {                                            // more tokens than the list holds: the whole row, by this workgroup
-            Logits<LT, 1024> L;
-            L.row = P.logits + row * P.vocab * Traits<LT>::ESZ; L.vocab = P.vocab; L.nvec = (P.vocab + Vec<LT>::N - 1) / Vec<LT>::N;
-            if (s.k < P.vocab) bound = bound_of(find_in_row<false>(L, R, s.max, S, bound, (u64)s.k, -1.0, with));
+            block_scan<1024>(m, S, total);
             if (s.top_p < 1.f) {
                 __syncthreads();
-                bound = bound_of(find_in_row<true>(L, R, s.max, S, bound, 0, fmax((double)s.top_p, 0.0), with));
+                bound = bound_of(find_in_list<1024>(S, n, 0, 0, fmax((double)s.top_p, 0.0), with, mass));
                 total = with;
             }
+        } else {
+            bound = bound_of(find_in_list<1024>(S, n, W.before, W.want, -1.0, with, mass));
+            total = with;
+        }
+    } else {                                                // more tokens than the list holds: the whole row, by this workgroup
+        __syncthreads();
+        Logits<LT, 1024> L;
+        L.row = P.logits + row * P.vocab * Traits<LT>::ESZ; L.vocab = P.vocab; L.nvec = (P.vocab + Vec<LT>::N - 1) / Vec<LT>::N;
+        if (s.k < P.vocab) bound = bound_of(find_in_row<false>(L, R, s.max, S, bound, (u64)s.k, -1.0, with));
+        if (s.top_p < 1.f) {
+            __syncthreads();
+            bound = bound_of(find_in_row<true>(L, R, s.max, S, bound, 0, fmax((double)s.top_p, 0.0), with));
+            total = with;
         }
     }
-    if (s.min_p > 0.f) {
-        const double least_e = ldexp((double)s.min_p, P.frac);
-        int kk;
-        const float least = least_float(s.max, R.near_e(s.min_p), [&](float l) { return R.scaled(l, kk) >= least_e; });
-        if (least > bound.l) { bound = {least, ~0u}; total = 0; }
-    }
+    apply_min_p(P, R, s.min_p, bound, total);
     if (tid == 0) { W.bound = bound; W.total = total; }
 }
 
@@ -847,12 +881,13 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void part_sum_kerne
     const size_t row = blockIdx.y;
     Work& W = reinterpret_cast<Work*>(P.work)[row];
     const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
-    if (s.plain() || (W.total && !P.ids)) return;
+    if (s.plain() || ((s.k == 1 || (s.search && W.total)) && !P.ids)) return;
     if (tid < TP_TABLE) s_table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
     __syncthreads();
     const Row R = {s.max, s.c, s_table};
-    const Bound bound = W.bound;
-    u64 m = 0;
+    Bound bound;
+    u64 total, m = 0;
+    bound_of_row(P, W, s, R, bound, total);
     const auto L = part_of<LT>(P, row, blockIdx.x);
     if (bound.all()) L.tokens([&](float l, int) { m += R.mass(l); });
     else L.tokens([&](float l, int id) { if (bound.keeps(l, id)) m += R.mass(l); });
@@ -872,19 +907,16 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void part_out_kerne
     const Setting s = setting_of(P, W, (int)(row / (unsigned)P.rows));
     const auto L = part_of<LT>(P, row, part);
     if (s.plain()) {
-        const float fill = s.bad ? __builtin_nanf("") : 0.f;
-        if (P.probs) for (int i = L.begin * Vec<LT>::N + tid; i < min(P.vocab, L.nvec * Vec<LT>::N); i += 1024) P.probs[row * P.vocab + i] = fill;
-        if (P.ids && part == 0 && tid == 0) {
-            P.ids[row] = -1;
-            if (P.id_probs) P.id_probs[row] = fill;
-        }
+        if (P.probs) for (int i = L.begin * Vec<LT>::N + tid; i < min(P.vocab, L.nvec * Vec<LT>::N); i += 1024) P.probs[row * P.vocab + i] = s.bad ? __builtin_nanf("") : 0.f;
+        if (P.ids && part == 0 && tid == 0) no_token(P, row, s.bad);
         return;
     }
     if (tid < TP_TABLE) S.table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
     __syncthreads();
     const Row R = {s.max, s.c, S.table};
-    const Bound bound = W.bound;
-    u64 total = W.total;
+    Bound bound;
+    u64 total;
+    bound_of_row(P, W, s, R, bound, total);
     if (P.ids || total == 0) {
         const u64 own = lane < P.parts ? W.sum[lane] : 0, upto = wave_scan(own);
         total = lane_u64(upto, 63);
@@ -898,23 +930,28 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void part_out_kerne
 }
 
 template <typename LT> void go(const TpParams& P, int total, hipStream_t s) {
-    if (P.parts > 1) {
+    if (P.work) {
         const dim3 grid(P.parts, total), block(1024);
         hipLaunchKernelGGL((part_max_kernel<LT>), grid, block, 0, s, P);
-        if (P.temperature || P.top_k || P.top_p) {          // (greedy rows have a bound, too)
+        if (P.top_k || P.top_p) {
             hipLaunchKernelGGL((part_hist_kernel<LT>), grid, block, 0, s, P);
             hipLaunchKernelGGL((part_list_kernel<LT>), grid, block, 0, s, P);
+            hipLaunchKernelGGL((row_bound_kernel<LT>), dim3(total), block, 0, s, P);
         }
-        hipLaunchKernelGGL((row_bound_kernel<LT>), dim3(total), block, 0, s, P);
         hipLaunchKernelGGL((part_sum_kernel<LT>), grid, block, 0, s, P);
         hipLaunchKernelGGL((part_out_kernel<LT>), grid, block, 0, s, P);
+    // (a workgroup per compute unit: all its threads; two: 512 each.  V 32000, top-p, us: 240 rows 34 with 1024 threads, 39 with 512, 300 rows 60 and 50)
     } else if (total <= 256) hipLaunchKernelGGL((target_probs_kernel<LT, 1024>), dim3(total), dim3(1024), 0, s, P);
     else hipLaunchKernelGGL((target_probs_kernel<LT, 512>), dim3(total), dim3(512), 0, s, P);
 }
 
-// workgroups per row
-int parts_of(const ps_target_probs_args* a) {
-    return a->vocab >= 4 * TP_PART && a->batch * a->rows <= TP_SPLIT_ROWS ? (a->vocab + TP_PART - 1) / TP_PART : 1;
+// tokens of a workgroup; 0: a row is one workgroup's
+int part_of(const ps_target_probs_args* a) {
+    const long long rows = (long long)a->batch * a->rows;
+    if (a->vocab < TP_SPLIT_VOCAB || rows > (a->top_k && !a->top_p ? TP_SPLIT_ROWS / 4 : TP_SPLIT_ROWS)) return 0;
+    // about as many workgroups as there are compute units (8 x V 128256 top-p, draws: parts of 8192 42 us, 16384 47, 32768 62; 64 rows 70 with 16384, 64 with 32768)
+    const long long least = std::max((a->vocab * rows + 255) / 256, (a->vocab + TP_MAX_PARTS - 1LL) / TP_MAX_PARTS);
+    return (int)((least + TP_PART - 1) / TP_PART * TP_PART);
 }
 
 int check(const ps_target_probs_args* a) {
@@ -928,7 +965,7 @@ int check(const ps_target_probs_args* a) {
 }   // namespace
 
 extern "C" size_t ps_target_probs_workspace_bytes(const ps_target_probs_args* a) {
-    return check(a) == PS_OK && parts_of(a) > 1 ? a256((size_t)a->batch * a->rows * sizeof(Work)) : 0;
+    return check(a) == PS_OK && part_of(a) ? a256((size_t)a->batch * a->rows * sizeof(Work)) : 0;
 }
 
 extern "C" int ps_target_probs(const ps_target_probs_args* a, void* stream) {
@@ -943,9 +980,10 @@ extern "C" int ps_target_probs(const ps_target_probs_args* a, void* stream) {
     if (need && (a->workspace_bytes < need || ((uintptr_t)a->workspace & 255))) return PS_ERR_WORKSPACE;
     TpParams P = {};
     P.logits = (const char*)a->logits; P.temperature = a->temperature; P.top_k = a->top_k; P.top_p = a->top_p; P.min_p = a->min_p; P.r = a->r;
-    P.parts = parts_of(a);
-    P.part_vecs = TP_PART / (a->dtype == PS_BF16 ? 8 : 4);
-    P.work = (char*)a->workspace;
+    const int part = part_of(a);
+    P.parts = part ? (a->vocab + part - 1) / part : 1;
+    P.part_vecs = part / (a->dtype == PS_BF16 ? 8 : 4);
+    P.work = part ? (char*)a->workspace : nullptr;
     P.probs = a->probs; P.ids = a->ids; P.id_probs = a->id_probs; P.rows = a->rows; P.vocab = a->vocab;
     int log = 0;
     while (1 << log < a->vocab) ++log;

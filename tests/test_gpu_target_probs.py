@@ -288,3 +288,39 @@ def test_a_row_is_the_same_alone_and_among_others():
     assert one.equal(out[:, :100]) and one_id.equal(ids[:, :100]) and one_p.equal(id_p[:, :100])
     few, few_id, few_p = call(x[:, 7:9].contiguous(), settings, r[:, 7:9].contiguous())
     assert few.equal(out[:, 7:9]) and few_id.equal(ids[:, 7:9]) and few_p.equal(id_p[:, 7:9])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,batch,rows", [(128256, 2, 2), (70001, 1, 64), (1 << 20, 1, 1)])
+def test_greedy_ties_in_and_across_the_parts_of_a_large_row(dtype, vocab, batch, rows):
+    """The largest logit at several places: the row's own lowest id, whichever workgroup had it; the settings given or not, with others or not."""
+    import torch
+    g = torch.Generator().manual_seed(5)
+    x = (torch.rand((batch, rows, vocab), generator=g) * 4 - 8).to(TU.torch_dtype(dtype))
+    first = torch.randint(0, vocab - 40000, (batch, rows), generator=g)
+    for b in range(batch):
+        for i in range(rows):
+            at = int(first[b, i])
+            x[b, i, [at, at + 1, at + 9000, at + 39000, vocab - 1]] = 1.5 - i   # (the largest of the first six rows, in bf16 of more; the others have one by chance)
+    want = (x == x.amax(-1, keepdim=True)).int().argmax(-1).int().cuda()
+    assert want[0, 0] == first[0, 0]
+    x = x.cuda()
+    r = torch.rand((batch, rows), generator=g).cuda()
+    for settings in (dict(temperature=[0.0] * batch), dict(top_k=[1] * batch), dict(temperature=[0.0] * batch, top_k=[50] * batch, top_p=[0.9] * batch, min_p=[0.5] * batch)):
+        out, ids, id_p = call(x, settings, r)
+        assert ids.equal(want) and (id_p == 1.0).all()
+        assert out.sum(-1).equal(torch.ones_like(id_p)) and out.gather(2, want[..., None].long()).eq(1.0).all()
+        _, ids, _ = call(x, settings, r, probs=False)
+        assert ids.equal(want)
+    # all equal ones are kept where nothing filters but min_p, and the draw is among them
+    out, ids, _ = call(x, dict(min_p=[0.999] * batch), r)
+    kept = x.double() >= x.double().amax(-1, keepdim=True) + math.log(0.999)
+    assert (out > 0).equal(kept) and (kept[0, 0].sum() == 5) and kept.gather(2, ids[..., None].long()).all()
+
+
+@pytest.mark.parametrize("rows", [16, 17, 64, 65])
+def test_rows_up_to_which_a_large_row_is_cut_up(rows):
+    logits, r = language(1, rows, 66000, "bf16", rows)
+    for settings in (dict(top_k=[40]), dict(top_p=[0.9]), dict(top_k=[40], top_p=[0.9], temperature=[0.7])):
+        out, ids, id_p = call(logits, settings, r)
+        check(logits, settings, r, out, ids, id_p, at=[0, 7, rows - 1])

@@ -343,3 +343,105 @@ def test_codes_beyond_32_bits_of_bytes(parent):
     k, v = (TU.normal((2, len(parent), heads, d), 6 + i, "bf16") for i in range(2))
     out, lse = call(cache, parent, q, k, v, list(lens), "bf16")
     _check_whole(cache, parent, q, k, v, lens, (0, heads - 1), out, lse)
+
+
+# Batches whose workgroups take four tiles of rows (blocks by way of LDS; float32: one wavefront per tile): many sequences or many blocks, three tiles and more
+MANY = tuple(37 * i % 211 for i in range(64))
+
+
+@pytest.mark.parametrize("dtype,heads,nq,d,parent", [("bf16", 4, 16, 128, fanout(4, 2, 2, 1, 1)), ("bf16", 4, 16, 64, fanout(4, 2, 2, 1, 1)),
+                                                    ("f32", 4, 16, 128, fanout(4, 2, 2, 1, 1)), ("f32", 4, 16, 64, fanout(4, 2, 2, 1, 1)),
+                                                    ("bf16", 8, 24, 64, chain(29)), ("bf16", 8, 24, 128, fanout(4, 2, 1, 1))])   # 87 rows: a wavefront without any
+def test_four_tiles(dtype, heads, nq, d, parent):
+    cache, q, k, v = make(dtype, heads, nq, d, MANY, len(parent), seed=3)
+    out, lse = call(cache, parent, q, k, v, list(MANY), dtype)
+    check(cache, parent, q, k, v, MANY, dtype, out, lse, heads=[0, heads - 1])
+    # the cached positions only
+    out, lse = call(cache, parent, q, None, None, list(MANY), dtype)
+    check(cache, parent, q, None, None, MANY, dtype, out, lse, heads=[1])
+
+
+@pytest.mark.parametrize("heads,nq,d,lens,splits", [(2, 16, 128, (9000, 4099, 12001, 5000, 7001, 8000, 31, 6000), 32), (4, 64, 64, (9000, 4099, 12001, 5000), 16)])
+def test_four_tiles_in_splits(heads, nq, d, lens, splits):
+    parent = fanout(4, 2, 2, 1, 1)
+    a = VF.make_tree_attn_args(TU.Cache(heads, d, [32 * ((n + 31) // 32) for n in lens]).struct, nq, "bf16", list(lens))
+    assert VF.ps_tree_attention_workspace_bytes(VF.make_tree(parent), a) == splits * heads * 61 * (nq // heads) * (d + 4) * 4   # (two tiles: other splits)
+    cache, q, k, v = make("bf16", heads, nq, d, lens, 61, seed=4)
+    out, lse = call(cache, parent, q, k, v, list(lens), "bf16")
+    _check_whole(cache, parent, q, k, v, lens, (0, heads - 1), out, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_four_tiles_what_is_hidden_does_not_enter(d):
+    import torch
+    parent, heads, nq = fanout(4, 2, 2, 1, 1), 4, 16
+    cache, q, k, v = make("bf16", heads, nq, d, MANY, 61, seed=5, capacity=[n + 32 for n in MANY])
+    out, lse = call(cache, parent, q, k, v, list(MANY), "bf16")
+    dirty = TU.Cache(heads, d, [32 * ((n + 63) // 32) for n in MANY])
+    for n, kind in (("k", cache.codes["k"]), ("v", cache.codes["v"])):
+        at = torch.from_numpy(TU.places(n, d)).cuda().reshape(32, d)
+        dirty.codes[n].fill_(0x7F)
+        dirty.scales[n].fill_(float("nan"))
+        for b, length in enumerate(MANY):
+            for i in range((length + 31) // 32):
+                block, seen = cache.offsets[b] // 32 + i, at[:min(32, length - 32 * i)].reshape(-1)
+                dirty.codes[n][block][:, seen] = kind[block][:, seen]
+                dirty.scales[n][block] = cache.scales[n][block]
+    got, got_lse = call(dirty, parent, q, k, v, list(MANY), "bf16")
+    assert got.equal(out) and got_lse.equal(lse)
+    # a node's Inf and NaN, and the rows that do not see it
+    v2 = v.clone()
+    v2[:, 2, :, 5], v2[:, 2, :, 40] = float("inf"), float("nan")
+    got, got_lse = call(cache, parent, q, k, v2, list(MANY), "bf16")
+    sees = [s for s in range(61) if any(t == 2 for t in _line(parent, s))]
+    blind = [s for s in range(61) if s not in sees]
+    assert got[:, blind].equal(out[:, blind]) and got_lse.equal(lse)
+    assert (got[:, sees][..., 5] == math.inf).all() and torch.isnan(got[:, sees][..., 40]).all()
+    rest = [i for i in range(d) if i not in (5, 40)]
+    # (the node's other values are what they were; a probability that met Inf is no less exact than before)
+    assert got[:, sees][..., rest].equal(out[:, sees][..., rest])
+
+
+def _line(parent, s):
+    while s >= 0:
+        yield s
+        s = parent[s]
+
+
+def test_four_tiles_captured_and_replayed_with_other_lengths():
+    import torch
+    parent = fanout(4, 2, 2, 1, 1)
+    cache, q, k, v = make("bf16", 4, 16, 64, MANY, 61, seed=6)
+    dev = torch.tensor(MANY, dtype=torch.int32, device="cuda:0")
+    keep, s = [], torch.cuda.Stream()
+    call(cache, parent, q, k, v, list(MANY), "bf16", dev=dev)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out, lse = call(cache, parent, q, k, v, list(MANY), "bf16", dev=dev, keep=keep)
+    for turn in range(4):
+        lens = [n if turn == 0 else n * turn // 4 for n in MANY]
+        dev.copy_(torch.tensor(lens, dtype=torch.int32))
+        g.replay()
+        torch.cuda.synchronize()
+        want, want_lse = call(cache, parent, q, k, v, list(MANY), "bf16", dev=dev)
+        assert out.equal(want) and lse.equal(want_lse)
+        check(cache, parent, q, k, v, lens, "bf16", out, lse, heads=[2])
+
+
+def test_four_tiles_beyond_32_bits_of_bytes():
+    import torch
+    heads, d, parent = 16, 128, fanout(4, 2, 2, 1, 1)
+    base = (1 << 32) // (heads * 32 * d) + 1
+    cache = TU.Cache(1, d, [32])
+    need = [(n + 31) // 32 for n in MANY]
+    cache.heads, cache.offsets = heads, [32 * (base + sum(need[:b])) for b in range(len(MANY) + 1)]
+    cache.codes = {n: torch.full((base + sum(need), heads, 32 * d), 0x7F, dtype=torch.uint8, device="cuda:0") for n in "kv"}
+    cache.scales = {n: torch.full((base + sum(need), heads), float("nan"), device="cuda:0") for n in "kv"}
+    cache.struct = VF.make_cache(heads, d, cache.codes["k"].data_ptr(), cache.codes["v"].data_ptr(), cache.scales["k"].data_ptr(), cache.scales["v"].data_ptr(), cache.offsets)
+    x = [TU.normal((len(MANY), max(MANY), heads, d), i, "bf16") for i in range(2)]
+    cache.write(x[0], x[1], [0] * len(MANY), "bf16", n_seq=MANY)
+    q = TU.normal((len(MANY), 61, 2 * heads, d), 5, "bf16")
+    k, v = (TU.normal((len(MANY), 61, heads, d), 6 + i, "bf16") for i in range(2))
+    out, lse = call(cache, parent, q, k, v, list(MANY), "bf16")
+    _check_whole(cache, parent, q, k, v, MANY, (0, heads - 1), out, lse)
