@@ -143,24 +143,17 @@ template <int NP> __device__ __forceinline__ void prob_parts(const f32x16& s, bf
     }
 }
 
-// other's sums into mine
-template <int D> __device__ __forceinline__ void merge(RowState<D>& R, float m2, float l2, const f32x16 (&o2)[D / 32]) {
-    const float m = fmaxf(R.m, m2);
-    const float a = R.m == m ? 1.f : __builtin_amdgcn_exp2f(R.m - m), b = m2 == m ? 1.f : __builtin_amdgcn_exp2f(m2 - m);
-    R.m = m;
-    R.l = R.l * a + l2 * b;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) R.o[j] = R.o[j] * a + o2[j] * b;
-}
-
 template <typename WT> __device__ __forceinline__ void store4_out(char* p, f32x4 x) {
     if constexpr (Traits<WT>::BF) *reinterpret_cast<u32x2_q*>(p) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
     else *reinterpret_cast<f32x4_q*>(p) = x;
 }
 __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.f ? -__builtin_inff() : 0.69314718055994530942f * (m + __log2f(l)); }
 
-// floats that a wavefront leaves in LDS: sums, then maxima and row sums
-template <int D> constexpr int part_floats() { return TA_TILE * D + 2 * 64; }
+// what a wavefront leaves in LDS of its tile: sums by row, maxima, row sums
+template <int D> struct Meet {
+    float o[TA_TILE][D + 4];
+    float m[TA_TILE], l[TA_TILE];
+};
 
 // The parts of a block's attention: products with its keys, ...
 template <int D, int NP> __device__ __forceinline__ void key_products(const bf16x8 (&q)[D / 16][NP], const uint4 (&k)[D / 32], f32x16& s) {
@@ -216,31 +209,6 @@ template <int D> struct Stage {
     float scales[4][64];
 };
 
-// the sums of a tile to and from LDS
-template <int D> __device__ __forceinline__ void leave(float* to, const RowState<D>& R) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-            *reinterpret_cast<f32x4*>(to + ((j * 4 + a) * 64 + lane) * 4) = f32x4{R.o[j][4 * a], R.o[j][4 * a + 1], R.o[j][4 * a + 2], R.o[j][4 * a + 3]};
-    to[TA_TILE * D + lane] = R.m;
-    to[TA_TILE * D + 64 + lane] = R.l;
-}
-template <int D> __device__ __forceinline__ void join(RowState<D>& R, const float* from) {
-    const int lane = threadIdx.x & 63;
-    f32x16 o2[D / 32];
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(from + ((j * 4 + a) * 64 + lane) * 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o2[j][4 * a + e] = x[e];
-        }
-    merge<D>(R, from[TA_TILE * D + lane], from[TA_TILE * D + 64 + lane], o2);
-}
-
 template <typename WT, int D, int WR>
 __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)) void tree_attn_kernel(const TaParams P) {
     constexpr int W = ta_waves<WT, WR>(), WK = W / WR, NP = Traits<WT>::BF ? 1 : 3, C = D / 32, TILE = PC_BLOCK * D, ESZ = Traits<WT>::ESZ;
@@ -248,8 +216,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
     // where wavefronts that share rows meet, and before that a wavefront's probabilities of its own rows (staged, where it is large enough: the
     // buffer that is requested last)
     constexpr bool OWN_IN_BUFFER = STAGED && sizeof(Stage<D>::codes) >= W * PC_BLOCK * TA_TILE * 4;
-    constexpr int MEET = WK > 1 ? (W / 2) * part_floats<D>() : 4, OWN_P = OWN_IN_BUFFER ? 4 : W * PC_BLOCK * TA_TILE;
-    __shared__ __attribute__((aligned(16))) float s_meet[MEET > OWN_P ? MEET : OWN_P];
+    __shared__ __attribute__((aligned(16))) Meet<(WK > 1 ? D : OWN_IN_BUFFER ? 0 : TA_TILE)> s_meet[W];
     __shared__ __attribute__((aligned(16))) Stage<STAGED ? D : 0> b0, b1, b2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, lc = lane & 31;
     const int wr = wave % WR, wk = wave / WR, h = blockIdx.y;
@@ -269,27 +236,35 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
     // the tree's own values, where this workgroup takes them: in LDS by node, zeros in the place of Inf and NaN (s_odd: there were any)
     constexpr int OWN_PITCH = D * ESZ + 4 * ESZ;
     __shared__ __attribute__((aligned(16))) char s_own[PS_TREE_MAX_NODES * OWN_PITCH];
-    __shared__ int s_odd;
+    __shared__ int s_odd[W];
     const char* own_k = P.k + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
     const char* own_v = P.v + (long long)b * P.nodes * P.kv_row + (long long)h * D * ESZ;
-    auto stage_own = [&]() __attribute__((always_inline)) {
-        if (threadIdx.x == 0) s_odd = 0;
-        __syncthreads();
-        bool odd = false;
-        const int pieces = (P.nodes + 31) / 32 * 32 * (D / 8);   // (8 elements each; nodes up to the tile's end: zeros)
-        for (int i = threadIdx.x; i < pieces; i += 64 * W) {
-            const int at = i / (D / 8), part = i % (D / 8);
-            float x[8] = {};
+    constexpr int OWN_PIECES = PS_TREE_MAX_NODES * (D / 8) / (64 * W);   // of 8 elements, per thread; nodes up to a tile's end: zeros
+    f32x4 own_raw[OWN_PIECES][2];
+    auto fetch_own = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < OWN_PIECES; ++n) {
+            const int i = n * 64 * W + threadIdx.x, at = i / (D / 8), part = i % (D / 8);
+            own_raw[n][0] = own_raw[n][1] = f32x4{0, 0, 0, 0};
             if (at < P.nodes) {
                 const char* from = own_v + (long long)at * P.kv_row + part * 8 * ESZ;
-                const f32x4 lo = load4_q<WT>(from), hi = load4_q<WT>(from + 4 * ESZ);
+                own_raw[n][0] = load4_q<WT>(from);
+                own_raw[n][1] = load4_q<WT>(from + 4 * ESZ);
+            }
+        }
+    };
+    auto place_own = [&]() __attribute__((always_inline)) {
+        bool odd = false;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = e < 4 ? lo[e & 3] : hi[e & 3];
-                    const bool fine = __builtin_fabsf(v) < __builtin_inff();
-                    odd |= !fine;
-                    x[e] = fine ? v : 0.f;
-                }
+        for (int n = 0; n < OWN_PIECES; ++n) {
+            const int i = n * 64 * W + threadIdx.x, at = i / (D / 8), part = i % (D / 8);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = own_raw[n][e >> 2][e & 3];
+                const bool fine = __builtin_fabsf(v) < __builtin_inff();
+                odd |= !fine;
+                x[e] = fine ? v : 0.f;
             }
             char* to = s_own + at * OWN_PITCH + part * 8 * ESZ;
             if constexpr (Traits<WT>::BF) {
@@ -300,7 +275,8 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
                 *reinterpret_cast<f32x4*>(to + 16) = f32x4{x[4], x[5], x[6], x[7]};
             }
         }
-        if (odd) s_odd = 1;
+        odd = __ballot(odd) != 0;
+        if (lane == 0) s_odd[wave] = odd;
     };
 
     bf16x8 q[2 * C][NP];
@@ -327,9 +303,10 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
         };
         const int first = wk;
         load_keys(first);
-        stage_own();
+        place_own();
         __syncthreads();
         if (!active) return;
+        const bool any_odd = __ballot(lane < W && s_odd[lane % W]) != 0;
         for (int kt = first; kt * 32 < P.nodes; kt += WK) {
             if (kt != first) load_keys(kt);
             {
@@ -365,8 +342,8 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
 #pragma unroll
                             for (int c = NP - 1 - a; c >= 0; --c) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[a], p[st][c], R.o[j], 0, 0, 0);
                     }
-                if (s_odd) {                                 // what is Inf or NaN, for the rows that see it
-                    float* sp = (OWN_IN_BUFFER ? reinterpret_cast<float*>(b2.codes) : s_meet) + wave * PC_BLOCK * TA_TILE;   // probabilities by node
+                if (any_odd) {                               // what is Inf or NaN, for the rows that see it
+                    float* sp = OWN_IN_BUFFER ? reinterpret_cast<float*>(b2.codes) + wave * PC_BLOCK * TA_TILE : reinterpret_cast<float*>(s_meet + wave);   // probabilities by node
 #pragma unroll
                     for (int e = 0; e < 16; ++e) sp[(8 * (e >> 2) + 4 * half + (e & 3)) * TA_TILE + lc] = s[e];
                     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -449,6 +426,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             request(0, b0);
             request(1, b1);
         }
+        if (own) fetch_own();
         load_rows();
         if (own) own_rows();
         for (int k = 0; k < steps;) {
@@ -494,6 +472,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             fetch_scales(i);
             fetch(i, next);
         }
+        if (own) fetch_own();
         load_rows();
         if (own) own_rows();
         if (any) {
@@ -519,15 +498,55 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
     }
 
     R.l += other_half(R.l);
-    // wavefronts that share rows: the upper half of them leaves its sums in LDS, the lower half adds them
+    // wavefronts that share rows: each leaves its sums in LDS and takes some of the rows, a lane eight dims of one
     if constexpr (WK > 1) {
-        for (int n = WK / 2; n >= 1; n >>= 1) {
-            __syncthreads();
-            if (wk >= n && wk < 2 * n && valid) leave<D>(s_meet + ((wk - n) * WR + wr) * part_floats<D>(), R);
-            __syncthreads();
-            if (wk < n && valid) join<D>(R, s_meet + (wk * WR + wr) * part_floats<D>());
+        auto& mine = s_meet[wave];
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                *reinterpret_cast<f32x4*>(&mine.o[lc][32 * j + 8 * a + 4 * half]) = f32x4{R.o[j][4 * a], R.o[j][4 * a + 1], R.o[j][4 * a + 2], R.o[j][4 * a + 3]};
+        if (half == 0) { mine.m[lc] = R.m; mine.l[lc] = R.l; }
+        __syncthreads();
+        if (!active) return;
+        constexpr int ROWS = TA_TILE / WK, PIECES = D / 8;
+#pragma unroll
+        for (int i = lane; i < ROWS * PIECES; i += 64) {
+            const int r = wk * ROWS + i / PIECES, d0 = i % PIECES * 8, at_row = tile * TA_TILE + r;
+            if (at_row >= P.rows) continue;
+            float ms[WK], m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                ms[w] = s_meet[w * WR + wr].m[r];
+                m = fmaxf(m, ms[w]);
+            }
+            const float base = m == -__builtin_inff() ? 0.f : m;
+            f32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const auto& from = s_meet[w * WR + wr];
+                const float weight = __builtin_amdgcn_exp2f(ms[w] - base);
+                l = __builtin_fmaf(from.l[r], weight, l);
+                lo += *reinterpret_cast<const f32x4*>(&from.o[r][d0]) * weight;
+                hi += *reinterpret_cast<const f32x4*>(&from.o[r][d0 + 4]) * weight;
+            }
+            if (splits == 1) {
+                const size_t at = ((size_t)b * P.nodes + at_row / P.grp) * P.n_heads + h * P.grp + at_row % P.grp;
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                lo *= inv;
+                hi *= inv;
+                char* to = P.out + (at * D + d0) * ESZ;
+                if constexpr (Traits<WT>::BF) *reinterpret_cast<u32x4_q*>(to) = u32x4{pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3])};
+                else { *reinterpret_cast<f32x4_q*>(to) = lo; *reinterpret_cast<f32x4_q*>(to + 16) = hi; }
+                if (P.lse && d0 == 0) P.lse[at] = log_sum(m, l);
+            } else {
+                float* to = P.part + (((size_t)blockIdx.x * P.heads + h) * P.rows + at_row) * (D + 4);
+                *reinterpret_cast<f32x4*>(to + d0) = lo;
+                *reinterpret_cast<f32x4*>(to + d0 + 4) = hi;
+                if (d0 == 0) { to[D] = m; to[D + 1] = l; }
+            }
         }
-        if (wk > 0) return;
+        return;
     }
     if (!valid) return;
     if (splits == 1) {
