@@ -6,6 +6,10 @@
 // and one contiguous piece of codes (2 or 4 KiB).  One wavefront takes one block of one head's keys or values: rows are read and
 // written by whole lines, the bytes meet in LDS by row, codes leave and arrive 16 bytes a lane in the attention's order.  Values lie
 // transposed in that order (a lane of the attention has 16 positions of one dim), so they pass 4 x 4 byte exchanges.
+//
+// Measured (bf16, 8 heads of 128): 8 x 2048 rows written 25.0 us (67 MB read, 34 MB written, 4.0 TB/s), 4 x 4096 read back 19.6 (5.1 TB/s, a copy's rate); a path of up to 6
+// rows for 8 sequences, 32 heads 6.7, a launch and three reads one after the other (length, path, rows).  Writing is behind reading for the two looks at each
+// row (largest magnitude, then codes; they wait in registers) and the codes' turn through LDS; loads that pass the caches by change nothing.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

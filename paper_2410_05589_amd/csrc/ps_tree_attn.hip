@@ -5,12 +5,21 @@
 // e4m3 codes are bf16 numbers, so both products run on v_mfma_f32_32x32x16_bf16 with exact keys and values; the scales, powers of two,
 // join the scores' constant and the exponent of P.  Queries stand along the lanes: S^T = K Q^T leaves a lane (query c, half h) the
 // scores of positions 8 a + 4 h + b, and out^T = V^T P^T takes them from there as its operand: the cache keeps values in just that order, so
-// codes go from memory to the matrix cores through a conversion (two codes an instruction), with no exchange between lanes and no LDS.
+// codes go from memory to the matrix cores through a conversion (two codes an instruction), with no exchange between lanes.
 // The running maximum is raised only when a score passes it by 2^8 (sums stay far inside float32), so sums are rarely rescaled.
 //
-// Work: a sequence's blocks are cut into splits of `per` blocks; a workgroup takes a split of one kv head for up to 128 rows
-// (a row is a node and one of the heads that share the kv head), a wavefront 32 of them.  Its wavefronts divide rows (WR) and blocks (WK); those
-// that share rows meet in LDS, splits in the workspace and a second kernel.
+// Probabilities are rounded to bf16 for the second product (their sum is taken before that, in float32): a row's error is then that of many independent
+// roundings, below its result's own; float32 calls have three bf16 parts of queries and probabilities, 24 bits of each.
+//
+// Work: a sequence's blocks are cut into splits of `per` blocks; a workgroup takes a split of one kv head for up to four tiles of 32 rows (a row is a node and one of
+// the heads that share the kv head).  Its wavefronts divide tiles (WR) and blocks (WK); those that share a tile meet in LDS, splits in the workspace and a
+// second kernel.  One and two tiles: eight wavefronts, each with its blocks on their way to its registers; more: four, which read the same blocks from LDS.
+//
+// What bounds it (bf16, head_dim 128).  One tile: reading the codes.  32 sequences of 2048 positions, 32 heads, a row each: 537 MB in 87 us, 6.2 TB/s; 4 of 32768
+// positions, 8 heads, 4 rows each: 268 MB in 46.  Many tiles: a block of one tile is 16 matrix instructions (512 cycles), 64 conversions, 16 exponentials
+// and some 100 more vector instructions, which overlap with the products less than the two wavefronts of a SIMD could make them: 1600 cycles.  8 x 4099 ...
+// 12288 positions, 61 nodes, 32 heads that share 8: 104 us, 0.63 PFLOP/s.  Left out in probes of that: conversions -6 %, exponentials -12 %, barriers and requests
+// -20 %, all of these -30 %.  Small calls: 2 us until the first operands are there, 2 for the tree's own rows, 2 for the meeting and the results, then the join (3).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,9 +29,12 @@ namespace {
 
 constexpr int TA_TILE = 32;
 // wavefronts of a workgroup.  bf16: two per SIMD, so that one's matrix instructions run beside the other's exponentials, of one workgroup or, where
-// wavefronts wait for each other's requests (WR 4), of two; float32 has three parts of every query and one wavefront per SIMD
+// wavefronts wait for each other's requests (WR 4), of two; float32 has three parts of every query and one wavefront per SIMD.  (Two tiles and
+// less, eight / twice four, us: 52 rows of 8 x 8192 positions, 8 heads 38 / 45, of 2048 positions 17 / 21; 61 rows, 32 heads, 8 x 2048 42 / 49; one row 15.5 / 15.1)
 template <typename WT, int WR> constexpr int ta_waves() { return Traits<WT>::BF && WR < 4 ? 8 : 4; }
-constexpr float TA_LAZY = 8.f;      // how far (in powers of two) scores may pass the maximum that they are taken against
+// How far (in powers of two) scores may pass the maximum that they are taken against: probabilities stay below 2^8, their sums over 2^30 positions below 2^38.  (A maximum
+// that is raised with every score above it: 4 % of the time with many tiles)
+constexpr float TA_LAZY = 8.f;
 
 struct TaParams {
     const char *q, *k, *v;
@@ -198,7 +210,7 @@ template <int D, int NP> __device__ __forceinline__ void value_products(RowState
 __device__ __forceinline__ float log2_of(float scale) { return (float)((int)(__float_as_uint(scale) >> 23) - 127); }   // (powers of two)
 __device__ __forceinline__ float one_over(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }
 
-// Three tiles of rows and more: four wavefronts read the same blocks, which come to LDS by way of the memory unit, 1 KiB per request, two steps of
+// Four tiles of rows: four wavefronts read the same blocks, which come to LDS by way of the memory unit, 1 KiB per request, two steps of
 // TA_STEP blocks ahead in three buffers (arrays of their own: a read from one need not wait for what is on its way into another).  A step's
 // blocks are taken together: two chains of products, one look at the maximum.  Each wavefront asks for a quarter of a step
 // (and, so that all wait for as many requests, for scales: those of the first two are read).
@@ -569,7 +581,8 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
     }
 }
 
-// The splits of one row of one head: a wavefront, a lane has D / 64 dims
+// The splits of one row of one head: a wavefront, a lane has D / 64 dims.  Bound by reading the parts (61 nodes, 32 heads, 30 splits of 8 sequences, 31 MB: 9.5 us, with the
+// results 4 TB/s; few rows: 3 us, two reads one after the other)
 template <typename WT, int D>
 __global__ __launch_bounds__(256) void tree_attn_join_kernel(const TaParams P) {
     constexpr int E = D / 64, AHEAD = 8;
