@@ -6,13 +6,14 @@
 // either keeps is everything up to one token, the bound, and min_p is a bound too.  Nothing is sorted:
 //   top-k, small k   a histogram of the threads' own maxima gives a lower limit that k tokens reach; the few tokens above it are listed in LDS
 //   top-p, large k   a histogram of y in steps of 1/32 (sums of e, or counts) says which step the bound lies in; that step's tokens are listed
+//   a listed top-k   has all that may be kept: probabilities, further bounds and draws need the list alone
 //   the list         up to 64 tokens by comparing all with all in a wavefront, more by eleven bits of c at a time, from the highest that differs
 // e is a whole number of 2^-F (F = 62 - log2 V, at most 51), from a double: sums are exact in any order, whoever adds them, and
 // their error is far below what decides a draw.  (Doubles cost no more instructions here than floats, a histogram no more than its additions.)
 //
 // One workgroup per row (few rows of a large vocabulary: several, see below); the row is read again by each pass, from the caches.  What bounds it: a pass over a row
 // that makes masses is 25 instructions per token (V 128256: 12 us on one compute unit), one that only compares is a read.  Measured (us; V 32000 float32, 61 rows,
-// top-k 50 and top-p 0.95, probabilities: 20, 3 of them the bytes at a copy's rate; V 128256 bf16, 488 rows, a setting per sequence: 142, bytes 73).
+// top-k 50 and top-p 0.95, probabilities: 18, 3 of them the bytes at a copy's rate; V 128256 bf16, 488 rows, a setting per sequence: 142, bytes 73).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -154,6 +155,8 @@ __device__ __forceinline__ unsigned key_of(float l) {
 }
 __device__ __forceinline__ float logit_of(unsigned key) { return __uint_as_float(key >> 31 ? key : ~key & 0x7FFFFFFFu); }
 __device__ __forceinline__ u64 place(float l, int id) { return (u64)key_of(l) << TP_MAX_LOG | (unsigned)id; }
+__device__ __forceinline__ float logit_at(u64 c) { return logit_of((unsigned)(c >> TP_MAX_LOG)); }
+__device__ __forceinline__ unsigned id_at(u64 c) { return (unsigned)c & ((1u << TP_MAX_LOG) - 1); }
 struct Bound {
     float l;
     unsigned id;
@@ -269,13 +272,13 @@ template <int T> __device__ __forceinline__ u64 find_in_bins(Shared& S, u64 befo
     return want;
 }
 
-// Of the list's n tokens, with weights w(logit): the first, in the order of places, with which the sum (`before` in front of them) reaches `want`.
+// Of the list's n tokens, with weights w(entry): the first, in the order of entries, with which the sum (`before` in front of them) reaches `want`.
 // with: the sum up to and with that token.  Takes and leaves synchronised
 template <int T, typename W> __device__ __forceinline__ u64 find_in_list(Shared& S, int n, u64 before, u64 want, double of_all, u64& with, W w) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (n <= 64) {                                          // one wavefront
         if (wave == 0) {
-            const u64 c = lane < n ? S.list[lane] : ~0ull, m = lane < n ? w(logit_of((unsigned)(c >> TP_MAX_LOG))) : 0;
+            const u64 c = lane < n ? S.list[lane] : ~0ull, m = lane < n ? w(c) : 0;
             if (of_all >= 0.0) {
                 const u64 total = lane_u64(wave_scan(m), 63);
                 const double t = ceil(of_all * (double)total);
@@ -304,7 +307,7 @@ template <int T, typename W> __device__ __forceinline__ u64 find_in_list(Shared&
     for (int i = 0; i < PER; ++i) {
         const bool is = tid + i * T < n;
         c[i] = is ? S.list[tid + i * T] : 0;
-        m[i] = is ? w(logit_of((unsigned)(c[i] >> TP_MAX_LOG))) : 0;
+        m[i] = is ? w(c[i]) : 0;
         if (m[i]) live |= 1u << i;
     }
     for (int round = 0; round < 6; ++round) {               // (52 bits, eleven and more at a time)
@@ -348,11 +351,11 @@ template <int T, typename W> __device__ __forceinline__ u64 find_in_list(Shared&
 }
 
 // The bound of the row's tokens that `within` keeps: the first token with which the sum of e (BY_MASS) reaches top_p of their sum, or the
-// top_k-th.  with: the sum up to and with it
+// top_k-th.  with: the sum up to and with it.
 template <bool BY_MASS, typename LT, int T>
 __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R, float mx, Shared& S, Bound within, u64 want, double of_all, u64& with) {
     const int tid = threadIdx.x;
-    auto weight = [&](float l) { return BY_MASS ? R.mass(l) : (u64)1; };
+    auto weight = [&](u64 c) { return BY_MASS ? R.mass(logit_at(c)) : (u64)1; };
     for (int i = tid; i < TP_BINS; i += T) S.h.mass[i] = 0;
     if (tid == 0) S.n_list = 0;
     __syncthreads();
@@ -390,7 +393,7 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
             if (!(l >= least && l < above && within.keeps(l, id)) || c >> (shift + 11) != prefix || id >= L.vocab) return;
             const int digit = (int)(c >> shift) & (TP_BINS - 1);
             lds_add(&S.h.count[digit], 1u);
-            lds_add(&S.h.mass[digit], weight(l));
+            lds_add(&S.h.mass[digit], weight(c));
         });
         __syncthreads();
         find_in_bins<T>(S, before, want, -1.0);
@@ -487,21 +490,56 @@ __device__ __forceinline__ void draw(const TpParams& P, const Logits<LT, T>& L, 
     sum_cells<T>(L, R, S, bound);
     draw_from_cells<T>(P, L, R, S, bound, row, before, want, total);
 }
+// a kept token's probability
+struct Prob {
+    double max, c;
+    float inv;
+    __device__ __forceinline__ Prob(const Row& R, int frac, u64 total) : max(R.max), c(R.c / TP_TABLE), inv((float)(1.0 / ldexp((double)total, -frac))) {}
+    __device__ __forceinline__ float operator()(float l) const {
+        const double y = __builtin_fmax(((double)l - max) * c, -1000.0), t = y + 6755399441055744.0;   // (1.5 * 2^52: the low word is rint(y))
+        return ldexpf(__builtin_amdgcn_exp2f((float)(y - (t - 6755399441055744.0))) * inv, __double2loint(t));
+    }
+};
+// The probabilities of a row whose kept tokens are all in the list: zeros, which need no look at the logits, and theirs (488 rows of V 128256 bf16, greedy 110 -> 89 us, k 50
+// 114 -> 97)
+template <int T> __device__ __forceinline__ void write_listed(const TpParams& P, const Row& R, Shared& S, int n, Bound bound, size_t row, u64 total) {
+    float* out = P.probs + row * P.vocab;
+    const Prob prob(R, P.frac, total);
+    for (int i = threadIdx.x * 4; i < P.vocab; i += T * 4) {
+        if (i + 4 <= P.vocab) *reinterpret_cast<f32x4_q*>(out + i) = f32x4{0, 0, 0, 0};
+        else for (int e = i; e < P.vocab; ++e) out[e] = 0.f;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += T) {
+        const u64 c = S.list[i];
+        const float l = logit_at(c);
+        if (bound.keeps(l, id_at(c))) out[id_at(c)] = prob(l);
+    }
+}
+// The draw among them, in the order of ids; the list is turned into that of (id, logit)
+template <int T> __device__ __forceinline__ void draw_listed(const TpParams& P, const Row& R, Shared& S, int n, Bound bound, size_t row, u64 total) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += T) S.list[i] = (u64)id_at(S.list[i]) << 32 | (unsigned)(S.list[i] >> TP_MAX_LOG);
+    __syncthreads();
+    u64 with;
+    auto kept = [&](u64 c) { const float l = logit_of((unsigned)c); return bound.keeps(l, (unsigned)(c >> 32)) ? R.mass(l) : 0; };
+    const u64 at = find_in_list<T>(S, n, 0, drawn_mass(P.r[row], total) + 1, -1.0, with, kept);
+    if (threadIdx.x == 0) {
+        P.ids[row] = (int)(at >> 32);
+        int k;
+        if (P.id_probs) P.id_probs[row] = (float)(R.scaled(logit_of((unsigned)at), k) / (double)total);
+    }
+}
 template <int T, typename LT>
 __device__ __forceinline__ void write_probs(const TpParams& P, const Logits<LT, T>& L, const Row& R, Bound bound, size_t row, u64 total) {
     constexpr int N = Vec<LT>::N;
     const int V = L.vocab;
     float* out = P.probs + row * V;
     const bool all = bound.all();
-    const double cy = R.c / TP_TABLE;
-    const float inv = (float)(1.0 / ldexp((double)total, -P.frac));
+    const Prob prob(R, P.frac, total);
     L.each([&](const u32x4& x, int at) {
         if (at >= L.nvec) return;                           // (the next part's)
         float p[N], l[N];
-        auto prob = [&](float l) {
-            const double y = __builtin_fmax(((double)l - R.max) * cy, -1000.0), t = y + 6755399441055744.0;   // (1.5 * 2^52: the low word is rint(y))
-            return ldexpf(__builtin_amdgcn_exp2f((float)(y - (t - 6755399441055744.0))) * inv, __double2loint(t));
-        };
 #pragma unroll
         for (int e = 0; e < N; ++e) l[e] = Vec<LT>::get(x, e);
         if (all) {
@@ -593,18 +631,22 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
     R.max = mx; R.c = uniform(1.4426950408889634074 * TP_TABLE / (greedy ? 1.0 : (double)t_in)); R.table = S.table;
     Bound bound = {-__builtin_inff(), ~0u};
     u64 total = 0;                                          // the sum of the kept e, where it is known
-    auto mass = [&](float l) { return R.mass(l); };
-    auto one = [](float) { return (u64)1; };
+    auto mass = [&](u64 c) { return R.mass(logit_at(c)); };
+    auto one = [](u64) { return (u64)1; };
+    int listed = -1;                                        // tokens in S.list, where these are all that may be kept
     if (k == 1) {                                           // the first of the largest
         L.tokens([&](float l, int id) { if (l == mx) __hip_atomic_fetch_min(&S.found, id, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); });
         __syncthreads();
         bound = {mx, (unsigned)S.found};
         total = R.mass(mx);
+        if (tid == 0) S.list[0] = place(mx, S.found);
+        listed = 1;
+        __syncthreads();
     } else {
-        bool listed = false, all = k == V;                  // all: no top-k, or one that only drops tokens at -Inf
+        const bool all = k == V;                            // no top-k, or one that only drops tokens at -Inf
         u64 with = 0;
         if (k <= TP_SMALL_K && k <= min(T, L.nvec)) {
-            // k threads' maxima are at or above some step: so are the k largest tokens
+            // k threads' maxima are at or above some step: so are the k largest tokens, which are listed
             if (tid < L.nvec) lds_add((unsigned*)&S.h.mass[R.step(mine)], 1u);
             __syncthreads();
             find_in_bins<T>(S, 0, (u64)k, -1.0);
@@ -613,17 +655,17 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
                 const float least = least_float(mx, R.end_of(step), [&](float l) { return R.step(l) <= step; });
                 L.tokens([&](float l, int id) { if (l >= least) list_add(S, place(l, id), L.vocab); });
                 __syncthreads();
-                listed = S.n_list <= TP_LIST;
+                if (S.n_list <= TP_LIST) listed = S.n_list;
             }
         }
-        if (listed) {
-            const int n = S.n_list;
+        if (listed >= 0) {
+            const int n = listed;
             bound = bound_of(find_in_list<T>(S, n, 0, (u64)k, -1.0, with, one));
             u64 m = 0;
             for (int i = tid; i < n; i += T) {              // tokens behind the bound leave the list: the last place, without mass
                 const u64 c = S.list[i];
-                const float l = logit_of((unsigned)(c >> TP_MAX_LOG));
-                const unsigned id = (unsigned)c & ((1u << TP_MAX_LOG) - 1);
+                const float l = logit_at(c);
+                const unsigned id = id_at(c);
                 if (bound.keeps(l, id)) m += R.mass(l);
                 else S.list[i] = place(-__builtin_inff(), id);
             }
@@ -644,22 +686,34 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
     }
     apply_min_p(P, R, min_p, bound, total);
 
-    // the sum of the kept e, where it is not known or a token is drawn
-    if (P.ids || total == 0) {
+    // the sum of the kept e, where it is not known
+    if (total == 0 && listed >= 0) {
+        u64 m = 0;
+        for (int i = tid; i < listed; i += T)
+            if (bound.keeps(logit_at(S.list[i]), id_at(S.list[i]))) m += R.mass(logit_at(S.list[i]));
+        __syncthreads();
+        block_scan<T>(m, S, total);
+    } else if (listed < 0 && (P.ids || total == 0)) {
         __syncthreads();
         total = sum_cells<T>(L, R, S, bound);
-        if (P.ids) draw_from_cells<T>(P, L, R, S, bound, row, 0, drawn_mass(P.r[row], total), total);
     }
-    if (P.probs) write_probs(P, L, R, bound, row, total);
+    if (P.probs) {
+        if (listed >= 0) write_listed<T>(P, R, S, listed, bound, row, total);
+        else write_probs(P, L, R, bound, row, total);
+    }
+    if (P.ids) {
+        if (listed < 0) draw_from_cells<T>(P, L, R, S, bound, row, 0, drawn_mass(P.r[row], total), total);
+        else draw_listed<T>(P, R, S, listed, bound, row, total);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
 // Few rows of a large vocabulary: several workgroups per row, a kernel for each pass.  What a row's workgroups tell each other is in the workspace.
 // ------------------------------------------------------------------------------------------
 // A workgroup's tokens are a multiple of TP_PART (a pass of 1024 threads over bf16).  Up to TP_SPLIT_ROWS rows: masses of a row take one workgroup long, but every kernel reads
-// the row once more.  (V 128256 bf16, us, cut up / one workgroup per row: 8 rows top-p 35 / 78, no filter 20 / 48, top-k 50 27 / 31; 64 rows top-p 53 / 82, top-k 50
-// 41 / 34; 128 rows top-p 75 / 82, no filter 47 / 54, top-k 50 54 / 37.  So calls with top-k and no top-p, which have masses of a few tokens only, are cut up to a quarter of
-// the rows: 16 rows 28 / 31, 32 rows 33 / 32.  8 rows of V 64000: top-p 35 / 46, no filter 21 / 27, top-k 28 / 21, of V 32000: 36 / 30, 21 / 17, 30 / 16)
+// the row once more.  (V 128256 bf16, us, cut up / one workgroup per row: 8 rows top-p 35 / 78, no filter 20 / 48; 64 rows top-p 53 / 82, no filter 32 / 52; 128 rows top-p
+// 75 / 82, no filter 47 / 54.  8 rows of V 64000: top-p 35 / 46, no filter 21 / 27, of V 32000: 36 / 30, 21 / 17.)  Calls with top-k and no top-p have masses of a few
+// tokens only: one workgroup per row (k 50, 8 rows of V 70000 29 / 18, of 128256 27 / 24, drawn 32 / 22, of 260000 31 / 38, drawn 35 / 31; 64 rows of 128256 42 / 27)
 constexpr int TP_PART = 8192;
 constexpr int TP_SPLIT_ROWS = 64;                  // rows up to which they are cut up,
 constexpr int TP_SPLIT_VOCAB = 65536;              // from this vocabulary on
@@ -833,18 +887,18 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void row_bound_kern
     if (tid < TP_TABLE) S.table[tid] = ga_exp2(tid * (1.0 / TP_TABLE) + P.frac);
     Bound bound = {-__builtin_inff(), ~0u};
     u64 total = 0, with = 0;
-    auto mass = [&](float l) { return R.mass(l); };
+    auto mass = [&](u64 c) { return R.mass(logit_at(c)); };
     const int n = W.n_list;
     if (n <= TP_LIST) {
         for (int i = tid; i < n; i += 1024) S.list[i] = W.list[i];
         __syncthreads();
         if (s.k < P.vocab) {
-            bound = bound_of(find_in_list<1024>(S, n, 0, (u64)s.k, -1.0, with, [](float) { return (u64)1; }));
+            bound = bound_of(find_in_list<1024>(S, n, 0, (u64)s.k, -1.0, with, [](u64) { return (u64)1; }));
             u64 m = 0;
             for (int i = tid; i < n; i += 1024) {           // tokens behind the bound leave the list: the last place, without mass
                 const u64 c = S.list[i];
-                const float l = logit_of((unsigned)(c >> TP_MAX_LOG));
-                const unsigned id = (unsigned)c & ((1u << TP_MAX_LOG) - 1);
+                const float l = logit_at(c);
+                const unsigned id = id_at(c);
                 if (bound.keeps(l, id)) m += R.mass(l);
                 else S.list[i] = place(-__builtin_inff(), id);
             }
@@ -948,7 +1002,7 @@ template <typename LT> void go(const TpParams& P, int total, hipStream_t s) {
 // tokens of a workgroup; 0: a row is one workgroup's
 int part_of(const ps_target_probs_args* a) {
     const long long rows = (long long)a->batch * a->rows;
-    if (a->vocab < TP_SPLIT_VOCAB || rows > (a->top_k && !a->top_p ? TP_SPLIT_ROWS / 4 : TP_SPLIT_ROWS)) return 0;
+    if (a->vocab < TP_SPLIT_VOCAB || rows > TP_SPLIT_ROWS || (a->top_k && !a->top_p)) return 0;
     // about as many workgroups as there are compute units (8 x V 128256 top-p, draws: parts of 8192 42 us, 16384 47, 32768 62; 64 rows 70 with 16384, 64 with 32768)
     const long long least = std::max((a->vocab * rows + 255) / 256, (a->vocab + TP_MAX_PARTS - 1LL) / TP_MAX_PARTS);
     return (int)((least + TP_PART - 1) / TP_PART * TP_PART);
