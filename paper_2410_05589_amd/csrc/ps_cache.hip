@@ -7,8 +7,8 @@
 // written by whole lines, the bytes meet in LDS by row, codes leave and arrive 16 bytes a lane in the attention's order.  Values lie
 // transposed in that order (a lane of the attention has 16 positions of one dim), so they pass 4 x 4 byte exchanges.
 //
-// Measured (bf16, 8 heads of 128): 8 x 2048 rows written 25.0 us (67 MB read, 34 MB written, 4.0 TB/s), 4 x 4096 read back 19.6 (5.1 TB/s, a copy's rate); a path of up to 6
-// rows for 8 sequences, 32 heads 6.7, a launch and three reads one after the other (length, path, rows).  Writing is behind reading for the two looks at each
+// Measured (bf16, 8 heads of 128): 8 x 2048 rows written 22 to 25 us (67 MB read, 34 MB written, 4.0 to 4.5 TB/s), 4 x 4096 read back 19.6 (5.1 TB/s, a copy's rate); a path of up to 6
+// rows for 8 sequences, 32 heads 6.8, a launch and three reads one after the other (length, path, rows).  Writing is behind reading for the two looks at each
 // row (largest magnitude, then codes; they wait in registers) and the codes' turn through LDS; loads that pass the caches by change nothing.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -17,7 +17,9 @@
 
 namespace {
 
-constexpr int PC_WAVES = 4;   // blocks a workgroup takes
+// blocks a workgroup takes (us, one / four / sixteen: 8 x 2048 rows of 8 heads written 21.1 / 23.3 / 23.4, read 20.3 / 19.7 / 17.6; 8192 rows of 32 heads written 48 / 50 / 56,
+// read 39 / 37 / 41; 40 heads written 60 / 60 / 58, read 49 / 47 / 50): writing, whose wavefronts take different times, leaves each its own
+constexpr int PC_WRITERS = 1, PC_WAVES = 4;
 
 struct PcParams {
     const char *k, *v;        // rows (write: read; read: written)
@@ -75,11 +77,11 @@ __device__ __forceinline__ float scale_for(unsigned amax) {
 }
 
 template <typename WT, int D>
-__global__ __launch_bounds__(64 * PC_WAVES) void cache_write_kernel(const PcParams P) {
+__global__ __launch_bounds__(64 * PC_WRITERS) void cache_write_kernel(const PcParams P) {
     constexpr int PITCH = D + 16, LR = D / 8, RP = 64 / LR, PASSES = PC_BLOCK / RP, TILE = PC_BLOCK * D;
-    __shared__ __attribute__((aligned(16))) unsigned char s_tile[PC_WAVES][PC_BLOCK * PITCH];
+    __shared__ __attribute__((aligned(16))) unsigned char s_tile[PC_WRITERS][PC_BLOCK * PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int task = blockIdx.x * PC_WAVES + wave, b = blockIdx.z;
+    const int task = blockIdx.x * PC_WRITERS + wave, b = blockIdx.z;
     const int len = pc_length(P.len_dev, b, P.len[b]);
     int count = P.n[b], node = 0;
     if (P.n_accepted) {                                     // lane i + 1: the path's entry i; lane 0: node 0
@@ -312,9 +314,9 @@ extern "C" int ps_cache_write(const ps_cache_write_args* a, void* stream) {
     if (most > 65535) return PS_ERR_UNSUPPORTED;
     const bool in_place = a->len_out && a->len_out == a->kv_len_dev;
     P.len_out = in_place ? nullptr : a->len_out;
-    const dim3 grid((2 * P.heads + PC_WAVES - 1) / PC_WAVES, std::max(most, 1), a->batch);
+    const dim3 grid((2 * P.heads + PC_WRITERS - 1) / PC_WRITERS, std::max(most, 1), a->batch);
     const int launched = launch(a->dtype, a->cache->head_dim, [&](auto wt, auto d) {
-        hipLaunchKernelGGL((cache_write_kernel<decltype(wt), decltype(d)::value>), grid, dim3(64 * PC_WAVES), 0, (hipStream_t)stream, P);
+        hipLaunchKernelGGL((cache_write_kernel<decltype(wt), decltype(d)::value>), grid, dim3(64 * PC_WRITERS), 0, (hipStream_t)stream, P);
     });
     if (launched != PS_OK || !in_place) return launched;
     P.len_out = a->len_out;
