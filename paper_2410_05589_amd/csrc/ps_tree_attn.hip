@@ -18,7 +18,7 @@
 // What bounds it (bf16, head_dim 128).  One tile: reading the codes.  32 sequences of 2048 positions, 32 heads, a row each: 537 MB in 87 us, 6.2 TB/s; 4 of 32768
 // positions, 8 heads, 4 rows each: 268 MB in 46.  Many tiles: a block of one tile is 16 matrix instructions (512 cycles), 64 conversions, 16 exponentials
 // and some 100 more vector instructions, which overlap with the products less than the two wavefronts of a SIMD could make them: 1600 cycles.  8 x 4099 ...
-// 12288 positions, 61 nodes, 32 heads that share 8: 104 us, 0.63 PFLOP/s.  Left out in probes of that: conversions -6 %, exponentials -12 %, barriers and requests
+// 12288 positions, 61 nodes, 32 heads that share 8: 91 us, 0.72 PFLOP/s.  Left out in probes of that: conversions -6 %, exponentials -12 %, barriers and requests
 // -20 %, all of these -30 %.  Small calls: 2 us until the first operands are there, 2 for the tree's own rows, 2 for the meeting and the results, then the join (3).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -581,26 +581,28 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
     }
 }
 
-// The splits of one row of one head: a wavefront, a lane has D / 64 dims.  Bound by reading the parts (61 nodes, 32 heads, 30 splits of 8 sequences, 31 MB: 9.5 us, with the
-// results 4 TB/s; few rows: 3 us, two reads one after the other)
+// The splits of one row of one head: a lane has four dims, a wavefront 256 / D rows.  Bound by reading the parts (61 nodes, 32 heads, 32 splits of 8 sequences,
+// 33 MB: 8.6 us, 4.7 TB/s with the results; a wavefront per row 10.2; few rows: 3 to 4 us, two reads one after the other).  Eight splits ahead: four are 0.4 us better there
+// and 0.9 worse for 64 splits of 4 rows
 template <typename WT, int D>
 __global__ __launch_bounds__(256) void tree_attn_join_kernel(const TaParams P) {
-    constexpr int E = D / 64, AHEAD = 8;
-    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y, b = blockIdx.z;
+    constexpr int LANES = D / 4, AHEAD = 8;
+    const int lane = threadIdx.x % LANES, row = (blockIdx.x * 256 + threadIdx.x) / LANES, h = blockIdx.y, b = blockIdx.z;
     const int s0 = P.split0[b], splits = P.split0[b + 1] - s0;
     if (splits == 1 || row >= P.rows) return;
     const size_t step = (size_t)P.heads * P.rows * (D + 4);
     const float* from = P.part + (((size_t)s0 * P.heads + h) * P.rows + row) * (D + 4);
-    float m = -__builtin_inff(), l = 0.f, o[E] = {};
+    float m = -__builtin_inff(), l = 0.f;
+    f32x4 o = {0, 0, 0, 0};
     for (int s = 0; s < splits; s += AHEAD) {               // (as many splits' sums at a time: all asked for before the first is used)
-        float ms[AHEAD], ls[AHEAD], x[AHEAD][E];
+        float ms[AHEAD], ls[AHEAD];
+        f32x4 x[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const float* at = from + (size_t)min(s + u, splits - 1) * step;
             ms[u] = at[D];
             ls[u] = at[D + 1];
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[u][e] = at[lane * E + e];
+            x[u] = *reinterpret_cast<const f32x4*>(at + lane * 4);
         }
         float top = m;
 #pragma unroll
@@ -608,25 +610,17 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(const TaParams P) {
         const float base = top == -__builtin_inff() ? 0.f : top, w0 = __builtin_amdgcn_exp2f(m - base);
         m = top;
         l *= w0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= w0;
+        o *= w0;
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const float w = s + u < splits ? __builtin_amdgcn_exp2f(ms[u] - base) : 0.f;
             l = __builtin_fmaf(ls[u], w, l);
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(x[u][e], w, o[e]);
+            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(x[u][e], w, o[e]);
         }
     }
     const size_t at = ((size_t)b * P.nodes + row / P.grp) * P.n_heads + h * P.grp + row % P.grp;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if constexpr (Traits<WT>::BF) {
-        if constexpr (E == 2) *reinterpret_cast<unsigned*>(P.out + (at * D + lane * 2) * 2) = pack_bf16x2(o[0] * inv, o[1] * inv);
-        else reinterpret_cast<uint16_t*>(P.out)[at * D + lane] = (uint16_t)pack_bf16x2(o[0] * inv, 0.f);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) reinterpret_cast<float*>(P.out)[at * D + lane * E + e] = o[e] * inv;
-    }
+    store4_out<WT>(P.out + (at * D + lane * 4) * Traits<WT>::ESZ, o * (l == 0.f ? 0.f : 1.f / l));
     if (P.lse && lane == 0) P.lse[at] = log_sum(m, l);
 }
 
@@ -680,7 +674,7 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
             return n * units;
         };
         // (a split's codes stay below 2 GiB)
-        long long lo = 2 * (waves / wr), hi = (1LL << 31) / ((long long)heads * PC_BLOCK * d);
+        long long lo = 2 * (waves / wr), hi = std::max(lo, std::min(blocks_of_longest, (1LL << 31) / ((long long)heads * PC_BLOCK * d)));
         const long long most = std::max<long long>(at_once, count(hi));
         while (lo < hi) {
             const long long mid = (lo + hi) / 2;
@@ -722,7 +716,7 @@ template <typename WT, int D> void go(const TaParams& P, const TaPlan& L, hipStr
     if (L.wr == 1) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 1>), grid, block, 0, s, P);
     else if (L.wr == 2) hipLaunchKernelGGL((tree_attn_kernel<WT, D, 2>), grid, block, 0, s, P);
     else hipLaunchKernelGGL((tree_attn_kernel<WT, D, 4>), grid, block, 0, s, P);
-    if (L.bytes) hipLaunchKernelGGL((tree_attn_join_kernel<WT, D>), dim3((P.rows + 3) / 4, P.heads, P.batch), dim3(256), 0, s, P);
+    if (L.bytes) hipLaunchKernelGGL((tree_attn_join_kernel<WT, D>), dim3((P.rows + 1024 / D - 1) / (1024 / D), P.heads, P.batch), dim3(256), 0, s, P);
 }
 
 }   // namespace
