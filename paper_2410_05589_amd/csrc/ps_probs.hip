@@ -351,10 +351,11 @@ template <int T, typename W> __device__ __forceinline__ u64 find_in_list(Shared&
 }
 
 // The bound of the row's tokens that `within` keeps: the first token with which the sum of e (BY_MASS) reaches top_p of their sum, or the
-// top_k-th.  with: the sum up to and with it.
+// top_k-th.  with: the sum up to and with it.  Synchronises before it writes anything shared: wavefronts may still read what it resets
 template <bool BY_MASS, typename LT, int T>
 __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R, float mx, Shared& S, Bound within, u64 want, double of_all, u64& with) {
     const int tid = threadIdx.x;
+    __syncthreads();
     auto weight = [&](u64 c) { return BY_MASS ? R.mass(logit_at(c)) : (u64)1; };
     for (int i = tid; i < TP_BINS; i += T) S.h.mass[i] = 0;
     if (tid == 0) S.n_list = 0;
@@ -678,7 +679,6 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
         } else {
             if (!all) bound = bound_of(find_in_row<false>(L, R, mx, S, bound, (u64)k, -1.0, with));
             if (p_in < 1.f) {
-                __syncthreads();
                 bound = bound_of(find_in_row<true>(L, R, mx, S, bound, 0, fmax((double)p_in, 0.0), with));
                 total = with;
             }
@@ -913,12 +913,10 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void row_bound_kern
             total = with;
         }
     } else {                                                // more tokens than the list holds: the whole row, by this workgroup
-        __syncthreads();
         Logits<LT, 1024> L;
         L.row = P.logits + row * P.vocab * Traits<LT>::ESZ; L.vocab = P.vocab; L.nvec = (P.vocab + Vec<LT>::N - 1) / Vec<LT>::N;
         if (s.k < P.vocab) bound = bound_of(find_in_row<false>(L, R, s.max, S, bound, (u64)s.k, -1.0, with));
         if (s.top_p < 1.f) {
-            __syncthreads();
             bound = bound_of(find_in_row<true>(L, R, s.max, S, bound, 0, fmax((double)s.top_p, 0.0), with));
             total = with;
         }
