@@ -403,7 +403,7 @@ __device__ __forceinline__ u64 find_in_row(const Logits<LT, T>& L, const Row& R,
         if (S.h.count[S.found] > TP_LIST && shift > 0) continue;   // (at the last digit it is one token)
         L.tokens([&](float l, int id) {
             const u64 c = place(l, id);
-            if (c >> shift == prefix && within.keeps(l, id)) list_add(S, c, L.vocab);
+            if (c >> shift == prefix && l >= least && l < above && within.keeps(l, id)) list_add(S, c, L.vocab);   // (the step's: what is in front of it is in `before`)
         });
         __syncthreads();
         return find_in_list<T>(S, S.n_list, before, want, -1.0, with, weight);

@@ -1,4 +1,6 @@
 """GPU tests of the target's distributions (ps_target_probs) on crowded rows: more tokens at or near the bound than the kernels' lists hold (2048)."""
+import math
+
 import pytest
 
 from tests import target_util as TU
@@ -29,3 +31,66 @@ def test_a_small_top_k_among_thousands_of_equal_tokens(dtype, batch, vocab):
                 kept = (torch.arange(vocab).cuda()[None] < k[:, None])[:, None]
                 assert (out > 0).equal(kept)
                 assert ids.equal((r.double() * k[:, None]).floor().int())
+
+
+def _crowded(vocab, seed):
+    """float32 rows whose crowded step lies across a border of the numbers' exponents, with tokens of steps before it on one side."""
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    rows = []
+    x = torch.full((vocab,), -9.0)                           # across 8: 10 tokens in front of the step's 1500 and 1500
+    at = torch.randperm(vocab, generator=g)
+    x[at[:10]], x[at[10:1510]], x[at[1510:3010]] = 8.03, 8.001, 7.999
+    rows.append(x)
+    x = torch.full((vocab,), -9.0)                           # across 2, every number another one
+    x[at[:3500]] = 2.0 + (torch.rand(3500, generator=g) - 0.5) * 0.012
+    x[at[3500:4400]] = 2.03 + torch.rand(900, generator=g) * 0.08
+    x[at[4400]] = 2.0 + 5.5 * math.log(2) / 32               # (a step is 1/32 of a power of two)
+    rows.append(x)
+    x = torch.full((vocab,), -9.0)                           # across 0
+    x[at[:4000]] = torch.randn(4000, generator=g) * 0.003
+    x[at[4000:4600]] = 0.02 + torch.rand(600, generator=g) * 0.03
+    rows.append(x)
+    rows.append(torch.randn(vocab, generator=g) * 2.0)       # with a high temperature
+    return torch.stack(rows)[:, None].contiguous(), torch.rand((4, 1), generator=g)
+
+
+CROWDED = [                                                  # (the fourth row's: a temperature and a top_k for 128256 tokens, in proportion for fewer)
+    dict(top_k=[700, 2000, 2500, 20000], temperature=[1.0, 1.0, 1.0, 8.0]),
+    dict(top_k=[1511, 3000, 1500, 30000], temperature=[1.0, 1.0, 1.0, 16.0]),
+    dict(top_p=[0.3, 0.4, 0.5, 0.3], temperature=[1.0, 1.0, 1.0, 16.0]),
+    dict(top_k=[2900, 4300, 4500, 60000], top_p=[0.4, 0.6, 0.7, 0.8], temperature=[1.0, 1.0, 1.0, 20.0]),
+]
+
+
+def _settings(vocab, i):
+    s = {n: list(x) for n, x in CROWDED[i].items()}
+    s["temperature"][3] *= 128256 / vocab
+    if "top_k" in s:
+        s["top_k"][3] = s["top_k"][3] * vocab // 128256
+    return s
+
+
+@pytest.mark.parametrize("i", range(len(CROWDED)))
+@pytest.mark.parametrize("vocab,copies", [(9000, 1), (40000, 1), (70000, 1), (128256, 1), (70000, 17), (9000, 70)])
+def test_a_crowded_step_across_a_border_of_exponents(vocab, copies, i):
+    """One workgroup per row, several, and one of 512 threads (more than 256 rows); rows behind the first are copies and have to come out as it did."""
+    import torch
+    x, r = _crowded(vocab, 3 * vocab + i)
+    x, r = x.expand(4, copies, vocab).contiguous().cuda(), r.expand(4, copies).contiguous().cuda()
+    settings = _settings(vocab, i)
+    out, ids, id_p = call(x, settings, r)
+    check(x, settings, r, out, ids, id_p, at=[0])
+    assert out.equal(out[:, :1].expand_as(out)) and ids.equal(ids[:, :1].expand_as(ids)) and id_p.equal(id_p[:, :1].expand_as(id_p))
+    again, ids2, id_p2 = call(x, settings, r)
+    assert again.equal(out) and ids2.equal(ids) and id_p2.equal(id_p)
+
+
+def test_top_k_of_a_flat_row():
+    """20000 of 128256 tokens at a temperature of 8: a step of several hundred tokens' logits in a bucket with 20000 others, whole and cut up."""
+    import torch
+    x = (torch.randn((1, 1, 128256), generator=torch.Generator().manual_seed(2)) * 2.0).cuda()
+    for settings in (dict(top_k=[20000], temperature=[8.0]), dict(top_k=[20000], temperature=[8.0], top_p=[1.0])):
+        out, _, _ = call(x, settings)
+        check(x, settings, None, out, None, None)
+        assert int((out > 0).sum()) == 20000
