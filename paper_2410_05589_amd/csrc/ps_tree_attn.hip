@@ -2,8 +2,8 @@
 //
 //   S = scale q K^T,  P = exp(S - m),  out = P V / sum P,  K = k_scale code, V = v_scale code per block of 32 positions
 //
-// e4m3 codes are bf16 numbers, so both products run on v_mfma_f32_32x32x16_bf16 with exact keys and values; the scales, powers of two,
-// join the scores' constant and the exponent of P.  Queries stand along the lanes: S^T = K Q^T leaves a lane (query c, half h) the
+// e4m3 codes are bf16 numbers, so both products run on v_mfma_f32_32x32x16_bf16 with exact keys and values; the scales are powers of two:
+// the keys' join the scores' constant, the values' come in with the conversion of their codes.  Queries stand along the lanes: S^T = K Q^T leaves a lane (query c, half h) the
 // scores of positions 8 a + 4 h + b, and out^T = V^T P^T takes them from there as its operand: the cache keeps values in just that order, so
 // codes go from memory to the matrix cores through a conversion (two codes an instruction), with no exchange between lanes.
 // The running maximum is raised only when a score passes it by 2^8 (sums stay far inside float32), so sums are rarely rescaled.
@@ -56,11 +56,11 @@ struct TaParams {
 
 template <int D> struct Tile { uint4 k[D / 32], v[D / 32]; };
 
-// 8 codes as bf16
-__device__ __forceinline__ bf16x8 widen8(unsigned lo, unsigned hi) {
+// 8 codes times a power of two as bf16 (exact for 2^-124 and above; what comes to 2^128 is Inf)
+__device__ __forceinline__ bf16x8 widen8(unsigned lo, unsigned hi, float scale) {
     typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
-    const b2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+    const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const b2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 __device__ __forceinline__ unsigned word(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
@@ -115,8 +115,8 @@ template <int D> struct RowState {
     float m, l;                     // maximum (in powers of two), this half's sum
 };
 
-// One tile of 32 keys: scores (raw products) to probabilities against the running maximum.  c: what makes products powers of two; lv: log2 of
-// the values' scale, which the probabilities that meet codes carry
+// One tile of 32 keys: scores (raw products) to probabilities against the running maximum.  c: what makes products powers of two.  (The values' scale is no part of
+// them: with a block's 2^-100, zeros' scale, those below 2^-26 would not be in the sum)
 template <int D, int NB> __device__ __forceinline__ void raise_maximum(RowState<D>& R, const f32x16 (&s)[NB], const float (&c)[NB]) {
     float mx = -__builtin_inff();
 #pragma unroll
@@ -135,15 +135,15 @@ template <int D, int NB> __device__ __forceinline__ void raise_maximum(RowState<
         for (int j = 0; j < D / 32; ++j) R.o[j] *= alpha;
     }
 }
-template <int D> __device__ __forceinline__ void exponentials(RowState<D>& R, f32x16& s, float c, float lv, float inv_vs) {
-    const float off = (R.m == -__builtin_inff() ? 0.f : R.m) - lv;
+template <int D> __device__ __forceinline__ void exponentials(RowState<D>& R, f32x16& s, float c) {
+    const float off = R.m == -__builtin_inff() ? 0.f : R.m;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -off));
         sum += s[i];
     }
-    R.l = __builtin_fmaf(sum, inv_vs, R.l);
+    R.l += sum;
 }
 template <int NP> __device__ __forceinline__ void prob_parts(const f32x16& s, bf16x8 (&p)[2][NP]) {
 #pragma unroll
@@ -175,7 +175,7 @@ template <int D, int NP> __device__ __forceinline__ void key_products(const bf16
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const bf16x8 kf = widen8(word(k[c], 2 * u), word(k[c], 2 * u + 1));
+            const bf16x8 kf = widen8(word(k[c], 2 * u), word(k[c], 2 * u + 1), 1.f);
 #pragma unroll
             for (int p = NP - 1; p >= 0; --p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[2 * c + u][p], s, 0, 0, 0);
         }
@@ -195,20 +195,18 @@ template <int D> __device__ __forceinline__ void hide(f32x16& s, uint4 (&v)[D / 
     for (int c = 0; c < D / 32; ++c) v[c] = make_uint4(v[c].x & keep[0], v[c].y & keep[1], v[c].z & keep[2], v[c].w & keep[3]);
 }
 // ... products with its values
-template <int D, int NP> __device__ __forceinline__ void value_products(RowState<D>& R, const f32x16& s, const uint4 (&v)[D / 32]) {
+template <int D, int NP> __device__ __forceinline__ void value_products(RowState<D>& R, const f32x16& s, const uint4 (&v)[D / 32], float scale) {
     bf16x8 p[2][NP];
     prob_parts<NP>(s, p);
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-            const bf16x8 vf = widen8(word(v[j], 2 * st), word(v[j], 2 * st + 1));
+            const bf16x8 vf = widen8(word(v[j], 2 * st), word(v[j], 2 * st + 1), scale);
 #pragma unroll
             for (int n = NP - 1; n >= 0; --n) R.o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[st][n], R.o[j], 0, 0, 0);
         }
 }
-__device__ __forceinline__ float log2_of(float scale) { return (float)((int)(__float_as_uint(scale) >> 23) - 127); }   // (powers of two)
-__device__ __forceinline__ float one_over(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }
 
 // Four tiles of rows: four wavefronts read the same blocks, which come to LDS by way of the memory unit, 1 KiB per request, two steps of
 // TA_STEP blocks ahead in three buffers (arrays of their own: a read from one need not wait for what is on its way into another).  A step's
@@ -337,7 +335,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
                 f32x16 one[1] = {s};
                 const float c1[1] = {P.c};
                 raise_maximum<D, 1>(R, one, c1);
-                exponentials<D>(R, s, P.c, 0.f, 1.f);
+                exponentials<D>(R, s, P.c);
                 bf16x8 p[2][NP];
                 prob_parts<NP>(s, p);
 #pragma unroll
@@ -430,8 +428,8 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             raise_maximum<D, 2>(R, x, cs);
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                exponentials<D>(R, x[n], cs[n], log2_of(vs[n]), one_over(vs[n]));
-                value_products<D, NP>(R, x[n], t[n]);
+                exponentials<D>(R, x[n], cs[n]);
+                value_products<D, NP>(R, x[n], t[n], vs[n]);
             }
         };
         if (steps > 0) {
@@ -503,8 +501,8 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
                 if (tail && i == blocks - 1) hide<D>(x[0], t.v, tail);
                 const float cs[1] = {P.c * ks};
                 raise_maximum<D, 1>(R, x, cs);
-                exponentials<D>(R, x[0], cs[0], log2_of(vs), one_over(vs));
-                value_products<D, NP>(R, x[0], t.v);
+                exponentials<D>(R, x[0], cs[0]);
+                value_products<D, NP>(R, x[0], t.v, vs);
             }
         }
     }

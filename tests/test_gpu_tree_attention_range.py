@@ -1,0 +1,58 @@
+"""GPU tests of the tree attention (ps_tree_attention) with values of very different size: what has no weight in the results' numerator still has its part of the sum.
+
+All keys and values are numbers that the cache holds exactly, scores are powers of two in exponent (scale = log 2, or q in proportion), so results have closed forms."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2410_05589_amd import verify as VF
+from tests import target_util as TU
+from tests.test_gpu_tree_attention import call, chain
+
+pytestmark = pytest.mark.gpu
+
+# how rows are cut: one, two and four tiles of 32 rows per workgroup (17 nodes of 4 query heads per kv head are 68 rows); dtype, query heads per kv head, tree, wavefronts that
+# divide a tile's blocks
+SHAPES = [("bf16", 1, [-1], 8), ("f32", 1, [-1], 4), ("bf16", 2, chain(17), 4), ("f32", 2, chain(17), 2), ("bf16", 4, chain(17), 1), ("f32", 4, chain(17), 1)]
+
+
+def _filled(heads, d, k, v):
+    """A cache of one sequence with the rows k, v [n, d] of all heads (made on the device)."""
+    import torch
+    n = k.shape[0]
+    cache = TU.Cache(1, d, [32])
+    cache.heads, cache.offsets = heads, [0, (n + 31) // 32 * 32]
+    blocks = (n + 31) // 32
+    cache.codes = {x: torch.empty((blocks, heads, 32 * d), dtype=torch.uint8, device="cuda:0") for x in "kv"}
+    cache.scales = {x: torch.empty((blocks, heads), device="cuda:0") for x in "kv"}
+    cache.struct = VF.make_cache(heads, d, cache.codes["k"].data_ptr(), cache.codes["v"].data_ptr(), cache.scales["k"].data_ptr(), cache.scales["v"].data_ptr(), cache.offsets)
+    for at in range(0, n, 4096):
+        kk, vv = (x[None, at:at + 4096, None].expand(1, -1, heads, d).to(torch.bfloat16).contiguous() for x in (k, v))
+        cache.write(kk, vv, [at], "bf16")
+    return cache
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "%s-%d-%d" % (s[0], s[1], len(s[2])))
+def test_probabilities_of_values_that_are_zero_are_in_the_sum(shape, d):
+    """32768 positions whose score is 2^-27 of the first one's and whose values are all zero (their blocks' scale is the least there is): together 2^-12 of the sum.
+    256 kv heads, so that a workgroup has a whole sequence.  Tolerance: sums of positive terms, per wavefront 16 terms of a block and then block by block, then a
+    few joins, each addition off by 2^-24 of the sum; exponentials and the logarithm 2^-20."""
+    import torch
+    dtype, grp, parent, wk = shape
+    n, heads = 32768, 256
+    k = torch.zeros((n, d), device="cuda:0")
+    k[1:, 0], k[1:, 1] = -13.0, -14.0
+    v = torch.zeros((n, d), device="cuda:0")
+    v[0] = 1.0
+    cache = _filled(heads, d, k, v)
+    assert float(cache.scales["v"][1:].max()) == 2.0 ** -100
+    q = torch.zeros((1, len(parent), heads * grp, d), dtype=TU.torch_dtype(dtype), device="cuda:0")
+    q[..., 0] = q[..., 1] = 1.0
+    out, lse = call(cache, parent, q, None, None, [n], dtype, scale=math.log(2))
+    total = 1.0 + (n - 1) * 2.0 ** -27
+    tol = (n / 32 / wk + 64) * 2.0 ** -24 + 2.0 ** -20
+    assert tol < 0.75 * (n / wk) * 2.0 ** -27                 # (what one wavefront's positions add is seen)
+    assert np.abs(TU.np64(lse) - math.log(total)).max() <= tol
+    assert np.abs(TU.np64(out) * total - 1.0).max() <= tol + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -22)
