@@ -35,6 +35,9 @@ template <typename WT, int WR> constexpr int ta_waves() { return Traits<WT>::BF 
 // How far (in powers of two) scores may pass the maximum that they are taken against: probabilities stay below 2^8, their sums over 2^30 positions below 2^38.  (A maximum
 // that is raised with every score above it: 4 % of the time with many tiles)
 constexpr float TA_LAZY = 8.f;
+// Sums of values are held times this, so that probabilities of up to 2^8 of the largest floats stay floats (2^-12: sixteen of them): cached values by their scale
+// (2^-100 and above: still exact), own ones by their probabilities
+constexpr float TA_HELD = 0x1p-12f, TA_HELD_LOG = -12.f;
 
 struct TaParams {
     const char *q, *k, *v;
@@ -56,7 +59,7 @@ struct TaParams {
 
 template <int D> struct Tile { uint4 k[D / 32], v[D / 32]; };
 
-// 8 codes times a power of two as bf16 (exact for 2^-124 and above; what comes to 2^128 is Inf)
+// 8 codes times a power of two as bf16 (exact for 2^-124 and above)
 __device__ __forceinline__ bf16x8 widen8(unsigned lo, unsigned hi, float scale) {
     typedef __bf16 b2 __attribute__((ext_vector_type(2)));
     const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
@@ -109,7 +112,7 @@ __device__ __forceinline__ float other_half(float v) {
     return __uint_as_float(threadIdx.x & 32 ? r[0] : r[1]);
 }
 
-// What a wavefront has of one tile of 32 rows: lane (row c, half h) has of every 32 dims the dims 8 a + 4 h + b as o[.][4 a + b]
+// What a wavefront has of one tile of 32 rows: lane (row c, half h) has of every 32 dims the dims 8 a + 4 h + b as o[.][4 a + b] (times TA_HELD)
 template <int D> struct RowState {
     f32x16 o[D / 32];
     float m, l;                     // maximum (in powers of two), this half's sum
@@ -135,15 +138,15 @@ template <int D, int NB> __device__ __forceinline__ void raise_maximum(RowState<
         for (int j = 0; j < D / 32; ++j) R.o[j] *= alpha;
     }
 }
-template <int D> __device__ __forceinline__ void exponentials(RowState<D>& R, f32x16& s, float c) {
-    const float off = R.m == -__builtin_inff() ? 0.f : R.m;
+template <int D, bool OWN> __device__ __forceinline__ void exponentials(RowState<D>& R, f32x16& s, float c) {
+    const float off = (R.m == -__builtin_inff() ? 0.f : R.m) - (OWN ? TA_HELD_LOG : 0.f);
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -off));
         sum += s[i];
     }
-    R.l += sum;
+    R.l = OWN ? __builtin_fmaf(sum, 1.f / TA_HELD, R.l) : R.l + sum;
 }
 template <int NP> __device__ __forceinline__ void prob_parts(const f32x16& s, bf16x8 (&p)[2][NP]) {
 #pragma unroll
@@ -335,7 +338,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
                 f32x16 one[1] = {s};
                 const float c1[1] = {P.c};
                 raise_maximum<D, 1>(R, one, c1);
-                exponentials<D>(R, s, P.c);
+                exponentials<D, true>(R, s, P.c);
                 bf16x8 p[2][NP];
                 prob_parts<NP>(s, p);
 #pragma unroll
@@ -411,7 +414,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
 #pragma unroll
                 for (int c = 0; c < C; ++c) t[n][c] = ld16(mine.codes + (n * 2 * C + c) * 1024 + lane * 16);
                 cs[n] = P.c * mine.scales[0][n];
-                vs[n] = mine.scales[1][n];
+                vs[n] = mine.scales[1][n] * TA_HELD;
             }
 #pragma unroll
             for (int n = 0; n < 2; ++n) key_products<D, NP>(q, t[n], x[n]);
@@ -428,7 +431,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             raise_maximum<D, 2>(R, x, cs);
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                exponentials<D>(R, x[n], cs[n]);
+                exponentials<D, false>(R, x[n], cs[n]);
                 value_products<D, NP>(R, x[n], t[n], vs[n]);
             }
         };
@@ -490,7 +493,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             for (; i < end; i += WK) {
                 Tile<D> t = next;
                 const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k_scales), turn));
-                const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), turn));
+                const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v_scales), turn)) * TA_HELD;
                 if (i + WK < end) {
                     fetch(i + WK, next);
                     turn = (turn + 1) & 63;
@@ -501,7 +504,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
                 if (tail && i == blocks - 1) hide<D>(x[0], t.v, tail);
                 const float cs[1] = {P.c * ks};
                 raise_maximum<D, 1>(R, x, cs);
-                exponentials<D>(R, x[0], cs[0]);
+                exponentials<D, false>(R, x[0], cs[0]);
                 value_products<D, NP>(R, x[0], t.v, vs);
             }
         }
@@ -542,7 +545,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             }
             if (splits == 1) {
                 const size_t at = ((size_t)b * P.nodes + at_row / P.grp) * P.n_heads + h * P.grp + at_row % P.grp;
-                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const float inv = l == 0.f ? 0.f : 1.f / TA_HELD / l;
                 lo *= inv;
                 hi *= inv;
                 char* to = P.out + (at * D + d0) * ESZ;
@@ -561,7 +564,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
     if (!valid) return;
     if (splits == 1) {
         const size_t at = ((size_t)b * P.nodes + node) * P.n_heads + head;
-        const float inv = R.l == 0.f ? 0.f : 1.f / R.l;
+        const float inv = R.l == 0.f ? 0.f : 1.f / TA_HELD / R.l;
 #pragma unroll
         for (int j = 0; j < C; ++j)
 #pragma unroll
@@ -618,7 +621,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(const TaParams P) {
         }
     }
     const size_t at = ((size_t)b * P.nodes + row / P.grp) * P.n_heads + h * P.grp + row % P.grp;
-    store4_out<WT>(P.out + (at * D + lane * 4) * Traits<WT>::ESZ, o * (l == 0.f ? 0.f : 1.f / l));
+    store4_out<WT>(P.out + (at * D + lane * 4) * Traits<WT>::ESZ, o * (l == 0.f ? 0.f : 1.f / TA_HELD / l));
     if (P.lse && lane == 0) P.lse[at] = log_sum(m, l);
 }
 

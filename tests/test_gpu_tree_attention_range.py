@@ -56,3 +56,33 @@ def test_probabilities_of_values_that_are_zero_are_in_the_sum(shape, d):
     assert tol < 0.75 * (n / wk) * 2.0 ** -27                 # (what one wavefront's positions add is seen)
     assert np.abs(TU.np64(lse) - math.log(total)).max() <= tol
     assert np.abs(TU.np64(out) * total - 1.0).max() <= tol + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -22)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "%s-%d-%d" % (s[0], s[1], len(s[2])))
+@pytest.mark.parametrize("size", [2.0 ** 125, 2.0 ** 60, 2.0 ** -60, 2.0 ** -90])
+def test_values_at_the_ends_of_the_range(shape, d, size):
+    """Values near the largest and the smallest numbers, block by block with a score that is 1.75 powers of two higher than in the one before, so that the maximum that
+    exponentials are taken against is behind for some blocks."""
+    import torch
+    dtype, grp, parent, _ = shape
+    n, heads = 32 * 40, 64
+    block = torch.arange(n, device="cuda:0") // 32
+    k = torch.zeros((n, d), device="cuda:0")
+    score = 1.75 * block
+    k[:, 0] = torch.where(torch.arange(n, device="cuda:0") % 32 == 5, (block / 4).floor(), -1.0)    # (e4m3: whole numbers up to 16)
+    k[:, 1] = torch.where(torch.arange(n, device="cuda:0") % 32 == 5, block % 4, -64.0)
+    v = torch.zeros((n, d), device="cuda:0")
+    v[:] = (1.0 + (block % 4)[:, None] / 4) * size / 2
+    v[:, 1::2] *= -1
+    cache = _filled(heads, d, k, v)
+    q = torch.zeros((1, len(parent), heads * grp, d), dtype=TU.torch_dtype(dtype), device="cuda:0")
+    q[..., 0], q[..., 1] = 7.0, 1.75
+    out, lse = call(cache, parent, q, None, None, [n], dtype, scale=math.log(2))
+    s = np.where(np.arange(n) % 32 == 5, TU.np64(score.float()), -7.0 - 112.0)
+    p = np.exp2(s - s.max())
+    want = (p[:, None] * TU.np64(v)).sum(0) / p.sum()
+    # (a score of up to 70 is off by 2^-23 of itself, the rest as in the test before; bf16: probabilities and results by 2^-8 each)
+    tol = 70 * 2.0 ** -22 + 104 * 2.0 ** -24 + 2.0 ** -20 + (2.0 ** -7 if dtype == "bf16" else 0.0)
+    assert np.abs(TU.np64(out) / want - 1.0).max() <= tol
+    assert np.abs(TU.np64(lse) - (s.max() * math.log(2) + math.log(p.sum()))).max() <= 70 * 2.0 ** -22 + 104 * 2.0 ** -24 + 2.0 ** -20
