@@ -118,6 +118,9 @@ template <int D> struct RowState {
     float m, l;                     // maximum (in powers of two), this half's sum
 };
 
+// What makes a block's products powers of two; a float: keys above 2^100 and a scale above 1 would make it Inf, and a product of zero NaN
+__device__ __forceinline__ float score_factor(float c, float k_scale) { return __builtin_fminf(c * k_scale, 3.4028234663852886e38f); }
+
 // One tile of 32 keys: scores (raw products) to probabilities against the running maximum.  c: what makes products powers of two.  (The values' scale is no part of
 // them: with a block's 2^-100, zeros' scale, those below 2^-26 would not be in the sum)
 template <int D, int NB> __device__ __forceinline__ void raise_maximum(RowState<D>& R, const f32x16 (&s)[NB], const float (&c)[NB]) {
@@ -413,7 +416,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
             for (int n = 0; n < 2; ++n) {
 #pragma unroll
                 for (int c = 0; c < C; ++c) t[n][c] = ld16(mine.codes + (n * 2 * C + c) * 1024 + lane * 16);
-                cs[n] = P.c * mine.scales[0][n];
+                cs[n] = score_factor(P.c, mine.scales[0][n]);
                 vs[n] = mine.scales[1][n] * TA_HELD;
             }
 #pragma unroll
@@ -502,7 +505,7 @@ __global__ __launch_bounds__((64 * ta_waves<WT, WR>()), (Traits<WT>::BF ? 2 : 1)
                 f32x16 x[1];
                 key_products<D, NP>(q, t.k, x[0]);
                 if (tail && i == blocks - 1) hide<D>(x[0], t.v, tail);
-                const float cs[1] = {P.c * ks};
+                const float cs[1] = {score_factor(P.c, ks)};
                 raise_maximum<D, 1>(R, x, cs);
                 exponentials<D, false>(R, x[0], cs[0]);
                 value_products<D, NP>(R, x[0], t.v, vs);

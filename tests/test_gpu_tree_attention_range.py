@@ -86,3 +86,19 @@ def test_values_at_the_ends_of_the_range(shape, d, size):
     tol = 70 * 2.0 ** -22 + 104 * 2.0 ** -24 + 2.0 ** -20 + (2.0 ** -7 if dtype == "bf16" else 0.0)
     assert np.abs(TU.np64(out) / want - 1.0).max() <= tol
     assert np.abs(TU.np64(lse) - (s.max() * math.log(2) + math.log(p.sum()))).max() <= 70 * 2.0 ** -22 + 104 * 2.0 ** -24 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "%s-%d-%d" % (s[0], s[1], len(s[2])))
+def test_queries_of_zero_over_the_largest_keys(shape):
+    """All scores are zero, whatever the keys and the scale are: the mean of the values."""
+    import torch
+    dtype, grp, parent, _ = shape
+    n, heads, d = 75, 2, 64
+    k = torch.full((n, d), 2.0 ** 125, device="cuda:0")
+    v = (torch.arange(n, device="cuda:0") % 8).float()[:, None].expand(n, d).contiguous()
+    cache = _filled(heads, d, k, v)
+    q = torch.zeros((1, len(parent), heads * grp, d), dtype=TU.torch_dtype(dtype), device="cuda:0")
+    out, lse = call(cache, parent, q, None, None, [n], dtype, scale=2.0 ** 20)
+    want = float(v[:, 0].double().mean())
+    assert np.abs(TU.np64(out) - want).max() <= want * (2.0 ** -7 if dtype == "bf16" else 2.0 ** -18)
+    assert np.abs(TU.np64(lse) - math.log(n)).max() <= 2.0 ** -18
