@@ -580,9 +580,11 @@ __device__ __forceinline__ void no_token(const TpParams& P, size_t row, bool bad
 // min_p's bound, where it is above `bound`
 __device__ __forceinline__ void apply_min_p(const TpParams& P, const Row& R, float min_p, Bound& bound, u64& total) {
     if (!(min_p > 0.f)) return;
-    const double least_e = ldexp((double)min_p, P.frac);
+    // (exponentials stop at 2^-80: a min_p down there is compared in the exponent)
+    const bool tiny = min_p < 0x1p-79f;
+    const double least_e = tiny ? log2((double)min_p) * TP_TABLE : ldexp((double)min_p, P.frac);
     int kk;
-    const float least = least_float((float)R.max, R.near_e(min_p), [&](float l) { return R.scaled(l, kk) >= least_e; });
+    const float least = least_float((float)R.max, R.near_e(min_p), [&](float l) { return tiny ? ((double)l - R.max) * R.c >= least_e : R.scaled(l, kk) >= least_e; });
     if (least > bound.l) { bound = {least, ~0u}; total = 0; }
 }
 

@@ -94,3 +94,24 @@ def test_top_k_of_a_flat_row():
         out, _, _ = call(x, settings)
         check(x, settings, None, out, None, None)
         assert int((out > 0).sum()) == 20000
+
+
+@pytest.mark.parametrize("vocab,rows", [(50, 1), (70000, 1), (70000, 65)])
+@pytest.mark.parametrize("other", [{}, dict(top_p=[1.0]), dict(top_k=[40]), dict(top_k=[1500])])
+def test_a_min_p_of_almost_nothing(vocab, rows, other):
+    """min_p below 2^-80, which whole masses do not resolve: kept are the e that reach it all the same, and those below have probability zero."""
+    import torch
+    x = torch.full((1, rows, vocab), -math.inf)
+    logits = [0.0, -40.0, -55.0, -57.0, -60.0, -69.0, -69.2, -80.0, -85.0, -87.0]
+    x[:, :, 3:3 + len(logits)] = torch.tensor(logits)
+    r = torch.full((1, rows), 0.5)
+    for min_p in (2.0 ** -79.0, 2.0 ** -80.0, 2.0 ** -80.5, 1e-25, 1e-30, 1e-35, 1e-37, 2.0 ** -126):
+        out, ids, _ = call(x.cuda(), dict(min_p=[min_p], **other), r.cuda())
+        least = float(torch.tensor(min_p))
+        p = [math.exp(l) if math.exp(l) >= least else 0.0 for l in x[0, 0, 3:3 + len(logits)].tolist()]   # (the float32 numbers: -69.2 is none)
+        want = torch.zeros(vocab, dtype=torch.float64)
+        want[3:3 + len(logits)] = torch.tensor(p, dtype=torch.float64) / math.fsum(p)
+        got = out[0, -1].double().cpu()
+        assert (got > 0).equal(want > 0), (min_p, got[:14])
+        assert ((got - want).abs() <= want * 2.0 ** -20).all()
+        assert (ids == 3).all()
