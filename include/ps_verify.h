@@ -163,7 +163,7 @@ typedef struct ps_cache {
  * Calls that write the same sequence must not overlap in time, and no other call may read what one writes.
  * Errors: PS_ERR_NULL; PS_ERR_SHAPE; PS_ERR_OFFSETS (kv_offsets negative, decreasing or no multiples of 32); PS_ERR_KV_CAPACITY
  * (kv_len[b] and the most rows that can follow exceed the sequence's blocks); PS_ERR_UNSUPPORTED (head_dim, batch, alignment: rows
- * and row_stride to 4 bytes); PS_ERR_DEVICE.
+ * and row_stride to 4 bytes; kv_len[b] and the rows above 2^31 - 1); PS_ERR_DEVICE.
  */
 typedef struct ps_cache_write_args {
     int32_t batch, rows, dtype;

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(64 * PC_WRITERS) void cache_write_kernel(const PcPa
     const int h = value ? task - P.heads : task;
     const int block = (len >> 5) + (int)blockIdx.y;         // block of the sequence
     const int t0 = blockIdx.y == 0 ? len & 31 : 0;          // positions it has already
-    const int from = block * 32 + t0 - len;                 // the first row that goes there
+    const int from = (int)blockIdx.y * 32 + t0 - (len & 31);  // the first row that goes there
     const int n = min(count - from, 32 - t0);
     if (n <= 0) return;
 
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(64 * PC_WAVES) void cache_read_kernel(const PcParam
     if (!out) return;
     const int h = value ? task - P.heads : task;
     const int start = P.len[b], block = (start >> 5) + (int)blockIdx.y;
-    const int t0 = blockIdx.y == 0 ? start & 31 : 0, from = block * 32 + t0 - start;
+    const int t0 = blockIdx.y == 0 ? start & 31 : 0, from = (int)blockIdx.y * 32 + t0 - (start & 31);
     const int n = min(P.n[b] - from, 32 - t0);
     if (n <= 0) return;
     out += ((long long)b * P.rows + from) * P.row_bytes + (long long)h * D * Traits<WT>::ESZ;
@@ -282,7 +282,10 @@ template <typename A> int check(const A* a, PcParams& P) {
     }
     return PS_OK;
 }
-bool fits(const ps_cache* c, int b, long long tokens) { return tokens <= c->kv_offsets[b + 1] - c->kv_offsets[b]; }
+// positions 0 .. tokens - 1 of a sequence: its blocks have them, and the kernels' 32-bit lengths
+int fits(const ps_cache* c, int b, long long tokens) {
+    return tokens > c->kv_offsets[b + 1] - c->kv_offsets[b] ? PS_ERR_KV_CAPACITY : tokens > INT32_MAX ? PS_ERR_UNSUPPORTED : PS_OK;
+}
 
 template <typename F> int launch(int dtype, int d, F go) {
     if (dtype == PS_BF16) { if (d == 128) go(bf16_t{}, std::integral_constant<int, 128>{}); else go(bf16_t{}, std::integral_constant<int, 64>{}); }
@@ -306,7 +309,8 @@ extern "C" int ps_cache_write(const ps_cache_write_args* a, void* stream) {
         P.len[b] = a->kv_len[b];
         if (P.len[b] < 0) return PS_ERR_SHAPE;
         if (a->path) P.n[b] = 1 + a->path_rows;
-        if (!fits(a->cache, b, (long long)P.len[b] + P.n[b])) return PS_ERR_KV_CAPACITY;
+        const int fit = fits(a->cache, b, (long long)P.len[b] + P.n[b]);
+        if (fit != PS_OK) return fit;
         // blocks that this many positions can touch (where the device has the length: wherever they start)
         const int start = a->kv_len_dev ? PC_BLOCK - 1 : P.len[b] % PC_BLOCK;
         most = std::max(most, P.n[b] ? (int)(((long long)start + P.n[b] + PC_BLOCK - 1) / PC_BLOCK) : 0);
@@ -333,7 +337,8 @@ extern "C" int ps_cache_read(const ps_cache_read_args* a, void* stream) {
     for (int b = 0; b < a->batch; ++b) {
         P.len[b] = a->start ? a->start[b] : 0;
         if (P.len[b] < 0) return PS_ERR_SHAPE;
-        if (!fits(a->cache, b, (long long)P.len[b] + P.n[b])) return PS_ERR_KV_CAPACITY;
+        const int fit = fits(a->cache, b, (long long)P.len[b] + P.n[b]);
+        if (fit != PS_OK) return fit;
         most = std::max(most, P.n[b] ? (int)(((long long)P.len[b] % PC_BLOCK + P.n[b] + PC_BLOCK - 1) / PC_BLOCK) : 0);
     }
     if (most > 65535) return PS_ERR_UNSUPPORTED;
