@@ -212,7 +212,7 @@ PS_API int ps_cache_read(const ps_cache_read_args* args, void* stream);
  *   scale           0 stands for 1 / sqrt(head_dim); else 2^-20 .. 2^20
  *   out             DEVICE [batch][n_nodes][n_heads][head_dim], dtype, written
  *   lse             DEVICE [batch][n_nodes][n_heads] float32 or NULL, written: log of the sum of exp(scale * q k)
- *   kv_len, kv_len_dev  as for ps_cache_write
+ *   kv_len, kv_len_dev  as for ps_cache_write.  Work is divided by kv_len: bounds far above the lengths leave part of the card idle
  *   workspace       DEVICE, ps_tree_attention_workspace_bytes bytes, 256-byte aligned (NULL where that is 0); its contents do not
  *                   matter before or after the call.  Calls that overlap in time need one each
  * A row that sees nothing (no cached position, no own rows) has out = 0 and lse = -Inf.  A value row that is hidden from a row does
@@ -259,8 +259,8 @@ PS_API size_t ps_tree_attention_workspace_bytes(const ps_tree_shape* tree, const
  *   id_probs     DEVICE [batch][rows] float32 or NULL (needs ids), written: the drawn id's probability
  *   workspace    DEVICE, ps_target_probs_workspace_bytes bytes, 256-byte aligned (NULL where that is 0); its contents do not matter
  *                before or after the call.  Calls that overlap in time need one each
- * Which tokens are kept and which one is drawn is decided with exponentials and sums that carry more than 40 bits.  A logit of -Inf
- * has no mass; a row without any mass (all -Inf) has probs 0 and id -1, a row with a NaN or +Inf has probs NaN and id -1, id_probs
+ * How rows are divided among workgroups goes by the sizes and by which of top_k and top_p are given, not by what they hold.  Which tokens
+ * are kept and which one is drawn is decided with exponentials and sums that carry more than 40 bits.  A logit of -Inf has no mass; a row without any mass (all -Inf) has probs 0 and id -1, a row with a NaN or +Inf has probs NaN and id -1, id_probs
  * likewise.  Supported: vocab <= 2^20, batch * rows <= 2^20.
  * Errors: PS_ERR_NULL (args, logits, ids without r, neither probs nor ids); PS_ERR_SHAPE; PS_ERR_WORKSPACE; PS_ERR_UNSUPPORTED
  * (sizes; alignment: logits to their type, everything else to 4 bytes); PS_ERR_DEVICE.

@@ -13,7 +13,8 @@
 //
 // One workgroup per row (few rows of a large vocabulary: several, see below); the row is read again by each pass, from the caches.  What bounds it: a pass over a row
 // that makes masses is 25 instructions per token (V 128256: 12 us on one compute unit), one that only compares is a read.  Measured (us; V 32000 float32, 61 rows,
-// top-k 50 and top-p 0.95, probabilities: 18, 3 of them the bytes at a copy's rate; V 128256 bf16, 488 rows, a setting per sequence: 142, bytes 73).
+// top-k 50 and top-p 0.95, probabilities: 18, 3 of them the bytes at a copy's rate; V 128256 bf16, 488 rows: greedy 88, k 50 96, no filter but min-p 132, top-p 175,
+// settings of each sequence 139 to 171, bytes 73).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -712,10 +713,22 @@ __global__ __launch_bounds__(T, 4) void target_probs_kernel(const TpParams P) {
 // ------------------------------------------------------------------------------------------
 // Few rows of a large vocabulary: several workgroups per row, a kernel for each pass.  What a row's workgroups tell each other is in the workspace.
 // ------------------------------------------------------------------------------------------
-// A workgroup's tokens are a multiple of TP_PART (a pass of 1024 threads over bf16).  Up to TP_SPLIT_ROWS rows: masses of a row take one workgroup long, but every kernel reads
-// the row once more.  (V 128256 bf16, us, cut up / one workgroup per row: 8 rows top-p 35 / 78, no filter 20 / 48; 64 rows top-p 53 / 82, no filter 32 / 52; 128 rows top-p
-// 75 / 82, no filter 47 / 54.  8 rows of V 64000: top-p 35 / 46, no filter 21 / 27, of V 32000: 36 / 30, 21 / 17.)  Calls with top-k and no top-p have masses of a few
-// tokens only: one workgroup per row (k 50, 8 rows of V 70000 29 / 18, of 128256 27 / 24, drawn 32 / 22, of 260000 31 / 38, drawn 35 / 31; 64 rows of 128256 42 / 27)
+// A workgroup's tokens are a multiple of TP_PART (a pass of 1024 threads over bf16).  Masses of a row take one workgroup long, but every kernel reads the row once more,
+// and the chain is six kernels.  The host sees sizes and which settings are given, not what they say, so the rule goes by these; cut up / one workgroup per row,
+// bf16, probabilities (d: draws), us:
+//               no filter   top-p     top-p d    greedy   k 50, p   k 2000
+//   V 128256,  8 rows  20 / 49   35 / 78    42 / 88    19 / 19   30 / 27    69 / 83
+//   V 128256, 64 rows  32 / 53   54 / 81    66 / 90    23 / 22   44 / 30    90 / 86
+//   V 128256, 96 rows  53 / 53   82 / 82   111 / 91    35 / 22   62 / 31   127 / 87
+//   V 128256, 128      47 / 54   75 / 83    97 / 91    31 / 24   58 / 32   120 / 87
+//   V 70000,   8 rows  20 / 30   34 / 51    41 / 58    20 / 12   31 / 21    60 / 58
+//   V 64000,   8 rows  20 / 28   32 / 46    39 / 53    19 / 12   29 / 20    55 / 53
+//   V 48000,   8 rows  20 / 23   32 / 39    39 / 44    20 / 10   29 / 18    51 / 45
+//   V 32000,   8 rows  21 / 17   31 / 30    38 / 35    21 / 8    29 / 17    40 / 35
+// Rows are cut up from TP_SPLIT_VOCAB on, up to TP_SPLIT_ROWS: there rows with masses gain up to 2.5, those with few (greedy, a small k) lose 1.2 to 1.8, and 2 to 2.5
+// where they are only drawn (greedy, V 70000, 64 rows 26 / 11).  With more rows draws by top-p lose too; with a smaller vocabulary the gains go (48000: 1.2) and the losses stay.
+// Calls with top-k and no top-p: one workgroup per row, which is right for a small k and not for a large one (V 128256, k 50, 8 rows 27 / 24, drawn 32 / 22, 64 rows 41 / 27; k 2000,
+// 8 rows 69 / 83, drawn 72 / 64, 64 rows 90 / 86; V 260000, 8 rows, k 50 30 / 37, drawn 34 / 31, k 2000 91 / 134, drawn 94 / 100).
 constexpr int TP_PART = 8192;
 constexpr int TP_SPLIT_ROWS = 64;                  // rows up to which they are cut up,
 constexpr int TP_SPLIT_VOCAB = 65536;              // from this vocabulary on
@@ -914,7 +927,9 @@ template <typename LT> __global__ __launch_bounds__(1024, 4) void row_bound_kern
             bound = bound_of(find_in_list<1024>(S, n, W.before, W.want, -1.0, with, mass));
             total = with;
         }
-    } else {                                                // more tokens than the list holds: the whole row, by this workgroup
+    // More tokens than the list holds (a flat row, many equal logits, a top_k above 2000): the whole row, by this workgroup alone.  (8 rows of V 128256, top-p 0.9, us: temperature
+    // 2 41, temperature 8, where the step has 7000 tokens, 189; one workgroup per row does that in 363 for 488 rows, 175 at temperature 1)
+    } else {
         Logits<LT, 1024> L;
         L.row = P.logits + row * P.vocab * Traits<LT>::ESZ; L.vocab = P.vocab; L.nvec = (P.vocab + Vec<LT>::N - 1) / Vec<LT>::N;
         if (s.k < P.vocab) bound = bound_of(find_in_row<false>(L, R, s.max, S, bound, (u64)s.k, -1.0, with));

@@ -9,7 +9,8 @@
 // The running maximum is raised only when a score passes it by 2^8 (sums stay far inside float32), so sums are rarely rescaled.
 //
 // Probabilities are rounded to bf16 for the second product (their sum is taken before that, in float32): a row's error is then that of many independent
-// roundings, below its result's own; float32 calls have three bf16 parts of queries and probabilities, 24 bits of each.
+// roundings, below its result's own.  (Of the 2-norm, with the result's rounding: 0.0020 ... 0.0023; with probabilities in two parts 0.00165, the result's rounding alone, at 137 us
+// in the place of 107 for 8 x 61 nodes over 4099 ... 12288 positions, 46.8 / 45.8 for 4 x 32768.)  float32 calls have three bf16 parts of queries and probabilities, 24 bits of each.
 //
 // Work: a sequence's blocks are cut into splits of `per` blocks; a workgroup takes a split of one kv head for up to four tiles of 32 rows (a row is a node and one of
 // the heads that share the kv head).  Its wavefronts divide tiles (WR) and blocks (WK); those that share a tile meet in LDS, splits in the workspace and a
@@ -18,7 +19,7 @@
 // What bounds it (bf16, head_dim 128).  One tile: reading the codes.  32 sequences of 2048 positions, 32 heads, a row each: 537 MB in 87 us, 6.2 TB/s; 4 of 32768
 // positions, 8 heads, 4 rows each: 268 MB in 46.  Many tiles: a block of one tile is 16 matrix instructions (512 cycles), 64 conversions, 16 exponentials
 // and some 100 more vector instructions, which overlap with the products less than the two wavefronts of a SIMD could make them: 1600 cycles.  8 x 4099 ...
-// 12288 positions, 61 nodes, 32 heads that share 8: 91 us, 0.72 PFLOP/s.  Left out in probes of that: conversions -6 %, exponentials -12 %, barriers and requests
+// 12288 positions, 61 nodes, 32 heads that share 8: 89 us, 0.74 PFLOP/s.  Left out in probes of that: conversions -6 %, exponentials -12 %, barriers and requests
 // -20 %, all of these -30 %.  Small calls: 2 us until the first operands are there, 2 for the tree's own rows, 2 for the meeting and the results, then the join (3).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -667,6 +668,8 @@ int plan(const ps_tree_shape* tree, const ps_tree_attn_args* a, TaParams& P, TaP
     P.stream = P.tiles == 1 && total * heads * PC_BLOCK * d * 2 > 192LL << 20;
 
     const bool bf = a->dtype == PS_BF16;
+    // The cut is for the lengths that the host gives: a sequence whose length on the device is shorter has its blocks in the first splits only (one sequence, 2048 positions,
+    // 32 heads, us, exact / a bound of 4096 / of 32768: one row 12.5 / 10.5 / 19.8, 61 nodes 16.7 / 17.7 / 29.4; eight sequences of 8 heads, 61 nodes 28 / 30 / 28).
     // How rows and blocks are cut: two or four tiles of rows per workgroup, about 256 workgroups or 512, whichever is estimated to take least time.  (bf16, us,
     // four tiles and 512 always / as estimated: 61 nodes, 32 heads that share 8, 2048 positions: 27.3 / 17.8, 8 x 2048: 44.1 / 29.5, 16 x 2048: 68.8 / 54.7 (two tiles:
     // 61), 32 x 2048: 93.6 / 89.3 (two tiles: 133), 64 x 1000: 105.5 / 107.9 (168); float32, four / two: 2048 33.3 / 26.7, 64 x 1000 298 / 312)
